@@ -44,7 +44,8 @@ typedef enum {
   RLKV_ERR_TOO_LARGE = 6    /* rlkv_decode_attention_noalloc: the static scratch buffer is too small for the call */
 } rlkv_status_t;
 
-typedef enum { RLKV_F32 = 0, RLKV_BF16 = 1 } rlkv_dtype_t;
+/* RLKV_E4M3: 8 bits, 4 of exponent and 3 of mantissa, no infinities, largest value 448; the token-wise operators' matrices only */
+typedef enum { RLKV_F32 = 0, RLKV_BF16 = 1, RLKV_E4M3 = 2 } rlkv_dtype_t;
 
 /* Which decode kernel (and with it which in-HBM store layout) a cache uses.
  *   RLKV_KERNEL_VALU : row-major stores [slot][head_dim]; products of fp32 values on the
@@ -407,6 +408,33 @@ int64_t rlkv_plan_static_scratch(int32_t n_workgroups, int32_t n_pairs, int32_t 
 int32_t rlkv_plan_narrow_split(int32_t n_compute_units, int32_t group, int32_t n_full_heads, int32_t batch,
                                const int32_t* n_tokens /* host */, const int32_t* cached /* host */,
                                int32_t min_share_tiles);
+
+/* ---- Token-wise operators: a decoder's way into the cache and out of it again --------------------------------------------
+ * These need no cache handle.  They run on `stream` of the current device, keep no state, allocate nothing, wait for nothing
+ * and can be recorded into a HIP graph.  Matrices are row-major; a stride is the distance of two rows (of two groups, for
+ * scales) in elements.  Every pointer is aligned to its element type; no row has to be aligned beyond that unless a call says so
+ * (rows at multiples of 16 bytes are the fast case).  Sums, statistics and scales are fp32; every output is rounded once, to
+ * nearest even.  A call with no rows returns RLKV_OK and launches nothing. */
+
+/* Root-mean-square norm of rows, with the residual's addition in front of it:
+ *     h = x + residual        sum_out = h        out = h / sqrt(mean(h^2) + eps) * weight
+ * The norm is that of the unrounded h.
+ *   x, residual, weight, sum_out : device, in `dtype` (RLKV_F32 or RLKV_BF16); [rows][cols], weight [cols].  residual, weight and
+ *                        sum_out may be NULL (no addition; ones; h is not kept; sum_out needs a residual)
+ *   out : device; out_dtype is `dtype`, or RLKV_E4M3: then columns [128 g, 128 g + 128) of row r are divided by their scale,
+ *                        scales[g * scale_stride + r] = max(max |out| / 448, 2^-126)   (what rlkv_scaled_matmul takes)
+ *   scales : device, fp32, [ceil(cols / 128)][rows]; NULL unless out_dtype is RLKV_E4M3
+ * sum_out, and out in the type `dtype`, may be the very rows of x or residual (same pointer and stride).
+ * A NaN stays one and does not count in a scale; a group that holds an infinity gets an infinite scale and stands for NaN. */
+rlkv_status_t rlkv_rms_norm(const void* x /* device */, int64_t x_stride, const void* residual /* device */,
+                            int64_t residual_stride, const void* weight /* device */, float eps, int32_t rows, int32_t cols,
+                            int32_t dtype, void* sum_out /* device */, int64_t sum_stride, void* out /* device */,
+                            int64_t out_stride, int32_t out_dtype, float* scales /* device */, int64_t scale_stride, void* stream);
+
+/* Rows in 8 bits with a scale for each group of 128 columns, as above without the norm: out = round(x / scale). */
+rlkv_status_t rlkv_quantize(const void* x /* device */, int64_t x_stride, int32_t rows, int32_t cols, int32_t dtype,
+                            void* out /* device */, int64_t out_stride, float* scales /* device */, int64_t scale_stride,
+                            void* stream);
 
 /* Measurement aid, independent of any cache: one plain streaming read of `bytes` (rounded down to
  * whole 16 KiB blocks) of `buf` with 128-bit non-temporal loads and no arithmetic, launched with

@@ -16,7 +16,7 @@ _LIB_PATH = os.path.join(_PKG, "librlkv.so")
 _lib = None
 
 RLKV_OK, RLKV_ERR_INVALID_ARG, RLKV_ERR_OOM, RLKV_ERR_CAPACITY, RLKV_ERR_STATE, RLKV_ERR_HIP, RLKV_ERR_TOO_LARGE = range(7)
-RLKV_F32, RLKV_BF16 = 0, 1
+RLKV_F32, RLKV_BF16, RLKV_E4M3 = 0, 1, 2
 RLKV_KERNEL_AUTO, RLKV_KERNEL_VALU, RLKV_KERNEL_MFMA = 0, 1, 2
 
 
@@ -52,7 +52,7 @@ def load_library():
         raise ImportError(f"{_LIB_PATH} is not built: run `python -m paper_2510_08525_amd.build` "
                           "(there is no fallback path)")
     lib = ctypes.CDLL(_LIB_PATH)
-    vp, i32, sz, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_float
+    vp, i32, sz, f32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t, ctypes.c_float, ctypes.c_int64
     cfgp = ctypes.POINTER(_Config)
     sigs = {
         "rlkv_cache_required_bytes": (sz, [cfgp]),
@@ -91,6 +91,8 @@ def load_library():
         "rlkv_cache_kernel": (i32, [vp]),
         "rlkv_pool_pages_free": (ctypes.c_int64, [vp]),
         "rlkv_pool_shuffle": (i32, [vp, ctypes.c_uint64]),
+        "rlkv_rms_norm": (i32, [vp, i64, vp, i64, vp, f32, i32, i32, i32, vp, i64, vp, i64, i32, vp, i64, vp]),
+        "rlkv_quantize": (i32, [vp, i64, i32, i32, i32, vp, i64, vp, i64, vp]),
         "rlkv_status_string": (ctypes.c_char_p, [i32]),
     }
     for name, (res, args) in sigs.items():
@@ -106,6 +108,7 @@ EXPORTED_SYMBOLS = (
     "rlkv_profile_collect", "rlkv_get_lengths",
     "rlkv_get_slot_positions", "rlkv_resident_bytes", "rlkv_probe_stream_read", "rlkv_plan_shares", "rlkv_plan_whole_pairs", "rlkv_plan_list_whole", "rlkv_plan_list_kind", "rlkv_plan_merge_inside", "rlkv_plan_static_scratch", "rlkv_plan_narrow_split", "rlkv_plan_blend_form", "rlkv_plan_prefill_form", "rlkv_plan_prefill_rows", "rlkv_plan_prefill_block", "rlkv_plan_prefill_item", "rlkv_cache_kernel", "rlkv_pool_pages_free",
     "rlkv_pool_shuffle", "rlkv_status_string",
+    "rlkv_rms_norm", "rlkv_quantize",
 )
 
 

@@ -1,0 +1,142 @@
+// Root-mean-square norm of rows with the addition of a residual, into the storage type or into 8 bits with a scale for each group
+// of 128 columns; quantising alone is the same kernel without the norm.
+//
+//   h = x + r          y = h / sqrt(mean(h^2) + eps) * w          s_g = max(max_g |y| / 448, least)      out = round(y / s_g)
+//
+// h stays in fp32 registers between the sum of squares and the outputs, so it is read once and each output is rounded once: the norm is
+// that of the unrounded sum.  A thread holds pieces of eight columns, T apart: a wavefront's loads are whole lines, and the 16
+// lanes of a group of 128 columns lie next to each other, so that its maximum takes four steps over lanes and no LDS.
+// Bound: HBM for many rows, latency for few.
+#include "token_ops.h"
+
+namespace rlkv {
+namespace {
+
+// T threads a row, NC pieces each (T * NC * 8 columns at most, unless LOOP: then the pieces beyond are read a second time).
+template <typename X, int T, int NC, bool E4M3, bool LOOP>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(NormCall c, int rows_per_block) {
+  constexpr int kRowsAtOnce = T < 256 ? 256 / T : 1;
+  constexpr int kWaves = T / 64;
+  __shared__ float parts[2][kWaves > 1 ? kWaves : 1];
+  const int t = threadIdx.x % T, lane_row = threadIdx.x / T;
+  const int first = blockIdx.x * rows_per_block;
+  const int last = first + rows_per_block < c.rows ? first + rows_per_block : c.rows;
+  int turn = 0;
+  for (int row = first + lane_row; row < last; row += kRowsAtOnce) {
+    const X* x = static_cast<const X*>(c.x) + row * c.x_stride;
+    const X* res = c.residual ? static_cast<const X*>(c.residual) + row * c.residual_stride : nullptr;
+    float h[NC][8];
+    float squares = 0.f;
+    auto load = [&](int col, float (&f)[8]) {
+      load_piece(x, col, c.cols, c.whole_in, f);
+      if (res) {
+        float r[8];
+        load_piece(res, col, c.cols, c.whole_res, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] += r[i];
+      }
+    };
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+      const int col = (t + k * T) * 8;
+      if (col < c.cols) {
+        load(col, h[k]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[k][i] = 0.f;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < NC; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) squares += h[k][i] * h[k][i];
+    float factor = 1.f;
+    if (c.norm) {
+      if (LOOP)
+        for (int col = (t + NC * T) * 8; col < c.cols; col += T * 8) {
+          float f[8];
+          load(col, f);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) squares += f[i] * f[i];
+        }
+      squares = sum_of_wave(squares);
+      if (kWaves > 1) {
+        // (two buffers in turn: a wavefront may be at the next row while another still reads this one's sums)
+        if ((threadIdx.x & 63) == 0) parts[turn][threadIdx.x >> 6] = squares;
+        __syncthreads();
+        squares = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) squares += parts[turn][w];
+        turn ^= 1;
+      }
+      factor = rsqrtf(squares / (float)c.cols + c.eps);
+    }
+    auto finish = [&](int col, float (&f)[8]) {
+      if (col < c.cols) {
+        if (c.sum_out) store_piece(static_cast<X*>(c.sum_out) + row * c.sum_stride, col, c.cols, c.whole_sum, f);
+        if (c.norm) {
+          float w[8];
+          if (c.weight) {
+            load_piece(static_cast<const X*>(c.weight), col, c.cols, c.whole_weight, w);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = 1.f;
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f[i] = f[i] * factor * w[i];
+        }
+      }
+      if constexpr (E4M3) {
+        // the lanes of a group are 16 neighbours, those past the row's end among them (with zeros)
+        float most = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(f[i]));
+#pragma unroll
+        for (int m = 1; m < 16; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
+        const float scale = fmaxf(most / kE4m3Max, kLeastScale);
+        if (col < c.cols) {
+          const float inverse = 1.f / scale;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f[i] *= inverse;
+          store_e4m3(static_cast<uint8_t*>(c.out) + row * c.out_stride, col, c.cols, c.whole_out, f);
+          if ((t & 15) == 0) c.scales[(int64_t)(col / kGroup) * c.scale_stride + row] = scale;
+        }
+      } else if (col < c.cols) {
+        store_piece(static_cast<X*>(c.out) + row * c.out_stride, col, c.cols, c.whole_out, f);
+      }
+    };
+    if (LOOP)                       // (before the pieces in registers: where sum_out is the residual, what is read again here is not yet written)
+      for (int col = (t + NC * T) * 8; col - t * 8 < c.cols; col += T * 8) {
+        float f[8] = {};
+        if (col < c.cols) load(col, f);
+        finish(col, f);
+      }
+#pragma unroll
+    for (int k = 0; k < NC; ++k) finish((t + k * T) * 8, h[k]);
+  }
+}
+
+constexpr int kMostBlocks = 1 << 20;
+
+template <typename X, bool E4M3>
+hipError_t launch_typed(const NormCall& c, hipStream_t stream) {
+  auto run = [&](auto kernel, int threads, int rows_per_block) {
+    const unsigned grid = (unsigned)((c.rows + rows_per_block - 1) / rows_per_block);
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, stream, c, rows_per_block);
+    return hipGetLastError();
+  };
+  if (c.rows >= 1024 && c.cols <= 4096) return run(norm_kernel<X, 64, 8, E4M3, false>, 256, c.rows >= 8192 ? 32 : 4);
+  const int rows = c.rows > kMostBlocks ? (c.rows + kMostBlocks - 1) / kMostBlocks : 1;
+  if (c.cols <= 4096) return run(norm_kernel<X, 256, 2, E4M3, false>, 256, rows);
+  if (c.cols <= 8192) return run(norm_kernel<X, 256, 4, E4M3, false>, 256, rows);
+  return run(norm_kernel<X, 256, 8, E4M3, true>, 256, rows);
+}
+
+}  // namespace
+
+hipError_t launch_norm(const NormCall& c, int dtype, bool out_e4m3, hipStream_t stream) {
+  if (dtype == RLKV_F32) return out_e4m3 ? launch_typed<float, true>(c, stream) : launch_typed<float, false>(c, stream);
+  return out_e4m3 ? launch_typed<uint16_t, true>(c, stream) : launch_typed<uint16_t, false>(c, stream);
+}
+
+}  // namespace rlkv

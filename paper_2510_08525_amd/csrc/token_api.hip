@@ -1,0 +1,75 @@
+// Entry points of the token-wise operators: argument checks, all of them before the first HIP call.
+#include <math.h>
+
+#include "token_ops.h"
+
+using namespace rlkv;
+
+namespace {
+
+hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
+size_t bytes_of(int dtype) { return dtype == RLKV_F32 ? 4 : dtype == RLKV_BF16 ? 2 : 1; }
+bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+int groups_of(int cols) { return (int)(((int64_t)cols + kGroup - 1) / kGroup); }
+
+// A matrix the call reads: rows may repeat (a stride below the columns), but not run backwards.
+bool readable(const void* p, int64_t stride, int dtype) { return p && stride >= 0 && aligned(p, bytes_of(dtype)); }
+// One that it writes: rows are apart.
+bool writable(const void* p, int64_t stride, int64_t rows, int64_t cols, int dtype) {
+  return p && (stride >= cols || rows <= 1) && aligned(p, bytes_of(dtype));
+}
+// Whether every row starts at a multiple of `to` bytes.
+int32_t whole(const void* p, int64_t stride, int dtype, size_t to = 16) {
+  return p && aligned(p, to) && (stride * (int64_t)bytes_of(dtype)) % (int64_t)to == 0;
+}
+
+rlkv_status_t norm_call(NormCall& c, int dtype, int out_dtype, void* stream) {
+  if (dtype != RLKV_F32 && dtype != RLKV_BF16) return RLKV_ERR_INVALID_ARG;
+  if (out_dtype != dtype && out_dtype != RLKV_E4M3) return RLKV_ERR_INVALID_ARG;
+  if (c.rows < 0 || c.cols < 1) return RLKV_ERR_INVALID_ARG;
+  if (c.rows == 0) return RLKV_OK;
+  if (!readable(c.x, c.x_stride, dtype) || !writable(c.out, c.out_stride, c.rows, c.cols, out_dtype)) return RLKV_ERR_INVALID_ARG;
+  if (c.residual && !readable(c.residual, c.residual_stride, dtype)) return RLKV_ERR_INVALID_ARG;
+  if (c.sum_out && (!c.residual || !writable(c.sum_out, c.sum_stride, c.rows, c.cols, dtype))) return RLKV_ERR_INVALID_ARG;
+  if (c.weight && !aligned(c.weight, bytes_of(dtype))) return RLKV_ERR_INVALID_ARG;
+  const bool e4m3 = out_dtype == RLKV_E4M3;
+  if (e4m3 ? !writable(c.scales, c.scale_stride, groups_of(c.cols), c.rows, RLKV_F32) : c.scales != nullptr) return RLKV_ERR_INVALID_ARG;
+  c.whole_in = whole(c.x, c.x_stride, dtype);
+  c.whole_res = whole(c.residual, c.residual_stride, dtype);
+  c.whole_sum = whole(c.sum_out, c.sum_stride, dtype);
+  c.whole_weight = whole(c.weight, 0, dtype);
+  c.whole_out = whole(c.out, c.out_stride, out_dtype, e4m3 ? 8 : 16);
+  return launch_norm(c, dtype, e4m3, as_stream(stream)) == hipSuccess ? RLKV_OK : RLKV_ERR_HIP;
+}
+
+}  // namespace
+
+extern "C" {
+
+rlkv_status_t rlkv_rms_norm(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, const void* weight,
+                            float eps, int32_t rows, int32_t cols, int32_t dtype, void* sum_out, int64_t sum_stride, void* out,
+                            int64_t out_stride, int32_t out_dtype, float* scales, int64_t scale_stride, void* stream) {
+  if (!(eps >= 0.f) || isinf(eps)) return RLKV_ERR_INVALID_ARG;
+  NormCall c = {};
+  c.x = x; c.x_stride = x_stride;
+  c.residual = residual; c.residual_stride = residual_stride;
+  c.sum_out = sum_out; c.sum_stride = sum_stride;
+  c.out = out; c.out_stride = out_stride;
+  c.scales = scales; c.scale_stride = scale_stride;
+  c.weight = weight; c.eps = eps;
+  c.rows = rows; c.cols = cols;
+  c.norm = 1;
+  return norm_call(c, dtype, out_dtype, stream);
+}
+
+rlkv_status_t rlkv_quantize(const void* x, int64_t x_stride, int32_t rows, int32_t cols, int32_t dtype, void* out,
+                            int64_t out_stride, float* scales, int64_t scale_stride, void* stream) {
+  NormCall c = {};
+  c.x = x; c.x_stride = x_stride;
+  c.out = out; c.out_stride = out_stride;
+  c.scales = scales; c.scale_stride = scale_stride;
+  c.rows = rows; c.cols = cols;
+  return norm_call(c, dtype, RLKV_E4M3, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,120 @@
+// What the token-wise operators (norm, quantising, 8-bit product, log probabilities) share: pieces of eight columns, conversions,
+// reductions over lanes, and the launchers.
+#pragma once
+
+#include "rlkv_internal.h"
+
+namespace rlkv {
+
+constexpr int kGroup = 128;               // columns that share a scale of an 8-bit matrix
+constexpr float kE4m3Max = 448.f;         // largest finite value of the 8-bit type (4 exponent, 3 mantissa bits, no infinities)
+// The least scale, the smallest normal fp32 number: a group of zeros gets it (and stays zeros), and its reciprocal is finite.
+constexpr float kLeastScale = 1.17549435e-38f;
+
+typedef uint32_t words2 __attribute__((ext_vector_type(2)));
+typedef uint32_t words4 __attribute__((ext_vector_type(4)));
+typedef float floats2 __attribute__((ext_vector_type(2)));
+typedef float floats4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16s2 __attribute__((ext_vector_type(2)));
+
+// Eight values of a storage type as they come from memory.
+template <typename T> struct Piece;
+template <> struct Piece<uint16_t> { words4 w; };
+template <> struct Piece<float> { floats4 a, b; };
+
+__device__ __forceinline__ void widen(const Piece<uint16_t>& p, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = __uint_as_float(p.w[i] << 16);
+    f[2 * i + 1] = __uint_as_float(p.w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void widen(const Piece<float>& p, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { f[i] = p.a[i]; f[4 + i] = p.b[i]; }
+}
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {      // two values rounded to nearest even
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((floats2{a, b}), bf16s2));
+}
+__device__ __forceinline__ void narrow(const float (&f)[8], Piece<uint16_t>& p) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p.w[i] = bf16_pair(f[2 * i], f[2 * i + 1]);
+}
+__device__ __forceinline__ void narrow(const float (&f)[8], Piece<float>& p) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { p.a[i] = f[i]; p.b[i] = f[4 + i]; }
+}
+__device__ __forceinline__ float one_value(uint16_t v) { return bf16_bits_to_f32(v); }
+__device__ __forceinline__ float one_value(float v) { return v; }
+__device__ __forceinline__ void put_value(uint16_t* p, float v) { *p = (uint16_t)bf16_pair(v, 0.f); }
+__device__ __forceinline__ void put_value(float* p, float v) { *p = v; }
+
+// Columns [col, col + 8) of a row of n columns as fp32, zeros past its end; `whole`: the row starts at a multiple of 16 bytes, so that
+// a piece inside it is one or two 16-byte loads.
+template <typename T>
+__device__ __forceinline__ void load_piece(const T* row, int col, int n, bool whole, float (&f)[8]) {
+  if (whole && col + 8 <= n) {
+    widen(*reinterpret_cast<const Piece<T>*>(row + col), f);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = col + i < n ? one_value(row[col + i]) : 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_piece(T* row, int col, int n, bool whole, const float (&f)[8]) {
+  if (whole && col + 8 <= n) {
+    Piece<T> p;
+    narrow(f, p);
+    *reinterpret_cast<Piece<T>*>(row + col) = p;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (col + i < n) put_value(row + col + i, f[i]);
+  }
+}
+// Eight values as 8-bit ones (rounded to nearest even).
+__device__ __forceinline__ void store_e4m3(uint8_t* row, int col, int n, bool whole, const float (&f)[8]) {
+  words2 w;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i], f[4 * i + 1], 0, false);
+    w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i + 2], f[4 * i + 3], lo, true);
+  }
+  if (whole && col + 8 <= n) {
+    *reinterpret_cast<words2*>(row + col) = w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (col + i < n) row[col + i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+  }
+}
+
+__device__ __forceinline__ float sum_of_wave(float x) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
+  return x;
+}
+__device__ __forceinline__ float max_of_wave(float x) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) x = fmaxf(x, __shfl_xor(x, m));
+  return x;
+}
+
+// ---- launchers ---------------------------------------------------------------------------------------------------
+// One call of the norm (weight / eps) or of quantising alone (norm false); strides in elements.
+struct NormCall {
+  const void* x;
+  const void* residual;       // or null
+  void* sum_out;              // or null (with residual only)
+  const void* weight;         // or null: ones
+  void* out;
+  float* scales;              // [group][row], out_e4m3 only
+  int64_t x_stride, residual_stride, sum_stride, out_stride, scale_stride;
+  float eps;
+  int32_t rows, cols;
+  int32_t norm;
+  int32_t whole_in, whole_res, whole_sum, whole_weight, whole_out;    // rows at multiples of what a vector access needs
+};
+hipError_t launch_norm(const NormCall& call, int dtype, bool out_e4m3, hipStream_t stream);
+
+}  // namespace rlkv

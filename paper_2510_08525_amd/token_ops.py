@@ -1,0 +1,93 @@
+"""The token-wise operators on tensors: argument checks and marshalling around the calls of include/rlkv.h.
+
+Outputs are the caller's tensors; every call goes to the current stream of the tensors' device and returns its outputs.
+Matrices are two-dimensional with contiguous columns, rows at any stride.
+"""
+from __future__ import annotations
+
+import torch
+
+from .binding import RLKV_BF16, RLKV_E4M3, RLKV_F32, _check, load_library
+
+E4M3 = torch.float8_e4m3fn
+GROUP = 128                     # columns that share a scale
+_DTYPES = {torch.float32: RLKV_F32, torch.bfloat16: RLKV_BF16, E4M3: RLKV_E4M3}
+_fn: dict = {}
+
+
+def _call(name: str, device, *args):
+    """Calls the library on the tensors' device and its current stream."""
+    fn = _fn.get(name)
+    if fn is None:
+        fn = _fn[name] = getattr(load_library(), name)
+    index = device.index
+    if index == torch._C._cuda_getDevice():
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(index):
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    if status:
+        _check(status, name)
+
+
+def _matrix(t, what: str, device=None, dtypes=None, shape=None):
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{what}: need a matrix with contiguous columns")
+    return _checked(t, what, device, dtypes, shape)
+
+
+def _vector(t, what: str, device=None, dtypes=None, size=None):
+    if t.dim() != 1 or (t.stride(0) != 1 and t.shape[0] > 1):
+        raise ValueError(f"{what}: need a contiguous vector")
+    return _checked(t, what, device, dtypes, None if size is None else (size,))
+
+
+def _checked(t, what, device, dtypes, shape):
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{what}: need a tensor on {device if device is not None else 'the GPU'}")
+    if dtypes is not None and t.dtype not in dtypes:
+        raise ValueError(f"{what}: type {t.dtype} is not one of {', '.join(map(str, dtypes))}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: shape {tuple(t.shape)} != {tuple(shape)}")
+    return t.data_ptr()
+
+
+def groups(cols: int) -> int:
+    """Groups of columns that share a scale."""
+    return -(-cols // GROUP)
+
+
+def rms_norm(x, weight, eps: float, out, *, scales=None, residual=None, sum_out=None):
+    """out = h / sqrt(mean(h^2) + eps) * weight of h = x + residual, and sum_out = h (rlkv_rms_norm).
+
+    `out` has the type of x, or is float8_e4m3fn: then scales [groups(cols), rows] (fp32) takes the scale of each 128 columns.
+    weight, residual and sum_out may be None."""
+    kinds, device = (torch.float32, torch.bfloat16), x.device
+    xp = _matrix(x, "x", None, kinds)
+    rows, cols = x.shape
+    same = (x.dtype,)
+    rp = sp = gp = wp = None
+    r_stride = s_stride = g_stride = 0
+    if residual is not None:
+        rp, r_stride = _matrix(residual, "residual", device, same, (rows, cols)), residual.stride(0)
+    if sum_out is not None:
+        sp, s_stride = _matrix(sum_out, "sum_out", device, same, (rows, cols)), sum_out.stride(0)
+    if weight is not None:
+        wp = _vector(weight, "weight", device, same, cols)
+    if scales is not None:
+        gp, g_stride = _matrix(scales, "scales", device, (torch.float32,), (groups(cols), rows)), scales.stride(0)
+    op = _matrix(out, "out", device, (x.dtype, E4M3), (rows, cols))
+    _call("rlkv_rms_norm", device, xp, x.stride(0), rp, r_stride, wp, eps, rows, cols, _DTYPES[x.dtype], sp, s_stride, op,
+          out.stride(0), _DTYPES[out.dtype], gp, g_stride)
+    return out
+
+
+def quantize(x, out, scales):
+    """out = round(x / scale) in 8 bits, scales [groups(cols), rows]: one for each 128 columns of a row (rlkv_quantize)."""
+    device = x.device
+    xp = _matrix(x, "x", None, (torch.float32, torch.bfloat16))
+    rows, cols = x.shape
+    op = _matrix(out, "out", device, (E4M3,), (rows, cols))
+    gp = _matrix(scales, "scales", device, (torch.float32,), (groups(cols), rows))
+    _call("rlkv_quantize", device, xp, x.stride(0), rows, cols, _DTYPES[x.dtype], op, out.stride(0), gp, scales.stride(0))
+    return out
