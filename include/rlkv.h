@@ -436,6 +436,23 @@ rlkv_status_t rlkv_quantize(const void* x /* device */, int64_t x_stride, int32_
                             void* out /* device */, int64_t out_stride, float* scales /* device */, int64_t scale_stride,
                             void* stream);
 
+/* Product of 8-bit matrices with scales along the inner dimension (groups of 128):
+ *     out[r][c] = sum over groups g of  a_scales[g][r] * b_scales[c / 128][g] * sum over k in g of a[r][k] * b[c][k]
+ *   a        : device, RLKV_E4M3, [m][k]; a_scales: device, fp32, [ceil(k / 128)][m]: what rlkv_rms_norm and rlkv_quantize leave
+ *   b        : device, RLKV_E4M3, [n][k] (weights, a row per output); b_scales: device, fp32, [ceil(n / 128)][ceil(k / 128)]
+ *   out      : device, out_dtype = RLKV_F32 or RLKV_BF16, [m][n]
+ * k is a multiple of 16; rows of a and b start at multiples of 16 bytes and are at most 2^23 bytes apart (a_stride and b_stride below k
+ * repeat rows).  m, n and k are at most 2^24 and
+ * m * n below 2^44; with m = 0 or n = 0 nothing is done.  Scales and the sums over groups are fp32.
+ * Inside a group, products are exact and summed in fp32 for an fp32 output and for m <= 64; else, for a bf16 output, by the 8-bit
+ * matrix instruction, which drops what lies more than 13 binary places below the exponent of the largest of the products it sums
+ * (at most 2^-6 of the group's largest product altogether).  The order of the sums depends on the sizes only: equal calls
+ * give equal bits. */
+rlkv_status_t rlkv_scaled_matmul(const void* a /* device */, int64_t a_stride, const float* a_scales /* device */,
+                                 int64_t a_scale_stride, const void* b /* device */, int64_t b_stride,
+                                 const float* b_scales /* device */, int64_t b_scale_stride, int32_t m, int32_t n, int32_t k,
+                                 void* out /* device */, int64_t out_stride, int32_t out_dtype, void* stream);
+
 /* Measurement aid, independent of any cache: one plain streaming read of `bytes` (rounded down to
  * whole 16 KiB blocks) of `buf` with 128-bit non-temporal loads and no arithmetic, launched with
  * `workgroups` workgroups of 256 threads on `stream` of the current device.  Timed by the caller,

@@ -93,6 +93,7 @@ def load_library():
         "rlkv_pool_shuffle": (i32, [vp, ctypes.c_uint64]),
         "rlkv_rms_norm": (i32, [vp, i64, vp, i64, vp, f32, i32, i32, i32, vp, i64, vp, i64, i32, vp, i64, vp]),
         "rlkv_quantize": (i32, [vp, i64, i32, i32, i32, vp, i64, vp, i64, vp]),
+        "rlkv_scaled_matmul": (i32, [vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, i32, vp, i64, i32, vp]),
         "rlkv_status_string": (ctypes.c_char_p, [i32]),
     }
     for name, (res, args) in sigs.items():
@@ -108,7 +109,7 @@ EXPORTED_SYMBOLS = (
     "rlkv_profile_collect", "rlkv_get_lengths",
     "rlkv_get_slot_positions", "rlkv_resident_bytes", "rlkv_probe_stream_read", "rlkv_plan_shares", "rlkv_plan_whole_pairs", "rlkv_plan_list_whole", "rlkv_plan_list_kind", "rlkv_plan_merge_inside", "rlkv_plan_static_scratch", "rlkv_plan_narrow_split", "rlkv_plan_blend_form", "rlkv_plan_prefill_form", "rlkv_plan_prefill_rows", "rlkv_plan_prefill_block", "rlkv_plan_prefill_item", "rlkv_cache_kernel", "rlkv_pool_pages_free",
     "rlkv_pool_shuffle", "rlkv_status_string",
-    "rlkv_rms_norm", "rlkv_quantize",
+    "rlkv_rms_norm", "rlkv_quantize", "rlkv_scaled_matmul",
 )
 
 

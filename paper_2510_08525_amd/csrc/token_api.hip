@@ -72,4 +72,28 @@ rlkv_status_t rlkv_quantize(const void* x, int64_t x_stride, int32_t rows, int32
   return norm_call(c, dtype, RLKV_E4M3, stream);
 }
 
+rlkv_status_t rlkv_scaled_matmul(const void* a, int64_t a_stride, const float* a_scales, int64_t a_scale_stride, const void* b,
+                                 int64_t b_stride, const float* b_scales, int64_t b_scale_stride, int32_t m, int32_t n, int32_t k,
+                                 void* out, int64_t out_stride, int32_t out_dtype, void* stream) {
+  if (out_dtype != RLKV_F32 && out_dtype != RLKV_BF16) return RLKV_ERR_INVALID_ARG;
+  if (m < 0 || n < 0 || k < 1 || k % 16 != 0) return RLKV_ERR_INVALID_ARG;
+  if (m > (1 << 24) || n > (1 << 24) || k > (1 << 24)) return RLKV_ERR_INVALID_ARG;
+  if ((int64_t)(m / 128 + 1) * (n / 128 + 1) > (1 << 30)) return RLKV_ERR_INVALID_ARG;      // workgroups of a launch
+  if (m == 0 || n == 0) return RLKV_OK;
+  if (!readable(a, a_stride, RLKV_E4M3) || !readable(b, b_stride, RLKV_E4M3) || !whole(a, a_stride, RLKV_E4M3) ||
+      !whole(b, b_stride, RLKV_E4M3) || a_stride > kMostMatmulStride || b_stride > kMostMatmulStride)
+    return RLKV_ERR_INVALID_ARG;
+  if (!readable(a_scales, a_scale_stride, RLKV_F32) || !readable(b_scales, b_scale_stride, RLKV_F32)) return RLKV_ERR_INVALID_ARG;
+  if (!writable(out, out_stride, m, n, out_dtype)) return RLKV_ERR_INVALID_ARG;
+  MatmulCall c = {};
+  c.a = a; c.a_stride = a_stride;
+  c.a_scales = a_scales; c.a_scale_stride = a_scale_stride;
+  c.b = b; c.b_stride = b_stride;
+  c.b_scales = b_scales; c.b_scale_stride = b_scale_stride;
+  c.m = m; c.n = n; c.k = k;
+  c.out = out; c.out_stride = out_stride;
+  c.whole_out = whole(out, out_stride, out_dtype, 4 * bytes_of(out_dtype));
+  return launch_matmul(c, out_dtype == RLKV_BF16, as_stream(stream)) == hipSuccess ? RLKV_OK : RLKV_ERR_HIP;
+}
+
 }  // extern "C"

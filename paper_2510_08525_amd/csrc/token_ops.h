@@ -117,4 +117,18 @@ struct NormCall {
 };
 hipError_t launch_norm(const NormCall& call, int dtype, bool out_e4m3, hipStream_t stream);
 
+// One 8-bit product; strides in elements (bytes for a and b).
+struct MatmulCall {
+  const void* a;
+  const float* a_scales;
+  const void* b;
+  const float* b_scales;
+  void* out;
+  int64_t a_stride, a_scale_stride, b_stride, b_scale_stride, out_stride;
+  int32_t m, n, k;
+  int32_t whole_out;          // four neighbouring outputs, the first a multiple of four columns into a row, can be one store
+};
+constexpr int64_t kMostMatmulStride = 1 << 23;         // bytes between rows of a or b: a tile's rows are within 32 bits of its first
+hipError_t launch_matmul(const MatmulCall& call, bool out_bf16, hipStream_t stream);
+
 }  // namespace rlkv

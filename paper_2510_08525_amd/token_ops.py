@@ -91,3 +91,27 @@ def quantize(x, out, scales):
     gp = _matrix(scales, "scales", device, (torch.float32,), (groups(cols), rows))
     _call("rlkv_quantize", device, xp, x.stride(0), rows, cols, _DTYPES[x.dtype], op, out.stride(0), gp, scales.stride(0))
     return out
+
+
+def scaled_matmul(a, a_scales, b, b_scales, out):
+    """out [m, n] = a [m, k] @ b [n, k]^T of float8_e4m3fn matrices, a_scales [groups(k), m], b_scales [groups(n), groups(k)]
+    (rlkv_scaled_matmul); out is float32 or bfloat16."""
+    device, scale = a.device, (torch.float32,)
+    ap = _matrix(a, "a", None, (E4M3,))
+    m, k = a.shape
+    bp = _matrix(b, "b", device, (E4M3,))
+    n = b.shape[0]
+    if b.shape[1] != k:
+        raise ValueError(f"b: {b.shape[1]} columns, a has {k}")
+    g = groups(k)
+    sa = _matrix(a_scales, "a_scales", device, scale, (g, m))
+    sb = _matrix(b_scales, "b_scales", device, scale, (groups(n), g))
+    op = _matrix(out, "out", device, (torch.float32, torch.bfloat16), (m, n))
+    _call("rlkv_scaled_matmul", device, ap, _row_stride(a), sa, a_scales.stride(0), bp, _row_stride(b), sb, b_scales.stride(0), m, n,
+          k, op, out.stride(0), _DTYPES[out.dtype])
+    return out
+
+
+def _row_stride(t) -> int:
+    """Distance of two rows; that of a single row, which a tensor may report as anything, is its length."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]

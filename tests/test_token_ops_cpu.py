@@ -40,8 +40,28 @@ def test_quantize_refuses(bad):
     assert rl.load_library().rlkv_quantize(*a.values(), None) == BAD
 
 
+@pytest.mark.parametrize("bad", [
+    dict(a=None), dict(b=None), dict(a_scales=None), dict(b_scales=None), dict(out=None), dict(m=-1), dict(n=-1), dict(k=0), dict(k=-128),
+    dict(k=250), dict(k=8), dict(out_dtype=2), dict(out_dtype=5), dict(a=P + 8), dict(b=P + 4), dict(a_stride=264), dict(b_stride=250),
+    dict(a_stride=-256), dict(b_stride=-16), dict(a_stride=(1 << 23) + 16), dict(b_stride=(1 << 23) + 16), dict(out_stride=299),
+    dict(a_scale_stride=-1), dict(b_scale_stride=-1), dict(a_scales=P + 1), dict(out=P + 1), dict(m=(1 << 24) + 1), dict(n=(1 << 24) + 1),
+    dict(k=(1 << 24) + 16), dict(m=1 << 24, n=1 << 24, out_stride=1 << 24), dict(out_dtype=0, out=P + 2),
+])
+def test_matmul_refuses(bad):
+    a = dict(a=P, a_stride=256, a_scales=P, a_scale_stride=5, b=P, b_stride=256, b_scales=P, b_scale_stride=2, m=5, n=300, k=256, out=P,
+             out_stride=300, out_dtype=rl.RLKV_BF16)
+    a.update(bad)
+    assert rl.load_library().rlkv_scaled_matmul(*a.values(), None) == BAD
+
+
+def test_matmul_of_nothing():
+    call = rl.load_library().rlkv_scaled_matmul
+    assert call(None, 0, None, 0, P, 128, P, 1, 0, 7, 128, P, 7, 1, None) == OK
+    assert call(P, 128, P, 7, None, 0, None, 0, 7, 0, 128, P, 7, 1, None) == OK
+
+
 def test_the_package_offers_them():
-    for name in ("rms_norm", "quantize"):
+    for name in ("rms_norm", "quantize", "scaled_matmul"):
         assert callable(getattr(rl, name))
     with pytest.raises(AttributeError):
         rl.no_such_operator
