@@ -263,6 +263,39 @@ rlkv_status_t rlkv_prefill_attention(rlkv_cache_t* cache, int32_t layer, const v
                                      const int32_t* n_tokens /* host */, int32_t stride_tokens,
                                      void* out /* device */, float softmax_scale, void* stream);
 
+/* Rotation of queries and keys by their positions.  The call works on the packed projections of a token, one row of
+ *     [n_q_heads + 2 n_kv_heads][head_dim] = its query heads, key heads, value heads,
+ * so a projection's output goes into the cache without a copy in between.  The token at chunk index c of sequence b sits at
+ * position i = n + c (n = positions of `layer` cached so far).  Pair p of rotated columns (x, y) of a query or key head becomes
+ *     (x cos t - y sin t, y cos t + x sin t),   t = i * inv_freq[p],
+ * with t exact at any position (64-bit fractions of a turn) and fp32 arithmetic; outputs are rounded once.  The columns
+ * past 2 n_pairs, and values, stay as they are. */
+typedef struct {
+  const double* inv_freq; /* host [n_pairs]; radians a position, finite; copied                                         */
+  int32_t n_pairs;        /* rotated columns / 2: a multiple of 8, at most head_dim / 2                                 */
+  int32_t interleaved;    /* 0: pair p is columns p and p + n_pairs; 1: columns 2 p and 2 p + 1                         */
+} rlkv_rotary_t;
+
+/* rlkv_append / rlkv_append_ragged from packed projections: rotated keys and values go into the stores of `layer`, rotated
+ * queries to q_out.
+ *   qkv      : device, cfg.dtype, [batch][stride_tokens] rows, token_stride elements apart (>= (n_q_heads + 2 n_kv_heads) * head_dim)
+ *   n_tokens : host, [batch], 0 <= n_tokens[b] <= stride_tokens, copied: sequence b appends its first n_tokens[b] rows, as in
+ *              rlkv_append_ragged; NULL: every active sequence appends stride_tokens rows, as in rlkv_append
+ *   q_out    : device, cfg.dtype, [batch][n_q_heads][stride_tokens][head_dim] (with stride_tokens = 1 what
+ *              rlkv_decode_attention takes), or NULL where queries are not wanted; rows that are not appended are not written
+ * Errors as rlkv_append_ragged (RLKV_ERR_CAPACITY: nothing written).  Like the other appends it is not to be recorded into a graph. */
+rlkv_status_t rlkv_append_rotary(rlkv_cache_t* cache, int32_t layer, const void* qkv /* device */, int64_t token_stride,
+                                 const int32_t* n_tokens /* host */, int32_t stride_tokens, const rlkv_rotary_t* rotary /* host */,
+                                 void* q_out /* device */, void* stream);
+
+/* The same rotation with everything handed out, heads first, as rlkv_prefill_attention and rlkv_append_decode take it (they append
+ * by themselves); the cache does not change and only its lengths are read.
+ *   q_out        : device, [batch][n_q_heads][stride_tokens][head_dim]
+ *   k_out, v_out : device, [batch][n_kv_heads][stride_tokens][head_dim]; rows past a sequence's count are not written */
+rlkv_status_t rlkv_rotary(rlkv_cache_t* cache, int32_t layer, const void* qkv /* device */, int64_t token_stride,
+                          const int32_t* n_tokens /* host */, int32_t stride_tokens, const rlkv_rotary_t* rotary /* host */,
+                          void* q_out /* device */, void* k_out /* device */, void* v_out /* device */, void* stream);
+
 /* Measurement aid.  After rlkv_profile_enable, every rlkv_decode_attention / rlkv_append_decode /
  * rlkv_prefill_attention call on this cache attaches a pair of HIP events to its attention kernel
  * (the kernel that streams the K/V stores); they receive that kernel's own begin and end

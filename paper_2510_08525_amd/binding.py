@@ -39,6 +39,19 @@ class _Config(ctypes.Structure):
     ]
 
 
+class _Rotary(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("n_pairs", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+class Rotary:
+    """How queries and keys turn with their positions (rlkv_rotary_t): radians a position of each pair of columns."""
+
+    def __init__(self, inv_freq: Sequence[float], interleaved: bool = False):
+        self.inv_freq = np.ascontiguousarray(np.asarray(inv_freq, dtype=np.float64).reshape(-1))
+        self._struct = _Rotary(self.inv_freq.ctypes.data, self.inv_freq.size, 1 if interleaved else 0)
+        self.address = ctypes.addressof(self._struct)
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -91,6 +104,8 @@ def load_library():
         "rlkv_cache_kernel": (i32, [vp]),
         "rlkv_pool_pages_free": (ctypes.c_int64, [vp]),
         "rlkv_pool_shuffle": (i32, [vp, ctypes.c_uint64]),
+        "rlkv_append_rotary": (i32, [vp, i32, vp, i64, vp, i32, vp, vp, vp]),
+        "rlkv_rotary": (i32, [vp, i32, vp, i64, vp, i32, vp, vp, vp, vp, vp]),
         "rlkv_rms_norm": (i32, [vp, i64, vp, i64, vp, f32, i32, i32, i32, vp, i64, vp, i64, i32, vp, i64, vp]),
         "rlkv_quantize": (i32, [vp, i64, i32, i32, i32, vp, i64, vp, i64, vp]),
         "rlkv_scaled_matmul": (i32, [vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, i32, vp, i64, i32, vp]),
@@ -109,7 +124,7 @@ EXPORTED_SYMBOLS = (
     "rlkv_profile_collect", "rlkv_get_lengths",
     "rlkv_get_slot_positions", "rlkv_resident_bytes", "rlkv_probe_stream_read", "rlkv_plan_shares", "rlkv_plan_whole_pairs", "rlkv_plan_list_whole", "rlkv_plan_list_kind", "rlkv_plan_merge_inside", "rlkv_plan_static_scratch", "rlkv_plan_narrow_split", "rlkv_plan_blend_form", "rlkv_plan_prefill_form", "rlkv_plan_prefill_rows", "rlkv_plan_prefill_block", "rlkv_plan_prefill_item", "rlkv_cache_kernel", "rlkv_pool_pages_free",
     "rlkv_pool_shuffle", "rlkv_status_string",
-    "rlkv_rms_norm", "rlkv_quantize", "rlkv_scaled_matmul",
+    "rlkv_append_rotary", "rlkv_rotary", "rlkv_rms_norm", "rlkv_quantize", "rlkv_scaled_matmul",
 )
 
 
@@ -197,6 +212,21 @@ def rlkv_set_gates(handle: int, gates, stream: int = 0):
     arr = None if gates is None else np.ascontiguousarray(np.asarray(gates, dtype=np.float32).reshape(-1))
     _check(load_library().rlkv_set_gates(handle, arr.ctypes.data if arr is not None else None, stream or None),
            "rlkv_set_gates")
+
+
+def rlkv_append_rotary(handle: int, layer: int, qkv_ptr: int, token_stride: int, n_tokens: Optional[Sequence[int]],
+                       stride_tokens: int, rotary: Rotary, q_out_ptr: int, stream: int = 0):
+    cnt = None if n_tokens is None else np.ascontiguousarray(np.asarray(n_tokens, dtype=np.int32))
+    _check(load_library().rlkv_append_rotary(handle, layer, qkv_ptr or None, token_stride, None if cnt is None else cnt.ctypes.data,
+                                             stride_tokens, rotary.address, q_out_ptr or None, stream or None), "rlkv_append_rotary")
+
+
+def rlkv_rotary(handle: int, layer: int, qkv_ptr: int, token_stride: int, n_tokens: Optional[Sequence[int]], stride_tokens: int,
+                rotary: Rotary, q_out_ptr: int, k_out_ptr: int, v_out_ptr: int, stream: int = 0):
+    cnt = None if n_tokens is None else np.ascontiguousarray(np.asarray(n_tokens, dtype=np.int32))
+    _check(load_library().rlkv_rotary(handle, layer, qkv_ptr or None, token_stride, None if cnt is None else cnt.ctypes.data,
+                                      stride_tokens, rotary.address, q_out_ptr or None, k_out_ptr or None, v_out_ptr or None,
+                                      stream or None), "rlkv_rotary")
 
 
 def rlkv_append_decode(handle: int, layer: int, k_ptr: int, v_ptr: int, q_ptr: int, out_ptr: int,
@@ -419,6 +449,41 @@ class Cache:
         shp = (s["batch"], s["n_kv_heads"], stride, s["head_dim"])
         rlkv_append_ragged(self.handle, layer, self._ptr(k, shp, "k"), self._ptr(v, shp, "v"), n_tokens, stride,
                            self._stream())
+
+    def _packed(self, qkv, n_tokens):
+        """Address, token stride and tokens per sequence of packed projections [batch, tokens, >= (q + 2 kv heads) * head_dim]."""
+        s = self.shape
+        row = (s["n_q_heads"] + 2 * s["n_kv_heads"]) * s["head_dim"]
+        if qkv.device != self.device or qkv.dtype != self.torch_dtype:
+            raise ValueError(f"qkv: need a {self.torch_dtype} tensor on {self.device}")
+        if qkv.dim() != 3 or qkv.shape[0] != s["batch"] or qkv.shape[2] != row:
+            raise ValueError(f"qkv: shape {tuple(qkv.shape)} is not (batch, tokens, {row})")
+        B, T, _ = qkv.shape
+        token = qkv.stride(1) if T > 1 else qkv.stride(0) if B > 1 else row
+        if qkv.stride(2) != 1 or token < row or (B > 1 and T > 1 and qkv.stride(0) != T * token):
+            raise ValueError("qkv: need contiguous rows at equal distances")
+        if n_tokens is not None and len(n_tokens) != B:
+            raise ValueError("n_tokens must have batch entries")
+        return qkv.data_ptr(), token, T
+
+    def append_rotary(self, layer: int, qkv, n_tokens, rotary: Rotary, q_out=None):
+        """Rotates and appends packed projections [batch, tokens, (q + 2 kv heads) * head_dim]; rotated queries to q_out
+        ([batch, q heads, tokens, head_dim], for one token also without that axis).  n_tokens None: all tokens of every active sequence."""
+        s = self.shape
+        ptr, token, T = self._packed(qkv, n_tokens)
+        out = 0
+        if q_out is not None:
+            out = self._ptr(q_out, self._q_shape if T == 1 and q_out.dim() == 3 else (s["batch"], s["n_q_heads"], T, s["head_dim"]), "q_out")
+        rlkv_append_rotary(self.handle, layer, ptr, token, n_tokens, T, rotary, out, self._stream())
+
+    def rotary(self, layer: int, qkv, n_tokens, rotary: Rotary, q_out, k_out, v_out):
+        """Rotates packed projections and hands them out heads first, as prefill_attention and append_decode take them."""
+        s = self.shape
+        ptr, token, T = self._packed(qkv, n_tokens)
+        kv = (s["batch"], s["n_kv_heads"], T, s["head_dim"])
+        q = self._ptr(q_out, self._q_shape if T == 1 and q_out.dim() == 3 else (s["batch"], s["n_q_heads"], T, s["head_dim"]), "q_out")
+        rlkv_rotary(self.handle, layer, ptr, token, n_tokens, T, rotary, q, self._ptr(k_out, kv, "k_out"), self._ptr(v_out, kv, "v_out"),
+                    self._stream())
 
     def decode_attention(self, layer: int, q, out, softmax_scale: float):
         shp = self._q_shape

@@ -13,34 +13,12 @@
 #include <string.h>
 #include <type_traits>
 
+#include "append_slots.h"
 #include "rlkv_internal.h"
 #include "tile_rows.h"
 
 namespace rlkv {
 namespace {
-
-struct TileRange { int first, count; };
-
-__device__ inline TileRange tiles_of(int slot_lo, int slot_hi /* exclusive */) {
-  if (slot_hi <= slot_lo) return {0, 0};
-  const int t0 = slot_lo / kTile, t1 = (slot_hi - 1) / kTile;
-  return {t0, t1 - t0 + 1};
-}
-
-// Appended position that ends in `slot` after the append, or -1 if the slot is untouched.
-__device__ inline int source_position(bool full, int slot, int len_old, int len_new, int S, int R) {
-  int p;
-  if (full || slot < S) {
-    p = slot;
-  } else {
-    const int r = slot - S;
-    if (r >= R) return -1;                       // padding slot behind the ring
-    const int last = len_new - 1 - S;            // ring index space of the newest position
-    if (last < r) return -1;
-    p = S + r + R * ((last - r) / R);            // largest p < len_new with (p - S) % R == r
-  }
-  return (p >= len_old && p < len_new) ? p : -1;
-}
 
 // The compressed heads of a layer, in the arguments of an append that is for them only (n < 0: not given, all heads).
 struct NoRings {};
@@ -79,31 +57,7 @@ __global__ __launch_bounds__(kBlock) void append_kernel(DeviceView dv, int layer
   const int len_new = len_old + n_tok;
   const bool full = !given && dv.full_mask[layer * dv.n_kv_heads + h] != 0;
 
-  int tile = -1;
-  if (n_tok > 0 && !(RINGS && full)) {
-    if (full) {
-      const TileRange t = tiles_of(len_old, len_new);
-      if (job < t.count) tile = t.first + job;
-    } else {
-      // up to three slot ranges change: new sinks, and the ring range (which may wrap)
-      const TileRange ta = tiles_of(len_old < S ? len_old : S, len_new < S ? len_new : S);
-      const int p0 = len_old > S ? len_old : S;
-      const int c = len_new - p0;                 // positions that go to the ring
-      TileRange tb = {0, 0}, tc = {0, 0};
-      if (c >= R) {
-        tb = tiles_of(S, S + R);
-      } else if (c > 0) {
-        const int r0 = (p0 - S) % R;
-        const int r1 = r0 + c;
-        tb = tiles_of(S + r0, S + (r1 < R ? r1 : R));
-        if (r1 > R) tc = tiles_of(S, S + r1 - R);
-      }
-      int j = job;
-      if (j < ta.count) tile = ta.first + j;
-      else if ((j -= ta.count) < tb.count) tile = tb.first + j;
-      else if ((j -= tb.count) < tc.count) tile = tc.first + j;
-    }
-  }
+  const int tile = n_tok > 0 && !(RINGS && full) ? tile_of_job(full, job, len_old, len_new, S, R) : -1;
 
   if (tile >= 0) {
     constexpr int kChunks = kHeadDim * sizeof(T) / 16;    // 16-byte chunks per row
@@ -227,10 +181,7 @@ hipError_t launch_append(const DeviceView& dv, int layer, const int32_t* len_in,
   const SeqCounts none = {};
   const SeqCounts& sq = seqs ? *seqs : none;
   const int ragged = seqs != nullptr;
-  // Tiles a pair can touch: a range of c >= 1 slots touches at most (c + 30) / 32 + 1 tiles;
-  // a full head has one range, a compressed head up to three (new sinks, ring, wrapped
-  // ring) whose sizes add up to at most max_tokens.  One token touches one tile.
-  const int jobs = max_tokens <= 1 ? 1 : (max_tokens + 3 * (kTile - 2)) / kTile + 3;
+  const int jobs = append_jobs(max_tokens);
   const dim3 grid(jobs, dv.n_pairs), block(kBlock);
   if (dv.dtype == RLKV_F32) {
     hipLaunchKernelGGL((append_kernel<RLKV_KERNEL_VALU, float, false>), grid, block, 0, stream, dv, layer,

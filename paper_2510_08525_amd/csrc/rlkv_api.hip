@@ -1,5 +1,6 @@
 // Host side of librlkv: argument validation, arena planning, the C-ABI entry points.
 // All validation runs before the first HIP call, so the error paths work without a GPU.
+#include <math.h>
 #include <stdlib.h>
 #include <string.h>
 
@@ -10,6 +11,7 @@
 #include <vector>
 
 #include "rlkv_internal.h"
+#include "rotary.h"
 
 using namespace rlkv;
 
@@ -567,10 +569,25 @@ struct PrefillArgs {
   float softmax_scale;
 };
 
+// What rlkv_append_rotary has in the place of k and v.
+struct RotaryArgs {
+  RotaryCall call;
+  RotaryTurns turns;
+};
+
+static hipError_t launch_append_rotary(rlkv_cache& cache, int layer, const RotaryArgs& args, int uniform, int max_tokens,
+                                       const SeqCounts* seqs, hipStream_t s) {
+  RotaryCall call = args.call;
+  call.uniform = uniform;
+  call.max_tokens = max_tokens;
+  const int par = cache.parity[layer];
+  return launch_rotary(cache.dv, layer, len_of(cache.dv, par, layer), len_of(cache.dv, par ^ 1, layer), call, args.turns, seqs, true, s);
+}
+
 static rlkv_status_t append_impl(rlkv_cache_t* cache, int32_t layer, const void* k, const void* v,
                                  const int32_t* n_tokens, int32_t uniform, int32_t stride, void* stream,
-                                 const PrefillArgs* prefill = nullptr) {
-  if (!cache || !k || !v) return RLKV_ERR_INVALID_ARG;
+                                 const PrefillArgs* prefill = nullptr, const RotaryArgs* rotary = nullptr) {
+  if (!cache || (!rotary && (!k || !v))) return RLKV_ERR_INVALID_ARG;
   if (layer < 0 || layer >= cache->cfg.n_layers) return RLKV_ERR_INVALID_ARG;
   const int B = cache->cfg.batch;
   int max_tok = 0;
@@ -676,6 +693,7 @@ static rlkv_status_t append_impl(rlkv_cache_t* cache, int32_t layer, const void*
   }
   if (prefill ? launch_append_rings(cache->dv, layer, len_of(cache->dv, par, layer), k, v, stride, seqs, max_tok,
                                     cache->mask.data() + (size_t)layer * cache->cfg.n_kv_heads, s) != hipSuccess
+      : rotary ? launch_append_rotary(*cache, layer, *rotary, uniform, max_tok, n_tokens ? &seqs : nullptr, s) != hipSuccess
               : launch_append(cache->dv, layer, len_of(cache->dv, par, layer), len_of(cache->dv, par ^ 1, layer), k, v,
                               uniform, stride, n_tokens ? &seqs : nullptr, max_tok, s) != hipSuccess)
     return RLKV_ERR_HIP;
@@ -818,6 +836,77 @@ rlkv_status_t rlkv_prefill_attention(rlkv_cache_t* cache, int32_t layer, const v
   if (stride_tokens > cache->cfg.prefill_tokens) return RLKV_ERR_INVALID_ARG;
   const PrefillArgs args{q, out, softmax_scale};
   return append_impl(cache, layer, k, v, n_tokens, 0, stride_tokens, stream, &args);
+}
+
+// The checks of the two rotating calls, and what their kernels get.
+static rlkv_status_t rotary_args(rlkv_cache_t* cache, int32_t layer, const void* qkv, int64_t token_stride, int32_t stride_tokens,
+                                 const rlkv_rotary_t* rotary, RotaryArgs* args) {
+  if (!cache || !qkv || !rotary || !rotary->inv_freq) return RLKV_ERR_INVALID_ARG;
+  if (layer < 0 || layer >= cache->cfg.n_layers) return RLKV_ERR_INVALID_ARG;
+  const int pairs = rotary->n_pairs;
+  if (pairs < 8 || pairs > kHeadDim / 2 || pairs % 8 != 0) return RLKV_ERR_INVALID_ARG;
+  if (rotary->interleaved < 0 || rotary->interleaved > 1) return RLKV_ERR_INVALID_ARG;
+  const size_t e = cache->cfg.dtype == RLKV_F32 ? 4 : 2;
+  if (stride_tokens < 1 || token_stride < (int64_t)(cache->cfg.n_q_heads + 2 * cache->cfg.n_kv_heads) * kHeadDim) return RLKV_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(qkv) % e != 0) return RLKV_ERR_INVALID_ARG;
+  *args = {};
+  for (int i = 0; i < pairs; ++i) {
+    if (!isfinite(rotary->inv_freq[i])) return RLKV_ERR_INVALID_ARG;
+    // (whole turns do not matter, and what is left is below 1 unless it was rounded up to it)
+    double t = rotary->inv_freq[i] * 0.15915494309189533577;          // 1 / (2 pi)
+    t -= floor(t);
+    args->turns.turn[i] = t < 1.0 ? (uint64_t)ldexp(t, 64) : 0;
+  }
+  args->turns.pairs = pairs;
+  args->turns.interleaved = rotary->interleaved;
+  args->call.qkv = qkv;
+  args->call.token_stride = token_stride;
+  args->call.stride_tokens = stride_tokens;
+  args->call.whole_in = reinterpret_cast<uintptr_t>(qkv) % 16 == 0 && token_stride * (int64_t)e % 16 == 0;
+  return RLKV_OK;
+}
+
+rlkv_status_t rlkv_append_rotary(rlkv_cache_t* cache, int32_t layer, const void* qkv, int64_t token_stride, const int32_t* n_tokens,
+                                 int32_t stride_tokens, const rlkv_rotary_t* rotary, void* q_out, void* stream) {
+  RotaryArgs args;
+  if (rlkv_status_t st = rotary_args(cache, layer, qkv, token_stride, stride_tokens, rotary, &args)) return st;
+  if (reinterpret_cast<uintptr_t>(q_out) % (cache->cfg.dtype == RLKV_F32 ? 4 : 2) != 0) return RLKV_ERR_INVALID_ARG;
+  args.call.q_out = q_out;
+  args.call.whole_out = reinterpret_cast<uintptr_t>(q_out) % 16 == 0;
+  return append_impl(cache, layer, nullptr, nullptr, n_tokens, n_tokens ? 0 : stride_tokens, stride_tokens, stream, nullptr, &args);
+}
+
+rlkv_status_t rlkv_rotary(rlkv_cache_t* cache, int32_t layer, const void* qkv, int64_t token_stride, const int32_t* n_tokens,
+                          int32_t stride_tokens, const rlkv_rotary_t* rotary, void* q_out, void* k_out, void* v_out, void* stream) {
+  RotaryArgs args;
+  if (rlkv_status_t st = rotary_args(cache, layer, qkv, token_stride, stride_tokens, rotary, &args)) return st;
+  if (!q_out || !k_out || !v_out) return RLKV_ERR_INVALID_ARG;
+  const uintptr_t any = reinterpret_cast<uintptr_t>(q_out) | reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out);
+  if (any % (cache->cfg.dtype == RLKV_F32 ? 4 : 2) != 0) return RLKV_ERR_INVALID_ARG;
+  const int B = cache->cfg.batch;
+  int max_tok = n_tokens ? 0 : stride_tokens;
+  for (int b = 0; n_tokens && b < B; ++b) {
+    if (n_tokens[b] < 0 || n_tokens[b] > stride_tokens) return RLKV_ERR_INVALID_ARG;
+    max_tok = std::max(max_tok, n_tokens[b]);
+  }
+  if (max_tok == 0) return RLKV_OK;
+  if (hipSetDevice(cache->cfg.device) != hipSuccess) return RLKV_ERR_HIP;
+  hipStream_t s = as_stream(stream);
+  cache->last_stream = s;
+  SeqCounts seqs = {};
+  if (n_tokens) {
+    seqs.in_args = B <= kArgSeqs;
+    if (seqs.in_args) memcpy(seqs.tok, n_tokens, (size_t)B * sizeof(int32_t));
+    else if (launch_write_values(cache->dv.append_cnt, n_tokens, B, s) != hipSuccess) return RLKV_ERR_HIP;
+  }
+  args.call.q_out = q_out;
+  args.call.k_out = k_out;
+  args.call.v_out = v_out;
+  args.call.whole_out = any % 16 == 0;
+  args.call.uniform = n_tokens ? 0 : stride_tokens;
+  args.call.max_tokens = max_tok;
+  return launch_rotary(cache->dv, layer, len_of(cache->dv, cache->parity[layer], layer), nullptr, args.call, args.turns,
+                       n_tokens ? &seqs : nullptr, false, s) == hipSuccess ? RLKV_OK : RLKV_ERR_HIP;
 }
 
 // Is `s` recording into a graph?  (A failing query counts as "no".)

@@ -36,6 +36,42 @@ template <bool NT> __device__ __forceinline__ void tile_store(char* p, const uin
   __builtin_nontemporal_store(v, reinterpret_cast<row_x4*>(p));
 }
 
+// Where row `slot`'s 16-byte chunk of K is in the LDS image (V: lds.v + slot * kTileRowStride + chunk * 16).
+__device__ __forceinline__ int k_unit(int slot, int chunk) { return (slot >> 4) * 256 + chunk * 16 + ((slot + chunk) & 15); }
+
+// A tile whose rows are in LDS (all threads have passed a barrier) goes out; keep(slot): the slot keeps what it holds.
+template <bool NT, typename Keep>
+__device__ __forceinline__ void tile_from_lds(const TileRowsLds& lds, const Keep& keep, char* __restrict__ tile_base) {
+  constexpr int kUnits = kTile * 16 / kBlock;
+  const int tid = threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i) {                     // K: unit u of the tile = [half][chunk][slot % 16]
+    const int u = tid + i * kBlock, hf = u >> 8, chunk = (u >> 4) & 15, s16 = u & 15;
+    if (!keep(hf * 16 + s16))
+      tile_store<NT>(tile_base + u * 16, lds.k[hf * 256 + chunk * 16 + ((s16 + chunk) & 15)]);
+  }
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i) {                     // V: unit u = [d / 16][kb][d % 16], eight slots of one d
+    const int u = tid + i * kBlock, kb = (u >> 4) & 3, d = (u >> 6) * 16 + (u & 15);
+    uint32_t val[8];
+    unsigned have = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int slot = (e >> 2) * 16 + kb * 4 + (e & 3);
+      val[e] = *reinterpret_cast<const uint16_t*>(lds.v + slot * kTileRowStride + d * 2);
+      have |= keep(slot) ? 0u : 1u << e;
+    }
+    char* dst = tile_base + kTileBytes / 2 + u * 16;
+    if (have == 0xffu) {
+      tile_store<NT>(dst, make_uint4(val[0] | val[1] << 16, val[2] | val[3] << 16, val[4] | val[5] << 16, val[6] | val[7] << 16));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (have & (1u << e)) reinterpret_cast<uint16_t*>(dst)[e] = (uint16_t)val[e];
+    }
+  }
+}
+
 // row_of(slot): the slot's source row, -1 = none.  keep(slot): the slot keeps what it holds (it has no source row); the others
 // without one are written as zeros.  k_rows / v_rows: row 0 of the pair (row r at r * kHeadDim).  Returns whether this thread moved a V
 // value beyond the fp16 range.
@@ -65,37 +101,12 @@ __device__ __forceinline__ bool rows_to_tile(TileRowsLds& lds, const RowOf& row_
 #pragma unroll
   for (int i = 0; i < kUnits; ++i) {
     const int u = tid + i * kBlock, slot = u >> 4, chunk = u & 15;
-    lds.k[(slot >> 4) * 256 + chunk * 16 + ((slot + chunk) & 15)] = kv[i];
+    lds.k[k_unit(slot, chunk)] = kv[i];
     *reinterpret_cast<uint4*>(lds.v + slot * kTileRowStride + chunk * 16) = vv[i];
     wide |= any_beyond_fp16(vv[i].x) || any_beyond_fp16(vv[i].y) || any_beyond_fp16(vv[i].z) || any_beyond_fp16(vv[i].w);
   }
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kUnits; ++i) {                     // K: unit u of the tile = [half][chunk][slot % 16]
-    const int u = tid + i * kBlock, hf = u >> 8, chunk = (u >> 4) & 15, s16 = u & 15;
-    if (!keep(hf * 16 + s16))
-      tile_store<NT>(tile_base + u * 16, lds.k[hf * 256 + chunk * 16 + ((s16 + chunk) & 15)]);
-  }
-#pragma unroll
-  for (int i = 0; i < kUnits; ++i) {                     // V: unit u = [d / 16][kb][d % 16], eight slots of one d
-    const int u = tid + i * kBlock, kb = (u >> 4) & 3, d = (u >> 6) * 16 + (u & 15);
-    uint32_t val[8];
-    unsigned have = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int slot = (e >> 2) * 16 + kb * 4 + (e & 3);
-      val[e] = *reinterpret_cast<const uint16_t*>(lds.v + slot * kTileRowStride + d * 2);
-      have |= keep(slot) ? 0u : 1u << e;
-    }
-    char* dst = tile_base + kTileBytes / 2 + u * 16;
-    if (have == 0xffu) {
-      tile_store<NT>(dst, make_uint4(val[0] | val[1] << 16, val[2] | val[3] << 16, val[4] | val[5] << 16, val[6] | val[7] << 16));
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (have & (1u << e)) reinterpret_cast<uint16_t*>(dst)[e] = (uint16_t)val[e];
-    }
-  }
+  tile_from_lds<NT>(lds, keep, tile_base);
   return wide;
 }
 

@@ -65,3 +65,9 @@ def test_the_package_offers_them():
         assert callable(getattr(rl, name))
     with pytest.raises(AttributeError):
         rl.no_such_operator
+
+
+def test_rotary_without_a_cache_is_refused():
+    lib, r = rl.load_library(), rl.Rotary([1.0] * 64)
+    assert lib.rlkv_append_rotary(None, 0, P, 1024, None, 1, r.address, P, None) == BAD
+    assert lib.rlkv_rotary(None, 0, P, 1024, None, 1, r.address, P, P, P, None) == BAD
