@@ -486,6 +486,37 @@ rlkv_status_t rlkv_scaled_matmul(const void* a /* device */, int64_t a_stride, c
                                  const float* b_scales /* device */, int64_t b_scale_stride, int32_t m, int32_t n, int32_t k,
                                  void* out /* device */, int64_t out_stride, int32_t out_dtype, void* stream);
 
+/* Log probabilities of given tokens and what belongs to them, in one pass over rows of logits (x = scale * logits, scale > 0: one over
+ * the temperature; p = softmax(x)):
+ *     lse = log sum exp x      logprobs = x[token] - lse      entropy = - sum p log p
+ *   logits : device, `dtype` (RLKV_F32 or RLKV_BF16), [rows][vocab]; rows <= 2^20, vocab <= 2^24
+ *   tokens, logprobs : device, int32 and fp32 [rows]; both or neither.  A row whose token is not in [0, vocab) is not scored:
+ *                      its logprobs is 0
+ *   entropy, lse     : device, fp32 [rows]; may be NULL
+ *   top, top_ids, top_logprobs : the `top` (0 .. 32, at most vocab) most likely tokens of a row, int32 and fp32 [rows][top], most
+ *                      likely first, equal logits by the lower token
+ *   workspace : device, 8-byte aligned, at least rlkv_token_logprobs_workspace bytes (which may be 0; then it may be NULL); its
+ *               contents do not matter.  Calls that may overlap in time need one each.
+ * Masked logits (-inf) have probability 0 and count as 0 in the entropy.  A row of nothing else has lse and log probabilities of
+ * -inf and entropy 0; a row with +inf or NaN gives NaN (and NaN ranks above all in its list).  Equal calls give equal bits. */
+size_t rlkv_token_logprobs_workspace(int32_t rows, int32_t vocab, int32_t top);
+rlkv_status_t rlkv_token_logprobs(const void* logits /* device */, int64_t stride, int32_t rows, int32_t vocab, int32_t dtype,
+                                  float scale, const int32_t* tokens /* device */, float* logprobs /* device */,
+                                  float* entropy /* device */, float* lse /* device */, int32_t top, int32_t* top_ids /* device */,
+                                  float* top_logprobs /* device */, void* workspace /* device */, size_t workspace_bytes, void* stream);
+
+/* The way back (the policy gradient of a rollout): with p and x as above, lse and entropy as the call above left them,
+ *     grad_logits[i] = scale * (grad_logprobs * ((i == token) - p[i]) - grad_entropy * p[i] * (log p[i] + entropy))
+ *   tokens, grad_logprobs : device, int32 and fp32 [rows]; both or neither.  Rows that are not scored have no part of the first kind
+ *   entropy, grad_entropy : device, fp32 [rows]; both or neither
+ *   grad_logits : device, `dtype`, [rows][vocab]; may be logits itself (same pointer and stride)
+ * A row of masked logits only (lse below -1e30) has gradients of 0. */
+rlkv_status_t rlkv_token_logprobs_grad(const void* logits /* device */, int64_t stride, int32_t rows, int32_t vocab, int32_t dtype,
+                                       float scale, const int32_t* tokens /* device */, const float* lse /* device */,
+                                       const float* entropy /* device */, const float* grad_logprobs /* device */,
+                                       const float* grad_entropy /* device */, void* grad_logits /* device */, int64_t grad_stride,
+                                       void* stream);
+
 /* Measurement aid, independent of any cache: one plain streaming read of `bytes` (rounded down to
  * whole 16 KiB blocks) of `buf` with 128-bit non-temporal loads and no arithmetic, launched with
  * `workgroups` workgroups of 256 threads on `stream` of the current device.  Timed by the caller,

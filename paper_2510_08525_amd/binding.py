@@ -109,6 +109,9 @@ def load_library():
         "rlkv_rms_norm": (i32, [vp, i64, vp, i64, vp, f32, i32, i32, i32, vp, i64, vp, i64, i32, vp, i64, vp]),
         "rlkv_quantize": (i32, [vp, i64, i32, i32, i32, vp, i64, vp, i64, vp]),
         "rlkv_scaled_matmul": (i32, [vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, i32, vp, i64, i32, vp]),
+        "rlkv_token_logprobs_workspace": (sz, [i32, i32, i32]),
+        "rlkv_token_logprobs": (i32, [vp, i64, i32, i32, i32, f32, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]),
+        "rlkv_token_logprobs_grad": (i32, [vp, i64, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, i64, vp]),
         "rlkv_status_string": (ctypes.c_char_p, [i32]),
     }
     for name, (res, args) in sigs.items():
@@ -125,6 +128,7 @@ EXPORTED_SYMBOLS = (
     "rlkv_get_slot_positions", "rlkv_resident_bytes", "rlkv_probe_stream_read", "rlkv_plan_shares", "rlkv_plan_whole_pairs", "rlkv_plan_list_whole", "rlkv_plan_list_kind", "rlkv_plan_merge_inside", "rlkv_plan_static_scratch", "rlkv_plan_narrow_split", "rlkv_plan_blend_form", "rlkv_plan_prefill_form", "rlkv_plan_prefill_rows", "rlkv_plan_prefill_block", "rlkv_plan_prefill_item", "rlkv_cache_kernel", "rlkv_pool_pages_free",
     "rlkv_pool_shuffle", "rlkv_status_string",
     "rlkv_append_rotary", "rlkv_rotary", "rlkv_rms_norm", "rlkv_quantize", "rlkv_scaled_matmul",
+    "rlkv_token_logprobs_workspace", "rlkv_token_logprobs", "rlkv_token_logprobs_grad",
 )
 
 
@@ -285,6 +289,11 @@ def rlkv_get_slot_positions(handle: int, layer: int, kv_head: int, seq: int, win
 
 def rlkv_resident_bytes(handle: int) -> int:
     return int(load_library().rlkv_resident_bytes(handle))
+
+
+def rlkv_token_logprobs_workspace(rows: int, vocab: int, top: int = 0) -> int:
+    """Bytes of workspace a token_logprobs call of these sizes needs (0: none)."""
+    return int(load_library().rlkv_token_logprobs_workspace(rows, vocab, top))
 
 
 def rlkv_probe_stream_read(buf_ptr: int, nbytes: int, sink_ptr: int, workgroups: int, stream: int = 0):

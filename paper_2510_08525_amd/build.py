@@ -14,7 +14,7 @@ OBJ_DIR = os.path.join(PKG, "_build")
 
 SOURCES = ["rlkv_api.hip", "append_evict.hip", "worklist_combine.hip", "decode_valu.hip", "decode_mfma.hip",
            "prefill_mfma.hip", "stream_probe.hip", "share_plan.hip", "token_api.hip", "rms_norm.hip",
-           "scaled_matmul.hip", "rotary.hip"]
+           "scaled_matmul.hip", "rotary.hip", "token_logprobs.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall",

@@ -23,6 +23,8 @@ int32_t whole(const void* p, int64_t stride, int dtype, size_t to = 16) {
   return p && aligned(p, to) && (stride * (int64_t)bytes_of(dtype)) % (int64_t)to == 0;
 }
 
+constexpr int32_t kMostLogitRows = 1 << 20, kMostVocab = 1 << 24;
+
 rlkv_status_t norm_call(NormCall& c, int dtype, int out_dtype, void* stream) {
   if (dtype != RLKV_F32 && dtype != RLKV_BF16) return RLKV_ERR_INVALID_ARG;
   if (out_dtype != dtype && out_dtype != RLKV_E4M3) return RLKV_ERR_INVALID_ARG;
@@ -94,6 +96,59 @@ rlkv_status_t rlkv_scaled_matmul(const void* a, int64_t a_stride, const float* a
   c.out = out; c.out_stride = out_stride;
   c.whole_out = whole(out, out_stride, out_dtype, 4 * bytes_of(out_dtype));
   return launch_matmul(c, out_dtype == RLKV_BF16, as_stream(stream)) == hipSuccess ? RLKV_OK : RLKV_ERR_HIP;
+}
+
+static bool logits_valid(int32_t rows, int32_t vocab, int32_t dtype, float scale) {
+  if (dtype != RLKV_F32 && dtype != RLKV_BF16) return false;
+  return rows >= 0 && rows <= kMostLogitRows && vocab >= 1 && vocab <= kMostVocab && scale > 0.f && !isinf(scale);
+}
+
+size_t rlkv_token_logprobs_workspace(int32_t rows, int32_t vocab, int32_t top) {
+  if (rows < 1 || rows > kMostLogitRows || vocab < 1 || vocab > kMostVocab || top < 0 || top > kMostTop) return 0;
+  return logprob_workspace(rows, vocab, top);
+}
+
+rlkv_status_t rlkv_token_logprobs(const void* logits, int64_t stride, int32_t rows, int32_t vocab, int32_t dtype, float scale,
+                                  const int32_t* tokens, float* logprobs, float* entropy, float* lse, int32_t top, int32_t* top_ids,
+                                  float* top_logprobs, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!logits_valid(rows, vocab, dtype, scale)) return RLKV_ERR_INVALID_ARG;
+  if (top < 0 || top > kMostTop || top > vocab) return RLKV_ERR_INVALID_ARG;
+  if (rows == 0) return RLKV_OK;
+  if (!readable(logits, stride, dtype)) return RLKV_ERR_INVALID_ARG;
+  if ((tokens != nullptr) != (logprobs != nullptr)) return RLKV_ERR_INVALID_ARG;
+  if (top > 0 && (!top_ids || !top_logprobs)) return RLKV_ERR_INVALID_ARG;
+  if (!aligned(tokens, 4) || !aligned(logprobs, 4) || !aligned(entropy, 4) || !aligned(lse, 4) || !aligned(top_ids, 4) ||
+      !aligned(top_logprobs, 4) || !aligned(workspace, 8))
+    return RLKV_ERR_INVALID_ARG;
+  const size_t need = logprob_workspace(rows, vocab, top);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return RLKV_ERR_INVALID_ARG;
+  LogprobCall c = {};
+  c.logits = logits; c.stride = stride;
+  c.rows = rows; c.vocab = vocab; c.scale = scale;
+  c.tokens = tokens; c.logprobs = logprobs; c.entropy = entropy; c.lse = lse;
+  c.top = top; c.top_ids = top_ids; c.top_logprobs = top_logprobs;
+  c.workspace = workspace;
+  c.whole = whole(logits, stride, dtype);
+  return launch_logprobs(c, dtype, as_stream(stream)) == hipSuccess ? RLKV_OK : RLKV_ERR_HIP;
+}
+
+rlkv_status_t rlkv_token_logprobs_grad(const void* logits, int64_t stride, int32_t rows, int32_t vocab, int32_t dtype, float scale,
+                                       const int32_t* tokens, const float* lse, const float* entropy, const float* grad_logprobs,
+                                       const float* grad_entropy, void* grad_logits, int64_t grad_stride, void* stream) {
+  if (!logits_valid(rows, vocab, dtype, scale)) return RLKV_ERR_INVALID_ARG;
+  if (rows == 0) return RLKV_OK;
+  if (!readable(logits, stride, dtype) || !writable(grad_logits, grad_stride, rows, vocab, dtype) || !lse) return RLKV_ERR_INVALID_ARG;
+  if ((tokens != nullptr) != (grad_logprobs != nullptr) || (entropy != nullptr) != (grad_entropy != nullptr)) return RLKV_ERR_INVALID_ARG;
+  if (!aligned(tokens, 4) || !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(grad_logprobs, 4) || !aligned(grad_entropy, 4))
+    return RLKV_ERR_INVALID_ARG;
+  LogprobGradCall c = {};
+  c.logits = logits; c.stride = stride;
+  c.rows = rows; c.vocab = vocab; c.scale = scale;
+  c.tokens = tokens; c.lse = lse; c.entropy = entropy; c.grad_logprobs = grad_logprobs; c.grad_entropy = grad_entropy;
+  c.out = grad_logits; c.out_stride = grad_stride;
+  c.whole = whole(logits, stride, dtype);
+  c.whole_out = whole(grad_logits, grad_stride, dtype);
+  return launch_logprobs_grad(c, dtype, as_stream(stream)) == hipSuccess ? RLKV_OK : RLKV_ERR_HIP;
 }
 
 }  // extern "C"

@@ -131,4 +131,38 @@ struct MatmulCall {
 constexpr int64_t kMostMatmulStride = 1 << 23;         // bytes between rows of a or b: a tile's rows are within 32 bits of its first
 hipError_t launch_matmul(const MatmulCall& call, bool out_bf16, hipStream_t stream);
 
+constexpr int kMostTop = 32;          // most likely tokens a row can be asked for
+struct LogprobCall {
+  const void* logits;
+  const int32_t* tokens;      // or null (then logprobs is too)
+  float* logprobs;
+  float* entropy;             // any of these may be null
+  float* lse;
+  int32_t* top_ids;           // [rows][top], with top > 0
+  float* top_logprobs;
+  void* workspace;
+  int64_t stride;
+  float scale;
+  int32_t rows, vocab, top;
+  int32_t whole;              // rows of logits start at multiples of 16 bytes
+  int32_t chunks, splits;     // set by the launch
+};
+struct LogprobGradCall {
+  const void* logits;
+  const int32_t* tokens;
+  const float* lse;
+  const float* entropy;
+  const float* grad_logprobs;
+  const float* grad_entropy;
+  void* out;
+  int64_t stride, out_stride;
+  float scale;
+  int32_t rows, vocab;
+  int32_t whole, whole_out;
+  int32_t splits;             // set by the launch
+};
+size_t logprob_workspace(int rows, int vocab, int top);
+hipError_t launch_logprobs(LogprobCall call, int dtype, hipStream_t stream);
+hipError_t launch_logprobs_grad(LogprobGradCall call, int dtype, hipStream_t stream);
+
 }  // namespace rlkv

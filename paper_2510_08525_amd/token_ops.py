@@ -112,6 +112,50 @@ def scaled_matmul(a, a_scales, b, b_scales, out):
     return out
 
 
+def _rows(t, what, device, rows, dtype=torch.float32):
+    return None if t is None else _vector(t, what, device, (dtype,), rows)
+
+
+def token_logprobs(logits, tokens, logprobs, *, scale: float = 1.0, entropy=None, lse=None, top=None, workspace=None):
+    """Log probabilities of `tokens` (int32 [rows]) under softmax(scale * logits) into logprobs [rows], and where given entropy [rows],
+    lse [rows] and top = (log probabilities, int32 tokens) [rows, k] of the k most likely tokens (rlkv_token_logprobs).
+
+    tokens and logprobs may both be None.  workspace: a uint8 tensor of rlkv_token_logprobs_workspace(rows, vocab, k) bytes that the
+    caller keeps; without one the call takes one from torch's allocator."""
+    device = logits.device
+    xp = _matrix(logits, "logits", None, (torch.float32, torch.bfloat16))
+    rows, vocab = logits.shape
+    k, vp, ip = 0, None, None
+    if top is not None:
+        k = top[0].shape[1] if top[0].dim() == 2 else -1
+        vp = _matrix(top[0], "top log probabilities", device, (torch.float32,), (rows, k))
+        ip = _matrix(top[1], "top tokens", device, (torch.int32,), (rows, k))
+        if not (top[0].is_contiguous() and top[1].is_contiguous()):
+            raise ValueError("top: need contiguous tensors")
+    need = load_library().rlkv_token_logprobs_workspace(rows, vocab, k)
+    if workspace is None:
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
+    wp = _vector(workspace, "workspace", device, (torch.uint8,))
+    _call("rlkv_token_logprobs", device, xp, logits.stride(0), rows, vocab, _DTYPES[logits.dtype], scale,
+          _rows(tokens, "tokens", device, rows, torch.int32), _rows(logprobs, "logprobs", device, rows),
+          _rows(entropy, "entropy", device, rows), _rows(lse, "lse", device, rows), k, ip, vp, wp, workspace.numel())
+    return logprobs
+
+
+def token_logprobs_grad(logits, tokens, lse, grad_logprobs, grad_logits, *, scale: float = 1.0, entropy=None, grad_entropy=None):
+    """Gradient with respect to the logits, from the gradients of log probabilities and (where given) entropies; lse and entropy as
+    token_logprobs left them (rlkv_token_logprobs_grad).  grad_logits may be logits."""
+    device = logits.device
+    xp = _matrix(logits, "logits", None, (torch.float32, torch.bfloat16))
+    rows, vocab = logits.shape
+    op = _matrix(grad_logits, "grad_logits", device, (logits.dtype,), (rows, vocab))
+    _call("rlkv_token_logprobs_grad", device, xp, logits.stride(0), rows, vocab, _DTYPES[logits.dtype], scale,
+          _rows(tokens, "tokens", device, rows, torch.int32), _rows(lse, "lse", device, rows), _rows(entropy, "entropy", device, rows),
+          _rows(grad_logprobs, "grad_logprobs", device, rows), _rows(grad_entropy, "grad_entropy", device, rows), op,
+          grad_logits.stride(0))
+    return grad_logits
+
+
 def _row_stride(t) -> int:
     """Distance of two rows; that of a single row, which a tensor may report as anything, is its length."""
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]

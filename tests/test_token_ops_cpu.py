@@ -71,3 +71,35 @@ def test_rotary_without_a_cache_is_refused():
     lib, r = rl.load_library(), rl.Rotary([1.0] * 64)
     assert lib.rlkv_append_rotary(None, 0, P, 1024, None, 1, r.address, P, None) == BAD
     assert lib.rlkv_rotary(None, 0, P, 1024, None, 1, r.address, P, P, P, None) == BAD
+
+
+@pytest.mark.parametrize("bad", [
+    dict(logits=None), dict(rows=-1), dict(rows=(1 << 20) + 1), dict(vocab=0), dict(vocab=(1 << 24) + 1), dict(dtype=2), dict(scale=0.0),
+    dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(stride=-1), dict(logits=P + 1), dict(tokens=None),
+    dict(logprobs=None), dict(top=-1), dict(top=33), dict(top=20, vocab=19), dict(top_ids=None), dict(top_logprobs=None), dict(tokens=P + 2),
+    dict(entropy=P + 1), dict(lse=P + 1), dict(top_ids=P + 2), dict(workspace=None), dict(workspace=P + 4), dict(workspace_bytes=100),
+])
+def test_logprobs_refuse(bad):
+    a = dict(logits=P, stride=50000, rows=3, vocab=50000, dtype=rl.RLKV_BF16, scale=1.0, tokens=P, logprobs=P, entropy=P, lse=P, top=5,
+             top_ids=P, top_logprobs=P, workspace=P, workspace_bytes=1 << 20)
+    a.update(bad)
+    assert rl.load_library().rlkv_token_logprobs(*a.values(), None) == BAD
+
+
+@pytest.mark.parametrize("bad", [
+    dict(logits=None), dict(rows=-1), dict(vocab=0), dict(dtype=2), dict(scale=0.0), dict(tokens=None), dict(lse=None), dict(entropy=None),
+    dict(grad_logprobs=None), dict(grad_entropy=None), dict(grad_logits=None), dict(grad_stride=999), dict(stride=-1), dict(lse=P + 1),
+    dict(grad_logits=P + 1),
+])
+def test_logprobs_grad_refuses(bad):
+    a = dict(logits=P, stride=1000, rows=3, vocab=1000, dtype=rl.RLKV_BF16, scale=1.0, tokens=P, lse=P, entropy=P, grad_logprobs=P,
+             grad_entropy=P, grad_logits=P, grad_stride=1000)
+    a.update(bad)
+    assert rl.load_library().rlkv_token_logprobs_grad(*a.values(), None) == BAD
+
+
+def test_logprobs_workspace():
+    need = rl.rlkv_token_logprobs_workspace
+    assert need(0, 100, 0) == need(4, 0, 0) == need(4, 100, 33) == need(4, 100, -1) == need(-1, 100, 0) == 0
+    assert need(5000, 100000, 20) == 0 and need(1, 16384, 32) == 0            # nothing is split
+    assert 0 < need(2, 100000, 0) < need(2, 100000, 20)
