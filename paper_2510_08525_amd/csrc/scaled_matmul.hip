@@ -17,6 +17,8 @@
 // a lane's four results then belong to one row of a, whose scale is one register, and to four neighbouring columns of the output.  The order
 // of k inside a group does not matter as long as both operands have the same: lane (row, seg) holds bytes [16 seg, 16 seg + 16) and the
 // same 64 further on, so that a load of 16 lanes x 4 segments reads 64 contiguous bytes of each row.
+#include <type_traits>
+
 #include "token_ops.h"
 
 namespace rlkv {
@@ -233,8 +235,11 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(MatmulCall c, int t
 #pragma unroll
   for (int s = 0; s < STAGES - 1; ++s) issue(s, s < groups ? s : groups - 1);
   int stage = 0;
-  for (int g = 0; g < groups; ++g) {
-    if ((g & 63) == 0) sb_lanes = b_scales[g + lane < groups ? g + lane : groups - 1];
+  auto turn = [&](int g, auto tail) {
+    if ((g & 63) == 0) {
+      sb_lanes = b_scales[g + lane < groups ? g + lane : groups - 1];
+      asm volatile("" : "+v"(sb_lanes));                       // (waited for here, and not in every turn behind the loads to LDS)
+    }
     // This stage's loads are in, of all wavefronts, and nobody reads the stage that is written next.
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads * (STAGES - 2)) : "memory");
     {
@@ -243,34 +248,45 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(MatmulCall c, int t
     }
     const char* in = lds + stage * kStage;
     const float sb = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sb_lanes), g & 63));
-    const bool tail = (g + 1) * kGroup > c.k;
-    const bool lo_in = g * kGroup + seg * 16 < c.k, hi_in = g * kGroup + seg * 16 + 64 < c.k;
     auto fragment = [&](int at_row) {
       i32x4 lo = *reinterpret_cast<const i32x4*>(in + at_row), hi = *reinterpret_cast<const i32x4*>(in + (at_row ^ 64));
-      if (tail) {
-        lo = lo_in ? lo : i32x4{0, 0, 0, 0};
-        hi = hi_in ? hi : i32x4{0, 0, 0, 0};
+      if constexpr (decltype(tail)::value) {                   // (chunks past the end of k)
+        if (g * kGroup + seg * 16 >= c.k) lo = i32x4{0, 0, 0, 0};
+        if (g * kGroup + seg * 16 + 64 >= c.k) hi = i32x4{0, 0, 0, 0};
       }
       Operand<WAY> o;
       to_operand(both(lo, hi), o);
       return o;
     };
-    Operand<WAY> fb[TN];
+    Operand<WAY> fb[TN], fa[2];
+    floats4 p[2][TN];
+    float s[TM];
+    fa[0] = fragment(at_a);
 #pragma unroll
     for (int j = 0; j < TN; ++j) fb[j] = fragment(at_b + j * 16 * kGroup);
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const Operand<WAY> fa = fragment(at_a + i * 16 * kGroup);
-      const float s = sb * *reinterpret_cast<const float*>(in + (BM + BN) * kGroup + (wm * TM * 16 + i * 16 + row) * 4);
+    for (int i = 0; i < TM; ++i)
+      s[i] = *reinterpret_cast<const float*>(in + (BM + BN) * kGroup + (wm * TM * 16 + i * 16 + row) * 4);
+#pragma unroll
+    for (int i = 0; i <= TM; ++i) {
+      // products of one tile row beside the sums of the row before: the matrix cores and the vector ALU both have work
+      if (i + 1 < TM) fa[(i + 1) & 1] = fragment(at_a + (i + 1) * 16 * kGroup);
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
-        const floats4 p = group_product(fb[j], fa);
+        if (i < TM) p[i & 1][j] = group_product(fb[j], fa[i & 1]);
+        if (i > 0) {
+          const float by = sb * s[i - 1];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(p[e], s, acc[i][j][e]);
+          for (int e = 0; e < 4; ++e) acc[i - 1][j][e] = __builtin_fmaf(p[(i - 1) & 1][j][e], by, acc[i - 1][j][e]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     stage = stage == STAGES - 1 ? 0 : stage + 1;
-  }
+  };
+  const int whole_groups = c.k / kGroup;
+  for (int g = 0; g < whole_groups; ++g) turn(g, std::false_type{});
+  if (whole_groups < groups) turn(whole_groups, std::true_type{});
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // (no load to LDS outlives the workgroup)
 #pragma unroll
   for (int i = 0; i < TM; ++i)
