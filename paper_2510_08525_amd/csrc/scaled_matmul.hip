@@ -96,87 +96,6 @@ __device__ __forceinline__ void store_four(const MatmulCall& c, int m, int n, co
   }
 }
 
-// ---- few rows of a: b is read once, straight into registers -------------------------------------------------------------------
-// A workgroup has 16 rows of b; its wavefronts take every eighth group of k and add their sums in LDS.  NT tiles of 16 rows of a.
-constexpr int kFewWaves = 8;
-
-// No load stands behind a branch, so that all of them go out before the first is waited for: groups past the last one repeat it with a
-// scale of 0, and CUT (k is no multiple of 128) clears the bytes past the end of k in registers.
-template <int NT, bool CUT, bool BF16>
-__global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(MatmulCall c) {
-  constexpr int kAhead = 4;                                        // groups whose loads are in flight together
-  __shared__ floats4 parts[kFewWaves][NT][64];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, row = lane & 15, seg = lane >> 4;
-  const int n0 = blockIdx.x * 16;
-  const int groups = (c.k + kGroup - 1) / kGroup;
-  const int n_row = n0 + row < c.n ? n0 + row : c.n - 1;           // (rows past the end repeat the last one and are not stored)
-  const char* b = static_cast<const char*>(c.b) + n_row * c.b_stride + seg * 16;
-  const char* a[NT];
-  int m_row[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    m_row[t] = t * 16 + row < c.m ? t * 16 + row : c.m - 1;
-    a[t] = static_cast<const char*>(c.a) + m_row[t] * c.a_stride + seg * 16;
-  }
-  const float* b_scales = c.b_scales + (n0 / kGroup) * c.b_scale_stride;
-  floats4 acc[NT] = {};
-  auto at = [&](int k) { return CUT && k + seg * 16 >= c.k ? -seg * 16 : k; };
-  auto kept = [&](i32x4 v, int k) { return CUT && k + seg * 16 >= c.k ? i32x4{0, 0, 0, 0} : v; };
-  for (int g0 = wave; g0 < groups; g0 += kFewWaves * kAhead) {
-    i32x4 fb[kAhead][2], fa[kAhead][NT][2];
-    float sb[kAhead], sa[kAhead][NT];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int g = g0 + u * kFewWaves < groups ? g0 + u * kFewWaves : groups - 1;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) fb[u][h] = *reinterpret_cast<const i32x4*>(b + at(g * kGroup + h * 64));
-    }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int g = g0 + u * kFewWaves < groups ? g0 + u * kFewWaves : groups - 1;
-      sb[u] = b_scales[g];
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) fa[u][t][h] = *reinterpret_cast<const i32x4*>(a[t] + at(g * kGroup + h * 64));
-        sa[u][t] = c.a_scales[g * c.a_scale_stride + m_row[t]];
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const bool there = g0 + u * kFewWaves < groups;
-      const int k = (there ? g0 + u * kFewWaves : groups - 1) * kGroup;
-      halves8 ob[4], oa[4];
-      auto widen_both = [&](const i32x4 (&from)[2], halves8 (&to)[4]) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const i32x4 v = kept(from[h], k + h * 64);
-          to[2 * h] = widened(v[0], v[1]);
-          to[2 * h + 1] = widened(v[2], v[3]);
-        }
-      };
-      widen_both(fb[u], ob);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        widen_both(fa[u][t], oa);
-        const floats4 p = group_product(ob, oa);
-        const float s = there ? sb[u] * sa[u][t] : 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[t][i] = __builtin_fmaf(p[i], s, acc[t][i]);
-      }
-    }
-  }
-#pragma unroll
-  for (int t = 0; t < NT; ++t) parts[wave][t][lane] = acc[t];
-  __syncthreads();
-  for (int t = wave; t < NT; t += kFewWaves) {
-    floats4 sum = parts[0][t][lane];
-#pragma unroll
-    for (int w = 1; w < kFewWaves; ++w) sum += parts[w][t][lane];
-    store_four(c, t * 16 + row, n0 + seg * 4, sum, BF16);
-  }
-}
-
 // Loads that go straight to LDS, lane after lane behind `to`, from a base that is the same in all lanes.  (Buffer instructions: of the
 // global ones the compiler takes it that they may be read through flat addresses, and waits for all of LDS before every
 // use of a fragment.  Their bounds are not used: offsets are kept inside the matrices.)
@@ -196,6 +115,115 @@ typedef const void* Buffer;
 __device__ inline Buffer bounded(const void* base) { return base; }
 template <int BYTES> __device__ inline void load_to_lds(Buffer, char*, uint32_t) {}
 #endif
+
+// ---- few rows of a: b is read once -----------------------------------------------------------------------------------------------
+// A workgroup has 16 rows of b; each of its wavefronts takes every WAVES-th group of k, by itself, and their sums are added in LDS.  NT tiles
+// of 16 rows of a.  Fragments pass through LDS although nobody shares them: a load to LDS takes whole lines of 8 rows, where a
+// load of a fragment takes half lines of 16 (a workgroup by itself 80 GB/s against 27), and what is in flight holds no registers.  AHEAD groups
+// of a wavefront are under way; it waits for its own loads only, and there is no barrier before the sums.
+template <int NT, int WAVES, int AHEAD>
+struct FewShape {
+  static constexpr int kBytes = (1 + NT) * 16 * kGroup + 256;        // of a group: b, a, the scales of up to 64 rows of a
+  static constexpr int kLoads = 2 + 2 * NT + 1;
+  static constexpr int kLds = WAVES * AHEAD * kBytes;
+  static_assert(NT <= 4 && kLds >= WAVES * NT * 64 * 16 && (AHEAD - 1) * kLoads < 64, "the sums fit where the groups were");
+};
+
+template <int NT, int WAVES, int AHEAD, bool CUT, bool BF16>
+__global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(MatmulCall c) {
+  typedef FewShape<NT, WAVES, AHEAD> Shape;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, row = lane & 15, seg = lane >> 4;
+  const int n0 = blockIdx.x * 16, m0 = blockIdx.y * NT * 16, rows = c.m - m0;
+  const int groups = (c.k + kGroup - 1) / kGroup, mine = groups > wave ? (groups - wave + WAVES - 1) / WAVES : 0;
+  const Buffer from_a = bounded(static_cast<const char*>(c.a) + m0 * c.a_stride), from_b = bounded(static_cast<const char*>(c.b) + n0 * c.b_stride);
+  const int chunk = ((lane & 7) ^ (lane >> 3)) * 16;                 // which bytes of its row's 128 a lane brings
+  uint32_t a_at[2 * NT], b_at[2];                                   // (rows past the end repeat the last one and are not stored)
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = h * 8 + (lane >> 3);
+    b_at[h] = (uint32_t)(n0 + r < c.n ? r : c.n - 1 - n0) * (uint32_t)c.b_stride;
+  }
+#pragma unroll
+  for (int h = 0; h < 2 * NT; ++h) {
+    const int r = h * 8 + (lane >> 3);
+    a_at[h] = (uint32_t)(r < rows ? r : rows - 1) * (uint32_t)c.a_stride;
+  }
+  const uint32_t scale_at = (lane < rows ? lane : rows - 1) * 4;
+  char* const own = lds + wave * AHEAD * Shape::kBytes;
+  auto issue = [&](int i) {                                          // the wavefront's i-th group
+    const int g = wave + i * WAVES;
+    char* to = own + (i % AHEAD) * Shape::kBytes;
+    const uint32_t k = !CUT || g * kGroup + chunk < c.k ? g * kGroup + chunk : 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) load_to_lds<16>(from_b, to + h * 1024, b_at[h] + k);
+#pragma unroll
+    for (int h = 0; h < 2 * NT; ++h) load_to_lds<16>(from_a, to + 2048 + h * 1024, a_at[h] + k);
+    load_to_lds<4>(bounded(c.a_scales + m0 + g * c.a_scale_stride), to + 2048 * (1 + NT), scale_at);
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (i < mine) issue(i);
+  const float* b_scales = c.b_scales + (n0 / kGroup) * c.b_scale_stride;
+  float sb_lanes = 0.f;                                              // the scales of 64 of the wavefront's groups, one a lane
+  floats4 acc[NT] = {};
+  const int at = row * kGroup + ((seg ^ (lane & 7)) << 4);
+  auto take = [&](int i) {
+    const int k0 = (wave + i * WAVES) * kGroup;
+    const char* in = own + (i % AHEAD) * Shape::kBytes;
+    auto fragment = [&](int at_row) {
+      i32x4 lo = *reinterpret_cast<const i32x4*>(in + at_row), hi = *reinterpret_cast<const i32x4*>(in + (at_row ^ 64));
+      if (CUT && k0 + seg * 16 >= c.k) lo = i32x4{0, 0, 0, 0};
+      if (CUT && k0 + seg * 16 + 64 >= c.k) hi = i32x4{0, 0, 0, 0};
+      Operand<kWide> o;
+      to_operand(both(lo, hi), o);
+      return o;
+    };
+    const float sb = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sb_lanes), i & 63));
+    const Operand<kWide> fb = fragment(at);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const float s = sb * *reinterpret_cast<const float*>(in + 2048 * (1 + NT) + (t * 16 + row) * 4);
+      const floats4 p = group_product(fb, fragment(2048 * (1 + t) + at));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[t][e] = __builtin_fmaf(p[e], s, acc[t][e]);
+    }
+  };
+  auto scales = [&](int i) {
+    if ((i & 63) == 0) {
+      const int g = wave + (i + lane) * WAVES;
+      sb_lanes = b_scales[g < groups ? g : groups - 1];
+      asm volatile("" : "+v"(sb_lanes));                             // (waited for here)
+    }
+  };
+  int i = 0;
+  for (; i + AHEAD < mine; ++i) {
+    scales(i);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"((AHEAD - 1) * Shape::kLoads) : "memory");
+    take(i);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");               // (the reads are over before their place is written)
+    issue(i + AHEAD);
+  }
+  if (i < mine) {
+    scales(i);                                                       // (at most AHEAD groups are left: another reload only by their count)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    for (; i < mine; ++i) {
+      scales(i);
+      take(i);
+    }
+  }
+  __syncthreads();
+  floats4(*parts)[NT][64] = reinterpret_cast<floats4(*)[NT][64]>(lds);
+#pragma unroll
+  for (int t = 0; t < NT; ++t) parts[wave][t][lane] = acc[t];
+  __syncthreads();
+  for (int t = wave; t < NT; t += WAVES) {
+    floats4 sum = parts[0][t][lane];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) sum += parts[w][t][lane];
+    store_four(c, m0 + t * 16 + row, n0 + seg * 4, sum, BF16);
+  }
+}
 
 // ---- many rows: tiles through LDS ------------------------------------------------------------------------------------------------
 // A workgroup has BM rows of a and BN of b; a group of k of both is one stage in LDS (rows of 128 bytes, the 16-byte chunk c of
@@ -341,11 +369,15 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(MatmulCall c, int t
       store_four(c, m0 + (wm * TM + i) * 16 + row, n0 + (wn * TN + j) * 16 + seg * 4, acc[i][j], BF16);
 }
 
-template <int NT, bool BF16>
+template <int NT, int WAVES, int AHEAD, bool BF16>
 hipError_t launch_few(const MatmulCall& c, hipStream_t stream) {
-  const dim3 grid((c.n + 15) / 16), block(kFewWaves * 64);
-  if (c.k % kGroup) hipLaunchKernelGGL((few_rows_kernel<NT, true, BF16>), grid, block, 0, stream, c);
-  else hipLaunchKernelGGL((few_rows_kernel<NT, false, BF16>), grid, block, 0, stream, c);
+  constexpr int kLds = FewShape<NT, WAVES, AHEAD>::kLds;
+  auto whole = few_rows_kernel<NT, WAVES, AHEAD, false, BF16>;
+  auto cut = few_rows_kernel<NT, WAVES, AHEAD, true, BF16>;
+  static const hipError_t allowed[] = {hipFuncSetAttribute(reinterpret_cast<const void*>(whole), hipFuncAttributeMaxDynamicSharedMemorySize, kLds),
+                                       hipFuncSetAttribute(reinterpret_cast<const void*>(cut), hipFuncAttributeMaxDynamicSharedMemorySize, kLds)};
+  if (allowed[0] != hipSuccess || allowed[1] != hipSuccess) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(c.k % kGroup ? cut : whole, dim3((c.n + 15) / 16, (c.m + NT * 16 - 1) / (NT * 16)), dim3(WAVES * 64), kLds, stream, c);
   return hipGetLastError();
 }
 
@@ -362,6 +394,7 @@ hipError_t launch_tiled(const MatmulCall& c, hipStream_t stream) {
 
 // What a turn of a kernel's workgroups takes, in ns, where few compute units have one and where all have (the clock falls and L2 is
 // shared), and how many workgroups are resident: from calls of 96 .. 8192 rows, 3584 .. 14336 columns and k of 3584 .. 14336.
+constexpr int kFewRows = 64;
 struct TileCost { int bm, bn, slots, one, all; };
 inline double estimate(const TileCost& t, const MatmulCall& c) {
   const double tiles = (double)((c.m + t.bm - 1) / t.bm) * ((c.n + t.bn - 1) / t.bn);
@@ -371,15 +404,17 @@ inline double estimate(const TileCost& t, const MatmulCall& c) {
 
 template <bool BF16>
 hipError_t launch_typed(const MatmulCall& c, hipStream_t stream) {
-  if (c.m <= 16) return launch_few<1, BF16>(c, stream);
-  if (c.m <= 32) return launch_few<2, BF16>(c, stream);
+  // (us, 4 wavefronts a workgroup / 8: 1 x 6144 x 4096 7.5 / 8.0, 1 x 14336 x 4096 13.6 / 15.1; few workgroups want the wider: 1 x 1024 x 16384
+  // 10.4 / 7.7.  Up to 64 rows 32 at a time, against tiles of 64 x 64: 64 x 6144 x 4096 12.1 / 19.7, 64 x 14336 x 4096 25.1 / 20.6.)
+  if (c.m <= 16) return c.n <= 128 * 16 ? launch_few<1, 8, 2, BF16>(c, stream) : launch_few<1, 4, 2, BF16>(c, stream);
+  if (c.m <= kFewRows) return launch_few<2, 4, 2, BF16>(c, stream);
   // The shape of the tiles whose rounds over the compute units are estimated to take least: small ones fill the card, large ones read less.
   // (us measured, estimate in brackets: 333 x 4608 x 3584 64 x 64 15.3 (18), 128 x 128 19.6 (20), 256 x 128 27.8 (28); 1500 x 4608 x 4096
   // 52.7 (58), 45.6 (48), 35.9 (39), 192 x 256 44.0 (46), 256 x 256 53.0 (56); 4096 x 4608 x 3584 256 x 128 94, 192 x 256 85, 256 x 256 101.)
-  if (!BF16 || c.m <= 64) {
+  if constexpr (!BF16) {
     static const TileCost costs[] = {{64, 64, 512, 575, 770}, {128, 128, 256, 1100, 1180}};
-    if (estimate(costs[0], c) <= estimate(costs[1], c)) return launch_tiled<64, 64, 2, 2, 4, kWide, BF16>(c, stream);
-    return launch_tiled<128, 128, 2, 4, 3, kWide, BF16>(c, stream);
+    if (estimate(costs[0], c) <= estimate(costs[1], c)) return launch_tiled<64, 64, 2, 2, 4, kWide, false>(c, stream);
+    return launch_tiled<128, 128, 2, 4, 3, kWide, false>(c, stream);
   }
   if constexpr (BF16) {
     static const TileCost costs[] = {{64, 64, 768, 330, 697}, {128, 64, 512, 430, 830}, {128, 128, 256, 590, 741},
