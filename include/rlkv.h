@@ -445,8 +445,7 @@ int32_t rlkv_plan_narrow_split(int32_t n_compute_units, int32_t group, int32_t n
 /* ---- Token-wise operators: a decoder's way into the cache and out of it again --------------------------------------------
  * These need no cache handle.  They run on `stream` of the current device, keep no state, allocate nothing, wait for nothing
  * and can be recorded into a HIP graph.  Matrices are row-major; a stride is the distance of two rows (of two groups, for
- * scales) in elements.  Every pointer is aligned to its element type; no row has to be aligned beyond that unless a call says so
- * (rows at multiples of 16 bytes are the fast case).  Sums, statistics and scales are fp32; every output is rounded once, to
+ * scales) in elements.  Every pointer is aligned to its element type; no row has to be aligned beyond that unless a call says so.  Sums, statistics and scales are fp32; every output is rounded once, to
  * nearest even.  A call with no rows returns RLKV_OK and launches nothing. */
 
 /* Root-mean-square norm of rows, with the residual's addition in front of it:

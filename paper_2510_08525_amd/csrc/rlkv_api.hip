@@ -862,7 +862,6 @@ static rlkv_status_t rotary_args(rlkv_cache_t* cache, int32_t layer, const void*
   args->call.qkv = qkv;
   args->call.token_stride = token_stride;
   args->call.stride_tokens = stride_tokens;
-  args->call.whole_in = reinterpret_cast<uintptr_t>(qkv) % 16 == 0 && token_stride * (int64_t)e % 16 == 0;
   return RLKV_OK;
 }
 
@@ -872,7 +871,6 @@ rlkv_status_t rlkv_append_rotary(rlkv_cache_t* cache, int32_t layer, const void*
   if (rlkv_status_t st = rotary_args(cache, layer, qkv, token_stride, stride_tokens, rotary, &args)) return st;
   if (reinterpret_cast<uintptr_t>(q_out) % (cache->cfg.dtype == RLKV_F32 ? 4 : 2) != 0) return RLKV_ERR_INVALID_ARG;
   args.call.q_out = q_out;
-  args.call.whole_out = reinterpret_cast<uintptr_t>(q_out) % 16 == 0;
   return append_impl(cache, layer, nullptr, nullptr, n_tokens, n_tokens ? 0 : stride_tokens, stride_tokens, stream, nullptr, &args);
 }
 
@@ -902,7 +900,6 @@ rlkv_status_t rlkv_rotary(rlkv_cache_t* cache, int32_t layer, const void* qkv, i
   args.call.q_out = q_out;
   args.call.k_out = k_out;
   args.call.v_out = v_out;
-  args.call.whole_out = any % 16 == 0;
   args.call.uniform = n_tokens ? 0 : stride_tokens;
   args.call.max_tokens = max_tok;
   return launch_rotary(cache->dv, layer, len_of(cache->dv, cache->parity[layer], layer), nullptr, args.call, args.turns,

@@ -4,9 +4,12 @@
 //   h = x + r          y = h / sqrt(mean(h^2) + eps) * w          s_g = max(max_g |y| / 448, least)      out = round(y / s_g)
 //
 // h stays in fp32 registers between the sum of squares and the outputs, so it is read once and each output is rounded once: the norm is
-// that of the unrounded sum.  A thread holds pieces of eight columns, T apart: a wavefront's loads are whole lines, and the 16
-// lanes of a group of 128 columns lie next to each other, so that its maximum takes four steps over lanes and no LDS.
-// Bound: HBM for many rows, latency for few.
+// that of the unrounded sum.  A thread has one piece of eight columns (two beyond 8192 columns, and what is beyond 16384 is read a
+// second time): a row's loads are all in flight at once, a wavefront's are whole lines, and the 16 lanes of a group of 128 columns
+// lie next to each other, so that its maximum takes four steps over lanes and no LDS.
+// Bound: HBM for many rows (16384 x 3584 bf16 with residual into 8 bits: 413 MB in 83 us, 5.0 TB/s, what a copy reaches), latency for few
+// (one row of 4096: 4 us).  With 64 threads a row and eight pieces each, weights kept over several rows, the same call took
+// 134 us, with 256 threads and two pieces 90; several rows to a workgroup one after the other are slower in every shape.
 #include "token_ops.h"
 
 namespace rlkv {
@@ -14,24 +17,22 @@ namespace {
 
 // T threads a row, NC pieces each (T * NC * 8 columns at most, unless LOOP: then the pieces beyond are read a second time).
 template <typename X, int T, int NC, bool E4M3, bool LOOP>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(NormCall c, int rows_per_block) {
+__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(NormCall c) {
   constexpr int kRowsAtOnce = T < 256 ? 256 / T : 1;
   constexpr int kWaves = T / 64;
   __shared__ float parts[2][kWaves > 1 ? kWaves : 1];
   const int t = threadIdx.x % T, lane_row = threadIdx.x / T;
-  const int first = blockIdx.x * rows_per_block;
-  const int last = first + rows_per_block < c.rows ? first + rows_per_block : c.rows;
   int turn = 0;
-  for (int row = first + lane_row; row < last; row += kRowsAtOnce) {
+  for (int64_t row = (int64_t)blockIdx.x * kRowsAtOnce + lane_row; row < c.rows; row += (int64_t)gridDim.x * kRowsAtOnce) {
     const X* x = static_cast<const X*>(c.x) + row * c.x_stride;
     const X* res = c.residual ? static_cast<const X*>(c.residual) + row * c.residual_stride : nullptr;
     float h[NC][8];
     float squares = 0.f;
     auto load = [&](int col, float (&f)[8]) {
-      load_piece(x, col, c.cols, c.whole_in, f);
+      load_piece(x, col, c.cols, f);
       if (res) {
         float r[8];
-        load_piece(res, col, c.cols, c.whole_res, r);
+        load_piece(res, col, c.cols, r);
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] += r[i];
       }
@@ -73,11 +74,11 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(NormCall c, int
     }
     auto finish = [&](int col, float (&f)[8]) {
       if (col < c.cols) {
-        if (c.sum_out) store_piece(static_cast<X*>(c.sum_out) + row * c.sum_stride, col, c.cols, c.whole_sum, f);
+        if (c.sum_out) store_piece(static_cast<X*>(c.sum_out) + row * c.sum_stride, col, c.cols, f);
         if (c.norm) {
           float w[8];
           if (c.weight) {
-            load_piece(static_cast<const X*>(c.weight), col, c.cols, c.whole_weight, w);
+            load_piece(static_cast<const X*>(c.weight), col, c.cols, w);
           } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = 1.f;
@@ -98,11 +99,11 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(NormCall c, int
           const float inverse = 1.f / scale;
 #pragma unroll
           for (int i = 0; i < 8; ++i) f[i] *= inverse;
-          store_e4m3(static_cast<uint8_t*>(c.out) + row * c.out_stride, col, c.cols, c.whole_out, f);
+          store_e4m3(static_cast<uint8_t*>(c.out) + row * c.out_stride, col, c.cols, f);
           if ((t & 15) == 0) c.scales[(int64_t)(col / kGroup) * c.scale_stride + row] = scale;
         }
       } else if (col < c.cols) {
-        store_piece(static_cast<X*>(c.out) + row * c.out_stride, col, c.cols, c.whole_out, f);
+        store_piece(static_cast<X*>(c.out) + row * c.out_stride, col, c.cols, f);
       }
     };
     if (LOOP)                       // (before the pieces in registers: where sum_out is the residual, what is read again here is not yet written)
@@ -120,16 +121,16 @@ constexpr int kMostBlocks = 1 << 20;
 
 template <typename X, bool E4M3>
 hipError_t launch_typed(const NormCall& c, hipStream_t stream) {
-  auto run = [&](auto kernel, int threads, int rows_per_block) {
-    const unsigned grid = (unsigned)((c.rows + rows_per_block - 1) / rows_per_block);
-    hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, stream, c, rows_per_block);
+  auto run = [&](auto kernel, int threads, int rows_at_once) {
+    const int blocks = (int)(((int64_t)c.rows + rows_at_once - 1) / rows_at_once);
+    hipLaunchKernelGGL(kernel, dim3(blocks < kMostBlocks ? blocks : kMostBlocks), dim3(threads), 0, stream, c);
     return hipGetLastError();
   };
-  if (c.rows >= 1024 && c.cols <= 4096) return run(norm_kernel<X, 64, 8, E4M3, false>, 256, c.rows >= 8192 ? 32 : 4);
-  const int rows = c.rows > kMostBlocks ? (c.rows + kMostBlocks - 1) / kMostBlocks : 1;
-  if (c.cols <= 4096) return run(norm_kernel<X, 256, 2, E4M3, false>, 256, rows);
-  if (c.cols <= 8192) return run(norm_kernel<X, 256, 4, E4M3, false>, 256, rows);
-  return run(norm_kernel<X, 256, 8, E4M3, true>, 256, rows);
+  if (c.cols <= 512) return run(norm_kernel<X, 64, 1, E4M3, false>, 256, 4);
+  if (c.cols <= 2048) return run(norm_kernel<X, 256, 1, E4M3, false>, 256, 1);
+  if (c.cols <= 4096) return run(norm_kernel<X, 512, 1, E4M3, false>, 512, 1);
+  if (c.cols <= 8192) return run(norm_kernel<X, 1024, 1, E4M3, false>, 1024, 1);
+  return run(norm_kernel<X, 1024, 2, E4M3, true>, 1024, 1);
 }
 
 }  // namespace

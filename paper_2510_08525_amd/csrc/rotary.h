@@ -21,7 +21,6 @@ struct RotaryCall {
   void* q_out;                   // [batch][n_q_heads][stride_tokens][kHeadDim], or null with an append: q is not wanted
   void* k_out;                   // [batch][n_kv_heads][stride_tokens][kHeadDim] (no append)
   void* v_out;
-  int32_t whole_in, whole_out;   // rows of qkv / of the outputs start at multiples of 16 bytes
 };
 // `append`: the rotated keys and the values go into the layer's stores, lengths and list growth advance (as launch_append); else all
 // three go out, heads first.  `seqs` non-null: per-sequence counts.

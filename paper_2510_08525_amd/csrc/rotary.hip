@@ -104,10 +104,10 @@ __global__ __launch_bounds__(kBlock) void rotary_kernel(DeviceView dv, int layer
     float k0[8], k1[8], v0[8], v1[8];
     if (p >= 0) {
       const T* row = qkv + ((int64_t)b * call.stride_tokens + (p - len_old)) * call.token_stride + (int64_t)(Hq + h) * kHeadDim;
-      load_piece(row, c0, kHeadDim, call.whole_in, k0);
-      load_piece(row, c1, kHeadDim, call.whole_in, k1);
-      load_piece(row + (int64_t)H * kHeadDim, c0, kHeadDim, call.whole_in, v0);
-      load_piece(row + (int64_t)H * kHeadDim, c1, kHeadDim, call.whole_in, v1);
+      load_piece(row, c0, kHeadDim, k0);
+      load_piece(row, c1, kHeadDim, k1);
+      load_piece(row + (int64_t)H * kHeadDim, c0, kHeadDim, v0);
+      load_piece(row + (int64_t)H * kHeadDim, c1, kHeadDim, v1);
       if (turned) {
         Angles g;
         angles_of(turns, j, (uint32_t)p, g);
@@ -145,10 +145,10 @@ __global__ __launch_bounds__(kBlock) void rotary_kernel(DeviceView dv, int layer
       const int cap = full ? dv.cap_pad[b] : dv.window_pad;
       T* krow = reinterpret_cast<T*>(dv.kv_base + koff + (int64_t)slot * dv.row_bytes);
       T* vrow = reinterpret_cast<T*>(dv.kv_base + koff + (int64_t)(cap + slot) * dv.row_bytes);
-      store_piece(krow, c0, kHeadDim, true, k0);
-      store_piece(krow, c1, kHeadDim, true, k1);
-      store_piece(vrow, c0, kHeadDim, true, v0);
-      store_piece(vrow, c1, kHeadDim, true, v1);
+      store_piece(krow, c0, kHeadDim, k0);
+      store_piece(krow, c1, kHeadDim, k1);
+      store_piece(vrow, c0, kHeadDim, v0);
+      store_piece(vrow, c1, kHeadDim, v1);
     }
     return;
   }
@@ -169,15 +169,15 @@ __global__ __launch_bounds__(kBlock) void rotary_kernel(DeviceView dv, int layer
   if (turned && h_first < Hq + H) angles_of(turns, j, (uint32_t)(len_in[b] + c), g);
   for (int h = h_first; h < h_last; ++h) {
     float x[8], y[8];
-    load_piece(row + (int64_t)h * kHeadDim, c0, kHeadDim, call.whole_in, x);
-    load_piece(row + (int64_t)h * kHeadDim, c1, kHeadDim, call.whole_in, y);
+    load_piece(row + (int64_t)h * kHeadDim, c0, kHeadDim, x);
+    load_piece(row + (int64_t)h * kHeadDim, c1, kHeadDim, y);
     if (turned && h < Hq + H) rotate(turns, g, x, y);
     T* out = h < Hq ? static_cast<T*>(call.q_out) + ((int64_t)b * Hq + h) * call.stride_tokens * kHeadDim
              : h < Hq + H ? static_cast<T*>(call.k_out) + ((int64_t)b * H + h - Hq) * call.stride_tokens * kHeadDim
                           : static_cast<T*>(call.v_out) + ((int64_t)b * H + h - Hq - H) * call.stride_tokens * kHeadDim;
     out += (int64_t)c * kHeadDim;
-    store_piece(out, c0, kHeadDim, call.whole_out, x);
-    store_piece(out, c1, kHeadDim, call.whole_out, y);
+    store_piece(out, c0, kHeadDim, x);
+    store_piece(out, c1, kHeadDim, y);
   }
 }
 

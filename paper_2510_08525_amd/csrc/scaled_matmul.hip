@@ -77,8 +77,8 @@ __device__ __forceinline__ void store_four(const MatmulCall& c, int m, int n, co
   if (bf16) {
     uint16_t* p = static_cast<uint16_t*>(c.out) + m * c.out_stride + n;
     const words2 w = {bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
-    if (c.whole_out && n + 4 <= c.n) {
-      *reinterpret_cast<words2*>(p) = w;
+    if (n + 4 <= c.n) {
+      *reinterpret_cast<words2_of_halves*>(p) = w;
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -86,8 +86,8 @@ __device__ __forceinline__ void store_four(const MatmulCall& c, int m, int n, co
     }
   } else {
     float* p = static_cast<float*>(c.out) + m * c.out_stride + n;
-    if (c.whole_out && n + 4 <= c.n) {
-      *reinterpret_cast<floats4*>(p) = v;
+    if (n + 4 <= c.n) {
+      *reinterpret_cast<floats4_of_floats*>(p) = v;
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i)

@@ -18,10 +18,8 @@ bool readable(const void* p, int64_t stride, int dtype) { return p && stride >= 
 bool writable(const void* p, int64_t stride, int64_t rows, int64_t cols, int dtype) {
   return p && (stride >= cols || rows <= 1) && aligned(p, bytes_of(dtype));
 }
-// Whether every row starts at a multiple of `to` bytes.
-int32_t whole(const void* p, int64_t stride, int dtype, size_t to = 16) {
-  return p && aligned(p, to) && (stride * (int64_t)bytes_of(dtype)) % (int64_t)to == 0;
-}
+// Whether every row starts at a multiple of 16 bytes.
+bool whole(const void* p, int64_t stride, int dtype) { return aligned(p, 16) && (stride * (int64_t)bytes_of(dtype)) % 16 == 0; }
 
 constexpr int32_t kMostLogitRows = 1 << 20, kMostVocab = 1 << 24;
 
@@ -36,11 +34,6 @@ rlkv_status_t norm_call(NormCall& c, int dtype, int out_dtype, void* stream) {
   if (c.weight && !aligned(c.weight, bytes_of(dtype))) return RLKV_ERR_INVALID_ARG;
   const bool e4m3 = out_dtype == RLKV_E4M3;
   if (e4m3 ? !writable(c.scales, c.scale_stride, groups_of(c.cols), c.rows, RLKV_F32) : c.scales != nullptr) return RLKV_ERR_INVALID_ARG;
-  c.whole_in = whole(c.x, c.x_stride, dtype);
-  c.whole_res = whole(c.residual, c.residual_stride, dtype);
-  c.whole_sum = whole(c.sum_out, c.sum_stride, dtype);
-  c.whole_weight = whole(c.weight, 0, dtype);
-  c.whole_out = whole(c.out, c.out_stride, out_dtype, e4m3 ? 8 : 16);
   return launch_norm(c, dtype, e4m3, as_stream(stream)) == hipSuccess ? RLKV_OK : RLKV_ERR_HIP;
 }
 
@@ -94,7 +87,6 @@ rlkv_status_t rlkv_scaled_matmul(const void* a, int64_t a_stride, const float* a
   c.b_scales = b_scales; c.b_scale_stride = b_scale_stride;
   c.m = m; c.n = n; c.k = k;
   c.out = out; c.out_stride = out_stride;
-  c.whole_out = whole(out, out_stride, out_dtype, 4 * bytes_of(out_dtype));
   return launch_matmul(c, out_dtype == RLKV_BF16, as_stream(stream)) == hipSuccess ? RLKV_OK : RLKV_ERR_HIP;
 }
 
@@ -128,7 +120,6 @@ rlkv_status_t rlkv_token_logprobs(const void* logits, int64_t stride, int32_t ro
   c.tokens = tokens; c.logprobs = logprobs; c.entropy = entropy; c.lse = lse;
   c.top = top; c.top_ids = top_ids; c.top_logprobs = top_logprobs;
   c.workspace = workspace;
-  c.whole = whole(logits, stride, dtype);
   return launch_logprobs(c, dtype, as_stream(stream)) == hipSuccess ? RLKV_OK : RLKV_ERR_HIP;
 }
 
@@ -146,8 +137,6 @@ rlkv_status_t rlkv_token_logprobs_grad(const void* logits, int64_t stride, int32
   c.rows = rows; c.vocab = vocab; c.scale = scale;
   c.tokens = tokens; c.lse = lse; c.entropy = entropy; c.grad_logprobs = grad_logprobs; c.grad_entropy = grad_entropy;
   c.out = grad_logits; c.out_stride = grad_stride;
-  c.whole = whole(logits, stride, dtype);
-  c.whole_out = whole(grad_logits, grad_stride, dtype);
   return launch_logprobs_grad(c, dtype, as_stream(stream)) == hipSuccess ? RLKV_OK : RLKV_ERR_HIP;
 }
 

@@ -225,7 +225,7 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LogprobCall c) {
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
       const int col = first + (p * kThreads + (int)threadIdx.x) * 8;
-      if (c.whole && col + 8 <= last) {
+      if (col + 8 <= last) {
         widen(*reinterpret_cast<const Piece<T>*>(logits + col), x[p]);
       } else {
 #pragma unroll
@@ -289,6 +289,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(LogprobCall c) {
   finish_row<T, true>(c, row, v, lds.best);
 }
 
+constexpr int kGradPieces = 4;                          // pieces of a thread whose loads are in flight together
 template <typename T>
 __global__ __launch_bounds__(kThreads) void grad_kernel(LogprobGradCall c) {
   const int row = blockIdx.x / c.splits, split = blockIdx.x % c.splits;
@@ -308,22 +309,28 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(LogprobGradCall c) {
   const float a = -(g + gh * entropy), b = -gh * kLn2;
   const int pieces = (c.vocab + 7) / 8;
   const int first = (int)((int64_t)pieces * split / c.splits), end = (int)((int64_t)pieces * (split + 1) / c.splits);
-  for (int p = first + threadIdx.x; p < end; p += kThreads) {
-    const int col = p * 8;
-    float x[8];
-    load_piece(logits, col, c.vocab, c.whole, x);
+  for (int p0 = first + threadIdx.x; p0 < end; p0 += kThreads * kGradPieces) {
+    float x[kGradPieces][8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float d = __builtin_fmaf(x[i], scale2, -lse2);
-      const float w = __builtin_amdgcn_exp2f(d);
-      x[i] = w * __builtin_fmaf(b, fmaxf(d, kLow), a);
-    }
-    if (asked && (unsigned)(token - col) < 8u) {
+    for (int u = 0; u < kGradPieces; ++u)
+      if (p0 + u * kThreads < end) load_piece(logits, (p0 + u * kThreads) * 8, c.vocab, x[u]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (token - col == i) x[i] += g;
+    for (int u = 0; u < kGradPieces; ++u) {
+      const int col = (p0 + u * kThreads) * 8;
+      if (p0 + u * kThreads >= end) break;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float d = __builtin_fmaf(x[u][i], scale2, -lse2);
+        const float w = __builtin_amdgcn_exp2f(d);
+        x[u][i] = w * __builtin_fmaf(b, fmaxf(d, kLow), a);
+      }
+      if (asked && (unsigned)(token - col) < 8u) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (token - col == i) x[u][i] += g;
+      }
+      store_piece(out, col, c.vocab, x[u]);
     }
-    store_piece(out, col, c.vocab, c.whole_out, x);
   }
 }
 

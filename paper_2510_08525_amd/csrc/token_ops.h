@@ -17,10 +17,15 @@ typedef float floats2 __attribute__((ext_vector_type(2)));
 typedef float floats4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16s2 __attribute__((ext_vector_type(2)));
 
-// Eight values of a storage type as they come from memory.
+// Eight values of a storage type as they come from memory.  They are aligned to one of them only: the hardware takes vector accesses at any
+// address, so rows of odd lengths and views that begin anywhere go the same way as others (a gradient of 2048 x 128011 bf16 logits
+// into rows without a gap between them: 453 us with their values stored one by one).
 template <typename T> struct Piece;
-template <> struct Piece<uint16_t> { words4 w; };
-template <> struct Piece<float> { floats4 a, b; };
+template <> struct Piece<uint16_t> { words4 w; } __attribute__((packed, aligned(2)));
+template <> struct Piece<float> { floats4 a, b; } __attribute__((packed, aligned(4)));
+typedef words2 words2_at_any_byte __attribute__((aligned(1)));
+typedef words2 words2_of_halves __attribute__((aligned(2)));
+typedef floats4 floats4_of_floats __attribute__((aligned(4)));
 
 __device__ __forceinline__ void widen(const Piece<uint16_t>& p, float (&f)[8]) {
 #pragma unroll
@@ -49,11 +54,10 @@ __device__ __forceinline__ float one_value(float v) { return v; }
 __device__ __forceinline__ void put_value(uint16_t* p, float v) { *p = (uint16_t)bf16_pair(v, 0.f); }
 __device__ __forceinline__ void put_value(float* p, float v) { *p = v; }
 
-// Columns [col, col + 8) of a row of n columns as fp32, zeros past its end; `whole`: the row starts at a multiple of 16 bytes, so that
-// a piece inside it is one or two 16-byte loads.
+// Columns [col, col + 8) of a row of n columns as fp32, zeros past its end.
 template <typename T>
-__device__ __forceinline__ void load_piece(const T* row, int col, int n, bool whole, float (&f)[8]) {
-  if (whole && col + 8 <= n) {
+__device__ __forceinline__ void load_piece(const T* row, int col, int n, float (&f)[8]) {
+  if (col + 8 <= n) {
     widen(*reinterpret_cast<const Piece<T>*>(row + col), f);
   } else {
 #pragma unroll
@@ -61,8 +65,8 @@ __device__ __forceinline__ void load_piece(const T* row, int col, int n, bool wh
   }
 }
 template <typename T>
-__device__ __forceinline__ void store_piece(T* row, int col, int n, bool whole, const float (&f)[8]) {
-  if (whole && col + 8 <= n) {
+__device__ __forceinline__ void store_piece(T* row, int col, int n, const float (&f)[8]) {
+  if (col + 8 <= n) {
     Piece<T> p;
     narrow(f, p);
     *reinterpret_cast<Piece<T>*>(row + col) = p;
@@ -73,15 +77,15 @@ __device__ __forceinline__ void store_piece(T* row, int col, int n, bool whole, 
   }
 }
 // Eight values as 8-bit ones (rounded to nearest even).
-__device__ __forceinline__ void store_e4m3(uint8_t* row, int col, int n, bool whole, const float (&f)[8]) {
+__device__ __forceinline__ void store_e4m3(uint8_t* row, int col, int n, const float (&f)[8]) {
   words2 w;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i], f[4 * i + 1], 0, false);
     w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f[4 * i + 2], f[4 * i + 3], lo, true);
   }
-  if (whole && col + 8 <= n) {
-    *reinterpret_cast<words2*>(row + col) = w;
+  if (col + 8 <= n) {
+    *reinterpret_cast<words2_at_any_byte*>(row + col) = w;
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -113,7 +117,6 @@ struct NormCall {
   float eps;
   int32_t rows, cols;
   int32_t norm;
-  int32_t whole_in, whole_res, whole_sum, whole_weight, whole_out;    // rows at multiples of what a vector access needs
 };
 hipError_t launch_norm(const NormCall& call, int dtype, bool out_e4m3, hipStream_t stream);
 
@@ -126,7 +129,6 @@ struct MatmulCall {
   void* out;
   int64_t a_stride, a_scale_stride, b_stride, b_scale_stride, out_stride;
   int32_t m, n, k;
-  int32_t whole_out;          // four neighbouring outputs, the first a multiple of four columns into a row, can be one store
 };
 constexpr int64_t kMostMatmulStride = 1 << 23;         // bytes between rows of a or b: a tile's rows are within 32 bits of its first
 hipError_t launch_matmul(const MatmulCall& call, bool out_bf16, hipStream_t stream);
@@ -144,7 +146,6 @@ struct LogprobCall {
   int64_t stride;
   float scale;
   int32_t rows, vocab, top;
-  int32_t whole;              // rows of logits start at multiples of 16 bytes
   int32_t chunks, splits;     // set by the launch
 };
 struct LogprobGradCall {
@@ -158,7 +159,6 @@ struct LogprobGradCall {
   int64_t stride, out_stride;
   float scale;
   int32_t rows, vocab;
-  int32_t whole, whole_out;
   int32_t splits;             // set by the launch
 };
 size_t logprob_workspace(int rows, int vocab, int top);
