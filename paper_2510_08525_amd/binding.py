@@ -419,6 +419,9 @@ class Cache:
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self._device_index = self.device.index or 0
         self._append_decode = load_library().rlkv_append_decode
+        self._append_rotary = load_library().rlkv_append_rotary
+        self._decode_attention = load_library().rlkv_decode_attention
+        self._packed_shape = (batch, (n_q_heads + 2 * n_kv_heads) * head_dim)
         self._q_shape = (batch, n_q_heads, head_dim)
         self._row_shape = (batch, n_kv_heads, 1, head_dim)
 
@@ -460,44 +463,51 @@ class Cache:
                            self._stream())
 
     def _packed(self, qkv, n_tokens):
-        """Address, token stride and tokens per sequence of packed projections [batch, tokens, >= (q + 2 kv heads) * head_dim]."""
-        s = self.shape
-        row = (s["n_q_heads"] + 2 * s["n_kv_heads"]) * s["head_dim"]
+        """Address, token stride, tokens and counts of packed projections [batch, tokens, (q + 2 kv heads) * head_dim]."""
+        if qkv.dim() != 3:
+            raise ValueError("qkv: need [batch, tokens, (q heads + 2 kv heads) * head_dim]")
+        B, T, width = qkv.shape
+        step, token, one = qkv.stride()
         if qkv.device != self.device or qkv.dtype != self.torch_dtype:
             raise ValueError(f"qkv: need a {self.torch_dtype} tensor on {self.device}")
-        if qkv.dim() != 3 or qkv.shape[0] != s["batch"] or qkv.shape[2] != row:
-            raise ValueError(f"qkv: shape {tuple(qkv.shape)} is not (batch, tokens, {row})")
-        B, T, _ = qkv.shape
-        token = qkv.stride(1) if T > 1 else qkv.stride(0) if B > 1 else row
-        if qkv.stride(2) != 1 or token < row or (B > 1 and T > 1 and qkv.stride(0) != T * token):
+        if (B, width) != self._packed_shape:
+            raise ValueError(f"qkv: shape {tuple(qkv.shape)} is not ({self._packed_shape[0]}, tokens, {self._packed_shape[1]})")
+        if T == 1:
+            token = step if B > 1 else width           # (the rows of the sequences are at equal distances)
+        elif B > 1 and step != T * token:
+            token = -1
+        if one != 1 or token < width:
             raise ValueError("qkv: need contiguous rows at equal distances")
-        if n_tokens is not None and len(n_tokens) != B:
-            raise ValueError("n_tokens must have batch entries")
-        return qkv.data_ptr(), token, T
+        if n_tokens is not None:
+            n_tokens = np.ascontiguousarray(np.asarray(n_tokens, dtype=np.int32))
+            if n_tokens.shape != (B,):
+                raise ValueError("n_tokens must have batch entries")
+        return qkv.data_ptr(), token, T, n_tokens
 
     def append_rotary(self, layer: int, qkv, n_tokens, rotary: Rotary, q_out=None):
         """Rotates and appends packed projections [batch, tokens, (q + 2 kv heads) * head_dim]; rotated queries to q_out
         ([batch, q heads, tokens, head_dim], for one token also without that axis).  n_tokens None: all tokens of every active sequence."""
-        s = self.shape
-        ptr, token, T = self._packed(qkv, n_tokens)
-        out = 0
+        ptr, token, T, counts = self._packed(qkv, n_tokens)
+        out = None
         if q_out is not None:
-            out = self._ptr(q_out, self._q_shape if T == 1 and q_out.dim() == 3 else (s["batch"], s["n_q_heads"], T, s["head_dim"]), "q_out")
-        rlkv_append_rotary(self.handle, layer, ptr, token, n_tokens, T, rotary, out, self._stream())
+            B, Hq, D = self._q_shape
+            out = self._ptr(q_out, self._q_shape if T == 1 and q_out.dim() == 3 else (B, Hq, T, D), "q_out")
+        _check(self._append_rotary(self.handle, layer, ptr, token, None if counts is None else counts.ctypes.data, T, rotary.address, out,
+                                   self._stream()), "rlkv_append_rotary")
 
     def rotary(self, layer: int, qkv, n_tokens, rotary: Rotary, q_out, k_out, v_out):
         """Rotates packed projections and hands them out heads first, as prefill_attention and append_decode take them."""
         s = self.shape
-        ptr, token, T = self._packed(qkv, n_tokens)
+        ptr, token, T, counts = self._packed(qkv, n_tokens)
         kv = (s["batch"], s["n_kv_heads"], T, s["head_dim"])
         q = self._ptr(q_out, self._q_shape if T == 1 and q_out.dim() == 3 else (s["batch"], s["n_q_heads"], T, s["head_dim"]), "q_out")
-        rlkv_rotary(self.handle, layer, ptr, token, n_tokens, T, rotary, q, self._ptr(k_out, kv, "k_out"), self._ptr(v_out, kv, "v_out"),
+        rlkv_rotary(self.handle, layer, ptr, token, counts, T, rotary, q, self._ptr(k_out, kv, "k_out"), self._ptr(v_out, kv, "v_out"),
                     self._stream())
 
     def decode_attention(self, layer: int, q, out, softmax_scale: float):
         shp = self._q_shape
-        rlkv_decode_attention(self.handle, layer, self._ptr(q, shp, "q"), self._ptr(out, shp, "out"),
-                              softmax_scale, self._stream())
+        _check(self._decode_attention(self.handle, layer, self._ptr(q, shp, "q"), self._ptr(out, shp, "out"), softmax_scale,
+                                      self._stream()), "rlkv_decode_attention")
 
     def decode_attention_noalloc(self, layer: int, q, out, softmax_scale: float):
         s = self.shape

@@ -855,7 +855,7 @@ static rlkv_status_t rotary_args(rlkv_cache_t* cache, int32_t layer, const void*
     // (whole turns do not matter, and what is left is below 1 unless it was rounded up to it)
     double t = rotary->inv_freq[i] * 0.15915494309189533577;          // 1 / (2 pi)
     t -= floor(t);
-    args->turns.turn[i] = t < 1.0 ? (uint64_t)ldexp(t, 64) : 0;
+    args->turns.turn[i] = t < 1.0 ? (uint64_t)(t * 18446744073709551616.0) : 0;         // 2^64
   }
   args->turns.pairs = pairs;
   args->turns.interleaved = rotary->interleaved;

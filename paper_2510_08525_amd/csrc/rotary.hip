@@ -181,10 +181,93 @@ __global__ __launch_bounds__(kBlock) void rotary_kernel(DeviceView dv, int layer
   }
 }
 
+// One token a sequence (a decode step): the same work laid out for latency.  Eight threads have a query head's row, or a KV head's key and
+// value row; the rows are asked for before anything that says where they go, and a row's pieces are stored from registers.
+constexpr int kStepBlock = 64;
+template <int KERNEL, typename T>
+__global__ __launch_bounds__(kStepBlock) void rotary_step_kernel(DeviceView dv, int layer, const int32_t* __restrict__ len_in,
+                                                                 int32_t* __restrict__ len_out, RotaryCall call, RotaryTurns turns, int ragged,
+                                                                 SeqCounts seqs, int first_head) {
+  const int Hq = dv.n_q_heads, H = dv.n_kv_heads, heads = Hq + H - first_head;
+  const int index = blockIdx.x * (kStepBlock / kRowThreads) + threadIdx.x / kRowThreads, j = threadIdx.x % kRowThreads;
+  const int b = index / heads, head = first_head + index % heads, h = head - Hq;
+  if (b >= dv.batch) return;
+  const int c0 = first_piece(turns, j) * 8, c1 = second_piece(turns, j) * 8;
+  const T* row = static_cast<const T*>(call.qkv) + (int64_t)b * call.stride_tokens * call.token_stride + (int64_t)head * kHeadDim;
+  float x[8], y[8], v0[8], v1[8];
+  load_piece(row, c0, kHeadDim, x);
+  load_piece(row, c1, kHeadDim, y);
+  if (h >= 0) {
+    load_piece(row + (int64_t)H * kHeadDim, c0, kHeadDim, v0);
+    load_piece(row + (int64_t)H * kHeadDim, c1, kHeadDim, v1);
+  }
+  const int n = len_in[b];
+  const bool there = ragged ? (seqs.in_args ? seqs.tok[b] : dv.append_cnt[b]) != 0 : dv.active[b] != 0;
+  if (h == 0 && j == 0) len_out[b] = n + there;
+  if (!ragged && b == 0 && h == 0 && j == 0) list_header(dv, layer)->grow += 1;
+  if (!there) return;
+  if (j < turns.pairs / 8) {
+    Angles g;
+    angles_of(turns, j, (uint32_t)n, g);
+    rotate(turns, g, x, y);
+  }
+  if (h < 0) {
+    T* out = static_cast<T*>(call.q_out) + ((int64_t)b * Hq + head) * call.stride_tokens * kHeadDim;
+    store_piece(out, c0, kHeadDim, x);
+    store_piece(out, c1, kHeadDim, y);
+    return;
+  }
+  const bool full = dv.full_mask[layer * H + h] != 0;
+  const int S = dv.sink, slot = full || n < S ? n : S + (n - S) % dv.recent;
+  if (!full && j == 0) dv.slot_pos[dv.slotpos_off[layer * H + h] + (int64_t)b * dv.window + slot] = n;
+  char* store = dv.kv_base + dv.store_off[((int64_t)layer * dv.batch + b) * H + h];
+  if constexpr (KERNEL == RLKV_KERNEL_MFMA) {
+    const int tile = slot / kTile, s = slot % kTile, s16 = s & 15;
+    char* base = store + (int64_t)tile * kTileBytes;
+    if (full && dv.page_shift >= 0)
+      base = store + dv.block_table[(int64_t)b * dv.table_stride + (tile >> dv.page_shift)] * dv.page_bytes +
+             (int64_t)(tile & dv.page_mask) * kTileBytes;
+    // K: [half][chunk][slot % 16]; V: [d / 16][kb][d % 16][e] (rlkv_internal.h)
+    const int kb = (s16 >> 2), e = (s >> 4) * 4 + (s & 3);
+    bool wide = false;
+    auto put = [&](const float (&k)[8], const float (&v)[8], int col) {
+      Piece<uint16_t> piece;
+      narrow(k, piece);
+      *reinterpret_cast<words4*>(base + (s >> 4) * 4096 + (col >> 3) * 256 + s16 * 16) = piece.w;
+      narrow(v, piece);
+      uint16_t* to = reinterpret_cast<uint16_t*>(base + kTileBytes / 2) + (((col >> 4) * 4 + kb) * 16 + (col & 15)) * 8 + e;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) to[i * 8] = (uint16_t)(piece.w[i >> 1] >> (16 * (i & 1)));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) wide |= any_beyond_fp16(piece.w[i]);
+    };
+    put(x, v0, c0);
+    put(y, v1, c1);
+    if (wide) dv.v_wide[layer] = 1;        // the prefill kernel takes this layer's V as bf16 from now on
+  } else {
+    const int cap = full ? dv.cap_pad[b] : dv.window_pad;
+    T* krow = reinterpret_cast<T*>(store + (int64_t)slot * dv.row_bytes);
+    T* vrow = reinterpret_cast<T*>(store + (int64_t)(cap + slot) * dv.row_bytes);
+    store_piece(krow, c0, kHeadDim, x);
+    store_piece(krow, c1, kHeadDim, y);
+    store_piece(vrow, c0, kHeadDim, v0);
+    store_piece(vrow, c1, kHeadDim, v1);
+  }
+}
+
 template <int KERNEL, typename T, bool APPEND>
 hipError_t launch_typed(const DeviceView& dv, int layer, const int32_t* len_in, int32_t* len_out, const RotaryCall& call,
                         const RotaryTurns& turns, const SeqCounts* seqs, hipStream_t stream) {
   const SeqCounts none = {};
+  if constexpr (APPEND) {
+    if (call.max_tokens == 1) {
+      const int first_head = call.q_out ? 0 : dv.n_q_heads;
+      const int64_t threads = (int64_t)dv.batch * (dv.n_q_heads + dv.n_kv_heads - first_head) * kRowThreads;
+      hipLaunchKernelGGL((rotary_step_kernel<KERNEL, T>), dim3((unsigned)((threads + kStepBlock - 1) / kStepBlock)), dim3(kStepBlock), 0, stream,
+                         dv, layer, len_in, len_out, call, turns, seqs != nullptr, seqs ? *seqs : none, first_head);
+      return hipGetLastError();
+    }
+  }
   const int n_heads = APPEND ? (call.q_out ? dv.n_q_heads : 0) : dv.n_q_heads + 2 * dv.n_kv_heads;
   const int jobs = append_jobs(call.max_tokens);
   const int64_t tokens = (int64_t)dv.batch * call.max_tokens;

@@ -11,9 +11,11 @@
 // that; a row of nothing else has lse -inf.
 //
 // Most likely tokens: the key of a logit is (value, lowest index first) in 64 bits.  A workgroup works through its columns in chunks that
-// it holds in registers.  The k-th largest of the 64 lanes' maxima of a wavefront is a value that at least k logits of the chunk
-// reach; the largest such bound of the workgroup, or the k-th best so far where that is more, lets few logits through, which are collected in LDS and
-// ranked by counting.  A chunk that lets through more than the list holds (ties, masks) is searched maximum by maximum.
+// it holds in registers, and collects in LDS what may be among the k best: what reaches the k-th best known so far and, where
+// many lanes of a wavefront have something that does, the k-th largest of the lanes' maxima (k logits of this chunk reach that: 20 of 4096
+// random ones let 24 through).  The list is ranked by counting when it
+// has grown to some times k, which raises what the next chunks have to reach, and at the end.  A chunk that lets through
+// more than the list holds (ties, masks) is searched maximum by maximum.
 // Few rows are split over workgroups, whose partial results a second kernel joins in a fixed order.
 // Bound: HBM; 6 or 7 vector instructions and an exponential a logit are not far behind.
 #include <type_traits>
@@ -25,9 +27,9 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int kThreads = 256;
-constexpr int kPieces = 8;                              // pieces of eight logits of a thread in a chunk
-constexpr int kChunk = kThreads * kPieces * 8;
+constexpr int kPieces = 8, kFewPieces = 2;              // pieces of eight logits of a thread in a chunk, of many rows and of few
 constexpr int kList = 1024;                             // candidates a workgroup ranks at once
+constexpr int kMostSplits = 64;                         // workgroups a row is split over: a lane each when they are joined
 constexpr float kMaskedLse = -1e30f;
 constexpr float kLow = -256.f;                          // in the place of exponents so low that their weight is 0
 
@@ -64,106 +66,126 @@ __device__ __forceinline__ uint64_t max_of_wave(uint64_t x) {
   }
   return x;
 }
-// The k-th largest (k from 1) of the 64 lanes' values: how many are larger, and how many equal ones have a lower lane.
-__device__ __forceinline__ uint32_t kth_of_wave(uint32_t x, int k) {
-  const int lane = threadIdx.x & 63;
-  int rank = 0;
-  for (int i = 0; i < 64; ++i) {
-    const uint32_t y = __builtin_amdgcn_readlane(x, i);
-    rank += y > x || (y == x && i < lane);
+// A bound that k lanes (k from 1) of a wavefront reach: the k-th largest of their orders, cut to its upper 16 bits.
+__device__ __forceinline__ uint32_t kth_of_wave(uint32_t order, int k) {
+  const uint32_t upper = order >> 16;
+  uint32_t kth = 0;
+#pragma unroll
+  for (int bit = 15; bit >= 0; --bit) {
+    const uint32_t next = kth | 1u << bit;
+    if (__popcll(__ballot(upper >= next)) >= k) kth = next;
   }
-  const uint64_t at = __ballot(rank == k - 1);
-  return __builtin_amdgcn_readlane(x, __builtin_ctzll(at));
+  return kth << 16;
 }
+// The same as a value: what is at least that large reaches it.
+__device__ __forceinline__ float bound_of(uint32_t order) { return order < 0x00800000u ? -INFINITY : value_of(order); }
 
 struct TopLds {
   uint64_t best[kMostTop];          // the best so far, largest first, 0 = none
-  uint64_t list[kList];
+  alignas(16) uint64_t list[kList + 8];      // candidates, the best so far first, and room for zeros behind them
   uint64_t wave_best[kThreads / 64];
-  uint32_t bound[kThreads / 64];
   int32_t n;
 };
 
-// list[0, n) (distinct keys, n <= kList, all threads past a barrier) -> the k largest of them into best, in order.
+// list[0, n) (distinct keys and zeros, k <= n <= kList, all threads past a barrier) -> the k largest of them into best, in order.  (Equal zeros
+// take one place, and those behind it hold zeros already: what was there before is in the list too.)
 __device__ void rank_list(TopLds& lds, int n, int k) {
+  if (threadIdx.x < 8) lds.list[n + threadIdx.x] = 0;            // (eight keys a turn, all of them on their way at once)
+  __syncthreads();
   for (int i = threadIdx.x; i < n; i += kThreads) {
     const uint64_t x = lds.list[i];
     int rank = 0;
-    for (int o = 0; o < n; ++o) rank += lds.list[o] > x;
+    for (int o = 0; o < n; o += 8) {
+      uint64_t y[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) y[u] = lds.list[o + u];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) rank += y[u] > x;
+    }
     if (rank < k) lds.best[rank] = x;
   }
-  if ((int)threadIdx.x >= n && (int)threadIdx.x < k) lds.best[threadIdx.x] = 0;
+  __syncthreads();
+}
+// The list is the best so far and nothing else.
+__device__ void restart_list(TopLds& lds, int k) {
+  if ((int)threadIdx.x < k) lds.list[threadIdx.x] = lds.best[threadIdx.x];
+  if (threadIdx.x == 0) lds.n = k;
   __syncthreads();
 }
 
-// Brings the chunk that starts at column `first` (valid: below `last`), in x, into the best k.
-__device__ void top_of_chunk(TopLds& lds, const float (&x)[kPieces][8], int first, int last, int k) {
+template <typename T> __device__ __forceinline__ float value_at(const Piece<T>& p, int i);
+template <> __device__ __forceinline__ float value_at<uint16_t>(const Piece<uint16_t>& p, int i) {
+  return __uint_as_float(i & 1 ? p.w[i >> 1] & 0xffff0000u : p.w[i >> 1] << 16);
+}
+template <> __device__ __forceinline__ float value_at<float>(const Piece<float>& p, int i) { return i < 4 ? p.a[i] : p.b[i - 4]; }
+
+// Brings the chunk that starts at column `first` (valid: below `last`), in x, into the list.  most: a lane's largest logit of the chunk;
+// odd: the lane has met a NaN or an infinity; bound: what a logit has to reach to be among the k best, the same in all lanes; row: the logits again.
+template <typename T, int PIECES>
+__device__ void top_of_chunk(TopLds& lds, const Piece<T> (&x)[PIECES], const T* row, int first, int last, int k, float most, bool odd,
+                             float& bound) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  uint32_t most = 0;
-#pragma unroll
-  for (int p = 0; p < kPieces; ++p)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int col = first + (p * kThreads + tid) * 8 + i;
-      const uint32_t o = col < last ? order_of(x[p][i]) : 0;
-      most = o > most ? o : most;
-    }
-  const uint32_t own = kth_of_wave(most, k);
-  if (lane == 0) lds.bound[wave] = own;
-  if (tid < k) lds.list[tid] = lds.best[tid];
-  if (tid == 0) lds.n = k;
+  const int n_before = lds.n;
   __syncthreads();
-  uint64_t bound = 0;
+  const uint64_t some = __ballot(most >= bound);
+  const bool any_odd = __ballot(odd) != 0;
+  if (some != 0 || any_odd) {
+    float reach = bound;
+    if (!any_odd && __popcll(some) > k) reach = fmaxf(reach, bound_of(kth_of_wave(order_of(most), k)));
+    // Which logits of the lane pass (a NaN does), then their keys from the row itself: one counter update a wavefront, and no code per logit.
+    uint64_t pass = 0;
 #pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) bound = lds.bound[w] > bound ? lds.bound[w] : bound;
-  bound <<= 32;                                                  // (equal values pass, whatever their index)
-  const uint64_t worst = lds.best[k - 1];
-  bound = worst > bound ? worst : bound;
-  bool any = (uint64_t)most << 32 >= (bound & 0xffffffff00000000ull);
-  if (any) {
+    for (int p = 0; p < PIECES; ++p) {
+      uint32_t bits = 0;
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int col = first + (p * kThreads + tid) * 8 + i;
-        if (col >= last) continue;
-        const uint64_t key = key_of(x[p][i], col);
-        if (key < bound) continue;
-        const int at = atomicAdd(&lds.n, 1);
-        if (at < kList) lds.list[at] = key;
+      for (int i = 0; i < 8; ++i) bits |= value_at(x[p], i) < reach ? 0u : 1u << i;
+      const int col = first + (p * kThreads + tid) * 8;
+      if (col + 8 > last) bits &= col < last ? (1u << (last - col)) - 1u : 0u;
+      pass |= (uint64_t)bits << (8 * p);
+    }
+    if (pass != 0) {
+      int at = atomicAdd(&lds.n, __popcll(pass));
+      for (; pass != 0 && at < kList; pass &= pass - 1, ++at) {
+        const int bit = __builtin_ctzll(pass), col = first + ((bit >> 3) * kThreads + tid) * 8 + (bit & 7);
+        lds.list[at] = key_of(one_value(row[col]), col);
       }
+    }
   }
   __syncthreads();
   const int n = lds.n;
-  __syncthreads();
+  if (n <= 4 * k + 32) return;
   if (n <= kList) {
-    // (places that hold no key yet are 0 and equal: they rank behind all keys, where nothing reads more than a 0)
     rank_list(lds, n, k);
-    return;
-  }
-  // Maximum by maximum, each below the one before; list[0, k) still has the best of the chunks before.
-  uint64_t below = ~0ull;
-  for (int r = 0; r < k; ++r) {
-    uint64_t best = tid < k && lds.list[tid] < below ? lds.list[tid] : 0;
-#pragma unroll
-    for (int p = 0; p < kPieces; ++p)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int col = first + (p * kThreads + tid) * 8 + i;
-        if (col >= last) continue;
-        const uint64_t key = key_of(x[p][i], col);
+  } else {
+    // Maximum by maximum, each below the one before, of this chunk and of what was in the list before it.
+    __syncthreads();
+    uint64_t below = ~0ull;
+    for (int r = 0; r < k; ++r) {
+      uint64_t best = 0;
+      for (int i = tid; i < n_before; i += kThreads) {
+        const uint64_t key = lds.list[i];
         if (key < below && key > best) best = key;
       }
-    best = max_of_wave(best);
-    if (lane == 0) lds.wave_best[wave] = best;
-    __syncthreads();
-    best = 0;
+      const int end = first + kThreads * PIECES * 8 < last ? first + kThreads * PIECES * 8 : last;
+      for (int col = first + tid; col < end; col += kThreads) {
+        const uint64_t key = key_of(one_value(row[col]), col);
+        if (key < below && key > best) best = key;
+      }
+      best = max_of_wave(best);
+      if (lane == 0) lds.wave_best[wave] = best;
+      __syncthreads();
+      best = 0;
 #pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) best = lds.wave_best[w] > best ? lds.wave_best[w] : best;
-    if (tid == 0) lds.best[r] = best;
-    below = best;
-    __syncthreads();
+      for (int w = 0; w < kThreads / 64; ++w) best = lds.wave_best[w] > best ? lds.wave_best[w] : best;
+      if (tid == 0) lds.best[r] = best;
+      below = best;
+      __syncthreads();
+    }
   }
+  // (Later columns do not displace an equal logit: more than the k-th best's value is needed.  0: there are fewer than k yet.)
+  const uint32_t worst = (uint32_t)(lds.best[k - 1] >> 32);
+  bound = worst == 0 ? -INFINITY : worst >= order_of(INFINITY) ? INFINITY : value_of(worst + 1);
+  restart_list(lds, k);
 }
 
 __device__ __forceinline__ Stats stats_of_block(Stats v, Stats (&parts)[kThreads / 64], float scale2) {
@@ -205,8 +227,9 @@ __device__ void finish_row(const LogprobCall& c, int row, const Stats& v, const 
   }
 }
 
-template <typename T, bool TOP>
+template <typename T, bool TOP, int PIECES>
 __global__ __launch_bounds__(kThreads) void rows_kernel(LogprobCall c) {
+  constexpr int kChunk = kThreads * PIECES * 8;
   __shared__ Stats parts[kThreads / 64];
   __shared__ std::conditional_t<TOP, TopLds, char> lds;
   const int row = blockIdx.x / c.splits, split = blockIdx.x % c.splits;
@@ -214,29 +237,34 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LogprobCall c) {
   const T* logits = static_cast<const T*>(c.logits) + row * c.stride;
   const float scale2 = c.scale * kLog2e;
   Stats v = {-INFINITY, 0.f, 0.f};
+  float bound = -INFINITY;
   if constexpr (TOP) {
     if ((int)threadIdx.x < c.top) lds.best[threadIdx.x] = 0;
     __syncthreads();
+    restart_list(lds, c.top);
   }
   for (int chunk = begin; chunk < end; ++chunk) {
     const int first = chunk * kChunk;
     const int last = c.vocab;
-    float x[kPieces][8];
+    Piece<T> x[PIECES];
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p) {
+    for (int p = 0; p < PIECES; ++p) {
       const int col = first + (p * kThreads + (int)threadIdx.x) * 8;
       if (col + 8 <= last) {
-        widen(*reinterpret_cast<const Piece<T>*>(logits + col), x[p]);
+        x[p] = *reinterpret_cast<const Piece<T>*>(logits + col);
       } else {
+        float f[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[p][i] = col + i < last ? one_value(logits[col + i]) : -INFINITY;
+        for (int i = 0; i < 8; ++i) f[i] = col + i < last ? one_value(logits[col + i]) : -INFINITY;
+        narrow(f, x[p]);
       }
     }
-    float m = v.m;
+    float most = -INFINITY;
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p)
+    for (int p = 0; p < PIECES; ++p)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) m = fmaxf(m, x[p][i]);
+      for (int i = 0; i < 8; ++i) most = fmaxf(most, value_at(x[p], i));
+    const float m = fmaxf(v.m, most);
     const float base = m == -INFINITY ? 0.f : m;                // (all masked so far: exponents of -inf, not NaN)
     if (v.m != -INFINITY) {
       const float d = (v.m - base) * scale2, w = __builtin_amdgcn_exp2f(d);
@@ -245,19 +273,22 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LogprobCall c) {
     }
     v.m = m;
 #pragma unroll
-    for (int p = 0; p < kPieces; ++p)
+    for (int p = 0; p < PIECES; ++p)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float d = (x[p][i] - base) * scale2;
+        const float d = (value_at(x[p], i) - base) * scale2;
         const float e = __builtin_amdgcn_exp2f(d);
         v.s += e;
         v.t = __builtin_fmaf(e, fmaxf(d, kLow), v.t);
       }
-    if constexpr (TOP) top_of_chunk(lds, x, first, last, c.top);
+    if constexpr (TOP) top_of_chunk<T, PIECES>(lds, x, logits, first, last, c.top, most, v.s != v.s, bound);
+  }
+  const uint64_t* best = nullptr;
+  if constexpr (TOP) {
+    rank_list(lds, lds.n, c.top);
+    best = lds.best;
   }
   v = stats_of_block(v, parts, scale2);
-  const uint64_t* best = nullptr;
-  if constexpr (TOP) best = lds.best;
   if (c.splits == 1) {
     finish_row<T, TOP>(c, row, v, best);
   } else {
@@ -267,26 +298,50 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LogprobCall c) {
   }
 }
 
-template <typename T>
+// A row's parts: a lane each, joined over lanes; of their lists, what reaches a bound that k entries reach is ranked.
+template <typename T, bool TOP>
 __global__ __launch_bounds__(kThreads) void join_kernel(LogprobCall c) {
-  __shared__ TopLds lds;
-  const int row = blockIdx.x;
+  __shared__ std::conditional_t<TOP, TopLds, char> lds;
+  const int row = blockIdx.x, lane = threadIdx.x & 63;
   const int64_t at = (int64_t)row * c.splits;
-  Stats v = *part_stats(c, at);
-  for (int s = 1; s < c.splits; ++s) v = join(v, *part_stats(c, at + s), c.scale * kLog2e);
-  if (c.top) {
-    if ((int)threadIdx.x < c.top) lds.best[threadIdx.x] = 0;
-    __syncthreads();
-    const int n = c.splits * c.top;
-    for (int first = 0; first < n; first += kList - kMostTop) {
-      const int some = n - first < kList - kMostTop ? n - first : kList - kMostTop;
-      for (int i = threadIdx.x; i < some; i += kThreads) lds.list[c.top + i] = part_best(c, at)[first + i];
-      if ((int)threadIdx.x < c.top) lds.list[threadIdx.x] = lds.best[threadIdx.x];
-      __syncthreads();
-      rank_list(lds, c.top + some, c.top);
+  Stats v = {-INFINITY, 0.f, 0.f};
+  if (lane < c.splits) v = *part_stats(c, at + lane);
+#pragma unroll
+  for (int m = 1; m < kMostSplits; m <<= 1) v = join(v, Stats{__shfl_xor(v.m, m), __shfl_xor(v.s, m), __shfl_xor(v.t, m)}, c.scale * kLog2e);
+  const uint64_t* best = nullptr;
+  if constexpr (TOP) {
+    const int n = c.splits * c.top, k = c.top;
+    // Entry `deep` of every list and those before it are k at least: k entries reach the least of these; or, with as many lists as k, the
+    // k-th largest of their first.
+    const int deep = (k + c.splits - 1) / c.splits - 1;
+    const uint64_t* lists = part_best(c, at);
+    uint32_t bound;
+    if (deep == 0) {
+      bound = kth_of_wave(lane < c.splits ? (uint32_t)(lists[lane * k] >> 32) : 0u, k);
+    } else {
+      uint32_t least = lane < c.splits ? (uint32_t)(lists[lane * k + deep] >> 32) : 0xffffffffu;
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) least = min(least, (uint32_t)__shfl_xor(least, m));
+      bound = least;
     }
+    if ((int)threadIdx.x < k) lds.best[threadIdx.x] = 0;
+    __syncthreads();
+    restart_list(lds, k);
+    // (kList keys at a time, in case of ties: the rest of the lists is as many turns of the loop away)
+    for (int first = 0; first < n; first += kList - kMostTop) {
+      const int end = first + kList - kMostTop < n ? first + kList - kMostTop : n;
+      for (int i = first + threadIdx.x; i < end; i += kThreads) {
+        const uint64_t key = lists[i];
+        if (key != 0 && (uint32_t)(key >> 32) >= bound) lds.list[atomicAdd(&lds.n, 1)] = key;
+      }
+      __syncthreads();
+      const int some = lds.n;
+      rank_list(lds, some, k);
+      restart_list(lds, k);
+    }
+    best = lds.best;
   }
-  finish_row<T, true>(c, row, v, lds.best);
+  finish_row<T, TOP>(c, row, v, best);
 }
 
 constexpr int kGradPieces = 4;                          // pieces of a thread whose loads are in flight together
@@ -336,32 +391,41 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(LogprobGradCall c) {
 
 }  // namespace
 
-int logprob_chunks(int vocab) { return (vocab + kChunk - 1) / kChunk; }
-
-// Workgroups a row is split over: as many as fill the card some times over, one per chunk at most.
-int logprob_splits(int rows, int vocab) {
-  const int chunks = logprob_chunks(vocab);
-  if (rows >= 1024) return 1;
-  const int want = (1024 + rows - 1) / rows;
-  return want < chunks ? want : chunks;
+// Chunks of a row and workgroups it is split over.  Many rows fill the card by themselves, and rows of two chunks are not worth the launch
+// that joins them (64 x 32000 fp32: 4.7 + 3.2 us split, 5.7 whole); few rows are spread over workgroups, as many as fill the compute
+// units twice, in chunks of a quarter of the size where those of the full size do not fill them once.
+static int chunks_of(int vocab, int pieces) { return (int)(((int64_t)vocab + kThreads * 8 * pieces - 1) / (kThreads * 8 * pieces)); }
+static bool whole_rows(int rows, int vocab) { return rows >= 512 || chunks_of(vocab, kPieces) <= 2; }
+static bool small_chunks(int rows, int vocab) { return !whole_rows(rows, vocab) && (int64_t)rows * chunks_of(vocab, kPieces) < 256; }
+static int logprob_chunks(int rows, int vocab) { return chunks_of(vocab, small_chunks(rows, vocab) ? kFewPieces : kPieces); }
+static int logprob_splits(int rows, int vocab) {
+  if (whole_rows(rows, vocab)) return 1;
+  const int chunks = logprob_chunks(rows, vocab), want = (512 + rows - 1) / rows;
+  const int most = want < kMostSplits ? want : kMostSplits;
+  return most < chunks ? most : chunks;
 }
 size_t logprob_workspace(int rows, int vocab, int top) {
-  const size_t parts = (size_t)rows * logprob_splits(rows, vocab);
-  if (logprob_splits(rows, vocab) <= 1) return 0;
+  const int splits = logprob_splits(rows, vocab);
+  if (splits <= 1) return 0;
+  const size_t parts = (size_t)rows * splits;
   return (parts * sizeof(Stats) + 7) / 8 * 8 + parts * top * sizeof(uint64_t);
 }
 
+template <typename T, bool TOP>
+static hipError_t launch_rows(const LogprobCall& c, hipStream_t stream) {
+  const dim3 grid((unsigned)c.rows * c.splits), block(kThreads);
+  if (small_chunks(c.rows, c.vocab)) hipLaunchKernelGGL((rows_kernel<T, TOP, kFewPieces>), grid, block, 0, stream, c);
+  else hipLaunchKernelGGL((rows_kernel<T, TOP, kPieces>), grid, block, 0, stream, c);
+  if (hipError_t e = hipGetLastError()) return e;
+  if (c.splits > 1) hipLaunchKernelGGL((join_kernel<T, TOP>), dim3((unsigned)c.rows), block, 0, stream, c);
+  return hipGetLastError();
+}
+
 hipError_t launch_logprobs(LogprobCall c, int dtype, hipStream_t stream) {
-  c.chunks = logprob_chunks(c.vocab);
+  c.chunks = logprob_chunks(c.rows, c.vocab);
   c.splits = logprob_splits(c.rows, c.vocab);
-  auto run = [&](auto rows, auto join) {
-    hipLaunchKernelGGL(rows, dim3((unsigned)c.rows * c.splits), dim3(kThreads), 0, stream, c);
-    if (hipError_t e = hipGetLastError()) return e;
-    if (c.splits > 1) hipLaunchKernelGGL(join, dim3((unsigned)c.rows), dim3(kThreads), 0, stream, c);
-    return hipGetLastError();
-  };
-  if (dtype == RLKV_F32) return c.top ? run(rows_kernel<float, true>, join_kernel<float>) : run(rows_kernel<float, false>, join_kernel<float>);
-  return c.top ? run(rows_kernel<uint16_t, true>, join_kernel<uint16_t>) : run(rows_kernel<uint16_t, false>, join_kernel<uint16_t>);
+  if (dtype == RLKV_F32) return c.top ? launch_rows<float, true>(c, stream) : launch_rows<float, false>(c, stream);
+  return c.top ? launch_rows<uint16_t, true>(c, stream) : launch_rows<uint16_t, false>(c, stream);
 }
 
 hipError_t launch_logprobs_grad(LogprobGradCall c, int dtype, hipStream_t stream) {

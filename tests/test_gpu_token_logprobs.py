@@ -291,6 +291,6 @@ def test_tensor_checks():
     for bad in (lambda: rl.token_logprobs(x, tokens, None), lambda: rl.token_logprobs(x, tokens, f, scale=0.0),
                 lambda: rl.token_logprobs(x, tokens, f, scale=-1.0), lambda: rl.token_logprobs(x[:, :2], tokens, f, top=top),
                 lambda: rl.token_logprobs_grad(x, tokens, f, None, x.clone()), lambda: rl.token_logprobs_grad(x, tokens, f, f, x.clone(), entropy=f),
-                lambda: rl.token_logprobs(_logits(4, 20000, torch.bfloat16, 1)[0], tokens, f, workspace=torch.empty(1, dtype=torch.uint8, device="cuda"))):
+                lambda: rl.token_logprobs(_logits(4, 100000, torch.bfloat16, 1)[0], tokens, f, workspace=torch.empty(1, dtype=torch.uint8, device="cuda"))):
         with pytest.raises(rl.RlkvError):
             bad()
