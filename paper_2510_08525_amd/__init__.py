@@ -5,7 +5,7 @@ include/rlkv.h).  This package is the thin Python binding over it: argument mars
 only; PyTorch provides device memory and streams.
 """
 from .binding import (RLKV_BF16, RLKV_E4M3, RLKV_F32, RLKV_KERNEL_AUTO, RLKV_KERNEL_MFMA,  # noqa: F401
-                      RLKV_KERNEL_VALU, Cache, RlkvError, Rotary, library_path, load_library,
+                      RLKV_KERNEL_VALU, Cache, RlkvError, Rotary, library_path, load_library, tensor_calls,
                       rlkv_append, rlkv_append_rotary, rlkv_rotary, rlkv_append_decode, rlkv_append_decode_launch, rlkv_append_decode_prepare, rlkv_append_ragged, rlkv_cache_create, rlkv_cache_destroy,
                       rlkv_cache_kernel, rlkv_cache_required_bytes, rlkv_cache_reset,
                       rlkv_decode_attention, rlkv_decode_attention_noalloc, rlkv_get_lengths, rlkv_get_slot_positions, rlkv_profile_collect, rlkv_profile_enable,

@@ -121,6 +121,22 @@ def load_library():
     return lib
 
 
+_tensor_calls = None
+
+
+def tensor_calls():
+    """The module of the operators' calls on tensors, built in-tree beside librlkv.so (csrc/tensor_calls.cpp); raises if absent."""
+    global _tensor_calls
+    if _tensor_calls is None:
+        import torch  # noqa: F401  (its libraries have to be there first)
+
+        load_library()
+        from . import _tensor_calls as module
+
+        _tensor_calls = module
+    return _tensor_calls
+
+
 EXPORTED_SYMBOLS = (
     "rlkv_cache_required_bytes", "rlkv_cache_create", "rlkv_cache_destroy", "rlkv_cache_reset",
     "rlkv_append", "rlkv_append_ragged", "rlkv_decode_attention", "rlkv_decode_attention_noalloc", "rlkv_set_active", "rlkv_set_gates", "rlkv_append_decode", "rlkv_append_decode_prepare", "rlkv_append_decode_launch", "rlkv_worklists_built", "rlkv_prefill_attention", "rlkv_profile_enable",
@@ -419,9 +435,8 @@ class Cache:
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self._device_index = self.device.index or 0
         self._append_decode = load_library().rlkv_append_decode
-        self._append_rotary = load_library().rlkv_append_rotary
         self._decode_attention = load_library().rlkv_decode_attention
-        self._packed_shape = (batch, (n_q_heads + 2 * n_kv_heads) * head_dim)
+        self._call_shape = (self._device_index, dtype, batch, n_q_heads, n_kv_heads, head_dim)
         self._q_shape = (batch, n_q_heads, head_dim)
         self._row_shape = (batch, n_kv_heads, 1, head_dim)
 
@@ -462,47 +477,29 @@ class Cache:
         rlkv_append_ragged(self.handle, layer, self._ptr(k, shp, "k"), self._ptr(v, shp, "v"), n_tokens, stride,
                            self._stream())
 
-    def _packed(self, qkv, n_tokens):
-        """Address, token stride, tokens and counts of packed projections [batch, tokens, (q + 2 kv heads) * head_dim]."""
-        if qkv.dim() != 3:
-            raise ValueError("qkv: need [batch, tokens, (q heads + 2 kv heads) * head_dim]")
-        B, T, width = qkv.shape
-        step, token, one = qkv.stride()
-        if qkv.device != self.device or qkv.dtype != self.torch_dtype:
-            raise ValueError(f"qkv: need a {self.torch_dtype} tensor on {self.device}")
-        if (B, width) != self._packed_shape:
-            raise ValueError(f"qkv: shape {tuple(qkv.shape)} is not ({self._packed_shape[0]}, tokens, {self._packed_shape[1]})")
-        if T == 1:
-            token = step if B > 1 else width           # (the rows of the sequences are at equal distances)
-        elif B > 1 and step != T * token:
-            token = -1
-        if one != 1 or token < width:
-            raise ValueError("qkv: need contiguous rows at equal distances")
-        if n_tokens is not None:
-            n_tokens = np.ascontiguousarray(np.asarray(n_tokens, dtype=np.int32))
-            if n_tokens.shape != (B,):
-                raise ValueError("n_tokens must have batch entries")
-        return qkv.data_ptr(), token, T, n_tokens
+    def _counts(self, n_tokens):
+        """(address, the array that has to live until the call has returned) of per-sequence counts; None of None."""
+        if n_tokens is None:
+            return None, None
+        counts = np.ascontiguousarray(np.asarray(n_tokens, dtype=np.int32))
+        if counts.shape != (self.shape["batch"],):
+            raise ValueError("n_tokens must have batch entries")
+        return counts.ctypes.data, counts
 
     def append_rotary(self, layer: int, qkv, n_tokens, rotary: Rotary, q_out=None):
         """Rotates and appends packed projections [batch, tokens, (q + 2 kv heads) * head_dim]; rotated queries to q_out
         ([batch, q heads, tokens, head_dim], for one token also without that axis).  n_tokens None: all tokens of every active sequence."""
-        ptr, token, T, counts = self._packed(qkv, n_tokens)
-        out = None
-        if q_out is not None:
-            B, Hq, D = self._q_shape
-            out = self._ptr(q_out, self._q_shape if T == 1 and q_out.dim() == 3 else (B, Hq, T, D), "q_out")
-        _check(self._append_rotary(self.handle, layer, ptr, token, None if counts is None else counts.ctypes.data, T, rotary.address, out,
-                                   self._stream()), "rlkv_append_rotary")
+        at, _keep = self._counts(n_tokens)
+        status = tensor_calls().append_rotary(self.handle, layer, self._call_shape, qkv, at, rotary.address, q_out)
+        if status:
+            _check(status, "rlkv_append_rotary")
 
     def rotary(self, layer: int, qkv, n_tokens, rotary: Rotary, q_out, k_out, v_out):
         """Rotates packed projections and hands them out heads first, as prefill_attention and append_decode take them."""
-        s = self.shape
-        ptr, token, T, counts = self._packed(qkv, n_tokens)
-        kv = (s["batch"], s["n_kv_heads"], T, s["head_dim"])
-        q = self._ptr(q_out, self._q_shape if T == 1 and q_out.dim() == 3 else (s["batch"], s["n_q_heads"], T, s["head_dim"]), "q_out")
-        rlkv_rotary(self.handle, layer, ptr, token, counts, T, rotary, q, self._ptr(k_out, kv, "k_out"), self._ptr(v_out, kv, "v_out"),
-                    self._stream())
+        at, _keep = self._counts(n_tokens)
+        status = tensor_calls().rotary(self.handle, layer, self._call_shape, qkv, at, rotary.address, q_out, k_out, v_out)
+        if status:
+            _check(status, "rlkv_rotary")
 
     def decode_attention(self, layer: int, q, out, softmax_scale: float):
         shp = self._q_shape

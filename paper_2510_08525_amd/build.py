@@ -65,6 +65,31 @@ def build_library(verbose: bool = True) -> str:
     return LIB
 
 
+CALLS = os.path.join(PKG, "_tensor_calls.so")
+
+
+def build_tensor_calls(verbose: bool = True) -> str:
+    """The Python module of the operators' calls on torch tensors (host compiler; torch's headers), built against the library just linked."""
+    import sysconfig
+
+    import torch
+    from torch.utils.cpp_extension import include_paths
+
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    rocm = os.environ.get("ROCM_PATH", "/opt/rocm")
+    include = [*include_paths(), sysconfig.get_paths()["include"], os.path.join(rocm, "include"), os.path.join(ROOT, "include")]
+    cmd = [os.environ.get("CXX", "g++"), "-std=c++17", "-O2", "-Wall", "-fPIC", "-shared", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__",
+           "-DUSE_ROCM", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *(f"-isystem{p}" for p in include),
+           os.path.join(CSRC, "tensor_calls.cpp"), "-o", CALLS, "-L", PKG, "-lrlkv", "-L", lib, "-ltorch_python", "-ltorch", "-lc10",
+           "-lc10_hip", "-Wl,-rpath,$ORIGIN"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("building the calls on tensors failed:\n" + res.stderr)
+    if verbose:
+        print(f"built {CALLS}")
+    return CALLS
+
+
 EXAMPLE_SRC = os.path.join(ROOT, "examples", "c_abi_decode.c")
 EXAMPLE_BIN = os.path.join(ROOT, "examples", "c_abi_decode")
 
@@ -87,4 +112,5 @@ def build_example(verbose: bool = True) -> str:
 
 if __name__ == "__main__":
     build_library()
+    build_tensor_calls()
     build_example()

@@ -1,5 +1,6 @@
 """Refusals of the token-wise operators: every check runs on the host before the first HIP call."""
 import pytest
+import torch
 
 import paper_2510_08525_amd as rl
 from paper_2510_08525_amd import binding
@@ -103,3 +104,20 @@ def test_logprobs_workspace():
     assert need(0, 100, 0) == need(4, 0, 0) == need(4, 100, 33) == need(4, 100, -1) == need(-1, 100, 0) == 0
     assert need(5000, 100000, 20) == 0 and need(1, 16384, 32) == 0            # nothing is split
     assert 0 < need(2, 100000, 0) < need(2, 100000, 20)
+
+
+def test_what_is_no_tensor_of_a_device_is_refused():
+    x = torch.zeros(4, 256)
+    v = torch.zeros(4)
+    calls = rl.tensor_calls()
+    shape = (0, rl.RLKV_F32, 4, 2, 1, 64)
+    for f in (lambda: rl.rms_norm(x, None, 1e-5, x), lambda: rl.quantize(x, x, x), lambda: rl.scaled_matmul(x, x, x, x, x),
+              lambda: rl.token_logprobs(x, None, None, lse=v, workspace=v), lambda: rl.token_logprobs_grad(x, v, v, v, x),
+              lambda: rl.quantize(3, x, x), lambda: rl.rms_norm(None, None, 1e-5, x),
+              lambda: calls.append_rotary(0, 0, shape, x, None, 0, None), lambda: calls.rotary(None, 0, shape, 1, None, 0, x, x, x)):
+        with pytest.raises(ValueError):
+            f()
+    for f in (lambda: calls.quantize(x, x), lambda: calls.append_rotary(0, 0, shape[:5], x, None, 0, None),
+              lambda: calls.append_rotary(0, "0", shape, x, None, 0, None)):
+        with pytest.raises(TypeError):
+            f()
