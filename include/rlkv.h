@@ -445,13 +445,13 @@ int32_t rlkv_plan_narrow_split(int32_t n_compute_units, int32_t group, int32_t n
 /* ---- Token-wise operators: a decoder's way into the cache and out of it again --------------------------------------------
  * These need no cache handle.  They run on `stream` of the current device, keep no state, allocate nothing, wait for nothing
  * and can be recorded into a HIP graph.  Matrices are row-major; a stride is the distance of two rows (of two groups, for
- * scales) in elements.  Every pointer is aligned to its element type; no row has to be aligned beyond that unless a call says so.  Sums, statistics and scales are fp32; every output is rounded once, to
- * nearest even.  A call with no rows returns RLKV_OK and launches nothing. */
+ * scales) in elements.  Every pointer is aligned to its element type; no row has to be aligned beyond that unless a call says so.
+ * Sums, statistics and scales are fp32; every output is rounded once, to nearest even.  A call with no rows returns RLKV_OK and launches nothing. */
 
 /* Root-mean-square norm of rows, with the residual's addition in front of it:
  *     h = x + residual        sum_out = h        out = h / sqrt(mean(h^2) + eps) * weight
  * The norm is that of the unrounded h.
- *   x, residual, weight, sum_out : device, in `dtype` (RLKV_F32 or RLKV_BF16); [rows][cols], weight [cols].  residual, weight and
+ *   x, residual, weight, sum_out : device, in `dtype` (RLKV_F32 or RLKV_BF16); [rows][cols], weight [cols], cols <= 2^30.  residual, weight and
  *                        sum_out may be NULL (no addition; ones; h is not kept; sum_out needs a residual)
  *   out : device; out_dtype is `dtype`, or RLKV_E4M3: then columns [128 g, 128 g + 128) of row r are divided by their scale,
  *                        scales[g * scale_stride + r] = max(max |out| / 448, 2^-126)   (what rlkv_scaled_matmul takes)
@@ -474,8 +474,7 @@ rlkv_status_t rlkv_quantize(const void* x /* device */, int64_t x_stride, int32_
  *   b        : device, RLKV_E4M3, [n][k] (weights, a row per output); b_scales: device, fp32, [ceil(n / 128)][ceil(k / 128)]
  *   out      : device, out_dtype = RLKV_F32 or RLKV_BF16, [m][n]
  * k is a multiple of 16; rows of a and b start at multiples of 16 bytes and are at most 2^23 bytes apart (a_stride and b_stride below k
- * repeat rows).  m, n and k are at most 2^24 and
- * m * n below 2^44; with m = 0 or n = 0 nothing is done.  Scales and the sums over groups are fp32.
+ * repeat rows).  m, n and k are at most 2^24 and m * n below 2^35; with m = 0 or n = 0 nothing is done.  Scales and the sums over groups are fp32.
  * Inside a group, products are exact and summed in fp32 for an fp32 output and for m <= 64; else, for a bf16 output, by the 8-bit
  * matrix instruction, which drops what lies more than 13 binary places below the exponent of the largest of the products it sums
  * (at most 2^-6 of the group's largest product altogether).  The order of the sums depends on the sizes only: equal calls

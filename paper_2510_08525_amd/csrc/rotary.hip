@@ -274,7 +274,7 @@ hipError_t launch_typed(const DeviceView& dv, int layer, const int32_t* len_in, 
   const int heads_each = tokens >= 1024 ? 8 : 1;
   const int64_t items = n_heads ? tokens * ((n_heads + heads_each - 1) / heads_each) : 0;
   const int64_t blocks = (APPEND ? (int64_t)dv.n_pairs * jobs : 0) + (items + kItems - 1) / kItems;
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  if (blocks * kBlock > 0xffffffffll) return hipErrorInvalidValue;      // threads of a launch
   hipLaunchKernelGGL((rotary_kernel<KERNEL, T, APPEND>), dim3((unsigned)blocks), dim3(kBlock), 0, stream, dv, layer, len_in, len_out, call,
                      turns, seqs != nullptr, seqs ? *seqs : none, jobs, heads_each);
   return hipGetLastError();

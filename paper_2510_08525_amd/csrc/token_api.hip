@@ -22,11 +22,12 @@ bool writable(const void* p, int64_t stride, int64_t rows, int64_t cols, int dty
 bool whole(const void* p, int64_t stride, int dtype) { return aligned(p, 16) && (stride * (int64_t)bytes_of(dtype)) % 16 == 0; }
 
 constexpr int32_t kMostLogitRows = 1 << 20, kMostVocab = 1 << 24;
+constexpr int32_t kMostNormCols = 1 << 30;              // (a piece or a stride of threads further on is still an int)
 
 rlkv_status_t norm_call(NormCall& c, int dtype, int out_dtype, void* stream) {
   if (dtype != RLKV_F32 && dtype != RLKV_BF16) return RLKV_ERR_INVALID_ARG;
   if (out_dtype != dtype && out_dtype != RLKV_E4M3) return RLKV_ERR_INVALID_ARG;
-  if (c.rows < 0 || c.cols < 1) return RLKV_ERR_INVALID_ARG;
+  if (c.rows < 0 || c.cols < 1 || c.cols > kMostNormCols) return RLKV_ERR_INVALID_ARG;
   if (c.rows == 0) return RLKV_OK;
   if (!readable(c.x, c.x_stride, dtype) || !writable(c.out, c.out_stride, c.rows, c.cols, out_dtype)) return RLKV_ERR_INVALID_ARG;
   if (c.residual && !readable(c.residual, c.residual_stride, dtype)) return RLKV_ERR_INVALID_ARG;
@@ -73,7 +74,7 @@ rlkv_status_t rlkv_scaled_matmul(const void* a, int64_t a_stride, const float* a
   if (out_dtype != RLKV_F32 && out_dtype != RLKV_BF16) return RLKV_ERR_INVALID_ARG;
   if (m < 0 || n < 0 || k < 1 || k % 16 != 0) return RLKV_ERR_INVALID_ARG;
   if (m > (1 << 24) || n > (1 << 24) || k > (1 << 24)) return RLKV_ERR_INVALID_ARG;
-  if ((int64_t)(m / 128 + 1) * (n / 128 + 1) > (1 << 30)) return RLKV_ERR_INVALID_ARG;      // workgroups of a launch
+  if ((int64_t)(m / 128 + 1) * (n / 128 + 1) > (1 << 22)) return RLKV_ERR_INVALID_ARG;      // (threads of a launch are below 2^32)
   if (m == 0 || n == 0) return RLKV_OK;
   if (!readable(a, a_stride, RLKV_E4M3) || !readable(b, b_stride, RLKV_E4M3) || !whole(a, a_stride, RLKV_E4M3) ||
       !whole(b, b_stride, RLKV_E4M3) || a_stride > kMostMatmulStride || b_stride > kMostMatmulStride)

@@ -121,3 +121,14 @@ def test_what_is_no_tensor_of_a_device_is_refused():
               lambda: calls.append_rotary(0, "0", shape, x, None, 0, None)):
         with pytest.raises(TypeError):
             f()
+
+
+@pytest.mark.parametrize("cols", [(1 << 30) + 1, (1 << 31) - 1])
+def test_rows_longer_than_the_indexes_are_refused(cols):
+    assert _norm(cols=cols, x_stride=cols, residual_stride=cols, sum_stride=cols, out_stride=cols) == BAD
+
+
+@pytest.mark.parametrize("m, n", [(1 << 18, 1 << 18), (1 << 24, 1 << 13), (1 << 11, 1 << 24)])
+def test_products_of_more_threads_than_a_launch_has_are_refused(m, n):
+    call = rl.load_library().rlkv_scaled_matmul
+    assert call(P, 128, P, m, P, 128, P, 1, m, n, 128, P, n, rl.RLKV_BF16, None) == BAD
