@@ -12,8 +12,8 @@
 //
 // Most likely tokens: the key of a logit is (value, lowest index first) in 64 bits.  A workgroup works through its columns in chunks that
 // it holds in registers, and collects in LDS what may be among the k best: what reaches the k-th best known so far and, where
-// many lanes of a wavefront have something that does, the k-th largest of the lanes' maxima (k logits of this chunk reach that: 20 of 4096
-// random ones let 24 through).  The list is ranked by counting when it
+// more than k threads have something that does, the k-th largest of the threads' maxima (k logits of this chunk reach that: 20 of 4096
+// random ones let about 22 through).  The list is ranked by counting when it
 // has grown to some times k, which raises what the next chunks have to reach, and at the end.  A chunk that lets through
 // more than the list holds (ties, masks) is searched maximum by maximum.
 // Few rows are split over workgroups, whose partial results a second kernel joins in a fixed order.
@@ -35,12 +35,15 @@ constexpr float kLow = -256.f;                          // in the place of expon
 
 struct Stats { float m, s, t; };                        // maximum of the logits, sum, weighted sum (exponents of base 2)
 
-__device__ __forceinline__ Stats join(const Stats& a, const Stats& b, float scale2) {
-  const float m = fmaxf(a.m, b.m);
-  if (m == -INFINITY) return Stats{m, a.s + b.s, a.t + b.t};      // (sums of zeros; a NaN stays one)
-  const float da = (a.m - m) * scale2, db = (b.m - m) * scale2;
-  const float wa = __builtin_amdgcn_exp2f(da), wb = __builtin_amdgcn_exp2f(db);
-  return Stats{m, a.s * wa + b.s * wb, (a.t + a.s * fmaxf(da, kLow)) * wa + (b.t + b.s * fmaxf(db, kLow)) * wb};
+// Weighted by 2^(c (own maximum - m)); m is at least that maximum.
+__device__ __forceinline__ Stats rescaled(const Stats& v, float m, float scale2) {
+  if (m == -INFINITY) return v;                                 // (sums of zeros; a NaN stays one)
+  const float d = (v.m - m) * scale2, w = __builtin_amdgcn_exp2f(d);
+  return Stats{m, v.s * w, (v.t + v.s * fmaxf(d, kLow)) * w};
+}
+__device__ __forceinline__ Stats stats_of_wave(Stats v, float scale2) {
+  v = rescaled(v, max_of_wave(v.m), scale2);
+  return Stats{max_of_wave(v.m), sum_of_wave(v.s), sum_of_wave(v.t)};
 }
 
 // Order of logits as unsigned numbers: larger values first, NaN above all, and nothing at the end of the range, so that no key is ~0.
@@ -66,28 +69,49 @@ __device__ __forceinline__ uint64_t max_of_wave(uint64_t x) {
   }
   return x;
 }
-// A bound that k lanes (k from 1) of a wavefront reach: the k-th largest of their orders, cut to its upper 16 bits.
-__device__ __forceinline__ uint32_t kth_of_wave(uint32_t order, int k) {
-  const uint32_t upper = order >> 16;
+// The k-th largest (k from 1) of N values of 16 bits a lane.
+template <int N>
+__device__ __forceinline__ uint32_t kth_of_wave(const uint32_t (&upper)[N], int k) {
   uint32_t kth = 0;
 #pragma unroll
   for (int bit = 15; bit >= 0; --bit) {
     const uint32_t next = kth | 1u << bit;
-    if (__popcll(__ballot(upper >= next)) >= k) kth = next;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) n += __popcll(__ballot(upper[i] >= next));
+    if (n >= k) kth = next;
   }
-  return kth << 16;
+  return kth;
 }
-// The same as a value: what is at least that large reaches it.
+// An order as a value that it and larger ones reach.
 __device__ __forceinline__ float bound_of(uint32_t order) { return order < 0x00800000u ? -INFINITY : value_of(order); }
+
+// Inclusive prefix sums over the wavefront.
+__device__ __forceinline__ int prefix_of_wave(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);        // row_shr:1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);        // row_bcast:15, :31
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
 
 struct TopLds {
   uint64_t best[kMostTop];          // the best so far, largest first, 0 = none
   alignas(16) uint64_t list[kList + 8];      // candidates, the best so far first, and room for zeros behind them
   uint64_t wave_best[kThreads / 64];
+  alignas(8) uint16_t most[64][kThreads / 64];      // upper halves of the orders of the lanes' largest logits
+  int32_t some[kThreads / 64];
   int32_t n;
 };
+// Nothing yet.  (The next barrier is before the first use.)
+__device__ __forceinline__ void clear_list(TopLds& lds) {
+  if (threadIdx.x < kMostTop) lds.best[threadIdx.x] = 0;
+  if (threadIdx.x == 0) lds.n = 0;
+}
 
-// list[0, n) (distinct keys and zeros, k <= n <= kList, all threads past a barrier) -> the k largest of them into best, in order.  (Equal zeros
+// list[0, n) (distinct keys and zeros, n <= kList, all threads past a barrier) -> the k largest of them into best, in order.  (Equal zeros
 // take one place, and those behind it hold zeros already: what was there before is in the list too.)
 __device__ void rank_list(TopLds& lds, int n, int k) {
   if (threadIdx.x < 8) lds.list[n + threadIdx.x] = 0;            // (eight keys a turn, all of them on their way at once)
@@ -121,18 +145,29 @@ template <> __device__ __forceinline__ float value_at<float>(const Piece<float>&
 
 // Brings the chunk that starts at column `first` (valid: below `last`), in x, into the list.  most: a lane's largest logit of the chunk;
 // odd: the lane has met a NaN or an infinity; bound: what a logit has to reach to be among the k best, the same in all lanes; row: the logits again.
+// n_list: what the list holds.
 template <typename T, int PIECES>
 __device__ void top_of_chunk(TopLds& lds, const Piece<T> (&x)[PIECES], const T* row, int first, int last, int k, float most, bool odd,
-                             float& bound) {
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int n_before = lds.n;
-  __syncthreads();
+                             float& bound, int& n_list) {
+  constexpr int kWaves = kThreads / 64;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n_before = n_list;
   const uint64_t some = __ballot(most >= bound);
   const bool any_odd = __ballot(odd) != 0;
+  lds.most[lane][wave] = (uint16_t)(order_of(most) >> 16);
+  if (lane == 0) lds.some[wave] = __popcll(some);
+  __syncthreads();
+  float reach = bound;
+  int n_some = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) n_some += __builtin_amdgcn_readfirstlane(lds.some[w]);
+  if (n_some > k) {
+    uint32_t upper[kWaves];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) upper[w] = lds.most[lane][w];
+    reach = fmaxf(reach, bound_of(kth_of_wave(upper, k) << 16));
+  }
   if (some != 0 || any_odd) {
-    float reach = bound;
-    if (!any_odd && __popcll(some) > k) reach = fmaxf(reach, bound_of(kth_of_wave(order_of(most), k)));
-    // Which logits of the lane pass (a NaN does), then their keys from the row itself: one counter update a wavefront, and no code per logit.
+    // Which logits of the lane pass (a NaN does), then their keys: one counter update a wavefront.
     uint64_t pass = 0;
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
@@ -143,16 +178,17 @@ __device__ void top_of_chunk(TopLds& lds, const Piece<T> (&x)[PIECES], const T* 
       if (col + 8 > last) bits &= col < last ? (1u << (last - col)) - 1u : 0u;
       pass |= (uint64_t)bits << (8 * p);
     }
-    if (pass != 0) {
-      int at = atomicAdd(&lds.n, __popcll(pass));
-      for (; pass != 0 && at < kList; pass &= pass - 1, ++at) {
-        const int bit = __builtin_ctzll(pass), col = first + ((bit >> 3) * kThreads + tid) * 8 + (bit & 7);
-        lds.list[at] = key_of(one_value(row[col]), col);
-      }
+    const int mine = __popcll(pass), up_to = prefix_of_wave(mine), all = __builtin_amdgcn_readlane(up_to, 63);
+    int at = 0;
+    if (all != 0 && lane == 0) at = atomicAdd(&lds.n, all);
+    at = __builtin_amdgcn_readfirstlane(at) + up_to - mine;
+    for (; pass != 0 && at < kList; pass &= pass - 1, ++at) {          // (from the row itself: no code per logit)
+      const int bit = __builtin_ctzll(pass), col = first + ((bit >> 3) * kThreads + tid) * 8 + (bit & 7);
+      lds.list[at] = key_of(one_value(row[col]), col);
     }
   }
   __syncthreads();
-  const int n = lds.n;
+  const int n = n_list = lds.n;
   if (n <= 4 * k + 32) return;
   if (n <= kList) {
     rank_list(lds, n, k);
@@ -186,16 +222,23 @@ __device__ void top_of_chunk(TopLds& lds, const Piece<T> (&x)[PIECES], const T* 
   const uint32_t worst = (uint32_t)(lds.best[k - 1] >> 32);
   bound = worst == 0 ? -INFINITY : worst >= order_of(INFINITY) ? INFINITY : value_of(worst + 1);
   restart_list(lds, k);
+  n_list = k;
 }
 
 __device__ __forceinline__ Stats stats_of_block(Stats v, Stats (&parts)[kThreads / 64], float scale2) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) v = join(v, Stats{__shfl_xor(v.m, m), __shfl_xor(v.s, m), __shfl_xor(v.t, m)}, scale2);
+  v = stats_of_wave(v, scale2);
   if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = v;
   __syncthreads();
-  v = parts[0];
+  float m = parts[0].m;
 #pragma unroll
-  for (int w = 1; w < kThreads / 64; ++w) v = join(v, parts[w], scale2);
+  for (int w = 1; w < kThreads / 64; ++w) m = fmaxf(m, parts[w].m);
+  v = Stats{m, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < kThreads / 64; ++w) {
+    const Stats part = rescaled(parts[w], m, scale2);
+    v.s += part.s;
+    v.t += part.t;
+  }
   return v;
 }
 
@@ -206,19 +249,20 @@ __device__ __forceinline__ uint64_t* part_best(const LogprobCall& c, int64_t at)
   return reinterpret_cast<uint64_t*>(static_cast<char*>(c.workspace) + stats) + at * c.top;
 }
 
-template <typename T, bool TOP>
-__device__ void finish_row(const LogprobCall& c, int row, const Stats& v, const uint64_t* best) {
+// The logit of the row's token (thread 0, where it is asked for).
+template <typename T>
+__device__ __forceinline__ float logit_of(const LogprobCall& c, int row, int token) {
+  return token >= 0 && token < c.vocab ? one_value((static_cast<const T*>(c.logits) + row * c.stride)[token]) : 0.f;
+}
+template <bool TOP>
+__device__ void finish_row(const LogprobCall& c, int row, const Stats& v, const uint64_t* best, int token, float logit) {
   const float scale2 = c.scale * kLog2e, log2_s = log2f(v.s);
   const bool empty = v.s == 0.f;                                // (nothing but masked logits)
   auto logprob = [&](float x) { return empty ? -INFINITY : kLn2 * ((x - v.m) * scale2 - log2_s); };
   if (threadIdx.x == 0) {
     if (c.lse) c.lse[row] = empty ? -INFINITY : __builtin_fmaf(v.m, c.scale, kLn2 * log2_s);
     if (c.entropy) c.entropy[row] = empty ? 0.f : kLn2 * (log2_s - v.t / v.s);
-    if (c.logprobs) {
-      const int token = c.tokens[row];
-      const bool asked = token >= 0 && token < c.vocab;         // (a row that is not scored gets 0)
-      c.logprobs[row] = asked ? logprob(one_value((static_cast<const T*>(c.logits) + row * c.stride)[token])) : 0.f;
-    }
+    if (c.logprobs) c.logprobs[row] = token >= 0 && token < c.vocab ? logprob(logit) : 0.f;      // (a row that is not scored gets 0)
   }
   if (TOP && (int)threadIdx.x < c.top) {
     const uint64_t key = best[threadIdx.x];
@@ -238,11 +282,10 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LogprobCall c) {
   const float scale2 = c.scale * kLog2e;
   Stats v = {-INFINITY, 0.f, 0.f};
   float bound = -INFINITY;
-  if constexpr (TOP) {
-    if ((int)threadIdx.x < c.top) lds.best[threadIdx.x] = 0;
-    __syncthreads();
-    restart_list(lds, c.top);
-  }
+  int n_list = 0;
+  if constexpr (TOP) clear_list(lds);
+  const bool asked = c.splits == 1 && c.logprobs && threadIdx.x == 0;
+  const int token = asked ? c.tokens[row] : -1;
   for (int chunk = begin; chunk < end; ++chunk) {
     const int first = chunk * kChunk;
     const int last = c.vocab;
@@ -281,16 +324,17 @@ __global__ __launch_bounds__(kThreads) void rows_kernel(LogprobCall c) {
         v.s += e;
         v.t = __builtin_fmaf(e, fmaxf(d, kLow), v.t);
       }
-    if constexpr (TOP) top_of_chunk<T, PIECES>(lds, x, logits, first, last, c.top, most, v.s != v.s, bound);
+    if constexpr (TOP) top_of_chunk<T, PIECES>(lds, x, logits, first, last, c.top, most, v.s != v.s, bound, n_list);
   }
+  const float logit = logit_of<T>(c, row, token);
   const uint64_t* best = nullptr;
   if constexpr (TOP) {
-    rank_list(lds, lds.n, c.top);
+    rank_list(lds, n_list, c.top);
     best = lds.best;
   }
   v = stats_of_block(v, parts, scale2);
   if (c.splits == 1) {
-    finish_row<T, TOP>(c, row, v, best);
+    finish_row<TOP>(c, row, v, best, token, logit);
   } else {
     const int64_t at = (int64_t)row * c.splits + split;
     if (threadIdx.x == 0) *part_stats(c, at) = v;
@@ -304,44 +348,58 @@ __global__ __launch_bounds__(kThreads) void join_kernel(LogprobCall c) {
   __shared__ std::conditional_t<TOP, TopLds, char> lds;
   const int row = blockIdx.x, lane = threadIdx.x & 63;
   const int64_t at = (int64_t)row * c.splits;
+  // Everything that is read is asked for at once (keys: a batch of them).
+  constexpr int kEach = 3, kBatch = kEach * kThreads;
+  static_assert(kBatch + kMostTop <= kList, "a batch and the best before it");
+  const int n = c.splits * c.top, k = c.top;
+  const uint64_t* lists = part_best(c, at);
+  const int token = c.logprobs && threadIdx.x == 0 ? c.tokens[row] : -1;
   Stats v = {-INFINITY, 0.f, 0.f};
   if (lane < c.splits) v = *part_stats(c, at + lane);
+  uint64_t keys[kEach] = {};
+  // Entry `deep` of every list and those before it are k at least: k entries reach the least of these; or, with as many lists as k, the
+  // k-th largest of their first.
+  const int deep = (k + c.splits - 1) / c.splits - 1;
+  uint32_t head = 0;
+  if constexpr (TOP) {
+    if (lane < c.splits) head = (uint32_t)(lists[lane * k + deep] >> 32);
 #pragma unroll
-  for (int m = 1; m < kMostSplits; m <<= 1) v = join(v, Stats{__shfl_xor(v.m, m), __shfl_xor(v.s, m), __shfl_xor(v.t, m)}, c.scale * kLog2e);
+    for (int e = 0; e < kEach; ++e)
+      if (e * kThreads + (int)threadIdx.x < n) keys[e] = lists[e * kThreads + threadIdx.x];
+    clear_list(lds);
+  }
+  const float logit = logit_of<T>(c, row, token);
+  v = stats_of_wave(v, c.scale * kLog2e);
   const uint64_t* best = nullptr;
   if constexpr (TOP) {
-    const int n = c.splits * c.top, k = c.top;
-    // Entry `deep` of every list and those before it are k at least: k entries reach the least of these; or, with as many lists as k, the
-    // k-th largest of their first.
-    const int deep = (k + c.splits - 1) / c.splits - 1;
-    const uint64_t* lists = part_best(c, at);
     uint32_t bound;
     if (deep == 0) {
-      bound = kth_of_wave(lane < c.splits ? (uint32_t)(lists[lane * k] >> 32) : 0u, k);
+      const uint32_t upper[1] = {head >> 16};
+      bound = kth_of_wave(upper, k) << 16;
     } else {
-      uint32_t least = lane < c.splits ? (uint32_t)(lists[lane * k + deep] >> 32) : 0xffffffffu;
+      bound = lane < c.splits ? head : 0xffffffffu;
 #pragma unroll
-      for (int m = 1; m < 64; m <<= 1) least = min(least, (uint32_t)__shfl_xor(least, m));
-      bound = least;
+      for (int m = 1; m < 64; m <<= 1) bound = min(bound, (uint32_t)__shfl_xor(bound, m));
     }
-    if ((int)threadIdx.x < k) lds.best[threadIdx.x] = 0;
     __syncthreads();
-    restart_list(lds, k);
-    // (kList keys at a time, in case of ties: the rest of the lists is as many turns of the loop away)
-    for (int first = 0; first < n; first += kList - kMostTop) {
-      const int end = first + kList - kMostTop < n ? first + kList - kMostTop : n;
-      for (int i = first + threadIdx.x; i < end; i += kThreads) {
-        const uint64_t key = lists[i];
-        if (key != 0 && (uint32_t)(key >> 32) >= bound) lds.list[atomicAdd(&lds.n, 1)] = key;
-      }
+    for (int first = 0;;) {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e)
+        if (keys[e] != 0 && (uint32_t)(keys[e] >> 32) >= bound) lds.list[atomicAdd(&lds.n, 1)] = keys[e];
       __syncthreads();
-      const int some = lds.n;
-      rank_list(lds, some, k);
+      rank_list(lds, lds.n, k);
+      first += kBatch;
+      if (first >= n) break;
       restart_list(lds, k);
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const int i = first + e * kThreads + (int)threadIdx.x;
+        keys[e] = i < n ? lists[i] : 0;
+      }
     }
     best = lds.best;
   }
-  finish_row<T, TOP>(c, row, v, best);
+  finish_row<TOP>(c, row, v, best, token, logit);
 }
 
 constexpr int kGradPieces = 4;                          // pieces of a thread whose loads are in flight together

@@ -93,15 +93,27 @@ __device__ __forceinline__ void store_e4m3(uint8_t* row, int col, int n, const f
   }
 }
 
+// Over the wavefront, in all lanes (every lane is at the call): within rows of 16 lanes, then over the rows, a vector instruction a step
+// where a shuffle is an access to LDS.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float from_lane(float otherwise, float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(otherwise), __float_as_int(x), CTRL, ROWS, 0xf, false));
+}
+template <typename F>
+__device__ __forceinline__ float over_wave(float x, float neutral, F f) {
+  x = f(x, from_lane<0x111, 0xf>(neutral, x));        // row_shr:1, 2, 4, 8: the row's last lane has the row
+  x = f(x, from_lane<0x112, 0xf>(neutral, x));
+  x = f(x, from_lane<0x114, 0xf>(neutral, x));
+  x = f(x, from_lane<0x118, 0xf>(neutral, x));
+  x = f(x, from_lane<0x142, 0xa>(neutral, x));        // row_bcast:15 into rows 1 and 3
+  x = f(x, from_lane<0x143, 0xc>(neutral, x));        // row_bcast:31 into rows 2 and 3
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
 __device__ __forceinline__ float sum_of_wave(float x) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
-  return x;
+  return over_wave(x, 0.f, [](float a, float b) { return a + b; });
 }
 __device__ __forceinline__ float max_of_wave(float x) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) x = fmaxf(x, __shfl_xor(x, m));
-  return x;
+  return over_wave(x, -INFINITY, [](float a, float b) { return fmaxf(a, b); });
 }
 
 // ---- launchers ---------------------------------------------------------------------------------------------------
