@@ -11,8 +11,8 @@
 // that; a row of nothing else has lse -inf.
 //
 // Most likely tokens: the key of a logit is (value, lowest index first) in 64 bits.  A workgroup works through its columns in chunks that
-// it holds in registers, and collects in LDS what may be among the k best: what reaches the k-th best known so far and, where
-// more than k threads have something that does, the k-th largest of the threads' maxima (k logits of this chunk reach that: 20 of 4096
+// it holds in registers, and collects in LDS what may be among the k best: what reaches the k-th best known so far.  Where
+// many threads have something that does, that is raised to the k-th largest of the threads' maxima, which k logits reach (20 of 4096
 // random ones let about 22 through).  The list is ranked by counting when it
 // has grown to some times k, which raises what the next chunks have to reach, and at the end.  A chunk that lets through
 // more than the list holds (ties, masks) is searched maximum by maximum.
@@ -29,6 +29,7 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 constexpr int kThreads = 256;
 constexpr int kPieces = 8, kFewPieces = 2;              // pieces of eight logits of a thread in a chunk, of many rows and of few
 constexpr int kList = 1024;                             // candidates a workgroup ranks at once
+constexpr int kSomeMore = 4;                            // threads with candidates, in k, that a chunk may have before it raises the bound
 constexpr int kMostSplits = 64;                         // workgroups a row is split over: a lane each when they are joined
 constexpr float kMaskedLse = -1e30f;
 constexpr float kLow = -256.f;                          // in the place of exponents so low that their weight is 0
@@ -72,14 +73,19 @@ __device__ __forceinline__ uint64_t max_of_wave(uint64_t x) {
 // The k-th largest (k from 1) of N values of 16 bits a lane.
 template <int N>
 __device__ __forceinline__ uint32_t kth_of_wave(const uint32_t (&upper)[N], int k) {
+  constexpr int kBits = N == 1 ? 2 : 1;                         // (bits a step: of one value a lane, three counts side by side take no longer)
   uint32_t kth = 0;
 #pragma unroll
-  for (int bit = 15; bit >= 0; --bit) {
-    const uint32_t next = kth | 1u << bit;
-    int n = 0;
+  for (int bit = 16 - kBits; bit >= 0; bit -= kBits) {
+    uint32_t digit = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) n += __popcll(__ballot(upper[i] >= next));
-    if (n >= k) kth = next;
+    for (uint32_t t = 1; t < 1u << kBits; ++t) {
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) n += __popcll(__ballot(upper[i] >= (kth | t << bit)));
+      if (n >= k) digit = t;
+    }
+    kth |= digit << bit;
   }
   return kth;
 }
@@ -156,15 +162,14 @@ __device__ void top_of_chunk(TopLds& lds, const Piece<T> (&x)[PIECES], const T* 
   lds.most[lane][wave] = (uint16_t)(order_of(most) >> 16);
   if (lane == 0) lds.some[wave] = __popcll(some);
   __syncthreads();
-  float reach = bound;
   int n_some = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) n_some += __builtin_amdgcn_readfirstlane(lds.some[w]);
-  if (n_some > k) {
+  if (n_some > kSomeMore * k) {
     uint32_t upper[kWaves];
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) upper[w] = lds.most[lane][w];
-    reach = fmaxf(reach, bound_of(kth_of_wave(upper, k) << 16));
+    bound = fmaxf(bound, bound_of(kth_of_wave(upper, k) << 16));
   }
   if (some != 0 || any_odd) {
     // Which logits of the lane pass (a NaN does), then their keys: one counter update a wavefront.
@@ -173,7 +178,7 @@ __device__ void top_of_chunk(TopLds& lds, const Piece<T> (&x)[PIECES], const T* 
     for (int p = 0; p < PIECES; ++p) {
       uint32_t bits = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) bits |= value_at(x[p], i) < reach ? 0u : 1u << i;
+      for (int i = 0; i < 8; ++i) bits |= value_at(x[p], i) < bound ? 0u : 1u << i;
       const int col = first + (p * kThreads + tid) * 8;
       if (col + 8 > last) bits &= col < last ? (1u << (last - col)) - 1u : 0u;
       pass |= (uint64_t)bits << (8 * p);
@@ -450,20 +455,21 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(LogprobGradCall c) {
 }  // namespace
 
 // Chunks of a row and workgroups it is split over.  Many rows fill the card by themselves, and rows of two chunks are not worth the launch
-// that joins them (64 x 32000 fp32: 4.7 + 3.2 us split, 5.7 whole); few rows are spread over workgroups, as many as fill the compute
-// units twice, in chunks of a quarter of the size where those of the full size do not fill them once.
+// that joins them (64 x 32000 fp32: 4.7 + 3.2 us split, 5.7 whole; with the 20 most likely tokens 11.3 in all split, 11.5 whole, but
+// 4 x 32000 8.8 and 10.5); few rows are spread over workgroups, as many as fill the compute units twice, in chunks of a quarter of the
+// size where those of the full size do not fill them once.  (512 x 131072 bf16, 20 most likely: 48 us whole, 59 in two.)
 static int chunks_of(int vocab, int pieces) { return (int)(((int64_t)vocab + kThreads * 8 * pieces - 1) / (kThreads * 8 * pieces)); }
-static bool whole_rows(int rows, int vocab) { return rows >= 512 || chunks_of(vocab, kPieces) <= 2; }
-static bool small_chunks(int rows, int vocab) { return !whole_rows(rows, vocab) && (int64_t)rows * chunks_of(vocab, kPieces) < 256; }
-static int logprob_chunks(int rows, int vocab) { return chunks_of(vocab, small_chunks(rows, vocab) ? kFewPieces : kPieces); }
-static int logprob_splits(int rows, int vocab) {
-  if (whole_rows(rows, vocab)) return 1;
-  const int chunks = logprob_chunks(rows, vocab), want = (512 + rows - 1) / rows;
+static bool whole_rows(int rows, int vocab, int top) { return rows >= 512 || chunks_of(vocab, kPieces) <= (top > 0 && rows < 64 ? 1 : 2); }
+static bool small_chunks(int rows, int vocab, int top) { return !whole_rows(rows, vocab, top) && (int64_t)rows * chunks_of(vocab, kPieces) < 256; }
+static int logprob_chunks(int rows, int vocab, int top) { return chunks_of(vocab, small_chunks(rows, vocab, top) ? kFewPieces : kPieces); }
+static int logprob_splits(int rows, int vocab, int top) {
+  if (whole_rows(rows, vocab, top)) return 1;
+  const int chunks = logprob_chunks(rows, vocab, top), want = (512 + rows - 1) / rows;
   const int most = want < kMostSplits ? want : kMostSplits;
   return most < chunks ? most : chunks;
 }
 size_t logprob_workspace(int rows, int vocab, int top) {
-  const int splits = logprob_splits(rows, vocab);
+  const int splits = logprob_splits(rows, vocab, top);
   if (splits <= 1) return 0;
   const size_t parts = (size_t)rows * splits;
   return (parts * sizeof(Stats) + 7) / 8 * 8 + parts * top * sizeof(uint64_t);
@@ -472,7 +478,7 @@ size_t logprob_workspace(int rows, int vocab, int top) {
 template <typename T, bool TOP>
 static hipError_t launch_rows(const LogprobCall& c, hipStream_t stream) {
   const dim3 grid((unsigned)c.rows * c.splits), block(kThreads);
-  if (small_chunks(c.rows, c.vocab)) hipLaunchKernelGGL((rows_kernel<T, TOP, kFewPieces>), grid, block, 0, stream, c);
+  if (small_chunks(c.rows, c.vocab, c.top)) hipLaunchKernelGGL((rows_kernel<T, TOP, kFewPieces>), grid, block, 0, stream, c);
   else hipLaunchKernelGGL((rows_kernel<T, TOP, kPieces>), grid, block, 0, stream, c);
   if (hipError_t e = hipGetLastError()) return e;
   if (c.splits > 1) hipLaunchKernelGGL((join_kernel<T, TOP>), dim3((unsigned)c.rows), block, 0, stream, c);
@@ -480,8 +486,8 @@ static hipError_t launch_rows(const LogprobCall& c, hipStream_t stream) {
 }
 
 hipError_t launch_logprobs(LogprobCall c, int dtype, hipStream_t stream) {
-  c.chunks = logprob_chunks(c.rows, c.vocab);
-  c.splits = logprob_splits(c.rows, c.vocab);
+  c.chunks = logprob_chunks(c.rows, c.vocab, c.top);
+  c.splits = logprob_splits(c.rows, c.vocab, c.top);
   if (dtype == RLKV_F32) return c.top ? launch_rows<float, true>(c, stream) : launch_rows<float, false>(c, stream);
   return c.top ? launch_rows<uint16_t, true>(c, stream) : launch_rows<uint16_t, false>(c, stream);
 }
