@@ -17,8 +17,6 @@
 // a lane's four results then belong to one row of a, whose scale is one register, and to four neighbouring columns of the output.  The order
 // of k inside a group does not matter as long as both operands have the same: lane (row, seg) holds bytes [16 seg, 16 seg + 16) and the
 // same 64 further on, so that a load of 16 lanes x 4 segments reads 64 contiguous bytes of each row.
-#include <math.h>
-
 #include <type_traits>
 
 #include "token_ops.h"
@@ -229,17 +227,20 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(MatmulCall c) {
 // A workgroup has BM rows of a and BN of b; a group of k of both is one stage in LDS (rows of 128 bytes, the 16-byte chunk c of
 // row r at place c ^ (r & 7), so that 16 lanes reading one chunk of 16 rows meet all banks), with the rows' scales behind it.  STAGES of
 // them in a ring: loads go straight to LDS, a stage is asked for STAGES - 1 turns before its use, and a wait is for the loads of
-// one stage only.
-template <int BM, int BN, int WM, int WN, int STAGES, int WAY, bool BF16>
-__global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(MatmulCall c, int tiles_m, int tiles_n) {
+// one stage only.  PARTS sets of WM * WN wavefronts each take every PARTS-th group and have a ring of their own; their sums are added in LDS.
+template <int BM, int BN, int WM, int WN, int STAGES, int PARTS, int WAY, bool BF16>
+__global__ __launch_bounds__(WM * WN * PARTS * 64) void tiled_kernel(MatmulCall c, int tiles_m, int tiles_n) {
   constexpr int kWaves = WM * WN;
   constexpr int TM = BM / WM / 16, TN = BN / WN / 16;          // tiles of a wavefront
   constexpr int kLoadsA = BM / 8 / kWaves, kLoadsB = BN / 8 / kWaves;
   constexpr int kScaleBytes = kWaves * 256;
   constexpr int kStage = (BM + BN) * kGroup + kScaleBytes;
   static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && BN / WN <= kGroup && kWaves * 64 >= BM, "shape of a tile");
+  static_assert(PARTS == 1 || STAGES * kStage >= BM * BN * 4, "the sums fit where the groups were");
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wave_of_all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int part = PARTS > 1 ? wave_of_all / kWaves : 0, wave = PARTS > 1 ? wave_of_all % kWaves : wave_of_all;
+  char* const ring = lds + part * STAGES * kStage;
 
   // Workgroups go to the 8 XCDs in turn: each XCD gets a contiguous run of tiles, bands of 8 tiles of m one column of n after the other.
   const int total = tiles_m * tiles_n;
@@ -273,7 +274,7 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(MatmulCall c, int t
 
   // Load j of a stage: a piece of eight rows of a or b, or, the last one, the scales of 64 rows of a.
   auto issue = [&](int stage, int g, int j) {
-    char* to = lds + stage * kStage;
+    char* to = ring + stage * kStage;
     if (j < kLoadsA + kLoadsB) {
       const int k0 = g * kGroup;
       const uint32_t k = k0 + chunk < c.k ? k0 + chunk : 0;    // (bytes past the end of k are cleared in registers)
@@ -289,7 +290,7 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(MatmulCall c, int t
 
   const float* b_scales = c.b_scales + ((n0 + wn * TN * 16) / kGroup < (c.n + kGroup - 1) / kGroup
                                             ? (n0 + wn * TN * 16) / kGroup : 0) * c.b_scale_stride;
-  float sb_lanes = 0.f;                                        // the scales of 64 groups, one a lane
+  float sb_lanes = 0.f;                                        // the scales of 64 of the part's groups, one a lane
 
   const int row = lane & 15, seg = lane >> 4;
   const int at = row * kGroup + ((seg ^ (lane & 7)) << 4);
@@ -299,19 +300,22 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(MatmulCall c, int t
 #pragma unroll
   for (int s = 0; s < STAGES - 1; ++s)
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) issue(s, s < groups ? s : groups - 1, j);
+    for (int j = 0; j < kLoads; ++j) issue(s, s * PARTS + part < groups ? s * PARTS + part : groups - 1, j);
   int stage = 0;
-  auto turn = [&](int g, auto tail) {
-    if ((g & 63) == 0) {
-      sb_lanes = b_scales[g + lane < groups ? g + lane : groups - 1];
+  auto turn = [&](int t, auto tail) {
+    const int g = t * PARTS + part;
+    if ((t & 63) == 0) {
+      sb_lanes = b_scales[g + lane * PARTS < groups ? g + lane * PARTS : groups - 1];
       asm volatile("" : "+v"(sb_lanes));                       // (waited for here, and not in every turn behind the loads to LDS)
     }
     // This stage's loads are in, of all wavefronts, and nobody reads the stage that is written next.
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads * (STAGES - 2)) : "memory");
+    if (PARTS > 1 && decltype(tail)::value && g >= groups) return;      // (the last turn has no group for this part)
     // (past the end the last group once more: the count of loads stays)
-    const int to_stage = stage == 0 ? STAGES - 1 : stage - 1, to_group = g + STAGES - 1 < groups ? g + STAGES - 1 : groups - 1;
-    const char* in = lds + stage * kStage;
-    const float sb = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sb_lanes), g & 63));
+    const int next = g + (STAGES - 1) * PARTS;
+    const int to_stage = stage == 0 ? STAGES - 1 : stage - 1, to_group = next < groups ? next : groups - 1;
+    const char* in = ring + stage * kStage;
+    const float sb = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sb_lanes), t & 63));
     auto fragment = [&](int at_row) {
       i32x4 lo = *reinterpret_cast<const i32x4*>(in + at_row), hi = *reinterpret_cast<const i32x4*>(in + (at_row ^ 64));
       if constexpr (decltype(tail)::value) {                   // (chunks past the end of k)
@@ -358,15 +362,32 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(MatmulCall c, int t
     }
     stage = stage == STAGES - 1 ? 0 : stage + 1;
   };
-  const int whole_groups = c.k / kGroup;
-  for (int g = 0; g < whole_groups; ++g) turn(g, std::false_type{});
-  if (whole_groups < groups) turn(whole_groups, std::true_type{});
+  const int whole_turns = c.k / kGroup / PARTS;                // (and at most one that has the end of k or not a group for each part)
+  for (int t = 0; t < whole_turns; ++t) turn(t, std::false_type{});
+  if (whole_turns * PARTS < groups) turn(whole_turns, std::true_type{});
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // (no load to LDS outlives the workgroup)
+  floats4* const sums = reinterpret_cast<floats4*>(lds) + wave * TM * TN * 64 + lane;
+  constexpr int kPartSums = BM * BN / 4;                       // of a part, in units of four
+  if constexpr (PARTS > 1) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) sums[part * kPartSums + (i * TN + j) * 64] = acc[i][j];
+    __syncthreads();
+  }
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
+    for (int j = 0; j < TN; ++j) {
+      if constexpr (PARTS > 1) {
+        if ((i * TN + j) % PARTS != part) continue;
+        acc[i][j] = sums[(i * TN + j) * 64];
+#pragma unroll
+        for (int q = 1; q < PARTS; ++q) acc[i][j] += sums[q * kPartSums + (i * TN + j) * 64];
+      }
       store_four(c, m0 + (wm * TM + i) * 16 + row, n0 + (wn * TN + j) * 16 + seg * 4, acc[i][j], BF16);
+    }
 }
 
 template <int NT, int WAVES, int AHEAD, bool BF16>
@@ -381,25 +402,29 @@ hipError_t launch_few(const MatmulCall& c, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <int BM, int BN, int WM, int WN, int STAGES, int WAY, bool BF16>
+template <int BM, int BN, int WM, int WN, int STAGES, int PARTS, int WAY, bool BF16>
 hipError_t launch_tiled(const MatmulCall& c, hipStream_t stream) {
   const int tiles_m = (c.m + BM - 1) / BM, tiles_n = (c.n + BN - 1) / BN;
-  constexpr int kLds = STAGES * ((BM + BN) * kGroup + WM * WN * 256);
-  auto kernel = tiled_kernel<BM, BN, WM, WN, STAGES, WAY, BF16>;
+  constexpr int kLds = PARTS * STAGES * ((BM + BN) * kGroup + WM * WN * 256);
+  auto kernel = tiled_kernel<BM, BN, WM, WN, STAGES, PARTS, WAY, BF16>;
   static const hipError_t allowed = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
   if (allowed != hipSuccess) return allowed;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles_m * tiles_n)), dim3(WM * WN * 64), kLds, stream, c, tiles_m, tiles_n);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles_m * tiles_n)), dim3(WM * WN * PARTS * 64), kLds, stream, c, tiles_m, tiles_n);
   return hipGetLastError();
 }
 
-// What a turn of a kernel's workgroups takes, in ns, where few compute units have one and where all have (the clock falls and L2 is
-// shared), and how many workgroups are resident: from calls of 96 .. 8192 rows, 3584 .. 14336 columns and k of 3584 .. 14336.
-constexpr int kFewRows = 64;
-struct TileCost { int bm, bn, slots, one, all; };
+// What a group of k takes, in ns, of a shape's workgroups: a round of all that are resident; what is left over for the last round, by the
+// workgroups that a compute unit then has (with one a unit between few units and all: the clock falls and L2 is shared).
+// From calls of 70 .. 8192 rows, 1000 .. 14336 columns and k of 1000 .. 14336, less 2.5 us a call.
+constexpr int kFewRows = 64, kUnits = 256;
+struct TileCost { int bm, bn, per_unit, round, last[3], once; };      // once: more than the others, a call
 inline double estimate(const TileCost& t, const MatmulCall& c) {
-  const double tiles = (double)((c.m + t.bm - 1) / t.bm) * ((c.n + t.bn - 1) / t.bn);
-  const double full = floor(tiles / t.slots), rest = tiles - full * t.slots;
-  return full * t.all + (rest > 0 ? t.one + (t.all - t.one) * rest / t.slots : 0);
+  const int64_t tiles = ((int64_t)(c.m + t.bm - 1) / t.bm) * ((c.n + t.bn - 1) / t.bn), slots = (int64_t)t.per_unit * kUnits;
+  const int64_t rest = tiles % slots;
+  double ns = (double)(tiles / slots) * t.round;
+  if (rest > 0 && t.per_unit > 1) ns += t.last[(rest - 1) / kUnits];
+  if (rest > 0 && t.per_unit == 1) ns += t.last[0] + (t.last[1] - t.last[0]) * (double)rest / kUnits;
+  return ns * ((c.k + kGroup - 1) / kGroup) + t.once;
 }
 
 template <bool BF16>
@@ -408,27 +433,33 @@ hipError_t launch_typed(const MatmulCall& c, hipStream_t stream) {
   // 10.4 / 7.7.  Up to 64 rows 32 at a time, against tiles of 64 x 64: 64 x 6144 x 4096 12.1 / 19.7, 64 x 14336 x 4096 25.1 / 20.6.)
   if (c.m <= 16) return c.n <= 128 * 16 ? launch_few<1, 8, 2, BF16>(c, stream) : launch_few<1, 4, 2, BF16>(c, stream);
   if (c.m <= kFewRows) return launch_few<2, 4, 2, BF16>(c, stream);
-  // The shape of the tiles whose rounds over the compute units are estimated to take least: small ones fill the card, large ones read less.
-  // (us measured, estimate in brackets: 333 x 4608 x 3584 64 x 64 15.3 (18), 128 x 128 19.6 (20), 256 x 128 27.8 (28); 1500 x 4608 x 4096
-  // 52.7 (58), 45.6 (48), 35.9 (39), 192 x 256 44.0 (46), 256 x 256 53.0 (56); 4096 x 4608 x 3584 256 x 128 94, 192 x 256 85, 256 x 256 101.)
+  // The shape of the tiles whose rounds over the compute units are estimated to take least: small ones fill the card, large ones read less,
+  // and of few small ones each turn is a chain of latencies, which two parts of k side by side hide from each other.
+  // (us measured: 333 x 4608 x 3584 64 x 64 16.5, 128 x 64 14.6, in two parts 13.3, 128 x 128 19.2; 200 x 4096 x 4096 64 x 64 12.7, in two
+  // parts 10.5, in four 12.0; 512 x 4608 x 3584 64 x 64 20.8, in two parts 26.2, 128 x 128 19.5; 1000 x 1000 x 1008 64 x 64 5.5, in two
+  // parts 5.8; 1024 x 6144 x 4096 128 x 64 41.5, 256 x 128 34.4; 4096 x 4608 x 3584 256 x 128 94, 192 x 256 85, 256 x 256 101.)
   if constexpr (!BF16) {
-    static const TileCost costs[] = {{64, 64, 512, 575, 770}, {128, 128, 256, 1100, 1180}};
-    if (estimate(costs[0], c) <= estimate(costs[1], c)) return launch_tiled<64, 64, 2, 2, 4, kWide, false>(c, stream);
-    return launch_tiled<128, 128, 2, 4, 3, kWide, false>(c, stream);
+    static const TileCost costs[] = {{64, 64, 2, 770, {600, 770}, 0}, {128, 128, 1, 1180, {1100, 1180}, 0}};
+    if (estimate(costs[0], c) <= estimate(costs[1], c)) return launch_tiled<64, 64, 2, 2, 4, 1, kWide, false>(c, stream);
+    return launch_tiled<128, 128, 2, 4, 3, 1, kWide, false>(c, stream);
   }
   if constexpr (BF16) {
-    static const TileCost costs[] = {{64, 64, 768, 330, 697}, {128, 64, 512, 430, 830}, {128, 128, 256, 590, 741},
-                                     {256, 128, 256, 820, 1210}, {192, 256, 256, 1170, 1670}, {256, 256, 256, 1380, 2050}};
+    static const TileCost costs[] = {{64, 64, 3, 697, {320, 510, 690}, 0}, {64, 64, 1, 320, {255, 255}, 700},
+                                     {128, 64, 2, 800, {430, 700}, 0},     {128, 64, 1, 424, {390, 390}, 700},
+                                     {128, 128, 1, 741, {560, 650}, 0},    {256, 128, 1, 1210, {760, 1080}, 0},
+                                     {192, 256, 1, 1670, {1100, 1600}, 0}, {256, 256, 1, 2050, {1300, 1960}, 0}};
     int best = 0;
     for (int i = 1; i < (int)(sizeof(costs) / sizeof(costs[0])); ++i)
       if (estimate(costs[i], c) < estimate(costs[best], c)) best = i;
     switch (best) {
-      case 0: return launch_tiled<64, 64, 2, 2, 3, kFast, true>(c, stream);
-      case 1: return launch_tiled<128, 64, 2, 2, 3, kFast, true>(c, stream);
-      case 2: return launch_tiled<128, 128, 2, 4, 3, kFast, true>(c, stream);
-      case 3: return launch_tiled<256, 128, 4, 2, 3, kFast, true>(c, stream);
-      case 4: return launch_tiled<192, 256, 2, 4, 2, kFast, true>(c, stream);
-      default: return launch_tiled<256, 256, 2, 4, 2, kFast, true>(c, stream);
+      case 0: return launch_tiled<64, 64, 2, 2, 3, 1, kFast, true>(c, stream);
+      case 1: return launch_tiled<64, 64, 2, 2, 3, 2, kFast, true>(c, stream);
+      case 2: return launch_tiled<128, 64, 2, 2, 3, 1, kFast, true>(c, stream);
+      case 3: return launch_tiled<128, 64, 2, 2, 3, 2, kFast, true>(c, stream);
+      case 4: return launch_tiled<128, 128, 2, 4, 3, 1, kFast, true>(c, stream);
+      case 5: return launch_tiled<256, 128, 4, 2, 3, 1, kFast, true>(c, stream);
+      case 6: return launch_tiled<192, 256, 2, 4, 2, 1, kFast, true>(c, stream);
+      default: return launch_tiled<256, 256, 2, 4, 2, 1, kFast, true>(c, stream);
     }
   }
   return hipErrorInvalidValue;

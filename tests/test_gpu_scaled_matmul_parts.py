@@ -1,0 +1,65 @@
+"""Products whose groups of k are shared out between the wavefronts of a workgroup (few tiles, many groups): numbers of groups that do not
+come out even, an end of k inside a group, a last group of infinite scale, against the formula in 64 bits.
+
+Tolerance: as for other products of a bf16 output and more than 64 rows: fp32 sums of 128 products and of the groups (the parts' sums among
+them), two roundings for the scales, 2^-6 of the group's largest product for the 8-bit matrix instruction, the output's rounding.
+"""
+import pytest
+import torch
+
+import paper_2510_08525_amd as rl
+
+pytestmark = pytest.mark.gpu
+E4M3 = torch.float8_e4m3fn
+U = 2.0 ** -24
+
+
+def _g(n):
+    return -(-n // 128)
+
+
+def _inputs(m, n, k, seed):
+    g = torch.Generator().manual_seed(seed)
+    a, b = ((torch.randn(r, k, generator=g) * 100).clamp(-448, 448).to(E4M3).cuda() for r in (m, n))
+    return a, (torch.rand(_g(k), m, generator=g) + 0.5).cuda(), b, (torch.rand(_g(n), _g(k), generator=g) + 0.5).cuda()
+
+
+def _scaled(x, scales):
+    """scales: [rows, groups]"""
+    return x.float().double() * scales.double().repeat_interleave(128, 1)[:, :x.shape[1]]
+
+
+@pytest.mark.parametrize("m,n", [(65, 64), (100, 1000), (333, 4608), (129, 200)])
+@pytest.mark.parametrize("k", [16, 128, 144, 1536, 1648, 3584, 3712, 8192, 8208, 16512])
+def test_products(m, n, k):
+    a, sa, b, sb = _inputs(m, n, k, m + n + k)
+    out = torch.full((m, n + 3), 7.0, dtype=torch.bfloat16, device="cuda")
+    rl.scaled_matmul(a, sa, b, sb, out[:, :n])
+    left, right = _scaled(a, sa.t()), _scaled(b, sb.repeat_interleave(128, 0)[:n])
+    y, size = left @ right.t(), left.abs() @ right.abs().t()
+    most = lambda x: torch.nn.functional.pad(x.abs(), (0, _g(k) * 128 - k)).view(x.shape[0], -1, 128).amax(-1)      # noqa: E731
+    tol = (128 + _g(k) + 10) * U * size + 2.0 ** -8 * y.abs() + 2.0 ** -6 * most(left) @ most(right).t()
+    assert ((out[:, :n].double() - y).abs() <= tol).all() and (out[:, n:] == 7.0).all()
+    # most of them are much nearer: a part left out or counted twice would not be
+    assert (out[:, :n].double() - y).norm() <= 2.0 ** -8 * y.norm() * 1.1
+
+
+@pytest.mark.parametrize("k", [1792, 1920])
+def test_a_part_without_a_last_group_adds_nothing(k):
+    """An infinite scale of the last group: its rows are infinite (not NaN), the others finite."""
+    a, sa, b, sb = _inputs(70, 256, k, k)
+    a.view(torch.uint8).copy_(a.float().abs().clamp(min=1).to(E4M3).view(torch.uint8))
+    b.view(torch.uint8).copy_(b.float().abs().clamp(min=1).to(E4M3).view(torch.uint8))
+    sa[-1, 3] = float("inf")
+    out = torch.empty(70, 256, dtype=torch.bfloat16, device="cuda")
+    rl.scaled_matmul(a, sa, b, sb, out)
+    assert (out[3] == float("inf")).all()
+    assert torch.isfinite(out[[i for i in range(70) if i != 3]]).all()
+
+
+def test_equal_calls_give_equal_bits():
+    a, sa, b, sb = _inputs(333, 4608, 3584, 5)
+    out = [torch.empty(333, 4608, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for o in out:
+        rl.scaled_matmul(a, sa, b, sb, o)
+    assert torch.equal(*out)
