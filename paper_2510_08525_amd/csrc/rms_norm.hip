@@ -7,16 +7,18 @@
 // that of the unrounded sum.  A thread has one piece of eight columns (two beyond 8192 columns, and what is beyond 16384 is read a
 // second time): a row's loads are all in flight at once, a wavefront's are whole lines, and the 16 lanes of a group of 128 columns
 // lie next to each other, so that its maximum takes four steps over lanes and no LDS.
-// Bound: HBM for many rows (16384 x 3584 bf16 with residual into 8 bits: 413 MB in 83 us, 5.0 TB/s, what a copy reaches), latency for few
+// Bound: HBM for many rows (16384 x 3584 bf16 with residual into 8 bits: 413 MB in 75 to 78 us, 5.3 to 5.5 TB/s; a copy of 1 GiB reaches 5.05), latency for few
 // (one row of 4096: 4 us).  With 64 threads a row and eight pieces each, weights kept over several rows, the same call took
-// 134 us, with 256 threads and two pieces 90; several rows to a workgroup one after the other are slower in every shape.
+// 134 us, with 256 threads and two pieces 90 (both with plain accesses); several rows to a workgroup one after the other are slower in every shape.
+#include <type_traits>
+
 #include "token_ops.h"
 
 namespace rlkv {
 namespace {
 
 // T threads a row, NC pieces each (T * NC * 8 columns at most, unless LOOP: then the pieces beyond are read a second time).
-template <typename X, int T, int NC, bool E4M3, bool LOOP>
+template <typename X, int T, int NC, bool E4M3, bool LOOP, bool STREAM>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(NormCall c) {
   constexpr int kRowsAtOnce = T < 256 ? 256 / T : 1;
   constexpr int kWaves = T / 64;
@@ -29,10 +31,10 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(NormCall c) {
     float h[NC][8];
     float squares = 0.f;
     auto load = [&](int col, float (&f)[8]) {
-      load_piece(x, col, c.cols, f);
+      load_piece<STREAM>(x, col, c.cols, f);
       if (res) {
         float r[8];
-        load_piece(res, col, c.cols, r);
+        load_piece<STREAM>(res, col, c.cols, r);
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] += r[i];
       }
@@ -74,7 +76,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(NormCall c) {
     }
     auto finish = [&](int col, float (&f)[8]) {
       if (col < c.cols) {
-        if (c.sum_out) store_piece(static_cast<X*>(c.sum_out) + row * c.sum_stride, col, c.cols, f);
+        if (c.sum_out) store_piece<STREAM>(static_cast<X*>(c.sum_out) + row * c.sum_stride, col, c.cols, f);
         if (c.norm) {
           float w[8];
           if (c.weight) {
@@ -103,7 +105,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(NormCall c) {
           if ((t & 15) == 0) c.scales[(int64_t)(col / kGroup) * c.scale_stride + row] = scale;
         }
       } else if (col < c.cols) {
-        store_piece(static_cast<X*>(c.out) + row * c.out_stride, col, c.cols, f);
+        store_piece<STREAM>(static_cast<X*>(c.out) + row * c.out_stride, col, c.cols, f);
       }
     };
     if (LOOP)                       // (before the pieces in registers: where sum_out is the residual, what is read again here is not yet written)
@@ -119,25 +121,35 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(NormCall c) {
 
 constexpr int kMostBlocks = 1 << 20;
 
-template <typename X, bool E4M3>
+// (STREAM: 8-bit outputs, which the product behind the norm reads, are not meant.)
+template <typename X, bool E4M3, bool STREAM>
 hipError_t launch_typed(const NormCall& c, hipStream_t stream) {
   auto run = [&](auto kernel, int threads, int rows_at_once) {
     const int blocks = (int)(((int64_t)c.rows + rows_at_once - 1) / rows_at_once);
     hipLaunchKernelGGL(kernel, dim3(blocks < kMostBlocks ? blocks : kMostBlocks), dim3(threads), 0, stream, c);
     return hipGetLastError();
   };
-  if (c.cols <= 512) return run(norm_kernel<X, 64, 1, E4M3, false>, 256, 4);
-  if (c.cols <= 2048) return run(norm_kernel<X, 256, 1, E4M3, false>, 256, 1);
-  if (c.cols <= 4096) return run(norm_kernel<X, 512, 1, E4M3, false>, 512, 1);
-  if (c.cols <= 8192) return run(norm_kernel<X, 1024, 1, E4M3, false>, 1024, 1);
-  return run(norm_kernel<X, 1024, 2, E4M3, true>, 1024, 1);
+  if (c.cols <= 512) return run(norm_kernel<X, 64, 1, E4M3, false, STREAM>, 256, 4);
+  if (c.cols <= 2048) return run(norm_kernel<X, 256, 1, E4M3, false, STREAM>, 256, 1);
+  if (c.cols <= 4096) return run(norm_kernel<X, 512, 1, E4M3, false, STREAM>, 512, 1);
+  if (c.cols <= 8192) return run(norm_kernel<X, 1024, 1, E4M3, false, STREAM>, 1024, 1);
+  return run(norm_kernel<X, 1024, 2, E4M3, true, STREAM>, 1024, 1);
 }
 
 }  // namespace
 
 hipError_t launch_norm(const NormCall& c, int dtype, bool out_e4m3, hipStream_t stream) {
-  if (dtype == RLKV_F32) return out_e4m3 ? launch_typed<float, true>(c, stream) : launch_typed<float, false>(c, stream);
-  return out_e4m3 ? launch_typed<uint16_t, true>(c, stream) : launch_typed<uint16_t, false>(c, stream);
+  // (us, plain accesses / non-temporal ones, bf16 with residual into 8 bits: 16384 x 3584 79.0 / 74.7; 8192 x 3584, which a
+  // cache holds, 43.8 / 40.2 by itself: not taken)
+  const int64_t bytes = dtype == RLKV_F32 ? 4 : 2;
+  const bool through = c.rows * (int64_t)c.cols * (bytes * (1 + (c.residual != nullptr) + (c.sum_out != nullptr)) + (out_e4m3 ? 1 : bytes)) > kStreamBytes;
+  auto launch = [&](auto x, auto e4m3) {
+    typedef decltype(x) X;
+    constexpr bool E4M3 = decltype(e4m3)::value;
+    return through ? launch_typed<X, E4M3, true>(c, stream) : launch_typed<X, E4M3, false>(c, stream);
+  };
+  if (dtype == RLKV_F32) return out_e4m3 ? launch(float(), std::true_type{}) : launch(float(), std::false_type{});
+  return out_e4m3 ? launch(uint16_t(), std::true_type{}) : launch(uint16_t(), std::false_type{});
 }
 
 }  // namespace rlkv
