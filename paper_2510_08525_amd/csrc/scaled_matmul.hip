@@ -427,6 +427,14 @@ inline double estimate(const TileCost& t, const MatmulCall& c) {
   return ns * ((c.k + kGroup - 1) / kGroup) + t.once;
 }
 
+template <int N>
+int cheapest(const TileCost (&costs)[N], const MatmulCall& c) {
+  int best = 0;
+  for (int i = 1; i < N; ++i)
+    if (estimate(costs[i], c) < estimate(costs[best], c)) best = i;
+  return best;
+}
+
 template <bool BF16>
 hipError_t launch_typed(const MatmulCall& c, hipStream_t stream) {
   // (us, 4 wavefronts a workgroup / 8: 1 x 6144 x 4096 7.5 / 8.0, 1 x 14336 x 4096 13.6 / 15.1; few workgroups want the wider: 1 x 1024 x 16384
@@ -439,19 +447,25 @@ hipError_t launch_typed(const MatmulCall& c, hipStream_t stream) {
   // parts 10.5, in four 12.0; 512 x 4608 x 3584 64 x 64 20.8, in two parts 26.2, 128 x 128 19.5; 1000 x 1000 x 1008 64 x 64 5.5, in two
   // parts 5.8; 1024 x 6144 x 4096 128 x 64 41.5, 256 x 128 34.4; 4096 x 4608 x 3584 256 x 128 94, 192 x 256 85, 256 x 256 101.)
   if constexpr (!BF16) {
-    static const TileCost costs[] = {{64, 64, 2, 770, {600, 770}, 0}, {128, 128, 1, 1180, {1100, 1180}, 0}};
-    if (estimate(costs[0], c) <= estimate(costs[1], c)) return launch_tiled<64, 64, 2, 2, 4, 1, kWide, false>(c, stream);
-    return launch_tiled<128, 128, 2, 4, 3, 1, kWide, false>(c, stream);
-  }
-  if constexpr (BF16) {
+    // (us: 333 x 4608 x 3584 64 x 64 24.8, in four parts 23.5, 64 x 128 in two parts 19.3, 128 x 128 33.7; 200 x 4096 x 4096 64 x 64 19.3, in four parts
+    // 14.2; 512 x 4608 x 3584 30.8, 34.4, 64 x 128 36.5; 1024 x 6144 x 4096 64 x 64 68.8, 64 x 128 63.6, 256 x 128 61.0, 128 x 128 75.1; 2048 x 2048 x 2048
+    // 64 x 128 25.2, 128 x 128 23.2.)
+    static const TileCost costs[] = {{64, 64, 3, 1050, {525, 760, 1030}, 0}, {64, 64, 1, 370, {360, 360}, 500},
+                                     {64, 128, 1, 665, {590, 590}, 700},     {128, 128, 1, 1300, {1050, 1290}, 0},
+                                     {256, 128, 1, 1960, {1700, 1900}, 0}};
+    switch (cheapest(costs, c)) {
+      case 0: return launch_tiled<64, 64, 2, 2, 3, 1, kWide, false>(c, stream);
+      case 1: return launch_tiled<64, 64, 2, 1, 2, 4, kWide, false>(c, stream);
+      case 2: return launch_tiled<64, 128, 2, 2, 3, 2, kWide, false>(c, stream);
+      case 3: return launch_tiled<128, 128, 2, 4, 3, 1, kWide, false>(c, stream);
+      default: return launch_tiled<256, 128, 4, 2, 3, 1, kWide, false>(c, stream);
+    }
+  } else {
     static const TileCost costs[] = {{64, 64, 3, 697, {320, 510, 690}, 0}, {64, 64, 1, 320, {255, 255}, 700},
                                      {128, 64, 2, 800, {430, 700}, 0},     {128, 64, 1, 424, {390, 390}, 700},
                                      {128, 128, 1, 741, {560, 650}, 0},    {256, 128, 1, 1210, {760, 1080}, 0},
                                      {192, 256, 1, 1670, {1100, 1600}, 0}, {256, 256, 1, 2050, {1300, 1960}, 0}};
-    int best = 0;
-    for (int i = 1; i < (int)(sizeof(costs) / sizeof(costs[0])); ++i)
-      if (estimate(costs[i], c) < estimate(costs[best], c)) best = i;
-    switch (best) {
+    switch (cheapest(costs, c)) {
       case 0: return launch_tiled<64, 64, 2, 2, 3, 1, kFast, true>(c, stream);
       case 1: return launch_tiled<64, 64, 2, 2, 3, 2, kFast, true>(c, stream);
       case 2: return launch_tiled<128, 64, 2, 2, 3, 1, kFast, true>(c, stream);
@@ -462,7 +476,6 @@ hipError_t launch_typed(const MatmulCall& c, hipStream_t stream) {
       default: return launch_tiled<256, 256, 2, 4, 2, 1, kFast, true>(c, stream);
     }
   }
-  return hipErrorInvalidValue;
 }
 
 }  // namespace

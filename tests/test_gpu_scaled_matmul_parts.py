@@ -63,3 +63,15 @@ def test_equal_calls_give_equal_bits():
     for o in out:
         rl.scaled_matmul(a, sa, b, sb, o)
     assert torch.equal(*out)
+
+
+@pytest.mark.parametrize("m,n", [(65, 64), (100, 1000), (333, 4608), (129, 200), (600, 2100)])
+@pytest.mark.parametrize("k", [16, 128, 272, 384, 528, 1648, 3712, 8208])
+def test_products_in_32_bits(m, n, k):
+    """Exact products, fp32 sums of 128 products, of the groups and of up to four parts, two roundings for the scales and the output's."""
+    a, sa, b, sb = _inputs(m, n, k, m + n + k)
+    out = torch.full((m, n + 3), 7.0, device="cuda")
+    rl.scaled_matmul(a, sa, b, sb, out[:, :n])
+    left, right = _scaled(a, sa.t()), _scaled(b, sb.repeat_interleave(128, 0)[:n])
+    y, size = left @ right.t(), left.abs() @ right.abs().t()
+    assert ((out[:, :n].double() - y).abs() <= (128 + _g(k) + 10) * U * size).all() and (out[:, n:] == 7.0).all()
