@@ -438,9 +438,22 @@ int cheapest(const TileCost (&costs)[N], const MatmulCall& c) {
 template <bool BF16>
 hipError_t launch_typed(const MatmulCall& c, hipStream_t stream) {
   // (us, 4 wavefronts a workgroup / 8: 1 x 6144 x 4096 7.5 / 8.0, 1 x 14336 x 4096 13.6 / 15.1; few workgroups want the wider: 1 x 1024 x 16384
-  // 10.4 / 7.7.  Up to 64 rows 32 at a time, against tiles of 64 x 64: 64 x 6144 x 4096 12.1 / 19.7, 64 x 14336 x 4096 25.1 / 20.6.)
+  // 10.4 / 7.7.)
   if (c.m <= 16) return c.n <= 128 * 16 ? launch_few<1, 8, 2, BF16>(c, stream) : launch_few<1, 4, 2, BF16>(c, stream);
-  if (c.m <= kFewRows) return launch_few<2, 4, 2, BF16>(c, stream);
+  if (c.m <= kFewRows) {
+    // 32 rows at a time with b straight from memory, or for wide outputs, where a would be read too often, tiles as below with exact products.
+    // (us, 32 rows at a time, tiles 32 x 64 in four parts, 64 x 64 and 64 x 128 in two: 64 x 4096 x 4096 9.3, 9.2, 14.5, -; 64 x 6144 x 4096 11.8,
+    // 9.4, 14.6, -; 64 x 9000 x 4096 16.8, 17.4, 14.5, 20.4; 24 x 14336 x 4096 15.4, 11.9, 14.8, 20.3; 64 x 14336 x 4096 25.6, 17.8, 15.3, 20.9;
+    // 64 x 28672 x 2048 23.0, 22.6, 17.8, 14.6.)
+    static const TileCost costs[] = {{32, 16, 3, 310, {125, 235, 300}, 0}, {32, 64, 1, 260, {195, 270}, 500},
+                                     {64, 64, 1, 430, {345, 390}, 500},    {64, 128, 1, 640, {540, 640}, 1500}};
+    switch (cheapest(costs, c)) {
+      case 0: return launch_few<2, 4, 2, BF16>(c, stream);
+      case 1: return launch_tiled<32, 64, 1, 2, 3, 4, kWide, BF16>(c, stream);
+      case 2: return launch_tiled<64, 64, 2, 2, 3, 2, kWide, BF16>(c, stream);
+      default: return launch_tiled<64, 128, 2, 2, 3, 2, kWide, BF16>(c, stream);
+    }
+  }
   // The shape of the tiles whose rounds over the compute units are estimated to take least: small ones fill the card, large ones read less,
   // and of few small ones each turn is a chain of latencies, which two parts of k side by side hide from each other.
   // (us measured: 333 x 4608 x 3584 64 x 64 16.5, 128 x 64 14.6, in two parts 13.3, 128 x 128 19.2; 200 x 4096 x 4096 64 x 64 12.7, in two

@@ -75,3 +75,17 @@ def test_products_in_32_bits(m, n, k):
     left, right = _scaled(a, sa.t()), _scaled(b, sb.repeat_interleave(128, 0)[:n])
     y, size = left @ right.t(), left.abs() @ right.abs().t()
     assert ((out[:, :n].double() - y).abs() <= (128 + _g(k) + 10) * U * size).all() and (out[:, n:] == 7.0).all()
+
+
+@pytest.mark.parametrize("m,n", [(17, 6200), (24, 14336), (33, 6144), (64, 9000), (50, 14341), (64, 28675)])
+@pytest.mark.parametrize("k", [144, 384, 1040, 2048])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_wide_outputs_of_few_rows(m, n, k, dtype):
+    """Up to 64 rows: exact products and fp32 sums whatever the output's type."""
+    a, sa, b, sb = _inputs(m, n, k, m + n + k)
+    out = torch.full((m, n + 3), 7.0, dtype=dtype, device="cuda")
+    rl.scaled_matmul(a, sa, b, sb, out[:, :n])
+    left, right = _scaled(a, sa.t()), _scaled(b, sb.repeat_interleave(128, 0)[:n])
+    y, size = left @ right.t(), left.abs() @ right.abs().t()
+    half = 2.0 ** -8 if dtype == torch.bfloat16 else U
+    assert ((out[:, :n].double() - y).abs() <= (128 + _g(k) + 10) * U * size + half * y.abs()).all() and (out[:, n:] == 7.0).all()
