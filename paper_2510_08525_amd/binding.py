@@ -44,12 +44,22 @@ class _Rotary(ctypes.Structure):
 
 
 class Rotary:
-    """How queries and keys turn with their positions (rlkv_rotary_t): radians a position of each pair of columns."""
+    """How queries and keys turn with their positions (rlkv_rotary_t): radians a position of each pair of columns.  They are copied and stay
+    as they are: the library reads them at `address` in every call."""
 
     def __init__(self, inv_freq: Sequence[float], interleaved: bool = False):
-        self.inv_freq = np.ascontiguousarray(np.asarray(inv_freq, dtype=np.float64).reshape(-1))
-        self._struct = _Rotary(self.inv_freq.ctypes.data, self.inv_freq.size, 1 if interleaved else 0)
-        self.address = ctypes.addressof(self._struct)
+        self._inv_freq = np.array(inv_freq, dtype=np.float64).reshape(-1)
+        self._inv_freq.setflags(write=False)
+        self._struct = _Rotary(self._inv_freq.ctypes.data, self._inv_freq.size, 1 if interleaved else 0)
+        self._address = ctypes.addressof(self._struct)
+
+    @property
+    def inv_freq(self) -> np.ndarray:
+        return self._inv_freq
+
+    @property
+    def address(self) -> int:
+        return self._address
 
 
 def library_path() -> str:
