@@ -7,7 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Sequence
+from typing import Sequence
 
 import numpy as np
 
@@ -242,21 +242,6 @@ def rlkv_set_gates(handle: int, gates, stream: int = 0):
     arr = None if gates is None else np.ascontiguousarray(np.asarray(gates, dtype=np.float32).reshape(-1))
     _check(load_library().rlkv_set_gates(handle, arr.ctypes.data if arr is not None else None, stream or None),
            "rlkv_set_gates")
-
-
-def rlkv_append_rotary(handle: int, layer: int, qkv_ptr: int, token_stride: int, n_tokens: Optional[Sequence[int]],
-                       stride_tokens: int, rotary: Rotary, q_out_ptr: int, stream: int = 0):
-    cnt = None if n_tokens is None else np.ascontiguousarray(np.asarray(n_tokens, dtype=np.int32))
-    _check(load_library().rlkv_append_rotary(handle, layer, qkv_ptr or None, token_stride, None if cnt is None else cnt.ctypes.data,
-                                             stride_tokens, rotary.address, q_out_ptr or None, stream or None), "rlkv_append_rotary")
-
-
-def rlkv_rotary(handle: int, layer: int, qkv_ptr: int, token_stride: int, n_tokens: Optional[Sequence[int]], stride_tokens: int,
-                rotary: Rotary, q_out_ptr: int, k_out_ptr: int, v_out_ptr: int, stream: int = 0):
-    cnt = None if n_tokens is None else np.ascontiguousarray(np.asarray(n_tokens, dtype=np.int32))
-    _check(load_library().rlkv_rotary(handle, layer, qkv_ptr or None, token_stride, None if cnt is None else cnt.ctypes.data,
-                                      stride_tokens, rotary.address, q_out_ptr or None, k_out_ptr or None, v_out_ptr or None,
-                                      stream or None), "rlkv_rotary")
 
 
 def rlkv_append_decode(handle: int, layer: int, k_ptr: int, v_ptr: int, q_ptr: int, out_ptr: int,
