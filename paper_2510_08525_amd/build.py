@@ -110,7 +110,19 @@ def build_example(verbose: bool = True) -> str:
     return EXAMPLE_BIN
 
 
-if __name__ == "__main__":
+def main() -> None:
+    """What needs no torch first: the C library and its example are built also where there is none, without the calls on tensors."""
     build_library()
-    build_tensor_calls()
     build_example()
+    try:
+        import torch  # noqa: F401
+    except ModuleNotFoundError as e:
+        if e.name != "torch":
+            raise
+        print("torch is not installed: the calls on torch tensors (_tensor_calls.so) are not built")
+    else:
+        build_tensor_calls()
+
+
+if __name__ == "__main__":
+    main()
