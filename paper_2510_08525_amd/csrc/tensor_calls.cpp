@@ -4,8 +4,11 @@
 // Every function returns the call's status; what is wrong with a tensor raises ValueError.
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
+
+#include <initializer_list>
 
 #include "rlkv.h"
 
@@ -46,12 +49,24 @@ class OnDevice {
   int before_, index_;
 };
 
+// As of torch's own operators into given outputs: while gradients are recorded no tensor may ask for one, since autograd does not see the call.
 const at::Tensor* tensor(PyObject* o, const char* what) {
   if (!THPVariable_Check(o)) {
     PyErr_Format(PyExc_ValueError, "%s: need a tensor", what);
     return nullptr;
   }
-  return &THPVariable_Unpack(o);
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (t.requires_grad() && c10::GradMode::is_enabled()) {
+    PyErr_Format(PyExc_ValueError, "%s: requires a gradient, which the call does not record: detach it, or call under torch.no_grad()", what);
+    return nullptr;
+  }
+  return &t;
+}
+// What the call has written: a version further, by which autograd knows that what it saved is no longer there.
+void written(PyObject* o) {
+  if (o == Py_None) return;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
 bool on_device(const at::Tensor& t, const char* what, int index) {
   if (t.is_cuda() && (index < 0 || t.get_device() == index)) return true;
@@ -135,13 +150,16 @@ bool number(PyObject* o, float* f) {
   return !(d == -1.0 && PyErr_Occurred());
 }
 
-// The library's call, with the interpreter left to other threads meanwhile: a launch waits where the device's queue is full.
+// The library's call, with the interpreter left to other threads meanwhile: a launch waits where the device's queue is full.  outputs: tensors
+// and None.
 template <typename F>
-PyObject* status_of(F call) {
+PyObject* status_of(std::initializer_list<PyObject*> outputs, F call) {
   int32_t status;
   Py_BEGIN_ALLOW_THREADS
   status = call();
   Py_END_ALLOW_THREADS
+  if (status == RLKV_OK)
+    for (PyObject* o : outputs) written(o);
   return PyLong_FromLong(status);
 }
 
@@ -168,7 +186,7 @@ PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (a[5] != Py_None && !matrix(a[5], "residual", x.device, x.type, x.rows, x.cols, &residual)) return nullptr;
   if (a[6] != Py_None && !matrix(a[6], "sum_out", x.device, x.type, x.rows, x.cols, &sum)) return nullptr;
   const OnDevice on(x.device);
-  return status_of([&] {
+  return status_of({a[3], a[4], a[6]}, [&] {
     return rlkv_rms_norm(x.p, x.stride, residual.p, residual.stride, weight, eps, (int32_t)x.rows, (int32_t)x.cols, kind_of(x.type),
                          sum.p, sum.stride, out.p, out.stride, kind_of(out.type), static_cast<float*>(scales.p), scales.stride,
                          on.stream());
@@ -184,7 +202,7 @@ PyObject* quantize(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!matrix(a[1], "out", x.device, ScalarType::Float8_e4m3fn, x.rows, x.cols, &out)) return nullptr;
   if (!matrix(a[2], "scales", x.device, ScalarType::Float, groups_of(x.cols), x.rows, &scales)) return nullptr;
   const OnDevice on(x.device);
-  return status_of([&] {
+  return status_of({a[1], a[2]}, [&] {
     return rlkv_quantize(x.p, x.stride, (int32_t)x.rows, (int32_t)x.cols, kind_of(x.type), out.p, out.stride,
                          static_cast<float*>(scales.p), scales.stride, on.stream());
   });
@@ -204,7 +222,7 @@ PyObject* scaled_matmul(PyObject*, PyObject* const* v, Py_ssize_t n) {
   if (!matrix(v[3], "b_scales", a.device, ScalarType::Float, groups_of(b.rows), g, &sb)) return nullptr;
   if (!activations(v[4], "out", &out) || !matrix(v[4], "out", a.device, out.type, a.rows, b.rows, &out)) return nullptr;
   const OnDevice on(a.device);
-  return status_of([&] {
+  return status_of({v[4]}, [&] {
     return rlkv_scaled_matmul(a.p, a.stride, static_cast<float*>(sa.p), sa.stride, b.p, b.stride, static_cast<float*>(sb.p), sb.stride,
                               (int32_t)a.rows, (int32_t)b.rows, (int32_t)a.cols, out.p, out.stride, kind_of(out.type), on.stream());
   });
@@ -235,7 +253,7 @@ PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const at::Tensor* w = tensor(a[8], "workspace");
   if (!w || !vector(a[8], "workspace", x.device, ScalarType::Byte, w->numel(), &workspace)) return nullptr;
   const OnDevice on(x.device);
-  return status_of([&] {
+  return status_of({a[2], a[4], a[5], a[6], a[6] == Py_None ? Py_None : a[7]}, [&] {
     return rlkv_token_logprobs(x.p, x.stride, (int32_t)x.rows, (int32_t)x.cols, kind_of(x.type), scale, static_cast<int32_t*>(tokens),
                                static_cast<float*>(logprobs), static_cast<float*>(entropy), static_cast<float*>(lse),
                                values.cols <= INT32_MAX ? (int32_t)values.cols : -1, static_cast<int32_t*>(ids.p),
@@ -259,7 +277,7 @@ PyObject* token_logprobs_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!vector(a[6], "entropy", x.device, ScalarType::Float, x.rows, &entropy)) return nullptr;
   if (!vector(a[7], "grad_entropy", x.device, ScalarType::Float, x.rows, &gh)) return nullptr;
   const OnDevice on(x.device);
-  return status_of([&] {
+  return status_of({a[4]}, [&] {
     return rlkv_token_logprobs_grad(x.p, x.stride, (int32_t)x.rows, (int32_t)x.cols, kind_of(x.type), scale,
                                     static_cast<int32_t*>(tokens), static_cast<float*>(lse), static_cast<float*>(entropy),
                                     static_cast<float*>(g), static_cast<float*>(gh), out.p, out.stride, on.stream());
@@ -344,7 +362,7 @@ PyObject* append_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return nullptr;
   if (a[6] != Py_None && !heads_first(a[6], "q_out", s, s.q_heads, x.tokens, &q)) return nullptr;
   const OnDevice on(s.device);
-  return status_of([&] {
+  return status_of({a[6]}, [&] {
     return rlkv_append_rotary(s.cache, s.layer, x.p, x.token_stride, static_cast<int32_t*>(counts), (int32_t)x.tokens,
                               static_cast<rlkv_rotary_t*>(rotary), q, on.stream());
   });
@@ -363,7 +381,7 @@ PyObject* rotary_split(PyObject*, PyObject* const* a, Py_ssize_t n) {
       !heads_first(a[8], "v_out", s, s.kv_heads, x.tokens, &v))
     return nullptr;
   const OnDevice on(s.device);
-  return status_of([&] {
+  return status_of({a[6], a[7], a[8]}, [&] {
     return rlkv_rotary(s.cache, s.layer, x.p, x.token_stride, static_cast<int32_t*>(counts), (int32_t)x.tokens,
                        static_cast<rlkv_rotary_t*>(rotary), q, k, v, on.stream());
   });

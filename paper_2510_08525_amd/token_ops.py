@@ -2,7 +2,8 @@
 
 Outputs are the caller's tensors; every call goes to the current stream of the tensors' device and returns its outputs.
 Matrices are two-dimensional with contiguous columns, rows at any stride.  What is wrong with a tensor raises ValueError, what the library
-refuses RlkvError.
+refuses RlkvError.  Autograd does not see the calls: as with torch's own calls into given outputs, a tensor that requires a gradient is
+refused unless under torch.no_grad(), and what is written counts as changed in place (`token_logprobs_grad` is the way back).
 """
 from __future__ import annotations
 
