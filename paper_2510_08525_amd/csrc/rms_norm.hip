@@ -98,9 +98,15 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(NormCall c) {
         for (int m = 1; m < 16; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
         const float scale = fmaxf(most / kE4m3Max, kLeastScale);
         if (col < c.cols) {
-          const float inverse = 1.f / scale;
+          // The quotient: a product with the reciprocal is off by up to two roundings, which its remainder takes back (two instructions a value
+          // instead of a division's ten; 16384 x 3584 74.7 us without them, 76.1 with them).  Under an infinite scale there is no
+          // remainder: 0, and NaN of an infinity.
+          const float inverse = 1.f / scale, divisor = scale < INFINITY ? scale : 0.f;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) f[i] *= inverse;
+          for (int i = 0; i < 8; ++i) {
+            const float q = f[i] * inverse;
+            f[i] = __builtin_fmaf(-__builtin_fmaf(q, divisor, -f[i]), inverse, q);      // (in these signs -0 stays -0)
+          }
           store_e4m3(static_cast<uint8_t*>(c.out) + row * c.out_stride, col, c.cols, f);
           if ((t & 15) == 0) c.scales[(int64_t)(col / kGroup) * c.scale_stride + row] = scale;
         }
