@@ -413,11 +413,11 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(LogprobGradCall c) {
   const int row = blockIdx.x / c.splits, split = blockIdx.x % c.splits;
   const T* logits = static_cast<const T*>(c.logits) + row * c.stride;
   T* out = static_cast<T*>(c.out) + row * c.out_stride;
-  const float scale2 = c.scale * kLog2e;
   const float lse = c.lse[row];
   // A row of nothing but masked logits, by -inf or by a value so low that lse, in 32 bits, is that value: all its gradients are 0.
   const bool empty = lse < kMaskedLse;
-  const float lse2 = empty ? 0.f : lse * kLog2e;
+  // (subtracted before the change of base: both sides times log2(e) would each be rounded at the logits' size, not at their distance's)
+  const float from = empty ? 0.f : lse;
   const int token = c.tokens && !empty ? c.tokens[row] : -1;
   const bool asked = token >= 0 && token < c.vocab;
   const float g = c.grad_logprobs && asked ? c.grad_logprobs[row] * c.scale : 0.f;
@@ -438,7 +438,7 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(LogprobGradCall c) {
       if (p0 + u * kThreads >= end) break;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float d = __builtin_fmaf(x[u][i], scale2, -lse2);
+        const float d = __builtin_fmaf(x[u][i], c.scale, -from) * kLog2e;
         const float w = __builtin_amdgcn_exp2f(d);
         x[u][i] = w * __builtin_fmaf(b, fmaxf(d, kLow), a);
       }
