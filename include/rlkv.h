@@ -289,7 +289,8 @@ rlkv_status_t rlkv_append_rotary(rlkv_cache_t* cache, int32_t layer, const void*
                                  void* q_out /* device */, void* stream);
 
 /* The same rotation with everything handed out, heads first, as rlkv_prefill_attention and rlkv_append_decode take it (they append
- * by themselves); the cache does not change and only its lengths are read.
+ * by themselves); the cache does not change and only its lengths are read.  Recorded into a HIP graph, the call runs at every replay
+ * with the lengths and the active slots of then; the counts are those of the recording.
  *   q_out        : device, [batch][n_q_heads][stride_tokens][head_dim]
  *   k_out, v_out : device, [batch][n_kv_heads][stride_tokens][head_dim]; rows past a sequence's count are not written */
 rlkv_status_t rlkv_rotary(rlkv_cache_t* cache, int32_t layer, const void* qkv /* device */, int64_t token_stride,

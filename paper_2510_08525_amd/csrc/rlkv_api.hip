@@ -902,7 +902,7 @@ rlkv_status_t rlkv_rotary(rlkv_cache_t* cache, int32_t layer, const void* qkv, i
   args.call.v_out = v_out;
   args.call.uniform = n_tokens ? 0 : stride_tokens;
   args.call.max_tokens = max_tok;
-  return launch_rotary(cache->dv, layer, len_of(cache->dv, cache->parity[layer], layer), nullptr, args.call, args.turns,
+  return launch_rotary(cache->dv, layer, len_of(cache->dv, 0, layer), len_of(cache->dv, 1, layer), args.call, args.turns,
                        n_tokens ? &seqs : nullptr, false, s) == hipSuccess ? RLKV_OK : RLKV_ERR_HIP;
 }
 

@@ -23,7 +23,8 @@ struct RotaryCall {
   void* v_out;
 };
 // `append`: the rotated keys and the values go into the layer's stores, lengths and list growth advance (as launch_append); else all
-// three go out, heads first.  `seqs` non-null: per-sequence counts.
+// three go out, heads first, and len_in and len_out are the two copies of the lengths, of which the larger is the present one (appends write
+// theirs over the older copy, a step and a reset both): a recorded call finds it at every replay.  `seqs` non-null: per-sequence counts.
 hipError_t launch_rotary(const DeviceView& dv, int layer, const int32_t* len_in, int32_t* len_out, const RotaryCall& call,
                          const RotaryTurns& turns, const SeqCounts* seqs, bool append, hipStream_t stream);
 

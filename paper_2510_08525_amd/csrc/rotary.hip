@@ -166,7 +166,12 @@ __global__ __launch_bounds__(kBlock) void rotary_kernel(DeviceView dv, int layer
   const int h_last = h_first + heads_each < n_heads ? h_first + heads_each : n_heads;
   const T* row = qkv + ((int64_t)b * call.stride_tokens + c) * call.token_stride;
   Angles g = {};
-  if (turned && h_first < Hq + H) angles_of(turns, j, (uint32_t)(len_in[b] + c), g);
+  int n = len_in[b];
+  if constexpr (!APPEND) {
+    const int other = len_out[b];
+    n = other > n ? other : n;
+  }
+  if (turned && h_first < Hq + H) angles_of(turns, j, (uint32_t)(n + c), g);
   for (int h = h_first; h < h_last; ++h) {
     float x[8], y[8];
     load_piece<STREAM>(row + (int64_t)h * kHeadDim, c0, kHeadDim, x);
