@@ -485,8 +485,8 @@ rlkv_status_t rlkv_scaled_matmul(const void* a /* device */, int64_t a_stride, c
                                  const float* b_scales /* device */, int64_t b_scale_stride, int32_t m, int32_t n, int32_t k,
                                  void* out /* device */, int64_t out_stride, int32_t out_dtype, void* stream);
 
-/* Log probabilities of given tokens and what belongs to them, in one pass over rows of logits (x = scale * logits, scale > 0: one over
- * the temperature; p = softmax(x)):
+/* Log probabilities of given tokens and what belongs to them, in one pass over rows of logits (x = scale * logits, 0 < scale <= 2^127:
+ * one over the temperature; p = softmax(x)):
  *     lse = log sum exp x      logprobs = x[token] - lse      entropy = - sum p log p
  *   logits : device, `dtype` (RLKV_F32 or RLKV_BF16), [rows][vocab]; rows <= 2^20, vocab <= 2^24
  *   tokens, logprobs : device, int32 and fp32 [rows]; both or neither.  A row whose token is not in [0, vocab) is not scored:

@@ -22,6 +22,7 @@ bool writable(const void* p, int64_t stride, int64_t rows, int64_t cols, int dty
 bool whole(const void* p, int64_t stride, int dtype) { return aligned(p, 16) && (stride * (int64_t)bytes_of(dtype)) % 16 == 0; }
 
 constexpr int32_t kMostLogitRows = 1 << 20, kMostVocab = 1 << 24;
+constexpr float kMostScale = 1.70141183e38f;             // 2^127 (times log2(e) it is still finite)
 constexpr int32_t kMostNormCols = 1 << 30;              // (a piece or a stride of threads further on is still an int)
 
 rlkv_status_t norm_call(NormCall& c, int dtype, int out_dtype, void* stream) {
@@ -93,7 +94,7 @@ rlkv_status_t rlkv_scaled_matmul(const void* a, int64_t a_stride, const float* a
 
 static bool logits_valid(int32_t rows, int32_t vocab, int32_t dtype, float scale) {
   if (dtype != RLKV_F32 && dtype != RLKV_BF16) return false;
-  return rows >= 0 && rows <= kMostLogitRows && vocab >= 1 && vocab <= kMostVocab && scale > 0.f && !isinf(scale);
+  return rows >= 0 && rows <= kMostLogitRows && vocab >= 1 && vocab <= kMostVocab && scale > 0.f && scale <= kMostScale;
 }
 
 size_t rlkv_token_logprobs_workspace(int32_t rows, int32_t vocab, int32_t top) {
