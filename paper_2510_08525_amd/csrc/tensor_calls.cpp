@@ -296,8 +296,14 @@ struct CacheShape {
 // handle, layer, (device, kind, batch, q heads, kv heads, head_dim)
 bool cache_shape(PyObject* handle, PyObject* layer, PyObject* shape, CacheShape* s) {
   s->cache = handle == Py_None ? nullptr : static_cast<rlkv_cache_t*>(PyLong_AsVoidPtr(handle));   // (None: closed, which the library refuses)
-  s->layer = (int32_t)PyLong_AsLong(layer);
+  int beyond = 0;
+  const long at = PyLong_AsLongAndOverflow(layer, &beyond);
   if (PyErr_Occurred()) return false;
+  s->layer = (int32_t)at;
+  if (beyond || s->layer != at) {
+    PyErr_Format(PyExc_ValueError, "layer: %R is none", layer);
+    return false;
+  }
   if (!PyTuple_Check(shape) || PyTuple_GET_SIZE(shape) != 6) {
     PyErr_SetString(PyExc_TypeError, "shape of the cache");
     return false;
