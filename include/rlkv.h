@@ -443,6 +443,11 @@ int32_t rlkv_plan_narrow_split(int32_t n_compute_units, int32_t group, int32_t n
                                const int32_t* n_tokens /* host */, const int32_t* cached /* host */,
                                int32_t min_share_tiles);
 
+/* Which shape of workgroups rlkv_scaled_matmul takes for these sizes: plan[0], plan[1] = rows of a and rows of b that a workgroup has,
+ * plan[2] = parts of k side by side in it, plan[3] = the place of the shape in the list that the call chooses from (m <= 16; m <= 64; more rows
+ * with an fp32 output; with a bf16 output).  Returns the length of that list, -1 on an invalid argument.  Exposed for tests and tools. */
+int32_t rlkv_plan_matmul(int32_t m, int32_t n, int32_t k, int32_t out_dtype, int32_t* plan /* host [4] */);
+
 /* ---- Token-wise operators: a decoder's way into the cache and out of it again --------------------------------------------
  * These need no cache handle.  They run on `stream` of the current device, keep no state, allocate nothing, wait for nothing
  * and can be recorded into a HIP graph.  Matrices are row-major; a stride is the distance of two rows (of two groups, for

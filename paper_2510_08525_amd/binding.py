@@ -119,6 +119,7 @@ def load_library():
         "rlkv_rms_norm": (i32, [vp, i64, vp, i64, vp, f32, i32, i32, i32, vp, i64, vp, i64, i32, vp, i64, vp]),
         "rlkv_quantize": (i32, [vp, i64, i32, i32, i32, vp, i64, vp, i64, vp]),
         "rlkv_scaled_matmul": (i32, [vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, i32, vp, i64, i32, vp]),
+        "rlkv_plan_matmul": (i32, [i32, i32, i32, i32, vp]),
         "rlkv_token_logprobs_workspace": (sz, [i32, i32, i32]),
         "rlkv_token_logprobs": (i32, [vp, i64, i32, i32, i32, f32, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]),
         "rlkv_token_logprobs_grad": (i32, [vp, i64, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, i64, vp]),
@@ -153,7 +154,7 @@ EXPORTED_SYMBOLS = (
     "rlkv_profile_collect", "rlkv_get_lengths",
     "rlkv_get_slot_positions", "rlkv_resident_bytes", "rlkv_probe_stream_read", "rlkv_plan_shares", "rlkv_plan_whole_pairs", "rlkv_plan_list_whole", "rlkv_plan_list_kind", "rlkv_plan_merge_inside", "rlkv_plan_static_scratch", "rlkv_plan_narrow_split", "rlkv_plan_blend_form", "rlkv_plan_prefill_form", "rlkv_plan_prefill_rows", "rlkv_plan_prefill_block", "rlkv_plan_prefill_item", "rlkv_cache_kernel", "rlkv_pool_pages_free",
     "rlkv_pool_shuffle", "rlkv_status_string",
-    "rlkv_append_rotary", "rlkv_rotary", "rlkv_rms_norm", "rlkv_quantize", "rlkv_scaled_matmul",
+    "rlkv_append_rotary", "rlkv_rotary", "rlkv_rms_norm", "rlkv_quantize", "rlkv_scaled_matmul", "rlkv_plan_matmul",
     "rlkv_token_logprobs_workspace", "rlkv_token_logprobs", "rlkv_token_logprobs_grad",
 )
 
@@ -310,6 +311,15 @@ def rlkv_token_logprobs_workspace(rows: int, vocab: int, top: int = 0) -> int:
 def rlkv_probe_stream_read(buf_ptr: int, nbytes: int, sink_ptr: int, workgroups: int, stream: int = 0):
     _check(load_library().rlkv_probe_stream_read(buf_ptr or None, nbytes, sink_ptr or None, workgroups, stream or None),
            "rlkv_probe_stream_read")
+
+
+def rlkv_plan_matmul(m: int, n: int, k: int, out_dtype: int):
+    """(rows of a, rows of b, parts of k of a workgroup, place in the list, length of the list) for these sizes."""
+    plan = np.zeros(4, dtype=np.int32)
+    length = load_library().rlkv_plan_matmul(m, n, k, out_dtype, plan.ctypes.data)
+    if length < 0:
+        raise RlkvError(RLKV_ERR_INVALID_ARG, "rlkv_plan_matmul")
+    return (*(int(v) for v in plan), length)
 
 
 def rlkv_plan_shares(rounds, n_workgroups: int):

@@ -417,7 +417,7 @@ hipError_t launch_tiled(const MatmulCall& c, hipStream_t stream) {
 // workgroups that a compute unit then has (with one a unit between few units and all: the clock falls and L2 is shared).
 // From calls of 70 .. 8192 rows, 1000 .. 14336 columns and k of 1000 .. 14336, less 2.5 us a call.
 constexpr int kFewRows = 64, kUnits = 256;
-struct TileCost { int bm, bn, per_unit, round, last[3], once; };      // once: more than the others, a call
+struct TileCost { int bm, bn, parts, per_unit, round, last[3], once; };      // parts: of k, in a workgroup; once: more than the others, a call
 inline double estimate(const TileCost& t, const MatmulCall& c) {
   const int64_t tiles = ((int64_t)(c.m + t.bm - 1) / t.bm) * ((c.n + t.bn - 1) / t.bn), slots = (int64_t)t.per_unit * kUnits;
   const int64_t rest = tiles % slots;
@@ -435,58 +435,75 @@ int cheapest(const TileCost (&costs)[N], const MatmulCall& c) {
   return best;
 }
 
+// The shapes of workgroups, by the kind of the call, and which of its kind a call takes; launch_typed has the kernel of each.
+enum Kind { kSixteenRows, kSixtyFourRows, kManyInto32, kManyInto16 };
+inline Kind kind_of(const MatmulCall& c, bool out_bf16) {
+  return c.m <= 16 ? kSixteenRows : c.m <= kFewRows ? kSixtyFourRows : out_bf16 ? kManyInto16 : kManyInto32;
+}
+// (us, 4 wavefronts a workgroup / 8: 1 x 6144 x 4096 7.5 / 8.0, 1 x 14336 x 4096 13.6 / 15.1; few workgroups want the wider: 1 x 1024 x 16384
+// 10.4 / 7.7.)
+constexpr TileCost kSixteen[] = {{16, 16, 8}, {16, 16, 4}};
+inline int sixteen_rows(const MatmulCall& c) { return c.n <= 128 * 16 ? 0 : 1; }
+// 32 rows at a time with b straight from memory, or for wide outputs, where a would be read too often, tiles as below with exact products.
+// (us, 32 rows at a time, tiles 32 x 64 in four parts, 64 x 64 and 64 x 128 in two: 64 x 4096 x 4096 9.3, 9.2, 14.5, -; 64 x 6144 x 4096 11.8,
+// 9.4, 14.6, -; 64 x 9000 x 4096 16.8, 17.4, 14.5, 20.4; 24 x 14336 x 4096 15.4, 11.9, 14.8, 20.3; 64 x 14336 x 4096 25.6, 17.8, 15.3, 20.9;
+// 64 x 28672 x 2048 23.0, 22.6, 17.8, 14.6.)
+constexpr TileCost kSixtyFour[] = {{32, 16, 4, 3, 310, {125, 235, 300}, 0}, {32, 64, 4, 1, 260, {195, 270}, 500},
+                                   {64, 64, 2, 1, 430, {345, 390}, 500},    {64, 128, 2, 1, 640, {540, 640}, 1500}};
+// The shape of the tiles whose rounds over the compute units are estimated to take least: small ones fill the card, large ones read less,
+// and of few small ones each turn is a chain of latencies, which two parts of k side by side hide from each other.
+// (us measured, a bf16 output: 333 x 4608 x 3584 64 x 64 16.5, 128 x 64 14.6, in two parts 13.3, 128 x 128 19.2; 200 x 4096 x 4096 64 x 64 12.7, in
+// two parts 10.5, in four 12.0; 512 x 4608 x 3584 64 x 64 20.8, in two parts 26.2, 128 x 128 19.5; 1000 x 1000 x 1008 64 x 64 5.5, in two
+// parts 5.8; 1024 x 6144 x 4096 128 x 64 41.5, 256 x 128 34.4; 4096 x 4608 x 3584 256 x 128 94, 192 x 256 85, 256 x 256 101.)
+constexpr TileCost kInto16[] = {{64, 64, 1, 3, 697, {320, 510, 690}, 0}, {64, 64, 2, 1, 320, {255, 255}, 700},
+                                {128, 64, 1, 2, 800, {430, 700}, 0},     {128, 64, 2, 1, 424, {390, 390}, 700},
+                                {128, 128, 1, 1, 741, {560, 650}, 0},    {256, 128, 1, 1, 1210, {760, 1080}, 0},
+                                {192, 256, 1, 1, 1670, {1100, 1600}, 0}, {256, 256, 1, 1, 2050, {1300, 1960}, 0}};
+// (us, an fp32 output: 333 x 4608 x 3584 64 x 64 24.8, in four parts 23.5, 64 x 128 in two parts 19.3, 128 x 128 33.7; 200 x 4096 x 4096 64 x 64 19.3,
+// in four parts 14.2; 512 x 4608 x 3584 30.8, 34.4, 64 x 128 36.5; 1024 x 6144 x 4096 64 x 64 68.8, 64 x 128 63.6, 256 x 128 61.0, 128 x 128 75.1;
+// 2048 x 2048 x 2048 64 x 128 25.2, 128 x 128 23.2.)
+constexpr TileCost kInto32[] = {{64, 64, 1, 3, 1050, {525, 760, 1030}, 0}, {64, 64, 4, 1, 370, {360, 360}, 500},
+                                {64, 128, 2, 1, 665, {590, 590}, 700},     {128, 128, 1, 1, 1300, {1050, 1290}, 0},
+                                {256, 128, 1, 1, 1960, {1700, 1900}, 0}};
+inline int shape_of(const MatmulCall& c, Kind kind) {
+  return kind == kSixteenRows ? sixteen_rows(c) : kind == kSixtyFourRows ? cheapest(kSixtyFour, c)
+         : kind == kManyInto16 ? cheapest(kInto16, c) : cheapest(kInto32, c);
+}
+
 template <bool BF16>
 hipError_t launch_typed(const MatmulCall& c, hipStream_t stream) {
-  // (us, 4 wavefronts a workgroup / 8: 1 x 6144 x 4096 7.5 / 8.0, 1 x 14336 x 4096 13.6 / 15.1; few workgroups want the wider: 1 x 1024 x 16384
-  // 10.4 / 7.7.)
-  if (c.m <= 16) return c.n <= 128 * 16 ? launch_few<1, 8, 2, BF16>(c, stream) : launch_few<1, 4, 2, BF16>(c, stream);
-  if (c.m <= kFewRows) {
-    // 32 rows at a time with b straight from memory, or for wide outputs, where a would be read too often, tiles as below with exact products.
-    // (us, 32 rows at a time, tiles 32 x 64 in four parts, 64 x 64 and 64 x 128 in two: 64 x 4096 x 4096 9.3, 9.2, 14.5, -; 64 x 6144 x 4096 11.8,
-    // 9.4, 14.6, -; 64 x 9000 x 4096 16.8, 17.4, 14.5, 20.4; 24 x 14336 x 4096 15.4, 11.9, 14.8, 20.3; 64 x 14336 x 4096 25.6, 17.8, 15.3, 20.9;
-    // 64 x 28672 x 2048 23.0, 22.6, 17.8, 14.6.)
-    static const TileCost costs[] = {{32, 16, 3, 310, {125, 235, 300}, 0}, {32, 64, 1, 260, {195, 270}, 500},
-                                     {64, 64, 1, 430, {345, 390}, 500},    {64, 128, 1, 640, {540, 640}, 1500}};
-    switch (cheapest(costs, c)) {
-      case 0: return launch_few<2, 4, 2, BF16>(c, stream);
-      case 1: return launch_tiled<32, 64, 1, 2, 3, 4, kWide, BF16>(c, stream);
-      case 2: return launch_tiled<64, 64, 2, 2, 3, 2, kWide, BF16>(c, stream);
-      default: return launch_tiled<64, 128, 2, 2, 3, 2, kWide, BF16>(c, stream);
+  const Kind kind = kind_of(c, BF16);
+  const int at = shape_of(c, kind);
+  if (kind == kSixteenRows) return at == 0 ? launch_few<1, kSixteen[0].parts, 2, BF16>(c, stream) : launch_few<1, kSixteen[1].parts, 2, BF16>(c, stream);
+  if (kind == kSixtyFourRows) {
+    constexpr auto& t = kSixtyFour;
+    switch (at) {
+      case 0: return launch_few<t[0].bm / 16, t[0].parts, 2, BF16>(c, stream);
+      case 1: return launch_tiled<t[1].bm, t[1].bn, 1, 2, 3, t[1].parts, kWide, BF16>(c, stream);
+      case 2: return launch_tiled<t[2].bm, t[2].bn, 2, 2, 3, t[2].parts, kWide, BF16>(c, stream);
+      default: return launch_tiled<t[3].bm, t[3].bn, 2, 2, 3, t[3].parts, kWide, BF16>(c, stream);
     }
   }
-  // The shape of the tiles whose rounds over the compute units are estimated to take least: small ones fill the card, large ones read less,
-  // and of few small ones each turn is a chain of latencies, which two parts of k side by side hide from each other.
-  // (us measured: 333 x 4608 x 3584 64 x 64 16.5, 128 x 64 14.6, in two parts 13.3, 128 x 128 19.2; 200 x 4096 x 4096 64 x 64 12.7, in two
-  // parts 10.5, in four 12.0; 512 x 4608 x 3584 64 x 64 20.8, in two parts 26.2, 128 x 128 19.5; 1000 x 1000 x 1008 64 x 64 5.5, in two
-  // parts 5.8; 1024 x 6144 x 4096 128 x 64 41.5, 256 x 128 34.4; 4096 x 4608 x 3584 256 x 128 94, 192 x 256 85, 256 x 256 101.)
   if constexpr (!BF16) {
-    // (us: 333 x 4608 x 3584 64 x 64 24.8, in four parts 23.5, 64 x 128 in two parts 19.3, 128 x 128 33.7; 200 x 4096 x 4096 64 x 64 19.3, in four parts
-    // 14.2; 512 x 4608 x 3584 30.8, 34.4, 64 x 128 36.5; 1024 x 6144 x 4096 64 x 64 68.8, 64 x 128 63.6, 256 x 128 61.0, 128 x 128 75.1; 2048 x 2048 x 2048
-    // 64 x 128 25.2, 128 x 128 23.2.)
-    static const TileCost costs[] = {{64, 64, 3, 1050, {525, 760, 1030}, 0}, {64, 64, 1, 370, {360, 360}, 500},
-                                     {64, 128, 1, 665, {590, 590}, 700},     {128, 128, 1, 1300, {1050, 1290}, 0},
-                                     {256, 128, 1, 1960, {1700, 1900}, 0}};
-    switch (cheapest(costs, c)) {
-      case 0: return launch_tiled<64, 64, 2, 2, 3, 1, kWide, false>(c, stream);
-      case 1: return launch_tiled<64, 64, 2, 1, 2, 4, kWide, false>(c, stream);
-      case 2: return launch_tiled<64, 128, 2, 2, 3, 2, kWide, false>(c, stream);
-      case 3: return launch_tiled<128, 128, 2, 4, 3, 1, kWide, false>(c, stream);
-      default: return launch_tiled<256, 128, 4, 2, 3, 1, kWide, false>(c, stream);
+    constexpr auto& t = kInto32;
+    switch (at) {
+      case 0: return launch_tiled<t[0].bm, t[0].bn, 2, 2, 3, t[0].parts, kWide, false>(c, stream);
+      case 1: return launch_tiled<t[1].bm, t[1].bn, 2, 1, 2, t[1].parts, kWide, false>(c, stream);
+      case 2: return launch_tiled<t[2].bm, t[2].bn, 2, 2, 3, t[2].parts, kWide, false>(c, stream);
+      case 3: return launch_tiled<t[3].bm, t[3].bn, 2, 4, 3, t[3].parts, kWide, false>(c, stream);
+      default: return launch_tiled<t[4].bm, t[4].bn, 4, 2, 3, t[4].parts, kWide, false>(c, stream);
     }
   } else {
-    static const TileCost costs[] = {{64, 64, 3, 697, {320, 510, 690}, 0}, {64, 64, 1, 320, {255, 255}, 700},
-                                     {128, 64, 2, 800, {430, 700}, 0},     {128, 64, 1, 424, {390, 390}, 700},
-                                     {128, 128, 1, 741, {560, 650}, 0},    {256, 128, 1, 1210, {760, 1080}, 0},
-                                     {192, 256, 1, 1670, {1100, 1600}, 0}, {256, 256, 1, 2050, {1300, 1960}, 0}};
-    switch (cheapest(costs, c)) {
-      case 0: return launch_tiled<64, 64, 2, 2, 3, 1, kFast, true>(c, stream);
-      case 1: return launch_tiled<64, 64, 2, 2, 3, 2, kFast, true>(c, stream);
-      case 2: return launch_tiled<128, 64, 2, 2, 3, 1, kFast, true>(c, stream);
-      case 3: return launch_tiled<128, 64, 2, 2, 3, 2, kFast, true>(c, stream);
-      case 4: return launch_tiled<128, 128, 2, 4, 3, 1, kFast, true>(c, stream);
-      case 5: return launch_tiled<256, 128, 4, 2, 3, 1, kFast, true>(c, stream);
-      case 6: return launch_tiled<192, 256, 2, 4, 2, 1, kFast, true>(c, stream);
-      default: return launch_tiled<256, 256, 2, 4, 2, 1, kFast, true>(c, stream);
+    constexpr auto& t = kInto16;
+    switch (at) {
+      case 0: return launch_tiled<t[0].bm, t[0].bn, 2, 2, 3, t[0].parts, kFast, true>(c, stream);
+      case 1: return launch_tiled<t[1].bm, t[1].bn, 2, 2, 3, t[1].parts, kFast, true>(c, stream);
+      case 2: return launch_tiled<t[2].bm, t[2].bn, 2, 2, 3, t[2].parts, kFast, true>(c, stream);
+      case 3: return launch_tiled<t[3].bm, t[3].bn, 2, 2, 3, t[3].parts, kFast, true>(c, stream);
+      case 4: return launch_tiled<t[4].bm, t[4].bn, 2, 4, 3, t[4].parts, kFast, true>(c, stream);
+      case 5: return launch_tiled<t[5].bm, t[5].bn, 4, 2, 3, t[5].parts, kFast, true>(c, stream);
+      case 6: return launch_tiled<t[6].bm, t[6].bn, 2, 4, 2, t[6].parts, kFast, true>(c, stream);
+      default: return launch_tiled<t[7].bm, t[7].bn, 2, 4, 2, t[7].parts, kFast, true>(c, stream);
     }
   }
 }
@@ -495,6 +512,19 @@ hipError_t launch_typed(const MatmulCall& c, hipStream_t stream) {
 
 hipError_t launch_matmul(const MatmulCall& c, bool out_bf16, hipStream_t stream) {
   return out_bf16 ? launch_typed<true>(c, stream) : launch_typed<false>(c, stream);
+}
+
+int plan_matmul(const MatmulCall& c, bool out_bf16, int* plan) {
+  const Kind kind = kind_of(c, out_bf16);
+  const int at = shape_of(c, kind);
+  auto entry = [&](const auto& list) {
+    plan[0] = list[at].bm;
+    plan[1] = list[at].bn;
+    plan[2] = list[at].parts;
+    plan[3] = at;
+    return (int)(sizeof(list) / sizeof(list[0]));
+  };
+  return kind == kSixteenRows ? entry(kSixteen) : kind == kSixtyFourRows ? entry(kSixtyFour) : kind == kManyInto16 ? entry(kInto16) : entry(kInto32);
 }
 
 }  // namespace rlkv

@@ -69,13 +69,24 @@ rlkv_status_t rlkv_quantize(const void* x, int64_t x_stride, int32_t rows, int32
   return norm_call(c, dtype, RLKV_E4M3, stream);
 }
 
+static bool product_valid(int32_t m, int32_t n, int32_t k, int32_t out_dtype) {
+  if (out_dtype != RLKV_F32 && out_dtype != RLKV_BF16) return false;
+  if (m < 0 || n < 0 || k < 1 || k % 16 != 0) return false;
+  if (m > (1 << 24) || n > (1 << 24) || k > (1 << 24)) return false;
+  return (int64_t)(m / 128 + 1) * (n / 128 + 1) <= (1 << 22);      // (threads of a launch are below 2^32)
+}
+
+int32_t rlkv_plan_matmul(int32_t m, int32_t n, int32_t k, int32_t out_dtype, int32_t* plan) {
+  if (!plan || m < 1 || n < 1 || !product_valid(m, n, k, out_dtype)) return -1;
+  MatmulCall c = {};
+  c.m = m; c.n = n; c.k = k;
+  return plan_matmul(c, out_dtype == RLKV_BF16, plan);
+}
+
 rlkv_status_t rlkv_scaled_matmul(const void* a, int64_t a_stride, const float* a_scales, int64_t a_scale_stride, const void* b,
                                  int64_t b_stride, const float* b_scales, int64_t b_scale_stride, int32_t m, int32_t n, int32_t k,
                                  void* out, int64_t out_stride, int32_t out_dtype, void* stream) {
-  if (out_dtype != RLKV_F32 && out_dtype != RLKV_BF16) return RLKV_ERR_INVALID_ARG;
-  if (m < 0 || n < 0 || k < 1 || k % 16 != 0) return RLKV_ERR_INVALID_ARG;
-  if (m > (1 << 24) || n > (1 << 24) || k > (1 << 24)) return RLKV_ERR_INVALID_ARG;
-  if ((int64_t)(m / 128 + 1) * (n / 128 + 1) > (1 << 22)) return RLKV_ERR_INVALID_ARG;      // (threads of a launch are below 2^32)
+  if (!product_valid(m, n, k, out_dtype)) return RLKV_ERR_INVALID_ARG;
   if (m == 0 || n == 0) return RLKV_OK;
   if (!readable(a, a_stride, RLKV_E4M3) || !readable(b, b_stride, RLKV_E4M3) || !whole(a, a_stride, RLKV_E4M3) ||
       !whole(b, b_stride, RLKV_E4M3) || a_stride > kMostMatmulStride || b_stride > kMostMatmulStride)

@@ -180,6 +180,9 @@ struct MatmulCall {
 };
 constexpr int64_t kMostMatmulStride = 1 << 23;         // bytes between rows of a or b: a tile's rows are within 32 bits of its first
 hipError_t launch_matmul(const MatmulCall& call, bool out_bf16, hipStream_t stream);
+// What a workgroup of the launch has: rows of a, rows of b, parts of k, and the place of that shape among those of its kind, whose number is
+// the result (sizes of the call only).
+int plan_matmul(const MatmulCall& call, bool out_bf16, int* plan);
 
 constexpr int kMostTop = 32;          // most likely tokens a row can be asked for
 struct LogprobCall {
