@@ -440,10 +440,12 @@ enum Kind { kSixteenRows, kSixtyFourRows, kManyInto32, kManyInto16 };
 inline Kind kind_of(const MatmulCall& c, bool out_bf16) {
   return c.m <= 16 ? kSixteenRows : c.m <= kFewRows ? kSixtyFourRows : out_bf16 ? kManyInto16 : kManyInto32;
 }
-// (us, 4 wavefronts a workgroup / 8: 1 x 6144 x 4096 7.5 / 8.0, 1 x 14336 x 4096 13.6 / 15.1; few workgroups want the wider: 1 x 1024 x 16384
-// 10.4 / 7.7.)
+// Eight wavefronts where a compute unit has at most one workgroup, which has to keep its unit's loads going alone, and each of them a group; else
+// four.  (us of the kernel, 4 / 8, one row: n = 1024 with k = 512 2.3 / 2.4, 2048 3.5 / 3.3, 4096 4.7 / 4.3, 16384 12.4 / 8.9; n = 2048 with 4096 5.5 / 4.9,
+// 16384 13.5 / 10.8; n = 4096 with 512 2.7 / 2.8, 2048 4.3 / 4.2, 8192 9.7 / 8.8, 16384 16.0 / 16.0; n = 6144 with 2048 5.2 / 5.4, 4096 7.6 / 8.3,
+// 16384 22.8 / 23.4; sixteen rows: n = 1024 with 16384 12.6 / 10.9, n = 4096 with 4096 6.6 / 6.2, n = 6144 with 4096 8.5 / 8.7.)
 constexpr TileCost kSixteen[] = {{16, 16, 8}, {16, 16, 4}};
-inline int sixteen_rows(const MatmulCall& c) { return c.n <= 128 * 16 ? 0 : 1; }
+inline int sixteen_rows(const MatmulCall& c) { return c.n <= kUnits * 16 && c.k >= 8 * kGroup ? 0 : 1; }
 // 32 rows at a time with b straight from memory, or for wide outputs, where a would be read too often, tiles as below with exact products.
 // (us, 32 rows at a time, tiles 32 x 64 in four parts, 64 x 64 and 64 x 128 in two: 64 x 4096 x 4096 9.3, 9.2, 14.5, -; 64 x 6144 x 4096 11.8,
 // 9.4, 14.6, -; 64 x 9000 x 4096 16.8, 17.4, 14.5, 20.4; 24 x 14336 x 4096 15.4, 11.9, 14.8, 20.3; 64 x 14336 x 4096 25.6, 17.8, 15.3, 20.9;
