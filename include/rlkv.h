@@ -516,7 +516,8 @@ rlkv_status_t rlkv_token_logprobs(const void* logits /* device */, int64_t strid
  *   tokens, grad_logprobs : device, int32 and fp32 [rows]; both or neither.  Rows that are not scored have no part of the first kind
  *   entropy, grad_entropy : device, fp32 [rows]; both or neither
  *   grad_logits : device, `dtype`, [rows][vocab]; may be logits itself (same pointer and stride)
- * A row of masked logits only (lse below -1e30) has gradients of 0. */
+ * p is exp(x - lse) with lse as 32 bits hold it, which is off by 2^-24 |lse| of itself.  A row of masked logits only (lse below -1e30) has
+ * gradients of 0. */
 rlkv_status_t rlkv_token_logprobs_grad(const void* logits /* device */, int64_t stride, int32_t rows, int32_t vocab, int32_t dtype,
                                        float scale, const int32_t* tokens /* device */, const float* lse /* device */,
                                        const float* entropy /* device */, const float* grad_logprobs /* device */,

@@ -5,11 +5,12 @@
 //
 // h stays in fp32 registers between the sum of squares and the outputs, so it is read once and each output is rounded once: the norm is
 // that of the unrounded sum.  A thread has one piece of eight columns (two beyond 8192 columns, and what is beyond 16384 is read a
-// second time): a row's loads are all in flight at once, a wavefront's are whole lines, and the 16 lanes of a group of 128 columns
+// second time): all of a row's pieces are asked for at once, a wavefront's are whole lines, and the 16 lanes of a group of 128 columns
 // lie next to each other, so that its maximum takes four steps over lanes and no LDS.
-// Bound: HBM for many rows (16384 x 3584 bf16 with residual into 8 bits: 413 MB in 75 to 78 us, 5.3 to 5.5 TB/s; a copy of 1 GiB reaches 5.05), latency for few
-// (one row of 4096: 4 us).  With 64 threads a row and eight pieces each, weights kept over several rows, the same call took
-// 134 us, with 256 threads and two pieces 90 (both with plain accesses); several rows to a workgroup one after the other are slower in every shape.
+// Bound: HBM for many rows (16384 x 3584 bf16 with residual into 8 bits: 413 MB in 76 to 77 us, 5.4 TB/s; a copy of 1 GiB reaches 5.05), latency for few
+// (one row of 4096: 4 us, the kernel 2.9): x, in bf16 the residual behind it (each is widened as it arrives), and the weight behind the sum.
+// With 64 threads a row and eight pieces each, weights kept over several rows, the same call took 134 us, with 256 threads and two pieces 90
+// (both with plain accesses); several rows to a workgroup one after the other are slower in every shape.
 #include <type_traits>
 
 #include "token_ops.h"
@@ -145,8 +146,8 @@ hipError_t launch_typed(const NormCall& c, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_norm(const NormCall& c, int dtype, bool out_e4m3, hipStream_t stream) {
-  // (us, plain accesses / non-temporal ones, bf16 with residual into 8 bits: 16384 x 3584 79.0 / 74.7; 8192 x 3584, which a
-  // cache holds, 43.8 / 40.2 by itself: not taken)
+  // (us, plain accesses / non-temporal ones, bf16 with residual into 8 bits: 16384 x 3584 81.2 / 76.9; 8192 x 3584, which a
+  // cache holds, 43.9 / 40.5 by itself: not taken)
   const int64_t bytes = dtype == RLKV_F32 ? 4 : 2;
   const bool through = c.rows * (int64_t)c.cols * (bytes * (1 + (c.residual != nullptr) + (c.sum_out != nullptr)) + (out_e4m3 ? 1 : bytes)) > kStreamBytes;
   auto launch = [&](auto x, auto e4m3) {

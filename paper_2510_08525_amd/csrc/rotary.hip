@@ -8,7 +8,8 @@
 // Eight threads hold a row: thread j two pieces of eight columns, those that turn together (j and j + pairs / 8, or 2 j and
 // 2 j + 1), so all eight angles are its own.  Queries: a thread keeps its token's sines and cosines over several heads.  Keys and
 // values of an append: one workgroup per tile of 32 slots (destination driven, like append_kernel), whose row pieces pass through LDS into
-// the tile.  Bound: HBM for prompts, one chain of memory latencies for a single token.
+// the tile.  Bound: HBM for prompts (8 x 2000 tokens of 32 / 8 heads handed out heads first: 393 MB in 70.6 us, 5.6 TB/s), one chain of memory
+// latencies for a single token.
 #include <type_traits>
 
 #include "append_slots.h"
@@ -187,7 +188,8 @@ __global__ __launch_bounds__(kBlock) void rotary_kernel(DeviceView dv, int layer
 }
 
 // One token a sequence (a decode step): the same work laid out for latency.  Eight threads have a query head's row, or a KV head's key and
-// value row; the rows are asked for before anything that says where they go, and a row's pieces are stored from registers.
+// value row; the rows are asked for before anything that says where they go (fp32 rows are still under way then, bf16 ones, widened as they arrive,
+// are waited for), and a row's pieces are stored from registers.
 constexpr int kStepBlock = 64;
 template <int KERNEL, typename T>
 __global__ __launch_bounds__(kStepBlock) void rotary_step_kernel(DeviceView dv, int layer, const int32_t* __restrict__ len_in,

@@ -15,7 +15,7 @@
 // An fp32 output is always of the first kind, and so are few rows, where b's bytes are what counts; many rows with a bf16 output take the
 // second (so a row's bits differ between a call of 64 rows and one of 65).  Of 512 x 4608 x 3584 with the left side quantised from normal
 // activations, or with 0.5 % of the columns 21 or 0.1 % of them 100 times as large, both kinds are off by 1.66e-3 of the 2-norm, which is the bf16
-// output's rounding alone; one value in 50 or more comes out a bf16 step apart.  b is the instruction's first operand:
+// output's rounding alone; 1 to 2 % of the values come out a bf16 step apart.  b is the instruction's first operand:
 // a lane's four results then belong to one row of a, whose scale is one register, and to four neighbouring columns of the output.  The order
 // of k inside a group does not matter as long as both operands have the same: lane (row, seg) holds bytes [16 seg, 16 seg + 16) and the
 // same 64 further on, so that a load of 16 lanes x 4 segments reads 64 contiguous bytes of each row.

@@ -407,7 +407,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(LogprobCall c) {
   finish_row<TOP>(c, row, v, best, token, logit);
 }
 
-constexpr int kGradPieces = 4;                          // pieces of a thread whose loads are in flight together
+// Pieces of a thread a turn.  fp32 loads of all of them are in flight together; bf16 ones, which load_piece widens behind each load, one at a time.
+constexpr int kGradPieces = 4;
 template <typename T>
 __global__ __launch_bounds__(kThreads) void grad_kernel(LogprobGradCall c) {
   const int row = blockIdx.x / c.splits, split = blockIdx.x % c.splits;
