@@ -7,7 +7,7 @@
 // that of the unrounded sum.  A thread has one piece of eight columns (two beyond 8192 columns, and what is beyond 16384 is read a
 // second time): all of a row's pieces are asked for at once, a wavefront's are whole lines, and the 16 lanes of a group of 128 columns
 // lie next to each other, so that its maximum takes four steps over lanes and no LDS.
-// Bound: HBM for many rows (16384 x 3584 bf16 with residual into 8 bits: 413 MB in 76 to 77 us, 5.4 TB/s; a copy of 1 GiB reaches 5.05), latency for few
+// Bound: HBM for many rows (16384 x 3584 bf16 with residual into 8 bits: 413 MB in 75 to 77 us, 5.4 to 5.5 TB/s; a copy of 1 GiB reaches 5.05), latency for few
 // (one row of 4096: 4 us, the kernel 2.9): x, in bf16 the residual behind it (each is widened as it arrives), and the weight behind the sum.
 // With 64 threads a row and eight pieces each, weights kept over several rows, the same call took 134 us, with 256 threads and two pieces 90
 // (both with plain accesses); several rows to a workgroup one after the other are slower in every shape.
@@ -95,19 +95,22 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_kernel(NormCall c) {
         float most = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(f[i]));
-#pragma unroll
-        for (int m = 1; m < 16; m <<= 1) most = fmaxf(most, __shfl_xor(most, m));
+        most = fmaxf(most, from_lane<0x128, 0xf>(0.f, most));          // row_ror:8, 4, 2, 1
+        most = fmaxf(most, from_lane<0x124, 0xf>(0.f, most));
+        most = fmaxf(most, from_lane<0x122, 0xf>(0.f, most));
+        most = fmaxf(most, from_lane<0x121, 0xf>(0.f, most));
         const float scale = fmaxf(most / kE4m3Max, kLeastScale);
         if (col < c.cols) {
-          // The quotient: a product with the reciprocal is off by up to two roundings, which its remainder takes back (two instructions a value
-          // instead of a division's ten; 16384 x 3584 74.7 us without them, 76.1 with them).  Under an infinite scale there is no
-          // remainder: 0, and NaN of an infinity.
-          const float inverse = 1.f / scale, divisor = scale < INFINITY ? scale : 0.f;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float q = f[i] * inverse;
-            f[i] = __builtin_fmaf(-__builtin_fmaf(q, divisor, -f[i]), inverse, q);      // (in these signs -0 stays -0)
+          // The quotient, as a product with the reciprocal in two parts (the second is what the first leaves of 1 / scale, and not negative, so
+          // that -0 stays -0): rounded once, where the rounded reciprocal alone puts two roundings next to a tie.
+          float inverse = 1.f / scale, left = __builtin_fmaf(-inverse, scale, 1.f);
+          if (left < 0.f) {
+            inverse = __uint_as_float(__float_as_uint(inverse) - 1);
+            left = __builtin_fmaf(-inverse, scale, 1.f);
           }
+          const float rest = scale < INFINITY ? left * inverse : 0.f;          // (an infinite scale: 0, and NaN of an infinity)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f[i] = __builtin_fmaf(f[i], inverse, f[i] * rest);
           store_e4m3(static_cast<uint8_t*>(c.out) + row * c.out_stride, col, c.cols, f);
           if ((t & 15) == 0) c.scales[(int64_t)(col / kGroup) * c.scale_stride + row] = scale;
         }
@@ -146,8 +149,8 @@ hipError_t launch_typed(const NormCall& c, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_norm(const NormCall& c, int dtype, bool out_e4m3, hipStream_t stream) {
-  // (us, plain accesses / non-temporal ones, bf16 with residual into 8 bits: 16384 x 3584 81.2 / 76.9; 8192 x 3584, which a
-  // cache holds, 43.9 / 40.5 by itself: not taken)
+  // (us, plain accesses / non-temporal ones, bf16 with residual into 8 bits: 16384 x 3584 80.4 / 76.4; 8192 x 3584, which a
+  // cache holds, 43.2 / 39.9 by itself: not taken)
   const int64_t bytes = dtype == RLKV_F32 ? 4 : 2;
   const bool through = c.rows * (int64_t)c.cols * (bytes * (1 + (c.residual != nullptr) + (c.sum_out != nullptr)) + (out_e4m3 ? 1 : bytes)) > kStreamBytes;
   auto launch = [&](auto x, auto e4m3) {
