@@ -6,6 +6,9 @@ import torch
 import paper_2510_08525_amd as rl
 
 
+NAMES = ["rms_norm", "quantize", "scaled_matmul", "token_logprobs", "token_logprobs_grad", "append_rotary", "rotary"]
+
+
 def _calls():
     x, w, v = torch.zeros(4, 256, requires_grad=True), torch.zeros(256), torch.zeros(4)
     plain = torch.zeros(4, 256)
@@ -21,13 +24,13 @@ def _calls():
     }
 
 
-@pytest.mark.parametrize("name", list(_calls()))
+@pytest.mark.parametrize("name", NAMES)
 def test_what_requires_a_gradient_is_refused(name):
     with pytest.raises(ValueError, match="requires a gradient"):
         _calls()[name]()
 
 
-@pytest.mark.parametrize("name", list(_calls()))
+@pytest.mark.parametrize("name", NAMES)
 def test_where_no_gradients_are_recorded_it_is_not(name):
     for mode in (torch.no_grad, torch.inference_mode):
         with mode():
