@@ -524,6 +524,56 @@ rlkv_status_t rlkv_token_logprobs_grad(const void* logits /* device */, int64_t 
                                        const float* grad_entropy /* device */, void* grad_logits /* device */, int64_t grad_stride,
                                        void* stream);
 
+/* ---- The policy's training loop: packed rollouts ----------------------------------------------------------------------------
+ * What a policy is updated with on sequences that stand one behind the other in one buffer: attention without a cache, and its way back.
+ * Rules as for the token-wise operators above: no handle, nothing kept or allocated, recordable, work on `stream` of the current device. */
+
+/* Rows of head_dim (128) values: head h of token t is at data + t * token_stride + h * head_stride, in elements.  Every row starts at a multiple of
+ * 16 bytes; strides are not negative.  A view of packed projections is one, and so is a tensor with the heads in front. */
+typedef struct {
+  void* data; /* device */
+  int64_t token_stride, head_stride;
+} rlkv_heads_t;
+
+/* The sequences and who sees what of them: sequence s has the tokens offsets[s] .. offsets[s + 1] - 1 (none, where they are equal).  The query at token i
+ * attends over the keys j <= i of its own sequence; under a local KV head (Sec. 3.1: constant initial sink tokens plus recent tokens)
+ * over those of them with j - offsets[s] < sink or i - j < recent. */
+typedef struct {
+  const int32_t* offsets;   /* device [n_seqs + 1], not decreasing, in 0 .. tokens; read when the call runs.  (Others name no sequences that make sense, but
+                               nothing outside the tensors is read or written.) */
+  int32_t n_seqs;           /* >= 0                                                                               */
+  int32_t tokens;           /* rows of the tensors; those of no sequence are not written                                     */
+  int32_t n_q_heads;        /* multiple of n_kv_heads; query head i reads KV head i / (n_q_heads / n_kv_heads); group at most 16 */
+  int32_t n_kv_heads;       /* at most 256; tokens * group is below 2^30                                             */
+  const uint8_t* full_mask; /* host [n_kv_heads], 1 = full, 0 = local; copied; NULL: all are full                   */
+  int32_t sink, recent;     /* sink >= 0; recent >= 1 where a head is local                                         */
+  float softmax_scale;      /* positive, finite                                                                     */
+} rlkv_packed_t;
+
+/* out = softmax(softmax_scale * q . K^T) V over the admitted keys, and lse = log sum exp of their scaled scores.
+ *   q, out : RLKV_BF16, [tokens][n_q_heads];  k, v : [tokens][n_kv_heads]
+ *   lse    : device, fp32, [n_q_heads][tokens], or NULL
+ * Scores, softmax and sums are fp32; the weights enter their product with V in bf16.  What is not admitted does not count, whatever it holds
+ * (infinities and NaN among it).  Equal calls give equal bits. */
+rlkv_status_t rlkv_packed_attention(const rlkv_packed_t* shape /* host */, const rlkv_heads_t* q /* host */,
+                                    const rlkv_heads_t* k /* host */, const rlkv_heads_t* v /* host */,
+                                    const rlkv_heads_t* out /* host */, float* lse /* device */, void* stream);
+
+/* The way back: gradients of q, k and v from that of out, with out and lse as the call above left them.  With w = exp(score - lse):
+ *     z[i][j] = w[i][j] (grad_out[i] . v[j] - grad_out[i] . out[i])
+ *     grad_q[i] = softmax_scale * sum_j z[i][j] k[j]    grad_k[j] = softmax_scale * sum_i z[i][j] q[i]    grad_v[j] = sum_i w[i][j] grad_out[i]
+ * grad_k and grad_v are summed over the group's query heads.  All tensors RLKV_BF16; w and z enter their products in bf16, sums are fp32, in a fixed
+ * order: equal calls give equal bits.  The outputs are none of the inputs.
+ *   workspace : device, 16-byte aligned, rlkv_packed_attention_grad_workspace bytes; its contents do not matter.  Calls that may overlap in time
+ *               need one each (graphs that are replayed at the same time among them). */
+size_t rlkv_packed_attention_grad_workspace(int32_t tokens, int32_t n_q_heads, int32_t n_kv_heads);
+rlkv_status_t rlkv_packed_attention_grad(const rlkv_packed_t* shape /* host */, const rlkv_heads_t* q /* host */,
+                                         const rlkv_heads_t* k /* host */, const rlkv_heads_t* v /* host */,
+                                         const rlkv_heads_t* out /* host */, const float* lse /* device */,
+                                         const rlkv_heads_t* grad_out /* host */, const rlkv_heads_t* grad_q /* host */,
+                                         const rlkv_heads_t* grad_k /* host */, const rlkv_heads_t* grad_v /* host */,
+                                         void* workspace /* device */, size_t workspace_bytes, void* stream);
+
 /* Measurement aid, independent of any cache: one plain streaming read of `bytes` (rounded down to
  * whole 16 KiB blocks) of `buf` with 128-bit non-temporal loads and no arithmetic, launched with
  * `workgroups` workgroups of 256 threads on `stream` of the current device.  Timed by the caller,

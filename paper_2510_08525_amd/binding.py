@@ -43,6 +43,20 @@ class _Rotary(ctypes.Structure):
     _fields_ = [("inv_freq", ctypes.c_void_p), ("n_pairs", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
 
 
+class Heads(ctypes.Structure):
+    """rlkv_heads_t: address, element strides of tokens and heads."""
+
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class Packed(ctypes.Structure):
+    """rlkv_packed_t."""
+
+    _fields_ = [("offsets", ctypes.c_void_p), ("n_seqs", ctypes.c_int32), ("tokens", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("full_mask", ctypes.c_void_p), ("sink", ctypes.c_int32), ("recent", ctypes.c_int32),
+                ("softmax_scale", ctypes.c_float)]
+
+
 class Rotary:
     """How queries and keys turn with their positions (rlkv_rotary_t): radians a position of each pair of columns.  They are copied and stay
     as they are: the library reads them at `address` in every call."""
@@ -123,6 +137,9 @@ def load_library():
         "rlkv_token_logprobs_workspace": (sz, [i32, i32, i32]),
         "rlkv_token_logprobs": (i32, [vp, i64, i32, i32, i32, f32, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]),
         "rlkv_token_logprobs_grad": (i32, [vp, i64, i32, i32, i32, f32, vp, vp, vp, vp, vp, vp, i64, vp]),
+        "rlkv_packed_attention": (i32, [vp] * 7),
+        "rlkv_packed_attention_grad_workspace": (sz, [i32, i32, i32]),
+        "rlkv_packed_attention_grad": (i32, [vp] * 11 + [sz, vp]),
         "rlkv_status_string": (ctypes.c_char_p, [i32]),
     }
     for name, (res, args) in sigs.items():
@@ -156,6 +173,7 @@ EXPORTED_SYMBOLS = (
     "rlkv_pool_shuffle", "rlkv_status_string",
     "rlkv_append_rotary", "rlkv_rotary", "rlkv_rms_norm", "rlkv_quantize", "rlkv_scaled_matmul", "rlkv_plan_matmul",
     "rlkv_token_logprobs_workspace", "rlkv_token_logprobs", "rlkv_token_logprobs_grad",
+    "rlkv_packed_attention", "rlkv_packed_attention_grad_workspace", "rlkv_packed_attention_grad",
 )
 
 
@@ -306,6 +324,11 @@ def rlkv_resident_bytes(handle: int) -> int:
 def rlkv_token_logprobs_workspace(rows: int, vocab: int, top: int = 0) -> int:
     """Bytes of workspace a token_logprobs call of these sizes needs (0: none)."""
     return int(load_library().rlkv_token_logprobs_workspace(rows, vocab, top))
+
+
+def rlkv_packed_attention_grad_workspace(tokens: int, n_q_heads: int, n_kv_heads: int) -> int:
+    """Bytes of workspace a packed_attention_grad call of these sizes needs."""
+    return int(load_library().rlkv_packed_attention_grad_workspace(tokens, n_q_heads, n_kv_heads))
 
 
 def rlkv_probe_stream_read(buf_ptr: int, nbytes: int, sink_ptr: int, workgroups: int, stream: int = 0):

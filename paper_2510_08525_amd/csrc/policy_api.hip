@@ -1,0 +1,112 @@
+// Entry points of the policy's training loop: argument checks, all of them before the first HIP call.
+#include <math.h>
+
+#include "packed_attention.h"
+
+using namespace rlkv;
+
+namespace {
+
+hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
+bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+
+constexpr int64_t kMostStride = (int64_t)1 << 40;          // (a row's address is far from 64 bits)
+
+// Rows that the call reads: they may repeat, but not run backwards.
+bool readable(const rlkv_heads_t* t, size_t bytes) {
+  const int64_t row = 16 / (int64_t)bytes;
+  return t && t->data && aligned(t->data, 16) && t->token_stride >= 0 && t->head_stride >= 0 && t->token_stride <= kMostStride &&
+         t->head_stride <= kMostStride && t->token_stride % row == 0 && t->head_stride % row == 0;
+}
+// Rows that it writes: apart from each other, either heads within a token or tokens within a head.
+bool writable(const rlkv_heads_t* t, size_t bytes, int64_t tokens, int64_t heads) {
+  if (!readable(t, bytes)) return false;
+  const int64_t token = t->token_stride, head = t->head_stride;
+  const bool heads_inside = (heads <= 1 || head >= kHeadDim) && (tokens <= 1 || token >= (heads - 1) * head + kHeadDim);
+  const bool tokens_inside = (tokens <= 1 || token >= kHeadDim) && (heads <= 1 || head >= (tokens - 1) * token + kHeadDim);
+  return heads_inside || tokens_inside;
+}
+HeadRows rows_of(const rlkv_heads_t* t) { return {static_cast<uint16_t*>(t->data), t->token_stride, t->head_stride}; }
+
+bool heads_valid(int32_t tokens, int32_t n_q_heads, int32_t n_kv_heads) {
+  if (tokens < 0 || n_kv_heads < 1 || n_kv_heads > kPackedHeads || n_q_heads < 1 || n_q_heads % n_kv_heads != 0) return false;
+  const int group = n_q_heads / n_kv_heads;
+  return group <= kMaxGroup && (int64_t)tokens * group < ((int64_t)1 << 30);
+}
+bool packed_valid(const rlkv_packed_t* s) {
+  if (!s || !heads_valid(s->tokens, s->n_q_heads, s->n_kv_heads)) return false;
+  if (s->n_seqs < 0 || s->n_seqs == INT32_MAX || s->sink < 0) return false;
+  if (!(s->softmax_scale > 0.f) || isinf(s->softmax_scale)) return false;
+  for (int h = 0; s->full_mask && h < s->n_kv_heads; ++h)
+    if (s->full_mask[h] > 1 || (s->full_mask[h] == 0 && s->recent < 1)) return false;
+  return true;
+}
+PackedCall packed_call(const rlkv_packed_t* s) {
+  PackedCall c = {};
+  c.offsets = s->offsets;
+  c.n_seqs = s->n_seqs;
+  c.tokens = s->tokens;
+  c.n_q_heads = s->n_q_heads;
+  c.n_kv_heads = s->n_kv_heads;
+  c.group = s->n_q_heads / s->n_kv_heads;
+  c.sink = s->sink;
+  c.recent = s->recent;
+  c.scale = s->softmax_scale;
+  for (int h = 0; h < s->n_kv_heads; ++h)
+    if (!s->full_mask || s->full_mask[h]) c.full[h >> 6] |= (uint64_t)1 << (h & 63);
+  return c;
+}
+
+}  // namespace
+
+extern "C" {
+
+rlkv_status_t rlkv_packed_attention(const rlkv_packed_t* shape, const rlkv_heads_t* q, const rlkv_heads_t* k, const rlkv_heads_t* v,
+                                    const rlkv_heads_t* out, float* lse, void* stream) {
+  if (!packed_valid(shape)) return RLKV_ERR_INVALID_ARG;
+  if (shape->tokens == 0 || shape->n_seqs == 0) return RLKV_OK;
+  if (!shape->offsets || !aligned(shape->offsets, 4) || !aligned(lse, 4)) return RLKV_ERR_INVALID_ARG;
+  if (!readable(q, 2) || !readable(k, 2) || !readable(v, 2)) return RLKV_ERR_INVALID_ARG;
+  if (!writable(out, 2, shape->tokens, shape->n_q_heads)) return RLKV_ERR_INVALID_ARG;
+  PackedCall c = packed_call(shape);
+  c.q = rows_of(q);
+  c.k = rows_of(k);
+  c.v = rows_of(v);
+  c.out = rows_of(out);
+  c.lse = lse;
+  return launch_packed_attention(c, as_stream(stream)) == hipSuccess ? RLKV_OK : RLKV_ERR_HIP;
+}
+
+size_t rlkv_packed_attention_grad_workspace(int32_t tokens, int32_t n_q_heads, int32_t n_kv_heads) {
+  if (tokens < 1 || !heads_valid(tokens, n_q_heads, n_kv_heads)) return 0;
+  return packed_grad_workspace(tokens, n_q_heads, n_kv_heads);
+}
+
+rlkv_status_t rlkv_packed_attention_grad(const rlkv_packed_t* shape, const rlkv_heads_t* q, const rlkv_heads_t* k, const rlkv_heads_t* v,
+                                         const rlkv_heads_t* out, const float* lse, const rlkv_heads_t* grad_out,
+                                         const rlkv_heads_t* grad_q, const rlkv_heads_t* grad_k, const rlkv_heads_t* grad_v,
+                                         void* workspace, size_t workspace_bytes, void* stream) {
+  if (!packed_valid(shape)) return RLKV_ERR_INVALID_ARG;
+  if (shape->tokens == 0 || shape->n_seqs == 0) return RLKV_OK;
+  if (!shape->offsets || !aligned(shape->offsets, 4) || !lse || !aligned(lse, 4)) return RLKV_ERR_INVALID_ARG;
+  if (!readable(q, 2) || !readable(k, 2) || !readable(v, 2) || !readable(out, 2) || !readable(grad_out, 2)) return RLKV_ERR_INVALID_ARG;
+  if (!writable(grad_q, 2, shape->tokens, shape->n_q_heads) || !writable(grad_k, 2, shape->tokens, shape->n_kv_heads) ||
+      !writable(grad_v, 2, shape->tokens, shape->n_kv_heads))
+    return RLKV_ERR_INVALID_ARG;
+  if (!workspace || !aligned(workspace, 16) || workspace_bytes < packed_grad_workspace(shape->tokens, shape->n_q_heads, shape->n_kv_heads))
+    return RLKV_ERR_INVALID_ARG;
+  PackedCall c = packed_call(shape);
+  c.q = rows_of(q);
+  c.k = rows_of(k);
+  c.v = rows_of(v);
+  c.out = rows_of(out);
+  c.lse = const_cast<float*>(lse);
+  c.grad_out = rows_of(grad_out);
+  c.grad_q = rows_of(grad_q);
+  c.grad_k = rows_of(grad_k);
+  c.grad_v = rows_of(grad_v);
+  c.workspace = workspace;
+  return launch_packed_attention_grad(c, as_stream(stream)) == hipSuccess ? RLKV_OK : RLKV_ERR_HIP;
+}
+
+}  // extern "C"

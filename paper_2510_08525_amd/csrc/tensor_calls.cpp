@@ -113,6 +113,13 @@ bool matrix(PyObject* o, const char* what, int index, ScalarType type, int64_t r
   const at::Tensor& t = THPVariable_Unpack(o);
   return of_type(t, what, type) && of_size(t, what, 0, m->rows, rows) && of_size(t, what, 1, m->cols, cols);
 }
+// The same without a gap between rows.
+bool matrix_whole(PyObject* o, const char* what, int index, ScalarType type, int64_t rows, int64_t cols, Matrix* m) {
+  if (!matrix(o, what, index, type, rows, cols, m)) return false;
+  if (rows <= 1 || cols == 0 || m->stride == cols) return true;
+  PyErr_Format(PyExc_ValueError, "%s: need a contiguous tensor", what);
+  return false;
+}
 // fp32 or bf16: activations and logits
 bool activations(PyObject* o, const char* what, Matrix* m) {
   if (!any_matrix(o, what, -1, m)) return false;
@@ -394,6 +401,105 @@ PyObject* rotary_split(PyObject*, PyObject* const* a, Py_ssize_t n) {
   RLKV_CALL_END
 }
 
+// ---- calls on packed sequences -----------------------------------------------------------------------------------------------------------
+// [tokens, heads, head_dim] at any strides of tokens and heads; tokens and heads below 0: any.
+bool head_rows(PyObject* o, const char* what, int index, ScalarType type, int64_t tokens, int64_t heads, rlkv_heads_t* r) {
+  const at::Tensor* t = tensor(o, what);
+  if (!t || !on_device(*t, what, index) || !of_type(*t, what, type)) return false;
+  if (t->dim() != 3 || t->stride(2) != 1) {
+    PyErr_Format(PyExc_ValueError, "%s: need [tokens, heads, head_dim] with contiguous rows", what);
+    return false;
+  }
+  if ((tokens >= 0 && !of_size(*t, what, 0, t->size(0), tokens)) || (heads >= 0 && !of_size(*t, what, 1, t->size(1), heads)) ||
+      !of_size(*t, what, 2, t->size(2), 128) || !fits(t->size(0), what) || !fits(t->size(1), what))
+    return false;
+  r->data = t->data_ptr();
+  r->token_stride = t->size(0) > 1 ? t->stride(0) : 0;          // (the stride of an axis of one, which a tensor may report as anything)
+  r->head_stride = t->size(1) > 1 ? t->stride(1) : 0;
+  return true;
+}
+bool integer(PyObject* o, const char* what, int32_t* v) {
+  int beyond = 0;
+  const long x = PyLong_AsLongAndOverflow(o, &beyond);
+  if (PyErr_Occurred()) return false;
+  *v = (int32_t)x;
+  if (!beyond && *v == x) return true;
+  PyErr_Format(PyExc_ValueError, "%s: %R is out of range", what, o);
+  return false;
+}
+// q, k, v, offsets; scale, mask (bytes or None), sink, recent
+bool packed_shape(PyObject* const* qkv, PyObject* const* how, rlkv_heads_t* q, rlkv_heads_t* k, rlkv_heads_t* v, rlkv_packed_t* s, int* index) {
+  const ScalarType bf16 = ScalarType::BFloat16;
+  if (!head_rows(qkv[0], "q", -1, bf16, -1, -1, q)) return false;
+  const at::Tensor& t = THPVariable_Unpack(qkv[0]);
+  *index = t.get_device();
+  if (!head_rows(qkv[1], "k", *index, bf16, t.size(0), -1, k)) return false;
+  const at::Tensor& u = THPVariable_Unpack(qkv[1]);
+  if (!head_rows(qkv[2], "v", *index, bf16, t.size(0), u.size(1), v)) return false;
+  const at::Tensor* at = tensor(qkv[3], "offsets");
+  void* offsets;
+  if (!at || !vector(qkv[3], "offsets", *index, ScalarType::Int, at->numel(), &offsets) || !fits(at->numel(), "offsets")) return false;
+  if (at->numel() < 1) {
+    PyErr_SetString(PyExc_ValueError, "offsets: need one more than there are sequences");
+    return false;
+  }
+  *s = {};
+  s->offsets = static_cast<int32_t*>(offsets);
+  s->n_seqs = (int32_t)(at->numel() - 1);
+  s->tokens = (int32_t)t.size(0);
+  s->n_q_heads = (int32_t)t.size(1);
+  s->n_kv_heads = (int32_t)u.size(1);
+  if (how[1] != Py_None) {
+    if (!PyBytes_Check(how[1]) || PyBytes_GET_SIZE(how[1]) != u.size(1)) {
+      PyErr_SetString(PyExc_ValueError, "mask: need a 0 or 1 for each KV head");
+      return false;
+    }
+    s->full_mask = reinterpret_cast<const uint8_t*>(PyBytes_AS_STRING(how[1]));
+  }
+  return number(how[0], &s->softmax_scale) && integer(how[2], "sink", &s->sink) && integer(how[3], "recent", &s->recent);
+}
+
+// q, k, v, offsets, out, lse, scale, mask, sink, recent
+PyObject* packed_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  RLKV_CALL_BEGIN
+  rlkv_heads_t q, k, v, out;
+  rlkv_packed_t s;
+  Matrix lse;
+  int index;
+  if (!arguments(n, 10) || !packed_shape(a, a + 6, &q, &k, &v, &s, &index)) return nullptr;
+  if (!head_rows(a[4], "out", index, ScalarType::BFloat16, s.tokens, s.n_q_heads, &out)) return nullptr;
+  if (a[5] != Py_None && !matrix_whole(a[5], "lse", index, ScalarType::Float, s.n_q_heads, s.tokens, &lse)) return nullptr;
+  const OnDevice on(index);
+  return status_of({a[4], a[5]}, [&] { return rlkv_packed_attention(&s, &q, &k, &v, &out, static_cast<float*>(lse.p), on.stream()); });
+  RLKV_CALL_END
+}
+
+// q, k, v, offsets, out, lse, grad_out, grad_q, grad_k, grad_v, scale, mask, sink, recent, workspace
+PyObject* packed_attention_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  RLKV_CALL_BEGIN
+  rlkv_heads_t q, k, v, out, g, gq, gk, gv;
+  rlkv_packed_t s;
+  Matrix lse;
+  int index;
+  void* workspace;
+  const ScalarType bf16 = ScalarType::BFloat16;
+  if (!arguments(n, 15) || !packed_shape(a, a + 10, &q, &k, &v, &s, &index)) return nullptr;
+  if (!head_rows(a[4], "out", index, bf16, s.tokens, s.n_q_heads, &out)) return nullptr;
+  if (!matrix_whole(a[5], "lse", index, ScalarType::Float, s.n_q_heads, s.tokens, &lse)) return nullptr;
+  if (!head_rows(a[6], "grad_out", index, bf16, s.tokens, s.n_q_heads, &g)) return nullptr;
+  if (!head_rows(a[7], "grad_q", index, bf16, s.tokens, s.n_q_heads, &gq)) return nullptr;
+  if (!head_rows(a[8], "grad_k", index, bf16, s.tokens, s.n_kv_heads, &gk)) return nullptr;
+  if (!head_rows(a[9], "grad_v", index, bf16, s.tokens, s.n_kv_heads, &gv)) return nullptr;
+  const at::Tensor* w = tensor(a[14], "workspace");
+  if (!w || !vector(a[14], "workspace", index, ScalarType::Byte, w->numel(), &workspace)) return nullptr;
+  const OnDevice on(index);
+  return status_of({a[7], a[8], a[9]}, [&] {
+    return rlkv_packed_attention_grad(&s, &q, &k, &v, &out, static_cast<float*>(lse.p), &g, &gq, &gk, &gv, workspace,
+                                      static_cast<size_t>(w->numel()), on.stream());
+  });
+  RLKV_CALL_END
+}
+
 #define RLKV_METHOD(name, function) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(function)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {RLKV_METHOD("rms_norm", rms_norm),
                          RLKV_METHOD("quantize", quantize),
@@ -402,6 +508,8 @@ PyMethodDef methods[] = {RLKV_METHOD("rms_norm", rms_norm),
                          RLKV_METHOD("token_logprobs_grad", token_logprobs_grad),
                          RLKV_METHOD("append_rotary", append_rotary),
                          RLKV_METHOD("rotary", rotary_split),
+                         RLKV_METHOD("packed_attention", packed_attention),
+                         RLKV_METHOD("packed_attention_grad", packed_attention_grad),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef definition = {PyModuleDef_HEAD_INIT, "_tensor_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,9 +1,11 @@
-"""The token-wise operators on tensors, around the calls of include/rlkv.h (checks and marshalling: csrc/tensor_calls.cpp).
+"""The token-wise operators and those of packed sequences on tensors, around the calls of include/rlkv.h (checks and marshalling:
+csrc/tensor_calls.cpp).
 
 Outputs are the caller's tensors; every call goes to the current stream of the tensors' device and returns its outputs.
 Matrices are two-dimensional with contiguous columns, rows at any stride.  What is wrong with a tensor raises ValueError, what the library
 refuses RlkvError.  Autograd does not see the calls: as with torch's own calls into given outputs, a tensor that requires a gradient is
-refused unless under torch.no_grad(), and what is written counts as changed in place (`token_logprobs_grad` is the way back).
+refused unless under torch.no_grad(), and what is written counts as changed in place (`token_logprobs_grad` and
+`packed_attention_grad` are the ways back).
 """
 from __future__ import annotations
 
@@ -73,3 +75,33 @@ def token_logprobs_grad(logits, tokens, lse, grad_logprobs, grad_logits, *, scal
     if status:
         _check(status, "rlkv_token_logprobs_grad")
     return grad_logits
+
+
+def packed_attention(q, k, v, offsets, out, scale: float, *, lse=None, mask=None, sink: int = 0, recent: int = 0):
+    """Attention over sequences packed one behind the other, q and out [tokens, q heads, 128], k and v [tokens, kv heads, 128] in bfloat16
+    (heads and tokens at any stride, rows at multiples of 16 bytes): out = softmax(scale * q . k) v over the keys up to the query's own, and
+    lse [q heads, tokens] (float32) the log-sum-exp of the scores (rlkv_packed_attention).
+
+    offsets: int32 [sequences + 1] on the device, where the sequences begin and the last one ends; rows of none are not written.
+    mask: one 0 / 1 for each KV head, 1 = full, 0 = local (the first `sink` positions of the sequence and the last `recent`); None: all full."""
+    status = _calls.packed_attention(q, k, v, offsets, out, lse, scale, None if mask is None else bytes(mask), sink, recent)
+    if status:
+        _check(status, "rlkv_packed_attention")
+    return out
+
+
+def packed_attention_grad(q, k, v, offsets, out, lse, grad_out, grad_q, grad_k, grad_v, scale: float, *, mask=None, sink: int = 0,
+                          recent: int = 0, workspace=None):
+    """Gradients of packed_attention's q, k and v from that of its out; out and lse as it left them (rlkv_packed_attention_grad).
+
+    workspace: a uint8 tensor of rlkv_packed_attention_grad_workspace(tokens, q heads, kv heads) bytes that the caller keeps; without one the
+    call takes one from torch's allocator."""
+    if workspace is None:
+        tokens, q_heads, kv_heads = (*q.shape[:2], k.shape[1]) if q.dim() == 3 and k.dim() == 3 else (0, 1, 1)
+        need = load_library().rlkv_packed_attention_grad_workspace(tokens, q_heads, kv_heads)
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
+    status = _calls.packed_attention_grad(q, k, v, offsets, out, lse, grad_out, grad_q, grad_k, grad_v, scale,
+                                          None if mask is None else bytes(mask), sink, recent, workspace)
+    if status:
+        _check(status, "rlkv_packed_attention_grad")
+    return grad_q, grad_k, grad_v
