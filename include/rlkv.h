@@ -574,6 +574,42 @@ rlkv_status_t rlkv_packed_attention_grad(const rlkv_packed_t* shape /* host */, 
                                          const rlkv_heads_t* grad_k /* host */, const rlkv_heads_t* grad_v /* host */,
                                          void* workspace /* device */, size_t workspace_bytes, void* stream);
 
+/* Queries and keys from packed projections, as the attention above (and rlkv_append_decode, for one token a sequence) takes them: root-mean-square norm of
+ * every query and key head over its 128 columns, then the rotation by the token's position (rlkv_rotary_t), in one pass:
+ *     y = R(x / sqrt(mean(x^2) + eps) * weight)
+ *   qkv       : device, `dtype` (RLKV_F32 or RLKV_BF16): a token's query heads, key heads, value heads in a row of (n_q_heads + 2 n_kv_heads) * 128, rows
+ *               token_stride (at least that) apart, aligned to an element
+ *   positions : device, int32 [tokens], of any sign; NULL without a rotation
+ *   rotary    : host, or NULL: no rotation;   norm : host, or NULL: no norm
+ *   q_out, k_out, v_out : `dtype`; v_out (values, as they are) may be NULL.  Each may be the very rows of qkv that it is made of
+ * tokens * (n_q_heads + 2 n_kv_heads) is below 2^29, either number of heads at most 65536.  fp32 inside, outputs are rounded once. */
+typedef struct {
+  const void *q_weight, *k_weight; /* device, `dtype` [128], or NULL: ones */
+  float eps;                       /* finite, not negative                 */
+} rlkv_head_norm_t;
+rlkv_status_t rlkv_head_norm_rotary(const void* qkv /* device */, int64_t token_stride, const int32_t* positions /* device */,
+                                    const rlkv_rotary_t* rotary /* host */, const rlkv_head_norm_t* norm /* host */, int32_t tokens,
+                                    int32_t n_q_heads, int32_t n_kv_heads, int32_t dtype, const rlkv_heads_t* q_out /* host */,
+                                    const rlkv_heads_t* k_out /* host */, const rlkv_heads_t* v_out /* host */, void* stream);
+
+/* The way back, from the gradients of q_out and k_out (and v_out) to those of qkv and of the weights.  With u = x / sqrt(mean(x^2) + eps) and
+ * g = R^-1(grad_y):
+ *     grad_x = (g weight - u mean(g weight u)) / sqrt(mean(x^2) + eps)        grad_weight = sum over tokens and heads of g u
+ *   grad_v   : NULL: the values' columns of grad_qkv are not written (rlkv_packed_attention_grad can leave its grad_v there)
+ *   grad_qkv : device, `dtype`, rows grad_stride apart; the rows of grad_q, grad_k, grad_v may be its very own
+ *   grad_q_weight, grad_k_weight : device, fp32 [128], each may be NULL (both are, without a norm); written, not added to; 0 without tokens
+ *   workspace: device, 16-byte aligned, rlkv_head_norm_rotary_grad_workspace bytes, where a weight's gradient is wanted; its contents do not
+ *              matter.  Calls that may overlap in time need one each.
+ * Sums are fp32 over up to some hundred rows, then 64 bits, in a fixed order: equal calls give equal bits. */
+size_t rlkv_head_norm_rotary_grad_workspace(int32_t tokens, int32_t n_q_heads, int32_t n_kv_heads);
+rlkv_status_t rlkv_head_norm_rotary_grad(const void* qkv /* device */, int64_t token_stride, const int32_t* positions /* device */,
+                                         const rlkv_rotary_t* rotary /* host */, const rlkv_head_norm_t* norm /* host */, int32_t tokens,
+                                         int32_t n_q_heads, int32_t n_kv_heads, int32_t dtype, const rlkv_heads_t* grad_q /* host */,
+                                         const rlkv_heads_t* grad_k /* host */, const rlkv_heads_t* grad_v /* host */,
+                                         void* grad_qkv /* device */, int64_t grad_stride, float* grad_q_weight /* device */,
+                                         float* grad_k_weight /* device */, void* workspace /* device */, size_t workspace_bytes,
+                                         void* stream);
+
 /* Measurement aid, independent of any cache: one plain streaming read of `bytes` (rounded down to
  * whole 16 KiB blocks) of `buf` with 128-bit non-temporal loads and no arithmetic, launched with
  * `workgroups` workgroups of 256 threads on `stream` of the current device.  Timed by the caller,

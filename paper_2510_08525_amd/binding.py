@@ -49,6 +49,12 @@ class Heads(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
+class HeadNorm(ctypes.Structure):
+    """rlkv_head_norm_t."""
+
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float)]
+
+
 class Packed(ctypes.Structure):
     """rlkv_packed_t."""
 
@@ -140,6 +146,9 @@ def load_library():
         "rlkv_packed_attention": (i32, [vp] * 7),
         "rlkv_packed_attention_grad_workspace": (sz, [i32, i32, i32]),
         "rlkv_packed_attention_grad": (i32, [vp] * 11 + [sz, vp]),
+        "rlkv_head_norm_rotary": (i32, [vp, i64, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp]),
+        "rlkv_head_norm_rotary_grad_workspace": (sz, [i32, i32, i32]),
+        "rlkv_head_norm_rotary_grad": (i32, [vp, i64, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]),
         "rlkv_status_string": (ctypes.c_char_p, [i32]),
     }
     for name, (res, args) in sigs.items():
@@ -174,6 +183,7 @@ EXPORTED_SYMBOLS = (
     "rlkv_append_rotary", "rlkv_rotary", "rlkv_rms_norm", "rlkv_quantize", "rlkv_scaled_matmul", "rlkv_plan_matmul",
     "rlkv_token_logprobs_workspace", "rlkv_token_logprobs", "rlkv_token_logprobs_grad",
     "rlkv_packed_attention", "rlkv_packed_attention_grad_workspace", "rlkv_packed_attention_grad",
+    "rlkv_head_norm_rotary", "rlkv_head_norm_rotary_grad_workspace", "rlkv_head_norm_rotary_grad",
 )
 
 
@@ -329,6 +339,11 @@ def rlkv_token_logprobs_workspace(rows: int, vocab: int, top: int = 0) -> int:
 def rlkv_packed_attention_grad_workspace(tokens: int, n_q_heads: int, n_kv_heads: int) -> int:
     """Bytes of workspace a packed_attention_grad call of these sizes needs."""
     return int(load_library().rlkv_packed_attention_grad_workspace(tokens, n_q_heads, n_kv_heads))
+
+
+def rlkv_head_norm_rotary_grad_workspace(tokens: int, n_q_heads: int, n_kv_heads: int) -> int:
+    """Bytes of workspace a head_norm_rotary_grad call of these sizes needs for the gradients of weights."""
+    return int(load_library().rlkv_head_norm_rotary_grad_workspace(tokens, n_q_heads, n_kv_heads))
 
 
 def rlkv_probe_stream_read(buf_ptr: int, nbytes: int, sink_ptr: int, workgroups: int, stream: int = 0):

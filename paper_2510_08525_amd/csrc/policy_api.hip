@@ -1,6 +1,7 @@
 // Entry points of the policy's training loop: argument checks, all of them before the first HIP call.
 #include <math.h>
 
+#include "head_norm_rotary.h"
 #include "packed_attention.h"
 
 using namespace rlkv;
@@ -57,9 +58,96 @@ PackedCall packed_call(const rlkv_packed_t* s) {
   return c;
 }
 
+TokenHeads token_heads(const rlkv_heads_t* t) { return {t->data, t->token_stride, t->head_stride}; }
+constexpr int32_t kMostHeads = 1 << 16;
+bool head_norm_valid(int32_t tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t dtype) {
+  if (dtype != RLKV_F32 && dtype != RLKV_BF16) return false;
+  if (tokens < 0 || n_q_heads < 1 || n_kv_heads < 1 || n_q_heads > kMostHeads || n_kv_heads > kMostHeads) return false;
+  return (int64_t)tokens * (n_q_heads + 2 * (int64_t)n_kv_heads) < ((int64_t)1 << 29);      // (eight threads a row, below 2^32)
+}
+// What both directions have: false where it is wrong.
+bool head_norm_call(HeadNormCall* c, RotaryTurns* turns, const void* qkv, int64_t token_stride, const int32_t* positions,
+                    const rlkv_rotary_t* rotary, const rlkv_head_norm_t* norm, int32_t tokens, int32_t n_q_heads, int32_t n_kv_heads,
+                    int32_t dtype) {
+  if (!head_norm_valid(tokens, n_q_heads, n_kv_heads, dtype)) return false;
+  *c = {};
+  *turns = {};
+  if (rotary && (!turns_of(rotary, turns) || (tokens > 0 && !positions) || !aligned(positions, 4))) return false;
+  const size_t e = dtype == RLKV_F32 ? 4 : 2;
+  if (norm) {
+    if (!(norm->eps >= 0.f) || isinf(norm->eps) || !aligned(norm->q_weight, e) || !aligned(norm->k_weight, e)) return false;
+    c->norm = 1;
+    c->eps = norm->eps;
+    c->q_weight = norm->q_weight;
+    c->k_weight = norm->k_weight;
+  }
+  const int64_t width = (n_q_heads + 2 * (int64_t)n_kv_heads) * kHeadDim;
+  if (tokens > 0 && (!qkv || !aligned(qkv, e) || token_stride < width || token_stride > kMostStride)) return false;
+  c->qkv = qkv;
+  c->token_stride = token_stride;
+  c->positions = positions;
+  c->tokens = tokens;
+  c->n_q_heads = n_q_heads;
+  c->n_kv_heads = n_kv_heads;
+  return true;
+}
+
 }  // namespace
 
 extern "C" {
+
+rlkv_status_t rlkv_head_norm_rotary(const void* qkv, int64_t token_stride, const int32_t* positions, const rlkv_rotary_t* rotary,
+                                    const rlkv_head_norm_t* norm, int32_t tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t dtype,
+                                    const rlkv_heads_t* q_out, const rlkv_heads_t* k_out, const rlkv_heads_t* v_out, void* stream) {
+  HeadNormCall c;
+  RotaryTurns turns;
+  if (!head_norm_call(&c, &turns, qkv, token_stride, positions, rotary, norm, tokens, n_q_heads, n_kv_heads, dtype)) return RLKV_ERR_INVALID_ARG;
+  if (tokens == 0) return RLKV_OK;
+  const size_t e = dtype == RLKV_F32 ? 4 : 2;
+  if (!writable(q_out, e, tokens, n_q_heads) || !writable(k_out, e, tokens, n_kv_heads) || (v_out && !writable(v_out, e, tokens, n_kv_heads)))
+    return RLKV_ERR_INVALID_ARG;
+  c.q = token_heads(q_out);
+  c.k = token_heads(k_out);
+  if (v_out) c.v = token_heads(v_out);
+  return launch_head_norm_rotary(c, turns, dtype, as_stream(stream)) == hipSuccess ? RLKV_OK : RLKV_ERR_HIP;
+}
+
+size_t rlkv_head_norm_rotary_grad_workspace(int32_t tokens, int32_t n_q_heads, int32_t n_kv_heads) {
+  if (tokens < 1 || !head_norm_valid(tokens, n_q_heads, n_kv_heads, RLKV_F32)) return 0;
+  return head_norm_grad_workspace(tokens, n_q_heads, n_kv_heads);
+}
+
+rlkv_status_t rlkv_head_norm_rotary_grad(const void* qkv, int64_t token_stride, const int32_t* positions, const rlkv_rotary_t* rotary,
+                                         const rlkv_head_norm_t* norm, int32_t tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t dtype,
+                                         const rlkv_heads_t* grad_q, const rlkv_heads_t* grad_k, const rlkv_heads_t* grad_v, void* grad_qkv,
+                                         int64_t grad_stride, float* grad_q_weight, float* grad_k_weight, void* workspace,
+                                         size_t workspace_bytes, void* stream) {
+  HeadNormCall c;
+  RotaryTurns turns;
+  if (!head_norm_call(&c, &turns, qkv, token_stride, positions, rotary, norm, tokens, n_q_heads, n_kv_heads, dtype)) return RLKV_ERR_INVALID_ARG;
+  const bool sums = grad_q_weight || grad_k_weight;
+  if (sums && !norm) return RLKV_ERR_INVALID_ARG;
+  if (!aligned(grad_q_weight, 4) || !aligned(grad_k_weight, 4)) return RLKV_ERR_INVALID_ARG;
+  if (tokens == 0 && !sums) return RLKV_OK;
+  if (tokens > 0) {
+    const size_t e = dtype == RLKV_F32 ? 4 : 2;
+    if (!readable(grad_q, e) || !readable(grad_k, e) || (grad_v && !readable(grad_v, e))) return RLKV_ERR_INVALID_ARG;
+    if (!grad_qkv || !aligned(grad_qkv, e) || grad_stride > kMostStride ||
+        grad_stride < (n_q_heads + 2 * (int64_t)n_kv_heads) * kHeadDim)
+      return RLKV_ERR_INVALID_ARG;
+    if (sums && (!workspace || !aligned(workspace, 16) || workspace_bytes < head_norm_grad_workspace(tokens, n_q_heads, n_kv_heads)))
+      return RLKV_ERR_INVALID_ARG;
+    c.q = token_heads(grad_q);
+    c.k = token_heads(grad_k);
+    if (grad_v) c.v = token_heads(grad_v);
+  }
+  c.grad = grad_qkv;
+  c.grad_stride = grad_stride;
+  c.grad_q_weight = grad_q_weight;
+  c.grad_k_weight = grad_k_weight;
+  c.partials = static_cast<float*>(workspace);
+  return launch_head_norm_rotary_grad(c, turns, dtype, as_stream(stream)) == hipSuccess ? RLKV_OK : RLKV_ERR_HIP;
+}
 
 rlkv_status_t rlkv_packed_attention(const rlkv_packed_t* shape, const rlkv_heads_t* q, const rlkv_heads_t* k, const rlkv_heads_t* v,
                                     const rlkv_heads_t* out, float* lse, void* stream) {

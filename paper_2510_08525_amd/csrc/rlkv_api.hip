@@ -841,24 +841,13 @@ rlkv_status_t rlkv_prefill_attention(rlkv_cache_t* cache, int32_t layer, const v
 // The checks of the two rotating calls, and what their kernels get.
 static rlkv_status_t rotary_args(rlkv_cache_t* cache, int32_t layer, const void* qkv, int64_t token_stride, int32_t stride_tokens,
                                  const rlkv_rotary_t* rotary, RotaryArgs* args) {
-  if (!cache || !qkv || !rotary || !rotary->inv_freq) return RLKV_ERR_INVALID_ARG;
+  if (!cache || !qkv) return RLKV_ERR_INVALID_ARG;
   if (layer < 0 || layer >= cache->cfg.n_layers) return RLKV_ERR_INVALID_ARG;
-  const int pairs = rotary->n_pairs;
-  if (pairs < 8 || pairs > kHeadDim / 2 || pairs % 8 != 0) return RLKV_ERR_INVALID_ARG;
-  if (rotary->interleaved < 0 || rotary->interleaved > 1) return RLKV_ERR_INVALID_ARG;
+  *args = {};
+  if (!turns_of(rotary, &args->turns)) return RLKV_ERR_INVALID_ARG;
   const size_t e = cache->cfg.dtype == RLKV_F32 ? 4 : 2;
   if (stride_tokens < 1 || token_stride < (int64_t)(cache->cfg.n_q_heads + 2 * cache->cfg.n_kv_heads) * kHeadDim) return RLKV_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(qkv) % e != 0) return RLKV_ERR_INVALID_ARG;
-  *args = {};
-  for (int i = 0; i < pairs; ++i) {
-    if (!isfinite(rotary->inv_freq[i])) return RLKV_ERR_INVALID_ARG;
-    // (whole turns do not matter, and what is left is below 1 unless it was rounded up to it)
-    double t = rotary->inv_freq[i] * 0.15915494309189533577;          // 1 / (2 pi)
-    t -= floor(t);
-    args->turns.turn[i] = t < 1.0 ? (uint64_t)(t * 18446744073709551616.0) : 0;         // 2^64
-  }
-  args->turns.pairs = pairs;
-  args->turns.interleaved = rotary->interleaved;
   args->call.qkv = qkv;
   args->call.token_stride = token_stride;
   args->call.stride_tokens = stride_tokens;

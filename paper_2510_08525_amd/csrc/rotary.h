@@ -1,6 +1,8 @@
 // Rotation of queries and keys by their positions: what the host hands to the kernels of rotary.hip.
 #pragma once
 
+#include <math.h>
+
 #include "rlkv_internal.h"
 
 namespace rlkv {
@@ -12,6 +14,24 @@ struct RotaryTurns {
   int32_t pairs;                 // rotated columns / 2: a multiple of 8 (the columns past 2 * pairs stay as they are)
   int32_t interleaved;           // 1: pair i is columns 2 i and 2 i + 1; 0: columns i and i + pairs
 };
+// Those of a caller's frequencies; false where they are none.
+inline bool turns_of(const rlkv_rotary_t* rotary, RotaryTurns* turns) {
+  if (!rotary || !rotary->inv_freq) return false;
+  const int pairs = rotary->n_pairs;
+  if (pairs < 8 || pairs > kHeadDim / 2 || pairs % 8 != 0) return false;
+  if (rotary->interleaved < 0 || rotary->interleaved > 1) return false;
+  *turns = {};
+  for (int i = 0; i < pairs; ++i) {
+    if (!isfinite(rotary->inv_freq[i])) return false;
+    // (whole turns do not matter, and what is left is below 1 unless it was rounded up to it)
+    double t = rotary->inv_freq[i] * 0.15915494309189533577;          // 1 / (2 pi)
+    t -= floor(t);
+    turns->turn[i] = t < 1.0 ? (uint64_t)(t * 18446744073709551616.0) : 0;         // 2^64
+  }
+  turns->pairs = pairs;
+  turns->interleaved = rotary->interleaved;
+  return true;
+}
 struct RotaryCall {
   const void* qkv;               // [batch][stride_tokens] rows of token_stride elements: q heads, k heads, v heads of kHeadDim
   int64_t token_stride;

@@ -500,6 +500,82 @@ PyObject* packed_attention_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
   RLKV_CALL_END
 }
 
+// What both directions of the heads' norm have: qkv, positions, rotary (address or None), then the rows of queries, keys and (or None) values;
+// weights and eps (None: no norm).  The numbers of heads are those of the queries' and keys' rows.
+struct HeadNormShape {
+  Matrix qkv;
+  void *positions, *rotary;
+  rlkv_heads_t q, k, v;
+  bool values;
+  int32_t q_heads, kv_heads;
+  rlkv_head_norm_t norm;
+  bool normed;
+};
+bool head_norm_shape(PyObject* const* a, const char* const* names, PyObject* const* rows, PyObject* const* weights, HeadNormShape* s) {
+  if (!activations(a[0], "qkv", &s->qkv) || !fits(s->qkv.rows, "qkv") || !vector(a[1], "positions", s->qkv.device, ScalarType::Int, s->qkv.rows, &s->positions))
+    return false;
+  if (!address(a[2], &s->rotary)) return false;
+  const int at = s->qkv.device;
+  if (!head_rows(rows[0], names[0], at, s->qkv.type, s->qkv.rows, -1, &s->q) || !head_rows(rows[1], names[1], at, s->qkv.type, s->qkv.rows, -1, &s->k))
+    return false;
+  s->q_heads = (int32_t)THPVariable_Unpack(rows[0]).size(1);
+  s->kv_heads = (int32_t)THPVariable_Unpack(rows[1]).size(1);
+  s->values = rows[2] != Py_None;
+  if (s->values && !head_rows(rows[2], names[2], at, s->qkv.type, s->qkv.rows, s->kv_heads, &s->v)) return false;
+  if (!of_size(THPVariable_Unpack(a[0]), "qkv", 1, s->qkv.cols, 128 * (s->q_heads + 2 * (int64_t)s->kv_heads))) return false;
+  s->norm = {};
+  s->normed = weights[2] != Py_None;
+  void *wq, *wk;
+  if (!vector(weights[0], "q_weight", at, s->qkv.type, 128, &wq) || !vector(weights[1], "k_weight", at, s->qkv.type, 128, &wk)) return false;
+  if (!s->normed && (wq || wk)) {
+    PyErr_SetString(PyExc_ValueError, "eps: weights are those of a norm, which needs one");
+    return false;
+  }
+  s->norm.q_weight = wq;
+  s->norm.k_weight = wk;
+  return !s->normed || number(weights[2], &s->norm.eps);
+}
+
+// qkv, positions, rotary, q_out, k_out, v_out, q_weight, k_weight, eps
+PyObject* head_norm_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  RLKV_CALL_BEGIN
+  HeadNormShape s;
+  const char* names[] = {"q_out", "k_out", "v_out"};
+  if (!arguments(n, 9) || !head_norm_shape(a, names, a + 3, a + 6, &s)) return nullptr;
+  const OnDevice on(s.qkv.device);
+  return status_of({a[3], a[4], a[5]}, [&] {
+    return rlkv_head_norm_rotary(s.qkv.p, s.qkv.stride, static_cast<int32_t*>(s.positions), static_cast<rlkv_rotary_t*>(s.rotary),
+                                 s.normed ? &s.norm : nullptr, (int32_t)s.qkv.rows, s.q_heads, s.kv_heads, kind_of(s.qkv.type), &s.q, &s.k,
+                                 s.values ? &s.v : nullptr, on.stream());
+  });
+  RLKV_CALL_END
+}
+
+// qkv, positions, rotary, grad_q, grad_k, grad_qkv, grad_v, q_weight, k_weight, eps, grad_q_weight, grad_k_weight, workspace
+PyObject* head_norm_rotary_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  RLKV_CALL_BEGIN
+  HeadNormShape s;
+  Matrix grad;
+  void *gq, *gk, *workspace;
+  const char* names[] = {"grad_q", "grad_k", "grad_v"};
+  if (!arguments(n, 13)) return nullptr;
+  PyObject* const rows[] = {a[3], a[4], a[6]};
+  if (!head_norm_shape(a, names, rows, a + 7, &s)) return nullptr;
+  const int at = s.qkv.device;
+  if (!matrix(a[5], "grad_qkv", at, s.qkv.type, s.qkv.rows, s.qkv.cols, &grad)) return nullptr;
+  if (!vector(a[10], "grad_q_weight", at, ScalarType::Float, 128, &gq) || !vector(a[11], "grad_k_weight", at, ScalarType::Float, 128, &gk)) return nullptr;
+  const at::Tensor* w = tensor(a[12], "workspace");
+  if (!w || !vector(a[12], "workspace", at, ScalarType::Byte, w->numel(), &workspace)) return nullptr;
+  const OnDevice on(at);
+  return status_of({a[5], a[10], a[11]}, [&] {
+    return rlkv_head_norm_rotary_grad(s.qkv.p, s.qkv.stride, static_cast<int32_t*>(s.positions), static_cast<rlkv_rotary_t*>(s.rotary),
+                                      s.normed ? &s.norm : nullptr, (int32_t)s.qkv.rows, s.q_heads, s.kv_heads, kind_of(s.qkv.type), &s.q,
+                                      &s.k, s.values ? &s.v : nullptr, grad.p, grad.stride, static_cast<float*>(gq), static_cast<float*>(gk),
+                                      workspace, static_cast<size_t>(w->numel()), on.stream());
+  });
+  RLKV_CALL_END
+}
+
 #define RLKV_METHOD(name, function) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(function)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {RLKV_METHOD("rms_norm", rms_norm),
                          RLKV_METHOD("quantize", quantize),
@@ -508,6 +584,8 @@ PyMethodDef methods[] = {RLKV_METHOD("rms_norm", rms_norm),
                          RLKV_METHOD("token_logprobs_grad", token_logprobs_grad),
                          RLKV_METHOD("append_rotary", append_rotary),
                          RLKV_METHOD("rotary", rotary_split),
+                         RLKV_METHOD("head_norm_rotary", head_norm_rotary),
+                         RLKV_METHOD("head_norm_rotary_grad", head_norm_rotary_grad),
                          RLKV_METHOD("packed_attention", packed_attention),
                          RLKV_METHOD("packed_attention_grad", packed_attention_grad),
                          {nullptr, nullptr, 0, nullptr}};

@@ -4,8 +4,8 @@ csrc/tensor_calls.cpp).
 Outputs are the caller's tensors; every call goes to the current stream of the tensors' device and returns its outputs.
 Matrices are two-dimensional with contiguous columns, rows at any stride.  What is wrong with a tensor raises ValueError, what the library
 refuses RlkvError.  Autograd does not see the calls: as with torch's own calls into given outputs, a tensor that requires a gradient is
-refused unless under torch.no_grad(), and what is written counts as changed in place (`token_logprobs_grad` and
-`packed_attention_grad` are the ways back).
+refused unless under torch.no_grad(), and what is written counts as changed in place (`token_logprobs_grad`,
+`packed_attention_grad` and `head_norm_rotary_grad` are the ways back).
 """
 from __future__ import annotations
 
@@ -105,3 +105,32 @@ def packed_attention_grad(q, k, v, offsets, out, lse, grad_out, grad_q, grad_k, 
     if status:
         _check(status, "rlkv_packed_attention_grad")
     return grad_q, grad_k, grad_v
+
+
+def head_norm_rotary(qkv, positions, rotary, q_out, k_out, *, v_out=None, q_weight=None, k_weight=None, eps=None):
+    """Norm of every query and key head of packed projections qkv [tokens, (q heads + 2 kv heads) * 128] and rotation by `positions` (int32
+    [tokens]) into q_out [tokens, q heads, 128] and k_out [tokens, kv heads, 128] at any strides, values into v_out (rlkv_head_norm_rotary).
+
+    rotary: a Rotary, or None (with positions None): no rotation.  eps None: no norm; weights None: ones.  float32 or bfloat16."""
+    status = _calls.head_norm_rotary(qkv, positions, None if rotary is None else rotary.address, q_out, k_out, v_out, q_weight, k_weight, eps)
+    if status:
+        _check(status, "rlkv_head_norm_rotary")
+    return q_out, k_out
+
+
+def head_norm_rotary_grad(qkv, positions, rotary, grad_q, grad_k, grad_qkv, *, grad_v=None, q_weight=None, k_weight=None, eps=None,
+                          grad_q_weight=None, grad_k_weight=None, workspace=None):
+    """Gradients of head_norm_rotary's qkv into grad_qkv and of its weights into grad_q_weight and grad_k_weight (float32 [128], where given)
+    from those of its outputs; without grad_v the values' columns are left as they are (rlkv_head_norm_rotary_grad).
+
+    workspace: a uint8 tensor of rlkv_head_norm_rotary_grad_workspace(tokens, q heads, kv heads) bytes that the caller keeps; without one the
+    call takes one from torch's allocator."""
+    if workspace is None:
+        tokens, q_heads, kv_heads = (*grad_q.shape[:2], grad_k.shape[1]) if grad_q.dim() == 3 and grad_k.dim() == 3 else (0, 1, 1)
+        need = load_library().rlkv_head_norm_rotary_grad_workspace(tokens, q_heads, kv_heads)
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=qkv.device)
+    status = _calls.head_norm_rotary_grad(qkv, positions, None if rotary is None else rotary.address, grad_q, grad_k, grad_qkv, grad_v,
+                                          q_weight, k_weight, eps, grad_q_weight, grad_k_weight, workspace)
+    if status:
+        _check(status, "rlkv_head_norm_rotary_grad")
+    return grad_qkv
