@@ -524,9 +524,9 @@ rlkv_status_t rlkv_token_logprobs_grad(const void* logits /* device */, int64_t 
                                        const float* grad_entropy /* device */, void* grad_logits /* device */, int64_t grad_stride,
                                        void* stream);
 
-/* ---- The policy's training loop: packed rollouts ----------------------------------------------------------------------------
- * What a policy is updated with on sequences that stand one behind the other in one buffer: attention without a cache, and its way back.
- * Rules as for the token-wise operators above: no handle, nothing kept or allocated, recordable, work on `stream` of the current device. */
+/* ---- The policy's training loop: rollouts and the update on them ------------------------------------------------------------
+ * What a policy's tokens are drawn with, and what it is updated with on sequences that stand one behind the other in one buffer: attention without a
+ * cache, what stands in front of it, and the ways back.  Rules as for the token-wise operators above: no handle, nothing kept or allocated, recordable, work on `stream` of the current device. */
 
 /* Rows of head_dim (128) values: head h of token t is at data + t * token_stride + h * head_stride, in elements.  Every row starts at a multiple of
  * 16 bytes; strides are not negative.  A view of packed projections is one, and so is a tensor with the heads in front. */
@@ -609,6 +609,32 @@ rlkv_status_t rlkv_head_norm_rotary_grad(const void* qkv /* device */, int64_t t
                                          void* grad_qkv /* device */, int64_t grad_stride, float* grad_q_weight /* device */,
                                          float* grad_k_weight /* device */, void* workspace /* device */, size_t workspace_bytes,
                                          void* stream);
+
+/* A token of every row of logits, drawn by a given random number.  With w[i] = exp((x[i] - max x) / temperature):
+ *     in order of x, equal ones by the lower token, the first top_k tokens are kept; of those the first ones whose weights reach
+ *     top_p of their sum (the one that reaches it included); of those the ones with w >= min_p;
+ *     token = the first kept i with  sum of kept w[0 .. i]  >  u * sum of kept w     logprobs = log(w[token] / sum of kept w)
+ *   logits   : device, `dtype` (RLKV_F32 or RLKV_BF16), [rows][vocab]; rows <= 2^20, vocab <= 2^24
+ *   uniforms : device, fp32 [rows], u in [0, 1); below it, or NaN, counts as 0, from 1 on as what is just below 1
+ *   tokens, logprobs : device, int32 and fp32 [rows]; logprobs may be NULL
+ *   workspace : device, 16-byte aligned, rlkv_sample_tokens_workspace bytes (which may be 0; then it may be NULL); its contents do not matter.
+ *               Calls that may overlap in time need one each.
+ * A filter is off at top_k = 0, top_p >= 1, min_p = 0; the most likely token is kept by all.  A temperature of 0 draws the most likely token (the lowest
+ * of equal ones, log probability 0), whatever the filters are.  Masked logits (-inf) are never drawn.  A row with a NaN or +inf, or of masked logits
+ * only, gets token -1 and log probability NaN.  Weights are whole numbers of 2^-b, b = 62 - log2(vocab), summed exactly: equal calls give equal
+ * tokens, and a token less likely than 2^-b of the most likely one is never drawn. */
+typedef struct {
+  double temperature, top_p, min_p; /* temperature finite, >= 0; top_p >= 0; min_p in [0, 1] */
+  int32_t top_k;                    /* >= 0                                          */
+  /* Or one a row: device [rows], used in the place of the number above where not NULL.  What a number could not be counts as: a temperature
+   * that is not above 0 as 0, a top_k below 0 as 0, a top_p below 0 as 0 and NaN as 1, a min_p that is not above 0 as 0 and above 1 as 1. */
+  const float *temperatures, *top_ps, *min_ps;
+  const int32_t* top_ks;
+} rlkv_sampling_t;
+size_t rlkv_sample_tokens_workspace(int32_t rows, int32_t vocab);
+rlkv_status_t rlkv_sample_tokens(const void* logits /* device */, int64_t stride, int32_t rows, int32_t vocab, int32_t dtype,
+                                 const rlkv_sampling_t* how /* host */, const float* uniforms /* device */, int32_t* tokens /* device */,
+                                 float* logprobs /* device */, void* workspace /* device */, size_t workspace_bytes, void* stream);
 
 /* Measurement aid, independent of any cache: one plain streaming read of `bytes` (rounded down to
  * whole 16 KiB blocks) of `buf` with 128-bit non-temporal loads and no arithmetic, launched with

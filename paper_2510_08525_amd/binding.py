@@ -55,6 +55,13 @@ class HeadNorm(ctypes.Structure):
     _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float)]
 
 
+class Sampling(ctypes.Structure):
+    """rlkv_sampling_t."""
+
+    _fields_ = [("temperature", ctypes.c_double), ("top_p", ctypes.c_double), ("min_p", ctypes.c_double), ("top_k", ctypes.c_int32),
+                ("temperatures", ctypes.c_void_p), ("top_ps", ctypes.c_void_p), ("min_ps", ctypes.c_void_p), ("top_ks", ctypes.c_void_p)]
+
+
 class Packed(ctypes.Structure):
     """rlkv_packed_t."""
 
@@ -149,6 +156,8 @@ def load_library():
         "rlkv_head_norm_rotary": (i32, [vp, i64, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp]),
         "rlkv_head_norm_rotary_grad_workspace": (sz, [i32, i32, i32]),
         "rlkv_head_norm_rotary_grad": (i32, [vp, i64, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]),
+        "rlkv_sample_tokens_workspace": (sz, [i32, i32]),
+        "rlkv_sample_tokens": (i32, [vp, i64, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]),
         "rlkv_status_string": (ctypes.c_char_p, [i32]),
     }
     for name, (res, args) in sigs.items():
@@ -184,6 +193,7 @@ EXPORTED_SYMBOLS = (
     "rlkv_token_logprobs_workspace", "rlkv_token_logprobs", "rlkv_token_logprobs_grad",
     "rlkv_packed_attention", "rlkv_packed_attention_grad_workspace", "rlkv_packed_attention_grad",
     "rlkv_head_norm_rotary", "rlkv_head_norm_rotary_grad_workspace", "rlkv_head_norm_rotary_grad",
+    "rlkv_sample_tokens", "rlkv_sample_tokens_workspace",
 )
 
 
@@ -344,6 +354,11 @@ def rlkv_packed_attention_grad_workspace(tokens: int, n_q_heads: int, n_kv_heads
 def rlkv_head_norm_rotary_grad_workspace(tokens: int, n_q_heads: int, n_kv_heads: int) -> int:
     """Bytes of workspace a head_norm_rotary_grad call of these sizes needs for the gradients of weights."""
     return int(load_library().rlkv_head_norm_rotary_grad_workspace(tokens, n_q_heads, n_kv_heads))
+
+
+def rlkv_sample_tokens_workspace(rows: int, vocab: int) -> int:
+    """Bytes of workspace a sample_tokens call of these sizes needs (0: none)."""
+    return int(load_library().rlkv_sample_tokens_workspace(rows, vocab))
 
 
 def rlkv_probe_stream_read(buf_ptr: int, nbytes: int, sink_ptr: int, workgroups: int, stream: int = 0):

@@ -3,6 +3,7 @@
 
 #include "head_norm_rotary.h"
 #include "packed_attention.h"
+#include "sample_tokens.h"
 
 using namespace rlkv;
 
@@ -11,6 +12,7 @@ namespace {
 hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
 bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
+constexpr int32_t kMostLogitRows = 1 << 20, kMostVocab = 1 << 24;
 constexpr int64_t kMostStride = (int64_t)1 << 40;          // (a row's address is far from 64 bits)
 
 // Rows that the call reads: they may repeat, but not run backwards.
@@ -95,6 +97,43 @@ bool head_norm_call(HeadNormCall* c, RotaryTurns* turns, const void* qkv, int64_
 }  // namespace
 
 extern "C" {
+
+size_t rlkv_sample_tokens_workspace(int32_t rows, int32_t vocab) {
+  return rows < 1 || rows > kMostLogitRows || vocab < 1 || vocab > kMostVocab ? 0 : sample_workspace(rows, vocab);
+}
+
+rlkv_status_t rlkv_sample_tokens(const void* logits, int64_t stride, int32_t rows, int32_t vocab, int32_t dtype, const rlkv_sampling_t* how,
+                                 const float* uniforms, int32_t* tokens, float* logprobs, void* workspace, size_t workspace_bytes, void* stream) {
+  if (dtype != RLKV_F32 && dtype != RLKV_BF16) return RLKV_ERR_INVALID_ARG;
+  if (rows < 0 || rows > kMostLogitRows || vocab < 1 || vocab > kMostVocab || !how) return RLKV_ERR_INVALID_ARG;
+  if ((!how->temperatures && (!(how->temperature >= 0.) || isinf(how->temperature))) || (!how->top_ks && how->top_k < 0) ||
+      (!how->top_ps && !(how->top_p >= 0.)) || (!how->min_ps && !(how->min_p >= 0. && how->min_p <= 1.)))
+    return RLKV_ERR_INVALID_ARG;
+  if (!aligned(how->temperatures, 4) || !aligned(how->top_ks, 4) || !aligned(how->top_ps, 4) || !aligned(how->min_ps, 4)) return RLKV_ERR_INVALID_ARG;
+  if (rows == 0) return RLKV_OK;
+  if (!logits || !aligned(logits, dtype == RLKV_F32 ? 4 : 2) || stride < 0 || stride > kMostStride) return RLKV_ERR_INVALID_ARG;
+  if (!uniforms || !tokens || !aligned(uniforms, 4) || !aligned(tokens, 4) || !aligned(logprobs, 4)) return RLKV_ERR_INVALID_ARG;
+  const size_t need = sample_workspace(rows, vocab);
+  if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < need)) return RLKV_ERR_INVALID_ARG;
+  SampleCall c = {};
+  c.logits = logits;
+  c.stride = stride;
+  c.rows = rows;
+  c.vocab = vocab;
+  c.temperature = how->temperature;
+  c.top_k = how->top_k;
+  c.top_p = how->top_p;
+  c.min_p = how->min_p;
+  c.temperatures = how->temperatures;
+  c.top_ks = how->top_ks;
+  c.top_ps = how->top_ps;
+  c.min_ps = how->min_ps;
+  c.uniforms = uniforms;
+  c.tokens = tokens;
+  c.logprobs = logprobs;
+  c.workspace = workspace;
+  return launch_sample(c, dtype, as_stream(stream)) == hipSuccess ? RLKV_OK : RLKV_ERR_HIP;
+}
 
 rlkv_status_t rlkv_head_norm_rotary(const void* qkv, int64_t token_stride, const int32_t* positions, const rlkv_rotary_t* rotary,
                                     const rlkv_head_norm_t* norm, int32_t tokens, int32_t n_q_heads, int32_t n_kv_heads, int32_t dtype,

@@ -401,6 +401,56 @@ PyObject* rotary_split(PyObject*, PyObject* const* a, Py_ssize_t n) {
   RLKV_CALL_END
 }
 
+bool integer(PyObject* o, const char* what, int32_t* v) {
+  int beyond = 0;
+  const long x = PyLong_AsLongAndOverflow(o, &beyond);
+  if (PyErr_Occurred()) return false;
+  *v = (int32_t)x;
+  if (!beyond && *v == x) return true;
+  PyErr_Format(PyExc_ValueError, "%s: %R is out of range", what, o);
+  return false;
+}
+// A number, or a vector with one a row.
+bool number_or_vector(PyObject* o, const char* what, int index, int64_t rows, double* f, const float** p) {
+  void* at = nullptr;
+  if (THPVariable_Check(o)) {
+    if (!vector(o, what, index, ScalarType::Float, rows, &at)) return false;
+    *p = static_cast<float*>(at);
+    return true;
+  }
+  *f = PyFloat_AsDouble(o);
+  return !(*f == -1.0 && PyErr_Occurred());
+}
+
+// logits, uniforms, tokens, temperature, top_k, top_p, min_p, logprobs, workspace
+PyObject* sample_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  RLKV_CALL_BEGIN
+  Matrix x;
+  void *uniforms, *tokens, *logprobs, *workspace, *ks = nullptr;
+  rlkv_sampling_t how = {};
+  if (!arguments(n, 9) || !activations(a[0], "logits", &x) || !fits(x.rows, "logits") || !fits(x.cols, "logits")) return nullptr;
+  if (!vector(a[1], "uniforms", x.device, ScalarType::Float, x.rows, &uniforms)) return nullptr;
+  if (!vector(a[2], "tokens", x.device, ScalarType::Int, x.rows, &tokens)) return nullptr;
+  if (!number_or_vector(a[3], "temperature", x.device, x.rows, &how.temperature, &how.temperatures)) return nullptr;
+  if (THPVariable_Check(a[4])) {
+    if (!vector(a[4], "top_k", x.device, ScalarType::Int, x.rows, &ks)) return nullptr;
+    how.top_ks = static_cast<int32_t*>(ks);
+  } else if (!integer(a[4], "top_k", &how.top_k)) {
+    return nullptr;
+  }
+  if (!number_or_vector(a[5], "top_p", x.device, x.rows, &how.top_p, &how.top_ps)) return nullptr;
+  if (!number_or_vector(a[6], "min_p", x.device, x.rows, &how.min_p, &how.min_ps)) return nullptr;
+  if (!vector(a[7], "logprobs", x.device, ScalarType::Float, x.rows, &logprobs)) return nullptr;
+  const at::Tensor* w = tensor(a[8], "workspace");
+  if (!w || !vector(a[8], "workspace", x.device, ScalarType::Byte, w->numel(), &workspace)) return nullptr;
+  const OnDevice on(x.device);
+  return status_of({a[2], a[7]}, [&] {
+    return rlkv_sample_tokens(x.p, x.stride, (int32_t)x.rows, (int32_t)x.cols, kind_of(x.type), &how, static_cast<float*>(uniforms),
+                              static_cast<int32_t*>(tokens), static_cast<float*>(logprobs), workspace, static_cast<size_t>(w->numel()), on.stream());
+  });
+  RLKV_CALL_END
+}
+
 // ---- calls on packed sequences -----------------------------------------------------------------------------------------------------------
 // [tokens, heads, head_dim] at any strides of tokens and heads; tokens and heads below 0: any.
 bool head_rows(PyObject* o, const char* what, int index, ScalarType type, int64_t tokens, int64_t heads, rlkv_heads_t* r) {
@@ -417,15 +467,6 @@ bool head_rows(PyObject* o, const char* what, int index, ScalarType type, int64_
   r->token_stride = t->size(0) > 1 ? t->stride(0) : 0;          // (the stride of an axis of one, which a tensor may report as anything)
   r->head_stride = t->size(1) > 1 ? t->stride(1) : 0;
   return true;
-}
-bool integer(PyObject* o, const char* what, int32_t* v) {
-  int beyond = 0;
-  const long x = PyLong_AsLongAndOverflow(o, &beyond);
-  if (PyErr_Occurred()) return false;
-  *v = (int32_t)x;
-  if (!beyond && *v == x) return true;
-  PyErr_Format(PyExc_ValueError, "%s: %R is out of range", what, o);
-  return false;
 }
 // q, k, v, offsets; scale, mask (bytes or None), sink, recent
 bool packed_shape(PyObject* const* qkv, PyObject* const* how, rlkv_heads_t* q, rlkv_heads_t* k, rlkv_heads_t* v, rlkv_packed_t* s, int* index) {
@@ -584,6 +625,7 @@ PyMethodDef methods[] = {RLKV_METHOD("rms_norm", rms_norm),
                          RLKV_METHOD("token_logprobs_grad", token_logprobs_grad),
                          RLKV_METHOD("append_rotary", append_rotary),
                          RLKV_METHOD("rotary", rotary_split),
+                         RLKV_METHOD("sample_tokens", sample_tokens),
                          RLKV_METHOD("head_norm_rotary", head_norm_rotary),
                          RLKV_METHOD("head_norm_rotary_grad", head_norm_rotary_grad),
                          RLKV_METHOD("packed_attention", packed_attention),

@@ -134,3 +134,21 @@ def head_norm_rotary_grad(qkv, positions, rotary, grad_q, grad_k, grad_qkv, *, g
     if status:
         _check(status, "rlkv_head_norm_rotary_grad")
     return grad_qkv
+
+
+def sample_tokens(logits, uniforms, tokens, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, logprobs=None, workspace=None):
+    """A token of every row of logits [rows, vocab] (float32 or bfloat16) into tokens (int32 [rows]), drawn by uniforms (float32 [rows], in
+    [0, 1)) from softmax(logits / temperature) over what top_k, then top_p, then min_p keep, and where given its log probability there into
+    logprobs (float32 [rows]) (rlkv_sample_tokens).
+
+    temperature (0: the most likely token), top_k (0: off), top_p (1: off), min_p (0: off): each a number, or a tensor of one a row on the device
+    (float32; top_k int32).  workspace: a uint8 tensor of rlkv_sample_tokens_workspace(rows, vocab) bytes that the caller keeps; without one the call
+    takes one from torch's allocator."""
+    if workspace is None:
+        rows, vocab = logits.shape if logits.dim() == 2 else (0, 0)
+        need = load_library().rlkv_sample_tokens_workspace(rows, vocab)
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=logits.device)
+    status = _calls.sample_tokens(logits, uniforms, tokens, temperature, top_k, top_p, min_p, logprobs, workspace)
+    if status:
+        _check(status, "rlkv_sample_tokens")
+    return tokens
