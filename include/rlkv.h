@@ -547,11 +547,11 @@ typedef struct {
   int32_t n_kv_heads;       /* at most 256; tokens * group is below 2^30                                             */
   const uint8_t* full_mask; /* host [n_kv_heads], 1 = full, 0 = local; copied; NULL: all are full                   */
   int32_t sink, recent;     /* sink >= 0; recent >= 1 where a head is local                                         */
-  float softmax_scale;      /* positive, finite                                                                     */
+  float softmax_scale;      /* in [2^-60, 2^60]                                                                      */
 } rlkv_packed_t;
 
 /* out = softmax(softmax_scale * q . K^T) V over the admitted keys, and lse = log sum exp of their scaled scores.
- *   q, out : RLKV_BF16, [tokens][n_q_heads];  k, v : [tokens][n_kv_heads]
+ *   q, out : RLKV_BF16, [tokens][n_q_heads];  k, v : [tokens][n_kv_heads]; token strides at most 2^24
  *   lse    : device, fp32, [n_q_heads][tokens], or NULL
  * Scores, softmax and sums are fp32; the weights enter their product with V in bf16.  What is not admitted does not count, whatever it holds
  * (infinities and NaN among it).  Equal calls give equal bits. */

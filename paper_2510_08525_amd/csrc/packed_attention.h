@@ -29,10 +29,13 @@ struct HeadRows {
   uint16_t* p;
   int64_t token, head;
 };
+struct PackedPlan { int32_t items, pad[3]; };      // of the gradient's second launch (packed_attention_grad.hip)
 struct PackedCall {
   HeadRows q, k, v, out, grad_out, grad_q, grad_k, grad_v;
   float* lse;                       // [n_q_heads][tokens]
   float* delta;                     // the same (gradient only); set by the launch
+  PackedPlan* plan;         // gradient only; set by the launch
+  float* slots;                     // the same
   void* workspace;                  // gradient only
   const int32_t* offsets;           // [n_seqs + 1]
   int32_t n_seqs, tokens, n_q_heads, n_kv_heads, group;
@@ -121,6 +124,25 @@ __device__ __forceinline__ bf16x8 transposed_fragment(const uint4* tile, int row
   return f.all;
 #else
   return bf16x8{};
+#endif
+}
+
+// 64 rows from `token` on of a head's rows, straight from memory to a tile in LDS; of a workgroup of eight wavefronts, all of them at the call.  Rows from
+// `tokens` on are the last one.  (Buffer loads, whose base is the same in all lanes; a row's place from it fits 32 bits.)
+constexpr int kStageRows = 64;
+constexpr int64_t kMostTokenStride = 1 << 24;
+__device__ __forceinline__ void stage_rows(const HeadRows& t, int token, int head, int tokens, uint4* tile) {
+#ifdef __HIP_DEVICE_COMPILE__
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const __amdgpu_buffer_rsrc_t from =
+      __builtin_amdgcn_make_buffer_rsrc(t.p + (int64_t)token * t.token + (int64_t)head * t.head, 0, 0xffffffff, 0x00027000);
+  const int most = tokens - 1 - token;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = 8 * wave + 4 * i + (lane >> 4), r = row < most ? row : most;
+    const uint32_t at = (uint32_t)r * (uint32_t)(t.token * 2) + ((lane & 15) ^ ((row & 7) << 1)) * 16;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, RLKV_LDS_PTR(void, tile + (8 * wave + 4 * i) * 16), 16, (int)at, 0, 0, 0);
+  }
 #endif
 }
 

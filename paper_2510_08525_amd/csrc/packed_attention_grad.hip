@@ -6,6 +6,8 @@
 // Two kernels, each of which forms w and z for itself: one walks over the keys of its columns (queries) as the forward one does and leaves grad_q
 // and delta, the other over the columns of its keys and leaves grad_k and grad_v, summed over the group's heads in fp32 in a fixed order.
 // That is seven products where one kernel would do five, but none of them adds to memory that others add to: equal calls give equal bits.
+#include <type_traits>
+
 #include "packed_attention.h"
 
 namespace rlkv {
@@ -72,6 +74,83 @@ __device__ __forceinline__ float dot_of_units(uint4 a, uint4 b) {
   return sum;
 }
 
+// ---- the plan: what every workgroup of the second launch does ----
+constexpr int kKeysHere = 32 * kWaves, kStep = kStageRows;      // keys of a workgroup, positions of a step (below)
+constexpr int kMostParts = 512;           // workgroups that share keys, at most: two a compute unit
+constexpr int kLeastSteps = 4;            // steps that are worth a workgroup with a slot to write and to add up
+constexpr int kSlotFloats = 2 * kHeadDim * kKeysHere;
+
+struct PlanItem {
+  int32_t tile, head;                     // keys [256 tile, + 256) of KV head `head`
+  int32_t first, end;                     // the positions that admit any of them
+  int32_t step, last_step;                // of their steps the ones [step, last_step)
+  int32_t slot;                           // where the sums go; -1: into the gradients
+  int32_t pad;
+};
+struct PlanMerge { int32_t slot, parts; };      // of a tile and head: parts 0 where nothing is shared
+// (behind the PackedPlan: PlanItem[tiles * heads + kMostParts], PlanMerge[tiles * heads])
+__host__ __device__ inline int64_t tiles_of(int64_t tokens) { return (tokens + kKeysHere - 1) / kKeysHere; }
+__device__ __forceinline__ PlanItem* items_of(PackedPlan* p) { return reinterpret_cast<PlanItem*>(p + 1); }
+__device__ __forceinline__ PlanMerge* merges_of(PackedPlan* p, int64_t pairs) { return reinterpret_cast<PlanMerge*>(items_of(p) + pairs + kMostParts); }
+
+struct PlanSmem {
+  unsigned long long total;
+  int32_t items, slots;
+};
+// The positions of a tile's keys; end <= first: none.
+struct TileRange { int32_t first, end; };
+__device__ __forceinline__ TileRange range_of(const PackedCall& c, const int32_t* offsets, int tile, bool full) {
+  const int begin = offsets[0], end = offsets[c.n_seqs];
+  const int first = max(tile * kKeysHere, begin), last = min(min(tile * kKeysHere + kKeysHere, end), c.tokens) - 1;
+  if (first > last) return {0, 0};
+  const Span span = span_of(offsets, c.n_seqs, c.tokens, last);
+  if (span.begin < 0) return {0, 0};
+  if (full || max(span.begin, first) - span.begin < c.sink || span.end - last < c.recent) return {first, span.end};
+  return {first, last + c.recent};
+}
+__device__ __forceinline__ int steps_of(const TileRange& r, int group) {
+  return r.end <= r.first ? 0 : (r.end - r.first + kStep - 1) / kStep * group;
+}
+// One workgroup.
+__device__ void make_plan(const PackedCall& c, const int32_t* offsets, PlanSmem& sm) {
+  const int64_t pairs = tiles_of(c.tokens) * c.n_kv_heads;
+  if (threadIdx.x == 0) {
+    sm.total = 0;
+    sm.items = sm.slots = 0;
+  }
+  __syncthreads();
+  auto pair = [&](int64_t i, int& tile, int& h) {
+    tile = (int)(i / c.n_kv_heads);
+    h = (int)(i - (int64_t)tile * c.n_kv_heads);
+    return range_of(c, offsets, tile, (c.full[h >> 6] >> (h & 63)) & 1);
+  };
+  int tile, h;
+  unsigned long long mine = 0;
+  for (int64_t i = threadIdx.x; i < pairs; i += kThreads) mine += steps_of(pair(i, tile, h), c.group);
+  atomicAdd(&sm.total, mine);
+  __syncthreads();
+  // parts of at least `least` and less than twice as many steps, so at most kMostParts of them
+  const int64_t share = (int64_t)((sm.total + kMostParts - 1) / kMostParts);
+  const int least = (int)(share < kLeastSteps ? kLeastSteps : share);
+  PlanItem* items = items_of(c.plan);
+  PlanMerge* merges = merges_of(c.plan, pairs);
+  // (the long ones in front of the others)
+  for (int turn = 0; turn < 2; ++turn) {
+    for (int64_t i = threadIdx.x; i < pairs; i += kThreads) {
+      const TileRange r = pair(i, tile, h);
+      const int steps = steps_of(r, c.group), parts = max(1, steps / least);
+      if (turn == 0) merges[i] = {-1, 0};
+      if (steps == 0 || (steps >= least) != (turn == 0)) continue;
+      const int at = atomicAdd(&sm.items, parts), slot = parts > 1 ? atomicAdd(&sm.slots, parts) : -1;
+      if (parts > 1) merges[i] = {slot, parts};
+      for (int p = 0; p < parts; ++p)
+        items[at + p] = {tile, h, r.first, r.end, (int)((int64_t)steps * p / parts), (int)((int64_t)steps * (p + 1) / parts), parts > 1 ? slot + p : -1, 0};
+    }
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) c.plan->items = sm.items;
+}
+
 // ---- queries ------------------------------------------------------------------------------------------------------------------
 constexpr int kColumns = 32 * kWaves, kKeys = 64;
 constexpr int kKeyUnits = kKeys * 16 / kThreads;
@@ -80,6 +159,7 @@ struct QuerySmem {
   uint4 k[2][kKeys * 16], v[2][kKeys * 16];
   int32_t offsets[kOffsetsInLds];
   int32_t first[kWaves], begin[kWaves], last[kWaves];
+  PlanSmem plan;
 };
 
 __global__ __launch_bounds__(kThreads) void packed_grad_q_kernel(PackedCall c) {
@@ -93,7 +173,11 @@ __global__ __launch_bounds__(kThreads) void packed_grad_q_kernel(PackedCall c) {
     __syncthreads();
     offsets = sm.offsets;
   }
-  const int64_t column = (int64_t)blockIdx.x * kColumns + wave * 32 + (lane & 31);
+  if (blockIdx.x == 0) {                                     // (the first workgroup of the launch is none of its own)
+    if (h == 0) make_plan(c, offsets, sm.plan);
+    return;
+  }
+  const int64_t column = (int64_t)(blockIdx.x - 1) * kColumns + wave * 32 + (lane & 31);
   const int pos = (int)(column / group);
   const int head = h * group + (int)(column - (int64_t)pos * group);
   const Span span = span_of(offsets, c.n_seqs, c.tokens, pos);
@@ -211,162 +295,230 @@ __global__ __launch_bounds__(kThreads) void packed_grad_q_kernel(PackedCall c) {
 }
 
 // ---- keys and values ----------------------------------------------------------------------------------------------------------
-// A workgroup has 256 keys, 32 a wavefront and one a lane (both halves of the wavefront: the same), and walks over the columns that admit any of
-// them, 32 at a time.  Key j is admitted to the positions j <= i < limit: the end of its sequence, or of a local head's key that is no sink
-// j + recent if that is less.
-constexpr int kKeysHere = 32 * kWaves, kStep = 32;
+// A workgroup has 256 keys, 32 a wavefront and one a lane (both halves of the wavefront: the same), and walks over the positions that admit any of
+// them, 64 of one query head of the group at a time, a head after the other.  Key j is admitted to the positions j <= i < limit: the end of its
+// sequence, or of a local head's key that is no sink j + recent if that is less.
+//
+// How many steps that is differs by a thousand between the keys of a launch (the first keys of a long sequence, the sinks of a local head,
+// short sequences), so the launch in front plans: a workgroup is given at most some 2 / 512 of all steps, and where keys have more they are
+// divided among workgroups that leave their sums in slots of the workspace, which a third launch adds up in the order of the steps.
 
-struct KeySmem {
-  uint4 q[2][kStep * 16], g[2][kStep * 16];
-  float lse[2][kStep], delta[2][kStep];
-  int32_t pos[2][kStep];
-  int32_t offsets[kOffsetsInLds];
-  int32_t first[kWaves], limit[kWaves];
-};
+// Sums of a workgroup in its slot, and the way back: piece (which of the 32 float4 of a lane) after piece, lane after lane.
+__device__ __forceinline__ float* slot_piece(float* slots, int slot, int piece, int thread) {
+  return slots + (int64_t)slot * kSlotFloats + ((int64_t)piece * kThreads + thread) * 4;
+}
 
 __global__ __launch_bounds__(kThreads) void packed_grad_kv_kernel(PackedCall c) {
-  __shared__ KeySmem sm;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
-  const int h = blockIdx.y, group = c.group;
+  // (objects of their own, and the slot of a step known at compile time: else reads of one tile would wait for the loads of the next)
+  __shared__ uint4 q0[kStep * 16], q1[kStep * 16], g0[kStep * 16], g1[kStep * 16];
+  __shared__ float minus_lse[2][kStep], minus_delta[2][kStep];
+  __shared__ int32_t seqs[kOffsetsInLds];
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  if ((int)blockIdx.x >= c.plan->items) return;
+  const PlanItem item = items_of(c.plan)[blockIdx.x];
+  const int h = item.head, group = c.group;
   const bool full = (c.full[h >> 6] >> (h & 63)) & 1;
   const int32_t* offsets = c.offsets;
   if (c.n_seqs < kOffsetsInLds) {
-    for (int i = threadIdx.x; i <= c.n_seqs; i += kThreads) sm.offsets[i] = c.offsets[i];
+    for (int i = threadIdx.x; i <= c.n_seqs; i += kThreads) seqs[i] = c.offsets[i];
     __syncthreads();
-    offsets = sm.offsets;
+    offsets = seqs;
   }
-  const int key = blockIdx.x * kKeysHere + wave * 32 + (lane & 31);
-  const Span span = span_of(offsets, c.n_seqs, c.tokens, key);
+  const int at = item.tile * kKeysHere + (threadIdx.x >> 6) * 32 + (lane & 31);
+  const Span span = span_of(offsets, c.n_seqs, c.tokens, at);
   const bool valid = span.begin >= 0;
-  const int64_t row = valid ? key : 0;
-  const int limit = !valid ? -1 : full || key - span.begin < c.sink || span.end - key < c.recent ? span.end : key + c.recent;
+  const int key = valid ? at : 0;                                       // (a key of no sequence: nothing is admitted, nothing written)
+  int limit = !valid ? 0 : full || key - span.begin < c.sink || span.end - key < c.recent ? span.end : key + c.recent;
+  limit = min(limit, item.end);
+  const uint32_t width = valid ? max(limit - key, 0) : 0;
   const int key_lo = min_of_lanes(valid ? key : INT32_MAX), key_hi = max_of_lanes(valid ? key : -1);
-  const int limit_lo = min_of_lanes(valid ? limit : INT32_MAX), limit_hi = max_of_lanes(limit);
-  if (lane == 0) {
-    sm.first[wave] = key_lo;
-    sm.limit[wave] = limit_hi;
-  }
-  __syncthreads();
-  int first = INT32_MAX, end = -1;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    first = min(first, sm.first[w]);
-    end = max(end, sm.limit[w]);
-  }
-  if (end < 0) return;
+  const int limit_lo = min_of_lanes(valid ? limit : INT32_MAX), limit_hi = max_of_lanes(valid ? limit : -1);
 
   bf16x8 k[8], v[8];
-  const uint16_t* k_row = c.k.p + row * c.k.token + h * c.k.head + 8 * half;
-  const uint16_t* v_row = c.v.p + row * c.v.token + h * c.v.head + 8 * half;
+  {
+    const uint16_t* k_row = c.k.p + (int64_t)key * c.k.token + h * c.k.head + 8 * half;
+    const uint16_t* v_row = c.v.p + (int64_t)key * c.v.token + h * c.v.head + 8 * half;
 #pragma unroll
-  for (int s = 0; s < 8; ++s) {
-    k[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(k_row + 16 * s));
-    v[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(v_row + 16 * s));
+    for (int s = 0; s < 8; ++s) {
+      k[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(k_row + 16 * s));
+      v[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(v_row + 16 * s));
+    }
   }
 
-  // Columns past the last one are given position -1, which admits no key, and the row of the last one.
-  const int64_t column0 = (int64_t)first * group, column_end = (int64_t)end * group;
-  const int steps = (int)((column_end - column0 + kStep - 1) / kStep);
-  uint4 next_q, next_g;
-  float next_lse = 0.f, next_delta = 0.f;
-  int next_pos = -1;
-  auto fetch = [&](int t) {
-    const int r = threadIdx.x >> 4, u = threadIdx.x & 15;
-    const int64_t col = column0 + (int64_t)t * kStep + r, at = col < column_end ? col : column_end - 1;
-    const int p = (int)(at / group), head = h * group + (int)(at - (int64_t)p * group);
-    next_q = *reinterpret_cast<const uint4*>(c.q.p + (int64_t)p * c.q.token + head * c.q.head + u * 8);
-    next_g = *reinterpret_cast<const uint4*>(c.grad_out.p + (int64_t)p * c.grad_out.token + head * c.grad_out.head + u * 8);
-    if (u == 0) {
-      next_lse = c.lse[(int64_t)head * c.tokens + p] * kLog2e;
-      next_delta = c.delta[(int64_t)head * c.tokens + p];
-      next_pos = col < column_end ? p : -1;
+  const int per_head = (item.end - item.first + kStep - 1) / kStep;      // steps of a query head
+  const float scale = c.scale * kLog2e, inv_scale = 1.f / c.scale;
+  // the step that is asked for next: query head and first position
+  int next_head, next_pos;
+  auto ask = [&](auto odd) {
+    constexpr int kOdd = decltype(odd)::value;
+    stage_rows(c.q, next_pos, next_head, c.tokens, kOdd ? q1 : q0);
+    stage_rows(c.grad_out, next_pos, next_head, c.tokens, kOdd ? g1 : g0);
+    if (threadIdx.x < kStep) {
+      const int64_t row = (int64_t)next_head * c.tokens + min(next_pos + (int)threadIdx.x, c.tokens - 1);
+      minus_lse[kOdd][threadIdx.x] = -c.lse[row] * inv_scale;
+      minus_delta[kOdd][threadIdx.x] = -c.delta[row];
+    }
+    next_pos += kStep;
+    if (next_pos >= item.end) {
+      next_pos = item.first;
+      ++next_head;
     }
   };
-  auto place = [&](int slot) {
-    const int r = threadIdx.x >> 4, u = threadIdx.x & 15;
-    sm.q[slot][unit_at(r, u)] = next_q;
-    sm.g[slot][unit_at(r, u)] = next_g;
-    if (u == 0) {
-      sm.lse[slot][r] = next_lse;
-      sm.delta[slot][r] = next_delta;
-      sm.pos[slot][r] = next_pos;
-    }
-  };
-  const float scale = c.scale * kLog2e;
 
   floatx16 dk[4], dv[4];
-  for (int careful = 0;; careful = 1) {
+  auto walk = [&](auto careful) {
+    constexpr bool kCareful = decltype(careful)::value;
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
       clear(dk[b]);
       clear(dv[b]);
     }
-    fetch(0);
-    place(0);
-    __syncthreads();
-    for (int t = 0; t < steps; ++t) {
-      const int slot = t & 1;
-      if (t + 1 < steps) fetch(t + 1);
-      const int64_t c0 = column0 + (int64_t)t * kStep, c1 = c0 + kStep - 1;
-      const int pos_lo = (int)(c0 / group), pos_hi = (int)((c1 < column_end ? c1 : column_end - 1) / group);
-      if (pos_hi >= key_lo && pos_lo < limit_hi) {
-        const bool all = c1 < column_end && pos_lo >= key_hi && pos_hi < limit_lo;
+    next_head = h * group + item.step / per_head;
+    next_pos = item.first + item.step % per_head * kStep;
+    int pos = next_pos;
+    ask(std::integral_constant<int, 0>{});
+    auto step = [&](auto odd, bool more) {
+      constexpr int kOdd = decltype(odd)::value;
+      const uint4 *qt = kOdd ? q1 : q0, *gt = kOdd ? g1 : g0;
+      __syncthreads();
+      if (more) ask(std::integral_constant<int, 1 - kOdd>{});
+#pragma unroll
+      for (int sub = 0; sub < kStep; sub += 32) {
+        const int p0 = pos + sub;
+        if (p0 + 31 < key_lo || p0 >= limit_hi) continue;
+        const bool all = p0 >= key_hi && p0 + 32 <= limit_lo;
         floatx16 x, y;
-        clear(x);
-        clear(y);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int col = sub + 8 * (r >> 2) + 4 * half + (r & 3);
+          x[r] = minus_lse[kOdd][col];
+          y[r] = minus_delta[kOdd][col];
+        }
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
-          x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(sm.q[slot], 0, s), k[s], x, 0, 0, 0);
-          y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(sm.g[slot], 0, s), v[s], y, 0, 0, 0);
+          x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(qt, sub, s), k[s], x, 0, 0, 0);
+          y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(gt, sub, s), v[s], y, 0, 0, 0);
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const int col = 8 * (r >> 2) + 4 * half + (r & 3);
-          x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], scale, -sm.lse[slot][col]));
-          y[r] = x[r] * (y[r] - sm.delta[slot][col]);
+          x[r] = __builtin_amdgcn_exp2f(x[r] * scale);
+          y[r] *= x[r];
         }
-        auto admits = [&](int col) { return valid && sm.pos[slot][col] >= key && sm.pos[slot][col] < limit; };
         if (!all) {
+          const uint32_t from = p0 + 4 * half - key;
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            if (!admits(8 * (r >> 2) + 4 * half + (r & 3))) x[r] = y[r] = 0.f;
+            if (from + (8 * (r >> 2) + (r & 3)) >= width) x[r] = y[r] = 0.f;
         }
-        if (careful && !all) {
-          admitted_products(sm.g[slot], 0, x, dv, admits);
-          admitted_products(sm.q[slot], 0, y, dk, admits);
+        if (kCareful && !all) {
+          auto admits = [&](int col) { return (uint32_t)(p0 + col - key) < width; };
+          admitted_products(gt, sub, x, dv, admits);
+          admitted_products(qt, sub, y, dk, admits);
         } else {
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
             const bf16x8 w = weights_fragment(x, s), z = weights_fragment(y, s);
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-              dv[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_fragment(sm.g[slot], 16 * s, d), w, dv[d], 0, 0, 0);
-              dk[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_fragment(sm.q[slot], 16 * s, d), z, dk[d], 0, 0, 0);
+              dv[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_fragment(gt, sub + 16 * s, d), w, dv[d], 0, 0, 0);
+              dk[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_fragment(qt, sub + 16 * s, d), z, dk[d], 0, 0, 0);
             }
           }
         }
       }
-      if (t + 1 < steps) place(slot ^ 1);
-      __syncthreads();
+      pos += kStep;
+      if (pos >= item.end) pos = item.first;
+    };
+    int t = item.step;
+    for (; t + 1 < item.last_step; t += 2) {
+      step(std::integral_constant<int, 0>{}, true);
+      step(std::integral_constant<int, 1>{}, t + 2 < item.last_step);
     }
-    if (careful || !__syncthreads_or(valid && (zero_or_nan(dk) != 0.f || zero_or_nan(dv) != 0.f))) break;
+    if (t < item.last_step) step(std::integral_constant<int, 0>{}, false);
+  };
+  walk(std::false_type{});
+  // (a weight of 0 does not keep an infinity or a NaN of a row that is not admitted out of the products)
+  if (__syncthreads_or(valid && (zero_or_nan(dk) != 0.f || zero_or_nan(dv) != 0.f))) walk(std::true_type{});
+  if (item.slot >= 0) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      *reinterpret_cast<float4*>(slot_piece(c.slots, item.slot, i, threadIdx.x)) =
+          make_float4(dk[i >> 2][4 * (i & 3)], dk[i >> 2][4 * (i & 3) + 1], dk[i >> 2][4 * (i & 3) + 2], dk[i >> 2][4 * (i & 3) + 3]);
+      *reinterpret_cast<float4*>(slot_piece(c.slots, item.slot, 16 + i, threadIdx.x)) =
+          make_float4(dv[i >> 2][4 * (i & 3)], dv[i >> 2][4 * (i & 3) + 1], dv[i >> 2][4 * (i & 3) + 2], dv[i >> 2][4 * (i & 3) + 3]);
+    }
+    return;
   }
   if (!valid) return;
-  store_rows(c.grad_k.p + row * c.grad_k.token + h * c.grad_k.head, dk, c.scale);
-  store_rows(c.grad_v.p + row * c.grad_v.token + h * c.grad_v.head, dv, 1.f);
+  store_rows(c.grad_k.p + (int64_t)key * c.grad_k.token + h * c.grad_k.head, dk, c.scale);
+  store_rows(c.grad_v.p + (int64_t)key * c.grad_v.token + h * c.grad_v.head, dv, 1.f);
+}
+
+// The slots of keys that workgroups shared, added up in the order of their steps: four pieces of a lane a workgroup.
+__global__ __launch_bounds__(kThreads) void packed_grad_sum_kernel(PackedCall c) {
+  const int64_t pairs = tiles_of(c.tokens) * c.n_kv_heads;
+  const PlanMerge merge = merges_of(c.plan, pairs)[blockIdx.x];
+  if (merge.parts == 0) return;
+  const int tile = blockIdx.x / c.n_kv_heads, h = blockIdx.x % c.n_kv_heads, lane = threadIdx.x & 63;
+  float4 sum[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) sum[i] = *reinterpret_cast<const float4*>(slot_piece(c.slots, merge.slot, blockIdx.y * 4 + i, threadIdx.x));
+  for (int p = 1; p < merge.parts; ++p)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 x = *reinterpret_cast<const float4*>(slot_piece(c.slots, merge.slot + p, blockIdx.y * 4 + i, threadIdx.x));
+      sum[i].x += x.x;
+      sum[i].y += x.y;
+      sum[i].z += x.z;
+      sum[i].w += x.w;
+    }
+  const int key = tile * kKeysHere + (threadIdx.x >> 6) * 32 + (lane & 31);
+  if (span_of(c.offsets, c.n_seqs, c.tokens, key).begin < 0) return;
+  const HeadRows& to = blockIdx.y < 4 ? c.grad_k : c.grad_v;
+  const float scale = blockIdx.y < 4 ? c.scale : 1.f;
+  uint16_t* row = to.p + (int64_t)key * to.token + h * to.head + 32 * (blockIdx.y & 3) + 4 * (lane >> 5);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const words2 w = {two_bf16(sum[i].x * scale, sum[i].y * scale), two_bf16(sum[i].z * scale, sum[i].w * scale)};
+    *reinterpret_cast<words2*>(row + 8 * i) = w;
+  }
 }
 
 }  // namespace
 
-size_t packed_grad_workspace(int tokens, int n_q_heads, int) { return ((size_t)tokens * n_q_heads * sizeof(float) + 15) / 16 * 16; }
+// The workspace: delta, the plan, the slots.
+struct GradSpace {
+  size_t delta, plan, slots, bytes;
+};
+static GradSpace grad_space(int64_t tokens, int64_t n_q_heads, int64_t n_kv_heads) {
+  const int64_t pairs = tiles_of(tokens) * n_kv_heads, group = n_q_heads / n_kv_heads;
+  auto align = [](size_t x) { return (x + 255) / 256 * 256; };
+  GradSpace s;
+  s.delta = 0;
+  s.plan = align((size_t)(tokens * n_q_heads) * sizeof(float));
+  s.slots = s.plan + align(sizeof(PackedPlan) + (size_t)(pairs + kMostParts) * sizeof(PlanItem) + (size_t)pairs * sizeof(PlanMerge));
+  // (parts have kLeastSteps steps at least, of which a pair has one for each head and 64 positions at most)
+  const int64_t steps = pairs * ((tokens + kStep - 1) / kStep) * group, parts = steps / kLeastSteps;
+  s.bytes = s.slots + (size_t)(parts < kMostParts ? parts : kMostParts) * kSlotFloats * sizeof(float);
+  return s;
+}
+size_t packed_grad_workspace(int tokens, int n_q_heads, int n_kv_heads) { return grad_space(tokens, n_q_heads, n_kv_heads).bytes; }
 
 hipError_t launch_packed_attention_grad(PackedCall call, hipStream_t stream) {
-  call.delta = static_cast<float*>(call.workspace);
-  const int64_t columns = (int64_t)call.tokens * call.group;
-  packed_grad_q_kernel<<<dim3((uint32_t)((columns + kColumns - 1) / kColumns), (uint32_t)call.n_kv_heads), kThreads, 0, stream>>>(call);
+  const GradSpace space = grad_space(call.tokens, call.n_q_heads, call.n_kv_heads);
+  char* work = static_cast<char*>(call.workspace);
+  call.delta = reinterpret_cast<float*>(work + space.delta);
+  call.plan = reinterpret_cast<PackedPlan*>(work + space.plan);
+  call.slots = reinterpret_cast<float*>(work + space.slots);
+  const int64_t columns = (int64_t)call.tokens * call.group, pairs = tiles_of(call.tokens) * call.n_kv_heads;
+  packed_grad_q_kernel<<<dim3((uint32_t)((columns + kColumns - 1) / kColumns) + 1, (uint32_t)call.n_kv_heads), kThreads, 0, stream>>>(call);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  packed_grad_kv_kernel<<<dim3((uint32_t)((call.tokens + kKeysHere - 1) / kKeysHere), (uint32_t)call.n_kv_heads), kThreads, 0, stream>>>(call);
+  const int64_t parts = (int64_t)(space.bytes - space.slots) / (int64_t)(kSlotFloats * sizeof(float));
+  packed_grad_kv_kernel<<<dim3((uint32_t)(pairs + parts)), kThreads, 0, stream>>>(call);
+  err = hipGetLastError();
+  if (err != hipSuccess || parts == 0) return err;
+  packed_grad_sum_kernel<<<dim3((uint32_t)pairs, 8), kThreads, 0, stream>>>(call);
   return hipGetLastError();
 }
 

@@ -36,10 +36,14 @@ bool heads_valid(int32_t tokens, int32_t n_q_heads, int32_t n_kv_heads) {
   const int group = n_q_heads / n_kv_heads;
   return group <= kMaxGroup && (int64_t)tokens * group < ((int64_t)1 << 30);
 }
+constexpr float kLeastSoftmaxScale = 8.67361738e-19f;          // 2^-60
+// Rows of a packed call: a tile's 64 are within 32 bits of its first.
+bool packed_rows(const rlkv_heads_t* t) { return readable(t, 2) && t->token_stride <= kMostTokenStride; }
+bool packed_out(const rlkv_heads_t* t, int64_t tokens, int64_t heads) { return writable(t, 2, tokens, heads) && t->token_stride <= kMostTokenStride; }
 bool packed_valid(const rlkv_packed_t* s) {
   if (!s || !heads_valid(s->tokens, s->n_q_heads, s->n_kv_heads)) return false;
   if (s->n_seqs < 0 || s->n_seqs == INT32_MAX || s->sink < 0) return false;
-  if (!(s->softmax_scale > 0.f) || isinf(s->softmax_scale)) return false;
+  if (!(s->softmax_scale >= kLeastSoftmaxScale && s->softmax_scale <= 1.f / kLeastSoftmaxScale)) return false;
   for (int h = 0; s->full_mask && h < s->n_kv_heads; ++h)
     if (s->full_mask[h] > 1 || (s->full_mask[h] == 0 && s->recent < 1)) return false;
   return true;
@@ -193,8 +197,8 @@ rlkv_status_t rlkv_packed_attention(const rlkv_packed_t* shape, const rlkv_heads
   if (!packed_valid(shape)) return RLKV_ERR_INVALID_ARG;
   if (shape->tokens == 0 || shape->n_seqs == 0) return RLKV_OK;
   if (!shape->offsets || !aligned(shape->offsets, 4) || !aligned(lse, 4)) return RLKV_ERR_INVALID_ARG;
-  if (!readable(q, 2) || !readable(k, 2) || !readable(v, 2)) return RLKV_ERR_INVALID_ARG;
-  if (!writable(out, 2, shape->tokens, shape->n_q_heads)) return RLKV_ERR_INVALID_ARG;
+  if (!packed_rows(q) || !packed_rows(k) || !packed_rows(v)) return RLKV_ERR_INVALID_ARG;
+  if (!packed_out(out, shape->tokens, shape->n_q_heads)) return RLKV_ERR_INVALID_ARG;
   PackedCall c = packed_call(shape);
   c.q = rows_of(q);
   c.k = rows_of(k);
@@ -216,9 +220,9 @@ rlkv_status_t rlkv_packed_attention_grad(const rlkv_packed_t* shape, const rlkv_
   if (!packed_valid(shape)) return RLKV_ERR_INVALID_ARG;
   if (shape->tokens == 0 || shape->n_seqs == 0) return RLKV_OK;
   if (!shape->offsets || !aligned(shape->offsets, 4) || !lse || !aligned(lse, 4)) return RLKV_ERR_INVALID_ARG;
-  if (!readable(q, 2) || !readable(k, 2) || !readable(v, 2) || !readable(out, 2) || !readable(grad_out, 2)) return RLKV_ERR_INVALID_ARG;
-  if (!writable(grad_q, 2, shape->tokens, shape->n_q_heads) || !writable(grad_k, 2, shape->tokens, shape->n_kv_heads) ||
-      !writable(grad_v, 2, shape->tokens, shape->n_kv_heads))
+  if (!packed_rows(q) || !packed_rows(k) || !packed_rows(v) || !packed_rows(out) || !packed_rows(grad_out)) return RLKV_ERR_INVALID_ARG;
+  if (!packed_out(grad_q, shape->tokens, shape->n_q_heads) || !packed_out(grad_k, shape->tokens, shape->n_kv_heads) ||
+      !packed_out(grad_v, shape->tokens, shape->n_kv_heads))
     return RLKV_ERR_INVALID_ARG;
   if (!workspace || !aligned(workspace, 16) || workspace_bytes < packed_grad_workspace(shape->tokens, shape->n_q_heads, shape->n_kv_heads))
     return RLKV_ERR_INVALID_ARG;
