@@ -544,7 +544,7 @@ typedef struct {
   int32_t n_seqs;           /* >= 0                                                                               */
   int32_t tokens;           /* rows of the tensors; those of no sequence are not written                                     */
   int32_t n_q_heads;        /* multiple of n_kv_heads; query head i reads KV head i / (n_q_heads / n_kv_heads); group at most 16 */
-  int32_t n_kv_heads;       /* at most 256; tokens * group is below 2^30                                             */
+  int32_t n_kv_heads;       /* at most 256; tokens * n_q_heads is below 2^30                                        */
   const uint8_t* full_mask; /* host [n_kv_heads], 1 = full, 0 = local; copied; NULL: all are full                   */
   int32_t sink, recent;     /* sink >= 0; recent >= 1 where a head is local                                         */
   float softmax_scale;      /* in [2^-60, 2^60]                                                                      */

@@ -11,6 +11,8 @@
 // has to have too (transposed_fragment).  So softmax weights never pass through LDS, and what belongs to a column stays in its two lanes.
 #pragma once
 
+#include <type_traits>
+
 #include "rlkv_internal.h"
 
 namespace rlkv {
@@ -153,6 +155,176 @@ __device__ __forceinline__ bf16x8 weights_fragment(const floatx16& x, int step) 
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = two_bf16(x[8 * step + 2 * i], x[8 * step + 2 * i + 1]);
   return __builtin_bit_cast(bf16x8, w);
+}
+
+// Result [d][column] as a row of the column's lanes: 16 bytes of it a store (the halves of the wavefront swap words).
+__device__ __forceinline__ void store_rows(uint16_t* row, const floatx16 (&x)[4], float scale, bool valid) {
+  typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+  const int half = (threadIdx.x >> 5) & 1;
+#pragma unroll
+  for (int b = 0; b < 4; ++b)
+#pragma unroll
+    for (int g = 0; g < 4; g += 2) {
+      words4 w;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t even = two_bf16(x[b][4 * g + 2 * i] * scale, x[b][4 * g + 2 * i + 1] * scale);
+        const uint32_t odd = two_bf16(x[b][4 * g + 4 + 2 * i] * scale, x[b][4 * g + 5 + 2 * i] * scale);
+        const u32x2 r = __builtin_amdgcn_permlane32_swap(even, odd, false, false);
+        w[i] = r[0];
+        w[2 + i] = r[1];
+      }
+      if (valid) *reinterpret_cast<words4*>(row + 32 * b + 8 * (g + half)) = w;
+    }
+}
+
+// x * 0 summed: 0, or NaN where any is not finite.
+__device__ __forceinline__ float zero_or_nan(const floatx16 (&x)[4]) {
+  float all = 0.f;
+#pragma unroll
+  for (int b = 0; b < 4; ++b)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) all += x[b][r] * 0.f;
+  return all;
+}
+__device__ __forceinline__ void clear(floatx16& x) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) x[r] = 0.f;
+}
+// acc[d][column] += sum over the rows of a 32-row tile of tile[row][d] * w[row][column] of admitted pairs, without the matrix instruction: a
+// weight of 0 does not keep an infinity or a NaN in the tile out of its products.
+template <typename F>
+__device__ __forceinline__ void admitted_products(const uint4* tile, int row0, const floatx16& w, floatx16 (&acc)[4], F admits) {
+  const int half = (threadIdx.x >> 5) & 1;
+  for (int row = 0; row < 32; ++row) {
+    float x = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (8 * (r >> 2) + (r & 3) == (row & ~4)) x = w[r];
+    const float other = other_half(x);
+    if (((row >> 2) & 1) != half) x = other;
+    if (!admits(row)) continue;
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int d = 32 * b + 8 * g + 4 * half;
+        const words2 two = *reinterpret_cast<const words2*>(reinterpret_cast<const char*>(tile + unit_at(row0 + row, d >> 3)) + 2 * (d & 7));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[b][4 * g + e] += x * __uint_as_float(e & 1 ? two[e >> 1] & 0xffff0000u : two[e >> 1] << 16);
+      }
+  }
+}
+
+// ---- a workgroup of 256 columns and the tiles of keys that it walks over ----
+constexpr int kPackedWaves = 8, kPackedThreads = 64 * kPackedWaves;
+constexpr int kColumns = 32 * kPackedWaves, kKeys = kStageRows;
+
+// The n-th KV head of a launch: full ones in front of local ones, so that the long workgroups are handed out first, and neighbours in the launch
+// (which the hardware deals to the 8 XCDs in turn) are of different heads: a head's keys are then read by few of the L2s.
+__device__ __forceinline__ int head_in_order(const PackedCall& c, int n, bool& full) {
+  int n_full = 0;
+  for (int w = 0; w < kPackedMaskWords; ++w) n_full += __popcll(c.full[w]);
+  full = n < n_full;
+  if (!full) n -= n_full;
+  for (int w = 0;; ++w) {
+    uint64_t bits = full ? c.full[w] : ~c.full[w];
+    const int here = __popcll(bits);
+    if (n >= here) {
+      n -= here;
+      continue;
+    }
+    for (; n; --n) bits &= bits - 1;
+    return w * 64 + __builtin_ctzll(bits);
+  }
+}
+// Block and head of the launch's workgroup `index`: of all full heads the last blocks first, then of the local ones.
+struct ColumnBlock { int block, head; bool full; };
+__device__ __forceinline__ ColumnBlock column_block(const PackedCall& c, uint32_t index, uint32_t blocks) {
+  int n_full = 0;
+  for (int w = 0; w < kPackedMaskWords; ++w) n_full += __popcll(c.full[w]);
+  ColumnBlock b;
+  uint32_t n;
+  if (index < blocks * n_full) {
+    b.block = blocks - 1 - index / n_full;
+    n = index % n_full;
+  } else {
+    index -= blocks * n_full;
+    const uint32_t n_local = c.n_kv_heads - n_full;
+    b.block = blocks - 1 - index / n_local;
+    n = n_full + index % n_local;
+  }
+  b.head = head_in_order(c, n, b.full);
+  return b;
+}
+
+struct ColumnSmem {
+  int32_t offsets[kOffsetsInLds];
+  int32_t first[kPackedWaves], begin[kPackedWaves], last[kPackedWaves];
+};
+struct Columns {
+  int pos, head, begin;                            // of the lane's column; begin: of its sequence
+  bool valid, full;                                // a column of no sequence reads row 0 and writes nothing
+  int64_t row;
+  int pos_lo, pos_hi, begin_lo, begin_hi;          // of the wavefront's
+  int sink, recent;
+  int keys_begin, band, sink_tiles, tiles;         // of the workgroup: tiles of a full head from keys_begin on; of a local one those of the sinks
+                                                   // of the first sequence, then from the first position's band on (the block's later sequences
+                                                   // begin behind its first position)
+  __device__ __forceinline__ int tile_key(int t) const { return t < sink_tiles ? keys_begin + t * kKeys : band + (t - sink_tiles) * kKeys; }
+  __device__ __forceinline__ bool admits(int key) const {
+    return key <= pos && key >= begin && (full || key - begin < sink || pos - key < recent);
+  }
+  // whether any, and whether all columns of the wavefront admit any, all of `n` keys from k0 on
+  __device__ __forceinline__ bool any_of(int k0, int n) const {
+    return k0 <= pos_hi && k0 + n > begin_lo && (full || k0 - begin_hi < sink || pos_lo - (k0 + n - 1) < recent);
+  }
+  __device__ __forceinline__ bool all_of(int k0, int n) const {
+    return k0 + n - 1 <= pos_lo && k0 >= begin_hi && (full || k0 + n - 1 - begin_lo < sink || pos_hi - k0 < recent);
+  }
+};
+// False: no column of the block is of a sequence.
+__device__ __forceinline__ bool set_columns(const PackedCall& c, const int32_t* offsets, const ColumnBlock& b, ColumnSmem& sm, Columns& x) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const uint32_t column = (uint32_t)b.block * kColumns + wave * 32 + (lane & 31);
+  x.pos = (int)(column / (uint32_t)c.group);
+  x.head = b.head * c.group + (int)(column - (uint32_t)x.pos * c.group);
+  x.full = b.full;
+  x.sink = c.sink;
+  x.recent = c.recent;
+  const Span span = span_of(offsets, c.n_seqs, c.tokens, x.pos);
+  x.valid = span.begin >= 0;
+  x.begin = x.valid ? span.begin : 0;
+  x.row = x.valid ? x.pos : 0;
+  x.pos_lo = min_of_lanes(x.valid ? x.pos : INT32_MAX);
+  x.pos_hi = max_of_lanes(x.valid ? x.pos : -1);
+  x.begin_lo = min_of_lanes(x.valid ? x.begin : INT32_MAX);
+  x.begin_hi = max_of_lanes(x.valid ? x.begin : -1);
+  if (lane == 0) {
+    sm.first[wave] = x.pos_lo;
+    sm.begin[wave] = x.begin_lo;
+    sm.last[wave] = x.pos_hi;
+  }
+  __syncthreads();
+  int first = INT32_MAX, last = -1;
+  x.keys_begin = INT32_MAX;
+#pragma unroll
+  for (int w = 0; w < kPackedWaves; ++w) {
+    first = min(first, sm.first[w]);
+    x.keys_begin = min(x.keys_begin, sm.begin[w]);
+    last = max(last, sm.last[w]);
+  }
+  if (last < 0) return false;
+  x.sink_tiles = x.full ? 0 : (int)(((int64_t)min(c.sink, last + 1 - x.keys_begin) + kKeys - 1) / kKeys);
+  x.band = x.full ? x.keys_begin : max(x.keys_begin + x.sink_tiles * kKeys, first - c.recent + 1);
+  x.tiles = x.sink_tiles + (x.band > last ? 0 : (last - x.band) / kKeys + 1);
+  return true;
+}
+__device__ __forceinline__ const int32_t* offsets_of(const PackedCall& c, int32_t* here) {
+  if (c.n_seqs >= kOffsetsInLds) return c.offsets;
+  for (int i = threadIdx.x; i <= c.n_seqs; i += kPackedThreads) here[i] = c.offsets[i];
+  __syncthreads();
+  return here;
 }
 
 }  // namespace rlkv

@@ -13,56 +13,8 @@
 namespace rlkv {
 namespace {
 
-constexpr int kWaves = 8, kThreads = 64 * kWaves;
+constexpr int kWaves = kPackedWaves, kThreads = kPackedThreads;
 
-// x * 0 summed: 0, or NaN where any is not finite.
-__device__ __forceinline__ float zero_or_nan(const floatx16 (&x)[4]) {
-  float all = 0.f;
-#pragma unroll
-  for (int b = 0; b < 4; ++b)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) all += x[b][r] * 0.f;
-  return all;
-}
-__device__ __forceinline__ void clear(floatx16& x) {
-#pragma unroll
-  for (int r = 0; r < 16; ++r) x[r] = 0.f;
-}
-// acc[d][column] += sum over the rows of a 32-row tile of tile[row][d] * w[row][column] of admitted pairs, without the matrix instruction: a
-// weight of 0 does not keep an infinity or a NaN in the tile out of its products.
-template <typename F>
-__device__ __forceinline__ void admitted_products(const uint4* tile, int row0, const floatx16& w, floatx16 (&acc)[4], F admits) {
-  const int half = (threadIdx.x >> 5) & 1;
-  for (int row = 0; row < 32; ++row) {
-    float x = 0.f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-      if (8 * (r >> 2) + (r & 3) == (row & ~4)) x = w[r];
-    const float other = other_half(x);
-    if (((row >> 2) & 1) != half) x = other;
-    if (!admits(row)) continue;
-#pragma unroll
-    for (int b = 0; b < 4; ++b)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int d = 32 * b + 8 * g + 4 * half;
-        const words2 two = *reinterpret_cast<const words2*>(reinterpret_cast<const char*>(tile + unit_at(row0 + row, d >> 3)) + 2 * (d & 7));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[b][4 * g + e] += x * __uint_as_float(e & 1 ? two[e >> 1] & 0xffff0000u : two[e >> 1] << 16);
-      }
-  }
-}
-// Result [d][column] as a row of the column's lanes.
-__device__ __forceinline__ void store_rows(uint16_t* row, const floatx16 (&x)[4], float scale) {
-  const int half = (threadIdx.x >> 5) & 1;
-#pragma unroll
-  for (int b = 0; b < 4; ++b)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const words2 w = {two_bf16(x[b][4 * g] * scale, x[b][4 * g + 1] * scale), two_bf16(x[b][4 * g + 2] * scale, x[b][4 * g + 3] * scale)};
-      *reinterpret_cast<words2*>(row + 32 * b + 8 * g + 4 * half) = w;
-    }
-}
 __device__ __forceinline__ float dot_of_units(uint4 a, uint4 b) {
   const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
   float sum = 0.f;
@@ -152,146 +104,98 @@ __device__ void make_plan(const PackedCall& c, const int32_t* offsets, PlanSmem&
 }
 
 // ---- queries ------------------------------------------------------------------------------------------------------------------
-constexpr int kColumns = 32 * kWaves, kKeys = 64;
-constexpr int kKeyUnits = kKeys * 16 / kThreads;
-
-struct QuerySmem {
-  uint4 k[2][kKeys * 16], v[2][kKeys * 16];
-  int32_t offsets[kOffsetsInLds];
-  int32_t first[kWaves], begin[kWaves], last[kWaves];
-  PlanSmem plan;
-};
-
-__global__ __launch_bounds__(kThreads) void packed_grad_q_kernel(PackedCall c) {
-  __shared__ QuerySmem sm;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5;
-  const int h = blockIdx.y, group = c.group;
-  const bool full = (c.full[h >> 6] >> (h & 63)) & 1;
-  const int32_t* offsets = c.offsets;
-  if (c.n_seqs < kOffsetsInLds) {
-    for (int i = threadIdx.x; i <= c.n_seqs; i += kThreads) sm.offsets[i] = c.offsets[i];
-    __syncthreads();
-    offsets = sm.offsets;
-  }
-  if (blockIdx.x == 0) {                                     // (the first workgroup of the launch is none of its own)
-    if (h == 0) make_plan(c, offsets, sm.plan);
+__global__ __launch_bounds__(kThreads) void packed_grad_q_kernel(PackedCall c, uint32_t blocks) {
+  __shared__ uint4 k0[kKeys * 16], k1[kKeys * 16], v0[kKeys * 16], v1[kKeys * 16];
+  __shared__ ColumnSmem sm;
+  __shared__ PlanSmem plan;
+  const int half = (threadIdx.x >> 5) & 1;
+  const int32_t* offsets = offsets_of(c, sm.offsets);
+  if (blockIdx.x == 0) {                                     // (the launch's first workgroup plans the next launch)
+    make_plan(c, offsets, plan);
     return;
   }
-  const int64_t column = (int64_t)(blockIdx.x - 1) * kColumns + wave * 32 + (lane & 31);
-  const int pos = (int)(column / group);
-  const int head = h * group + (int)(column - (int64_t)pos * group);
-  const Span span = span_of(offsets, c.n_seqs, c.tokens, pos);
-  const bool valid = span.begin >= 0;
-  const int begin = valid ? span.begin : 0;
-  const int64_t row = valid ? pos : 0;
-  const int pos_lo = min_of_lanes(valid ? pos : INT32_MAX), pos_hi = max_of_lanes(valid ? pos : -1);
-  const int begin_lo = min_of_lanes(valid ? begin : INT32_MAX), begin_hi = max_of_lanes(valid ? begin : -1);
-  if (lane == 0) {
-    sm.first[wave] = pos_lo;
-    sm.begin[wave] = begin_lo;
-    sm.last[wave] = pos_hi;
-  }
-  __syncthreads();
-  int first = INT32_MAX, keys_begin = INT32_MAX, last = -1;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    first = min(first, sm.first[w]);
-    keys_begin = min(keys_begin, sm.begin[w]);
-    last = max(last, sm.last[w]);
-  }
-  if (last < 0) return;
+  const ColumnBlock block = column_block(c, blockIdx.x - 1, blocks);
+  Columns x;
+  if (!set_columns(c, offsets, block, sm, x)) return;
 
   bf16x8 q[8], g[8];
-  float delta = 0.f;
-  const uint16_t* q_row = c.q.p + row * c.q.token + head * c.q.head + 8 * half;
-  const uint16_t* g_row = c.grad_out.p + row * c.grad_out.token + head * c.grad_out.head + 8 * half;
-  const uint16_t* o_row = c.out.p + row * c.out.token + head * c.out.head + 8 * half;
+  float delta = 0.f, lse = 0.f;
+  {
+    const uint16_t* q_row = c.q.p + x.row * c.q.token + x.head * c.q.head + 8 * half;
+    const uint16_t* g_row = c.grad_out.p + x.row * c.grad_out.token + x.head * c.grad_out.head + 8 * half;
+    const uint16_t* o_row = c.out.p + x.row * c.out.token + x.head * c.out.head + 8 * half;
+    const int64_t at = (int64_t)x.head * c.tokens + x.pos;
+    if (x.valid) lse = c.lse[at] * kLog2e;
 #pragma unroll
-  for (int s = 0; s < 8; ++s) {
-    q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(q_row + 16 * s));
-    const uint4 gw = *reinterpret_cast<const uint4*>(g_row + 16 * s);
-    g[s] = __builtin_bit_cast(bf16x8, gw);
-    delta += dot_of_units(gw, *reinterpret_cast<const uint4*>(o_row + 16 * s));
+    for (int s = 0; s < 8; ++s) {
+      q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(q_row + 16 * s));
+      const uint4 gw = *reinterpret_cast<const uint4*>(g_row + 16 * s);
+      g[s] = __builtin_bit_cast(bf16x8, gw);
+      delta += dot_of_units(gw, *reinterpret_cast<const uint4*>(o_row + 16 * s));
+    }
+    delta = sum_of_halves(delta);
+    if (x.valid && half == 0) c.delta[at] = delta;
   }
-  delta = sum_of_halves(delta);
-  const float lse = valid ? c.lse[(int64_t)head * c.tokens + pos] * kLog2e : 0.f;
-  if (valid && half == 0) c.delta[(int64_t)head * c.tokens + pos] = delta;
-
-  const int sink_tiles = full ? 0 : (int)(((int64_t)min(c.sink, last + 1 - keys_begin) + kKeys - 1) / kKeys);
-  const int band = full ? keys_begin : max(keys_begin + sink_tiles * kKeys, first - c.recent + 1);
-  const int tiles = sink_tiles + (band > last ? 0 : (last - band) / kKeys + 1);
-  auto tile_key = [&](int t) { return t < sink_tiles ? keys_begin + t * kKeys : band + (t - sink_tiles) * kKeys; };
-
-  uint4 next_k[kKeyUnits], next_v[kKeyUnits];
-  auto fetch = [&](int t) {
-    const int k0 = tile_key(t);
-#pragma unroll
-    for (int i = 0; i < kKeyUnits; ++i) {
-      const int at = threadIdx.x + i * kThreads, r = min(k0 + (at >> 4), c.tokens - 1), u = at & 15;
-      next_k[i] = *reinterpret_cast<const uint4*>(c.k.p + (int64_t)r * c.k.token + h * c.k.head + u * 8);
-      next_v[i] = *reinterpret_cast<const uint4*>(c.v.p + (int64_t)r * c.v.token + h * c.v.head + u * 8);
-    }
-  };
-  auto place = [&](int slot) {
-#pragma unroll
-    for (int i = 0; i < kKeyUnits; ++i) {
-      const int at = threadIdx.x + i * kThreads;
-      sm.k[slot][unit_at(at >> 4, at & 15)] = next_k[i];
-      sm.v[slot][unit_at(at >> 4, at & 15)] = next_v[i];
-    }
-  };
   const float scale = c.scale * kLog2e;
-  auto admits = [&](int key) { return key <= pos && key >= begin && (full || key - begin < c.sink || pos - key < c.recent); };
+  auto ask = [&](auto odd, int t) {
+    constexpr int kOdd = decltype(odd)::value;
+    stage_rows(c.k, x.tile_key(t), block.head, c.tokens, kOdd ? k1 : k0);
+    stage_rows(c.v, x.tile_key(t), block.head, c.tokens, kOdd ? v1 : v0);
+  };
 
   floatx16 dq[4];
-  for (int careful = 0;; careful = 1) {
+  auto walk = [&](auto careful) {
+    constexpr bool kCareful = decltype(careful)::value;
 #pragma unroll
     for (int b = 0; b < 4; ++b) clear(dq[b]);
-    fetch(0);
-    place(0);
-    __syncthreads();
-    for (int t = 0; t < tiles; ++t) {
-      const int slot = t & 1, k0 = tile_key(t), k1 = k0 + kKeys - 1;
-      if (t + 1 < tiles) fetch(t + 1);
-      const bool some = k0 <= pos_hi && k1 >= begin_lo && (full || k0 - begin_hi < c.sink || pos_lo - k1 < c.recent);
-      if (some) {
-        const bool all = k1 <= pos_lo && k0 >= begin_hi && (full || k1 - begin_lo < c.sink || pos_hi - k0 < c.recent);
+    ask(std::integral_constant<int, 0>{}, 0);
+    auto step = [&](auto odd, int t) {
+      constexpr int kOdd = decltype(odd)::value;
+      const uint4 *kt = kOdd ? k1 : k0, *vt = kOdd ? v1 : v0;
+      __syncthreads();
+      if (t + 1 < x.tiles) ask(std::integral_constant<int, 1 - kOdd>{}, t + 1);
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          floatx16 x, y;
-          clear(x);
-          clear(y);
+      for (int b = 0; b < kKeys; b += 32) {
+        const int key = x.tile_key(t) + b;
+        if (!x.any_of(key, 32)) continue;
+        const bool all = x.all_of(key, 32);
+        floatx16 w, z;
+        clear(w);
+        clear(z);
 #pragma unroll
-          for (int s = 0; s < 8; ++s) {
-            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(sm.k[slot], 32 * b, s), q[s], x, 0, 0, 0);
-            y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(sm.v[slot], 32 * b, s), g[s], y, 0, 0, 0);
-          }
+        for (int s = 0; s < 8; ++s) {
+          w = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(kt, b, s), q[s], w, 0, 0, 0);
+          z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(vt, b, s), g[s], z, 0, 0, 0);
+        }
 #pragma unroll
-          for (int r = 0; r < 16; ++r) x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[r], scale, -lse)) * (y[r] - delta);
-          if (!all) {
+        for (int r = 0; r < 16; ++r) z[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(w[r], scale, -lse)) * (z[r] - delta);
+        if (!all) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-              if (!admits(k0 + 32 * b + 8 * (r >> 2) + 4 * half + (r & 3))) x[r] = 0.f;
-          }
-          if (careful && !all) {
-            admitted_products(sm.k[slot], 32 * b, x, dq, [&](int r) { return admits(k0 + 32 * b + r); });
-          } else {
+          for (int r = 0; r < 16; ++r)
+            if (!x.admits(key + 8 * (r >> 2) + 4 * half + (r & 3))) z[r] = 0.f;
+        }
+        if (kCareful && !all) {
+          admitted_products(kt, b, z, dq, [&](int r) { return x.admits(key + r); });
+        } else {
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-              const bf16x8 z = weights_fragment(x, s);
+          for (int s = 0; s < 2; ++s) {
+            const bf16x8 p = weights_fragment(z, s);
 #pragma unroll
-              for (int d = 0; d < 4; ++d)
-                dq[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_fragment(sm.k[slot], 32 * b + 16 * s, d), z, dq[d], 0, 0, 0);
-            }
+            for (int d = 0; d < 4; ++d) dq[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_fragment(kt, b + 16 * s, d), p, dq[d], 0, 0, 0);
           }
         }
       }
-      if (t + 1 < tiles) place(slot ^ 1);
-      __syncthreads();
+    };
+    int t = 0;
+    for (; t + 1 < x.tiles; t += 2) {
+      step(std::integral_constant<int, 0>{}, t);
+      step(std::integral_constant<int, 1>{}, t + 1);
     }
-    if (careful || !__syncthreads_or(valid && zero_or_nan(dq) != 0.f)) break;
-  }
-  if (valid) store_rows(c.grad_q.p + row * c.grad_q.token + head * c.grad_q.head, dq, c.scale);
+    if (t < x.tiles) step(std::integral_constant<int, 0>{}, t);
+  };
+  walk(std::false_type{});
+  if (__syncthreads_or(x.valid && zero_or_nan(dq) != 0.f)) walk(std::true_type{});
+  store_rows(c.grad_q.p + x.row * c.grad_q.token + x.head * c.grad_q.head, dq, c.scale, x.valid);
 }
 
 // ---- keys and values ----------------------------------------------------------------------------------------------------------
@@ -318,12 +222,7 @@ __global__ __launch_bounds__(kThreads) void packed_grad_kv_kernel(PackedCall c) 
   const PlanItem item = items_of(c.plan)[blockIdx.x];
   const int h = item.head, group = c.group;
   const bool full = (c.full[h >> 6] >> (h & 63)) & 1;
-  const int32_t* offsets = c.offsets;
-  if (c.n_seqs < kOffsetsInLds) {
-    for (int i = threadIdx.x; i <= c.n_seqs; i += kThreads) seqs[i] = c.offsets[i];
-    __syncthreads();
-    offsets = seqs;
-  }
+  const int32_t* offsets = offsets_of(c, seqs);
   const int at = item.tile * kKeysHere + (threadIdx.x >> 6) * 32 + (lane & 31);
   const Span span = span_of(offsets, c.n_seqs, c.tokens, at);
   const bool valid = span.begin >= 0;
@@ -449,9 +348,8 @@ __global__ __launch_bounds__(kThreads) void packed_grad_kv_kernel(PackedCall c) 
     }
     return;
   }
-  if (!valid) return;
-  store_rows(c.grad_k.p + (int64_t)key * c.grad_k.token + h * c.grad_k.head, dk, c.scale);
-  store_rows(c.grad_v.p + (int64_t)key * c.grad_v.token + h * c.grad_v.head, dv, 1.f);
+  store_rows(c.grad_k.p + (int64_t)key * c.grad_k.token + h * c.grad_k.head, dk, c.scale, valid);
+  store_rows(c.grad_v.p + (int64_t)key * c.grad_v.token + h * c.grad_v.head, dv, 1.f, valid);
 }
 
 // The slots of keys that workgroups shared, added up in the order of their steps: four pieces of a lane a workgroup.
@@ -510,8 +408,9 @@ hipError_t launch_packed_attention_grad(PackedCall call, hipStream_t stream) {
   call.delta = reinterpret_cast<float*>(work + space.delta);
   call.plan = reinterpret_cast<PackedPlan*>(work + space.plan);
   call.slots = reinterpret_cast<float*>(work + space.slots);
-  const int64_t columns = (int64_t)call.tokens * call.group, pairs = tiles_of(call.tokens) * call.n_kv_heads;
-  packed_grad_q_kernel<<<dim3((uint32_t)((columns + kColumns - 1) / kColumns) + 1, (uint32_t)call.n_kv_heads), kThreads, 0, stream>>>(call);
+  const uint32_t blocks = (uint32_t)(((int64_t)call.tokens * call.group + kColumns - 1) / kColumns);
+  const int64_t pairs = tiles_of(call.tokens) * call.n_kv_heads;
+  packed_grad_q_kernel<<<blocks * (uint32_t)call.n_kv_heads + 1, kThreads, 0, stream>>>(call, blocks);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
   const int64_t parts = (int64_t)(space.bytes - space.slots) / (int64_t)(kSlotFloats * sizeof(float));

@@ -34,7 +34,7 @@ HeadRows rows_of(const rlkv_heads_t* t) { return {static_cast<uint16_t*>(t->data
 bool heads_valid(int32_t tokens, int32_t n_q_heads, int32_t n_kv_heads) {
   if (tokens < 0 || n_kv_heads < 1 || n_kv_heads > kPackedHeads || n_q_heads < 1 || n_q_heads % n_kv_heads != 0) return false;
   const int group = n_q_heads / n_kv_heads;
-  return group <= kMaxGroup && (int64_t)tokens * group < ((int64_t)1 << 30);
+  return group <= kMaxGroup && (int64_t)tokens * n_q_heads < ((int64_t)1 << 30);      // (two threads a column, below 2^32)
 }
 constexpr float kLeastSoftmaxScale = 8.67361738e-19f;          // 2^-60
 // Rows of a packed call: a tile's 64 are within 32 bits of its first.
