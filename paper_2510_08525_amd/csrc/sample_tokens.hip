@@ -4,8 +4,15 @@
 //   weights reach top_p of their sum, of those the ones with w >= min_p;  token = first kept i with  sum of kept w[0 .. i] > u * sum of kept w
 //
 // Weights are whole numbers of 2^-bits, bits = 62 - log2(vocab), from an exponential in 64 bits: their sums are exact in 64-bit integers, in whatever
-// order they are formed, so atomics and scans give the same token at every call, and borders between tokens are within 2^-bits of where the
-// formula has them (2^-45 for 131072 tokens; what fp32 sums leave, 2^-24 of a border's place, changes a token of 128k in one of hundred rows).
+// order they are formed, so atomics and scans give the same token at every call, and borders between tokens are where the formula has them to 2^-39
+// of the weights (what sums in 32 bits leave, 2^-24 of a border's place, changes a token of 128k in one of hundred rows).
+//
+// A row is read by as many workgroups as it has parts of 2048 or 8192 tokens.  Launches, of which rows without filters need the first and the last:
+//   parts    largest logit and, for rows whose sum is asked for, the sum of weights of a part
+//   bins     of rows with top_k or top_p: how many tokens, and what weight, lie in each of 2048 steps down from the largest logit
+//   collect  the step in which the cut falls: its tokens go into a list; the weight of a part's tokens above it
+//   draw     one workgroup a row: the cut among the list's tokens, the part that the number falls into, the token in it
+// A row whose list would be too long (thousands of like logits at the cut, a top_k of thousands) is cut by its last workgroup alone, in passes over the row.
 #include "sample_tokens.h"
 #include "token_ops.h"
 
@@ -14,13 +21,121 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 2048;
 constexpr int kTileTokens = kThreads * 8;
-constexpr float kBinsPerUnit = 32.f;      // bins of the first turn: the way from the largest logit over the temperature, 64 of it
+constexpr float kBinsPerUnit = 32.f;      // bins: the way from the largest logit over the temperature, 64 of it
+constexpr int kList = 2048;               // tokens of a row's list
+constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64;
+constexpr int kRowsAtOnce = 512;          // rows that have a workspace
 
 // Ascending with x; zeros of either sign are the same.
 __device__ __forceinline__ uint32_t key_of(float x) {
   const uint32_t b = __float_as_uint(x + 0.f);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ unsigned long long sum_over_wave(unsigned long long x) {
+  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
+  return x;
+}
+
+// 2^(j / 32)
+__constant__ double kRoots[32] = {
+    0x1.0000000000000p+0, 0x1.059b0d3158574p+0, 0x1.0b5586cf9890fp+0, 0x1.11301d0125b51p+0,
+    0x1.172b83c7d517bp+0, 0x1.1d4873168b9aap+0, 0x1.2387a6e756238p+0, 0x1.29e9df51fdee1p+0,
+    0x1.306fe0a31b715p+0, 0x1.371a7373aa9cbp+0, 0x1.3dea64c123422p+0, 0x1.44e086061892dp+0,
+    0x1.4bfdad5362a27p+0, 0x1.5342b569d4f82p+0, 0x1.5ab07dd485429p+0, 0x1.6247eb03a5585p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.71f75e8ec5f74p+0, 0x1.7a11473eb0187p+0, 0x1.82589994cce13p+0,
+    0x1.8ace5422aa0dbp+0, 0x1.93737b0cdc5e5p+0, 0x1.9c49182a3f090p+0, 0x1.a5503b23e255dp+0,
+    0x1.ae89f995ad3adp+0, 0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0,
+    0x1.d5818dcfba487p+0, 0x1.dfc97337b9b5fp+0, 0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0};
+
+// The weight of a logit: 2^bits exp((x - ref) / t), rounded to a whole number; 0 below a half and for what is masked.
+// With z = 32 log2(e) (x - ref) / t = 32 n + j + r, |r| <= 1/2:  2^n 2^(j / 32) (1 + a r + .. + (a r)^4 / 24), a = ln(2) / 32: the series ends 1.2e-12 of it.
+struct Weight {
+  const double* roots;       // in LDS: the lanes' places are in banks of their own
+  double ref, c;             // 32 log2(e) / t
+  int bits;
+  double least;              // least weight that counts, of 2^bits (min_p)
+  __device__ __forceinline__ unsigned long long operator()(float x) const {
+    const double z = ((double)x - ref) * c;
+    if (!(z >= -32. * (bits + 1))) return 0;             // (a masked logit's place is -infinity, or NaN where the temperature is infinite)
+    const double shifted = z + 6755399441055744.;        // 1.5 * 2^52: the nearest whole number in the low bits
+    const int k = (int)(uint32_t)__double_as_longlong(shifted);
+    const double r = z - (shifted - 6755399441055744.);
+    constexpr double a = 0.69314718055994530942 / 32;
+    double p = __builtin_fma(r, a * a * a * a / 24, a * a * a / 6);
+    p = __builtin_fma(r, p, a * a / 2);
+    p = __builtin_fma(r, p, a);
+    p = __builtin_fma(r, p, 1.);
+    const double w = ldexp(roots[k & 31] * p, (k >> 5) + bits);
+    return w >= least ? (unsigned long long)__double_as_longlong(w + 4503599627370496.) - 0x4330000000000000ull : 0;      // 2^52
+  }
+};
+// (w below 2^51: bits is at most 50 then)
+__host__ __device__ inline int bits_of(int vocab) {
+  int bits = 62;
+  for (int64_t n = 1; n < vocab; n *= 2) --bits;
+  return bits < 50 ? bits : 50;
+}
+
+struct Settings {
+  double t, top_p, min_p;
+  int top_k;                 // 0: off, and so where it is no less than vocab
+  __device__ bool greedy() const { return !(t > 0.); }
+  __device__ bool cut() const { return !greedy() && (top_k > 0 || top_p < 1.); }
+  __device__ bool filter() const { return cut() || (!greedy() && min_p > 0.); }
+};
+__device__ __forceinline__ Settings settings_of(const SampleCall& c, int64_t n) {
+  Settings s;
+  s.t = c.temperatures ? c.temperatures[n] : c.temperature;
+  s.top_p = c.top_ps ? c.top_ps[n] : c.top_p;
+  s.min_p = c.min_ps ? c.min_ps[n] : c.min_p;
+  s.top_k = c.top_ks ? c.top_ks[n] : c.top_k;
+  if (s.top_k >= c.vocab || s.top_k < 0) s.top_k = 0;
+  if (!(s.top_p < 1.)) s.top_p = 1.;
+  if (s.top_p < 0.) s.top_p = 0.;
+  s.min_p = s.min_p > 0. ? (s.min_p < 1. ? s.min_p : 1.) : 0.;
+  return s;
+}
+// (1 / t is at most 1e300: a way of 0 stays 0)
+__device__ __forceinline__ double inverse(double t) { return t > 1e-300 ? 1. / t : 1e300; }
+__device__ __forceinline__ Weight weight_of(const Settings& s, const double* roots, double ref, int bits, double least) {
+  return {roots, ref, inverse(s.t) * (32 * 1.4426950408889634074), bits, least};
+}
+
+// Steps down from the largest logit; not decreasing as x falls.
+struct FirstBin {
+  float top, per;
+  __device__ __forceinline__ int operator()(float x) const {
+    const float z = (top - x) * per;
+    return z < (float)(kBins - 1) ? (int)z : kBins - 1;       // (NaN, of a masked logit at an infinite temperature: the last)
+  }
+};
+__device__ __forceinline__ FirstBin first_bin(float top, const Settings& s) { return {top, (float)inverse(s.t) * kBinsPerUnit}; }
+
+// ---- the workspace ----
+struct Part {
+  float top;
+  int32_t bad;                     // a NaN or +inf is there
+  unsigned long long sum;          // of weights with the part's largest logit for reference
+  unsigned long long above;        // of weights above the cut's bin that min_p keeps, with the row's largest for reference
+};
+struct RowCut {
+  int32_t listed;                  // tokens of the list; more than kList: there is no list
+  int32_t pad;
+  unsigned long long before;       // weight of the tokens above the list's
+};
+struct RowSpace {
+  unsigned long long mass[kBins];
+  uint32_t count[kBins];
+  unsigned long long list[kList];  // ~key, token: ascending is the order of the cut
+  RowCut cut;
+};
+__host__ __device__ inline int part_tokens(int64_t rows, int64_t vocab) { return rows * ((vocab + 8191) / 8192) >= 512 ? 8192 : 2048; }
+struct Space {
+  RowSpace* rows;
+  Part* parts;                     // [rows][n_parts]
+  int32_t n_parts, part;
+  int64_t first_row;               // of the launch
+};
 
 struct Smem {
   unsigned long long mass[kBins];
@@ -30,28 +145,16 @@ struct Smem {
   unsigned long long found_before, found_mass;
   uint32_t found, found_count;
   int32_t index;
+  double roots[32];
 };
 
-__device__ __forceinline__ unsigned long long sum_over_wave(unsigned long long x) {
-  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
-  return x;
-}
-
+// What is kept: keys above `key`, and `key` itself up to the place `last`.
 struct Row {
-  double top, inv_t;        // largest logit, 1 / temperature
-  double unit;              // weight 1 in whole numbers
-  double least;             // the logit's way from the largest over the temperature below which a weight is 0
-  double min_w;             // least weight that is kept
-  // a token is kept if its key is above `key`, or is `key` and its place is at most `last`
+  float top;
+  Settings how;
   uint32_t key;
   int32_t last;
 };
-__device__ __forceinline__ unsigned long long weight_of(const Row& r, float x) {
-  const double z = ((double)x - r.top) * r.inv_t;
-  if (!(z >= r.least)) return 0;           // (a masked logit's place is -infinity, or NaN where the temperature is infinite)
-  const double w = exp(z);
-  return w >= r.min_w ? (unsigned long long)(w * r.unit + 0.5) : 0;
-}
 __device__ __forceinline__ bool keeps(const Row& r, float x, int i) {
   const uint32_t key = key_of(x);
   return key > r.key || (key == r.key && i <= r.last);
@@ -143,16 +246,12 @@ __device__ void bin_of(Smem& sm, bool by_mass, unsigned long long target) {
 // Cuts the kept tokens of `r` to the first ones in order of their logits: to `target` of them, or (by_mass) to those in front of which the weights
 // sum to less than `target`.  There are more of them.
 template <typename T>
-__device__ void cut(Smem& sm, const T* row, int vocab, Row& r, bool by_mass, unsigned long long target) {
-  const float top = (float)r.top, per = (float)r.inv_t * kBinsPerUnit;
-  auto first_bin = [&](float x) {
-    const float z = (top - x) * per;
-    return z < (float)(kBins - 1) ? (int)z : kBins - 1;       // (NaN, of a masked logit at an infinite temperature: the last)
-  };
+__device__ void cut(Smem& sm, const T* row, int vocab, Row& r, const Weight& weight, bool by_mass, unsigned long long target) {
+  const FirstBin bin_at = first_bin(r.top, r.how);
   auto add = [&](int bin, float x) {
     atomicAdd(&sm.count[bin], 1u);
     if (by_mass) {
-      const unsigned long long w = weight_of(r, x);
+      const unsigned long long w = weight(x);
       if (w) atomicAdd(&sm.mass[bin], w);
     }
   };
@@ -167,7 +266,7 @@ __device__ void cut(Smem& sm, const T* row, int vocab, Row& r, bool by_mass, uns
   const unsigned long long last = target - 1;      // (the token that reaches the target is kept)
   clear();
   each_token(row, 0, vocab, threadIdx.x, kThreads, [&](float x, int i) {
-    if (keeps(r, x, i)) add(first_bin(x), x);
+    if (keeps(r, x, i)) add(bin_at(x), x);
   });
   __syncthreads();
   bin_of(sm, by_mass, last);
@@ -176,7 +275,7 @@ __device__ void cut(Smem& sm, const T* row, int vocab, Row& r, bool by_mass, uns
   // the keys of that bin, and by them bins of fewer and fewer keys
   uint32_t low = 0xffffffffu, high = 0;
   each_token(row, 0, vocab, threadIdx.x, kThreads, [&](float x, int i) {
-    if (first_bin(x) != bin || !keeps(r, x, i)) return;
+    if (bin_at(x) != bin || !keeps(r, x, i)) return;
     const uint32_t k = key_of(x);
     low = k < low ? k : low;
     high = k > high ? k : high;
@@ -226,51 +325,425 @@ __device__ void cut(Smem& sm, const T* row, int vocab, Row& r, bool by_mass, uns
   r.last = place;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void sample_kernel(SampleCall c, int bits) {
-  __shared__ Smem sm;
-  const int64_t n = blockIdx.x;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+// ---- the launches ------------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void load_roots(double* roots) {
+  if (threadIdx.x < 32) roots[threadIdx.x] = kRoots[threadIdx.x];
+}
+// Largest logit of a row, from its parts (a few dozen); false where there is nothing to draw from.
+__device__ __forceinline__ bool top_of(const Part* parts, int n, float& top) {
+  bool bad = false;
+  top = -INFINITY;
+  for (int p = threadIdx.x & 63; p < n; p += 64) {
+    top = fmaxf(top, parts[p].top);
+    bad |= parts[p].bad != 0;
+  }
+  top = max_of_wave(top);
+  return !__any(bad) && top != -INFINITY;
+}
+
+template <typename T, int PIECES>
+__global__ __launch_bounds__(kPartThreads) void parts_kernel(SampleCall c, Space space, int bits, int cuts) {
+  __shared__ double roots[32];
+  __shared__ float tops[kPartWaves];
+  __shared__ unsigned long long sums[kPartWaves];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, p = blockIdx.x;
+  const int64_t n = space.first_row + blockIdx.y;
   const T* row = static_cast<const T*>(c.logits) + n * c.stride;
-  const double t = c.temperatures ? c.temperatures[n] : c.temperature;
-  const double top_p = c.top_ps ? c.top_ps[n] : c.top_p, min_p = c.min_ps ? c.min_ps[n] : c.min_p;
-  const int top_k = c.top_ks ? c.top_ks[n] : c.top_k;
+  const int lo = p * (PIECES * kPartThreads * 8);
+  float x[PIECES][8];
+#pragma unroll
+  for (int k = 0; k < PIECES; ++k) {
+    const int at = lo + (k * kPartThreads + (int)threadIdx.x) * 8;
+    if (at + 8 <= c.vocab) {
+      widen(piece_at<false>(row + at), x[k]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[k][i] = at + i < c.vocab ? one_value(row[at + i]) : -INFINITY;
+    }
+  }
+  const Settings s = settings_of(c, n);
+  load_roots(roots);
+  // (what the next launches add up starts at 0)
+  if (cuts && s.cut()) {
+    RowSpace& r = space.rows[blockIdx.y];
+    for (int b = p * kPartThreads + threadIdx.x; b < kBins; b += space.n_parts * kPartThreads) {
+      r.mass[b] = 0;
+      r.count[b] = 0;
+    }
+    if (p == 0 && threadIdx.x == 0) r.cut.listed = 0;
+  }
   float top = -INFINITY;
   bool bad = false;
-  each_token(row, 0, c.vocab, threadIdx.x, kThreads, [&](float x, int) {
-    top = fmaxf(top, x);
-    bad |= !(x < INFINITY);
-  });
+#pragma unroll
+  for (int k = 0; k < PIECES; ++k)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      top = fmaxf(top, x[k][i]);
+      bad |= !(x[k][i] < INFINITY);
+    }
   top = max_of_wave(top);
-  if (lane == 0) sm.sums[wave] = __float_as_uint(top);
+  if (lane == 0) tops[wave] = top;
   bad = __syncthreads_or(bad);
-  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, __uint_as_float((uint32_t)sm.sums[w]));
+#pragma unroll
+  for (int w = 0; w < kPartWaves; ++w) top = fmaxf(top, tops[w]);
+  unsigned long long sum = 0;
+  // (a top_k's weights are those of its list, and what min_p alone keeps is summed later)
+  if (!bad && top != -INFINITY && !s.greedy() && s.top_k == 0 && (s.top_p < 1. || !s.filter())) {
+    const Weight weight = weight_of(s, roots, top, bits, 0.);
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += weight(x[k][i]);
+    sum = sum_over_wave(sum);
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    sum = 0;
+#pragma unroll
+    for (int w = 0; w < kPartWaves; ++w) sum += sums[w];
+  }
+  if (threadIdx.x == 0) space.parts[(int64_t)blockIdx.y * space.n_parts + p] = {top, bad, sum, 0};
+}
+
+// Sum of a row's weights with its largest logit for reference, of 2^bits: parts in their order, the same in every wavefront that asks.
+__device__ __forceinline__ double total_of_parts(const Part* parts, int n, float top, const Settings& s) {
+  const double inv = inverse(s.t);
+  double sum = 0.;
+  for (int p = threadIdx.x & 63; p < n; p += 64)
+    if (parts[p].top != -INFINITY) sum += (double)parts[p].sum * exp(((double)parts[p].top - (double)top) * inv);
+  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+  return sum;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void bins_kernel(SampleCall c, Space space, int bits) {
+  __shared__ double roots[32];
+  __shared__ unsigned long long mass[kBins];
+  __shared__ uint32_t count[kBins];
+  const int64_t n = space.first_row + blockIdx.y;
+  const T* row = static_cast<const T*>(c.logits) + n * c.stride;
+  const Settings s = settings_of(c, n);
+  float top;
+  if (!s.cut() || !top_of(space.parts + (int64_t)blockIdx.y * space.n_parts, space.n_parts, top)) return;
+  load_roots(roots);
+  for (int b = threadIdx.x; b < kBins; b += kPartThreads) {
+    mass[b] = 0;
+    count[b] = 0;
+  }
   __syncthreads();
-  if (bad || top == -INFINITY) {             // nothing to draw from
+  const FirstBin bin_at = first_bin(top, s);
+  const Weight weight = weight_of(s, roots, top, bits, 0.);
+  const bool by_mass = s.top_k == 0;
+  const int lo = blockIdx.x * space.part, hi = min(lo + space.part, c.vocab);
+  // Tokens that top_p keeps for sure not: those of a weight below (1 - p) sum / vocab have less than 1 - p of the sum together.
+  unsigned long long least = 0;
+  if (by_mass) {
+    const double sum = total_of_parts(space.parts + (int64_t)blockIdx.y * space.n_parts, space.n_parts, top, s);
+    least = (unsigned long long)((1. - s.top_p) * sum * 0.99 / c.vocab);
+  }
+  each_token(row, lo, hi, threadIdx.x, kPartThreads, [&](float x, int) {
+    const int b = bin_at(x);
+    if (by_mass) {
+      const unsigned long long w = weight(x);
+      if (w < least || w == 0) return;
+      atomicAdd(&mass[b], w);
+    }
+    atomicAdd(&count[b], 1u);
+  });
+  __syncthreads();
+  RowSpace& r = space.rows[blockIdx.y];
+  for (int b = threadIdx.x; b < kBins; b += kPartThreads) {
+    if (count[b]) atomicAdd(&r.count[b], count[b]);
+    if (mass[b]) atomicAdd(&r.mass[b], mass[b]);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void collect_kernel(SampleCall c, Space space, int bits) {
+  __shared__ double roots[32];
+  __shared__ unsigned long long sums[kPartWaves];
+  __shared__ int32_t found, found_count;
+  __shared__ unsigned long long found_before;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t n = space.first_row + blockIdx.y;
+  const T* row = static_cast<const T*>(c.logits) + n * c.stride;
+  Part* parts = space.parts + (int64_t)blockIdx.y * space.n_parts;
+  const Settings s = settings_of(c, n);
+  float top;
+  if (!s.filter() || !top_of(parts, space.n_parts, top)) return;
+  load_roots(roots);
+  RowSpace& r = space.rows[blockIdx.y];
+  int first = kBins, last = kBins;                  // bins [first, last] are listed
+  if (s.cut()) {
+    const bool by_mass = s.top_k == 0;
+    const double target = by_mass ? s.top_p * total_of_parts(parts, space.n_parts, top, s) : 0.;
+    constexpr int kEach = kBins / kPartThreads;
+    unsigned long long v[kEach], run = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      v[i] = by_mass ? r.mass[threadIdx.x * kEach + i] : r.count[threadIdx.x * kEach + i];
+      run += v[i];
+    }
+    const unsigned long long own = run;
+    for (int d = 1; d < 64; d <<= 1) {
+      const unsigned long long other = __shfl_up(run, d);
+      if (lane >= d) run += other;
+    }
+    if (lane == 63) sums[wave] = run;
+    if (threadIdx.x == 0) found = kBins;
+    __syncthreads();
+    run -= own;
+    for (int w = 0; w < wave; ++w) run += sums[w];
+    // the bin that reaches the target (the first with any weight, where the target is 0)
+    auto reached = [&](unsigned long long x) { return by_mass ? x > 0 && (double)x >= target : x >= (unsigned long long)s.top_k; };
+    if (!reached(run)) {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        if (reached(run + v[i]) && !reached(run)) {
+          found = threadIdx.x * kEach + i;
+          found_count = (int)(by_mass ? r.count[threadIdx.x * kEach + i] : run + v[i]);
+          found_before = run;
+        }
+        run += v[i];
+      }
+    }
+    __syncthreads();
+    last = found;
+    first = by_mass ? last : 0;
+    if (last < kBins && blockIdx.x == 0 && threadIdx.x == 0) {
+      r.cut.before = by_mass ? found_before : 0;
+      if (found_count > kList) atomicAdd(&r.cut.listed, kList + 1);
+    }
+    // (none reaches it, by the roundings of the target: nothing is cut)
+    if (last < kBins && found_count > kList) return;
+  }
+  __syncthreads();
+  const FirstBin bin_at = first_bin(top, s);
+  const Weight weight = weight_of(s, roots, top, bits, s.min_p * (double)(1ull << bits));
+  const int lo = blockIdx.x * space.part, hi = min(lo + space.part, c.vocab);
+  unsigned long long sum = 0;
+  each_token(row, lo, hi, threadIdx.x, kPartThreads, [&](float x, int i) {
+    const int b = first == kBins ? 0 : bin_at(x);
+    if (b < first) {
+      sum += weight(x);
+    } else if (b <= last) {
+      const int at = atomicAdd(&r.cut.listed, 1);
+      if (at < kList) r.list[at] = (unsigned long long)~key_of(x) << 32 | (uint32_t)i;
+    }
+  });
+  sum = sum_over_wave(sum);
+  __syncthreads();
+  if (lane == 0) sums[wave] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    sum = 0;
+#pragma unroll
+    for (int w = 0; w < kPartWaves; ++w) sum += sums[w];
+    parts[blockIdx.x].above = sum;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space space, int bits) {
+  __shared__ Smem sm;
+  const int64_t n = space.first_row + blockIdx.x;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const T* row = static_cast<const T*>(c.logits) + n * c.stride;
+  const Part* parts = space.parts + (int64_t)blockIdx.x * space.n_parts;
+  RowSpace& space_of_row = space.rows[blockIdx.x];
+  Row r;
+  r.how = settings_of(c, n);
+  r.key = 0;
+  r.last = 0x7fffffff;
+  const Settings& s = r.how;
+  if (!top_of(parts, space.n_parts, r.top)) {             // nothing to draw from
     if (threadIdx.x == 0) {
       c.tokens[n] = -1;
       if (c.logprobs) c.logprobs[n] = NAN;
     }
     return;
   }
-  if (!(t > 0.)) {
-    const int i = place_of(sm, row, 0, c.vocab, 0, [&](float x, int) { return (unsigned long long)(x == top); });
+  load_roots(sm.roots);
+  const double unit = (double)(1ull << bits), inv = inverse(s.t);
+  const float u = c.uniforms[n];
+  auto write = [&](int i, double total) {
+    if (threadIdx.x != 0) return;
+    c.tokens[n] = i;
+    if (c.logprobs) c.logprobs[n] = (float)(((double)one_value(row[i]) - (double)r.top) * inv - log(total / unit));
+  };
+  if (s.greedy()) {
+    if (threadIdx.x == 0) sm.index = space.n_parts;
+    __syncthreads();
+    for (int p = threadIdx.x; p < space.n_parts; p += kThreads)
+      if (parts[p].top == r.top) atomicMin(&sm.index, p);
+    __syncthreads();
+    const int lo = sm.index * space.part;
+    __syncthreads();
+    const int i = place_of(sm, row, lo, min(lo + space.part, c.vocab), 0, [&](float x, int) { return (unsigned long long)(x == r.top); });
     if (threadIdx.x == 0) {
       c.tokens[n] = i;
       if (c.logprobs) c.logprobs[n] = 0.f;
     }
     return;
   }
-  Row r;
-  r.top = top;
-  r.inv_t = 1. / t;
-  r.unit = (double)(1ull << bits);
-  r.least = -(bits + 1) * 0.69314718055994530942;
-  r.min_w = 0.;
-  r.key = 0;
-  r.last = 0x7fffffff;
-  auto kept_weight = [&](float x, int i) { return keeps(r, x, i) ? weight_of(r, x) : 0ull; };
-  auto total_of = [&]() {
+  // Parts of the whole: (weight of the parts in front, weight) of the part that the number falls into; parts in rounds of a thread each.
+  const unsigned long long u64 = !(u > 0.f) ? 0 : u < 1.f ? (unsigned long long)((double)u * 18446744073709551616.) : ~0ull;
+  if (!s.filter()) {
+    // every part has its own reference: sums in 64-bit floating point, in a fixed order
+    double total = 0.;
+    if (wave == 0) {
+      double run = 0.;
+      for (int turn = 0; turn < 2; ++turn) {                 // the sum, then the part
+        const double target = turn ? (u > 0.f ? (u < 1.f ? (double)u : 1. - 1e-16) : 0.) * total : 0.;
+        run = 0.;
+        int last = -1;
+        double before_last = 0.;
+        bool done = false;
+        for (int p0 = 0; p0 < space.n_parts && !done; p0 += 64) {
+          const int p = p0 + lane;
+          double w = 0.;
+          if (p < space.n_parts && parts[p].top != -INFINITY) w = (double)parts[p].sum * exp(((double)parts[p].top - (double)r.top) * inv);
+          double upto = w;
+          for (int d = 1; d < 64; d <<= 1) {
+            const double other = __shfl_up(upto, d);
+            if (lane >= d) upto += other;
+          }
+          upto += run;
+          if (turn) {
+            const double before = upto - w;
+            unsigned long long here = __ballot(w > 0.);
+            if (here) {
+              const int at = 63 - __builtin_clzll(here);
+              last = p0 + at;
+              before_last = __shfl(before, at);
+            }
+            here = __ballot(w > 0. && target < upto);
+            if (here) {
+              const int at = __builtin_ctzll(here);
+              last = p0 + at;
+              before_last = __shfl(before, at);
+              done = true;
+            }
+          }
+          run = __shfl(upto, 63);
+        }
+        if (!turn) total = run;
+        else if (lane == 0) {
+          // (the way into the part, in its own unit)
+          double way = (target - before_last) / exp(((double)parts[last].top - (double)r.top) * inv);
+          const unsigned long long most = parts[last].sum - 1;
+          sm.found = last;
+          sm.found_before = !(way > 0.) ? 0 : way < (double)most ? (unsigned long long)way : most;
+          sm.found_mass = (unsigned long long)__double_as_longlong(total);
+        }
+      }
+    }
+    __syncthreads();
+    const int p = sm.found, lo = p * space.part;
+    total = __longlong_as_double((long long)sm.found_mass);
+    const Weight weight = weight_of(s, sm.roots, parts[p].top, bits, 0.);
+    write(place_of(sm, row, lo, min(lo + space.part, c.vocab), sm.found_before, [&](float x, int) { return weight(x); }), total);
+    return;
+  }
+
+  const Weight all = weight_of(s, sm.roots, r.top, bits, 0.), weight = weight_of(s, sm.roots, r.top, bits, s.min_p * unit);
+  auto kept_weight = [&](float x, int i) { return keeps(r, x, i) ? weight(x) : 0ull; };
+  bool listed = true;
+  __syncthreads();
+  if (s.cut()) {
+    const RowCut cut_of_row = space_of_row.cut;
+    listed = cut_of_row.listed <= kList;
+    if (listed && cut_of_row.listed > 0) {
+      // every token of the list by how many, and what weight, stand in front of it
+      const int count = cut_of_row.listed;
+      unsigned long long* order = sm.mass;                 // (2048 of each)
+      __shared__ unsigned long long weights[kList];
+      for (int j = threadIdx.x; j < count; j += kThreads) {
+        const unsigned long long e = space_of_row.list[j];
+        order[j] = e;
+        const uint32_t key = ~(uint32_t)(e >> 32);
+        weights[j] = all(__uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key));
+      }
+      __syncthreads();
+      uint32_t rank[kList / kThreads];
+      unsigned long long before[kList / kThreads], mine[kList / kThreads], total = 0;
+#pragma unroll
+      for (int q = 0; q < kList / kThreads; ++q) {
+        const int j = q * kThreads + threadIdx.x;
+        rank[q] = 0xffffffffu;
+        before[q] = 0;
+        if (j >= count) continue;
+        mine[q] = order[j];
+        uint32_t ahead = 0;
+        unsigned long long sum = 0;
+        for (int i = 0; i < count; ++i)
+          if (order[i] < mine[q]) {
+            ++ahead;
+            sum += weights[i];
+          }
+        rank[q] = ahead;
+        before[q] = sum;
+        if (s.top_k > 0 && ahead < (uint32_t)s.top_k) total += weights[j];
+      }
+      double target = INFINITY;
+      if (s.top_p < 1.) {
+        if (s.top_k > 0) {
+          total = sum_over_wave(total);
+          if (lane == 0) sm.sums[wave] = total;
+          __syncthreads();
+          total = 0;
+          for (int w = 0; w < kWaves; ++w) total += sm.sums[w];
+          target = s.top_p * (double)total;
+        } else {
+          target = s.top_p * total_of_parts(parts, space.n_parts, r.top, s);
+        }
+      }
+      if (threadIdx.x == 0) sm.found = 0;
+      __syncthreads();
+      // the last one that is kept; the most likely one always is
+      int keep = -1;
+#pragma unroll
+      for (int q = 0; q < kList / kThreads; ++q) {
+        if (rank[q] == 0xffffffffu || (s.top_k > 0 && rank[q] >= (uint32_t)s.top_k)) continue;
+        const unsigned long long in_front = cut_of_row.before + before[q];
+        if (in_front == 0 ? rank[q] != 0 : !((double)in_front < target)) continue;
+        keep = max(keep, (int)rank[q]);
+      }
+      if (keep >= 0) atomicMax(&sm.found, (uint32_t)keep);
+      __syncthreads();
+#pragma unroll
+      for (int q = 0; q < kList / kThreads; ++q)
+        if (rank[q] == sm.found) {
+          sm.low[0] = ~(uint32_t)(mine[q] >> 32);
+          sm.index = (int32_t)(uint32_t)mine[q];
+        }
+      __syncthreads();
+      r.key = sm.low[0];
+      r.last = sm.index;
+      __syncthreads();
+    } else if (!listed) {
+      auto total_of = [&]() {
+        unsigned long long sum = 0;
+        each_token(row, 0, c.vocab, threadIdx.x, kThreads, [&](float x, int i) { sum += keeps(r, x, i) ? all(x) : 0ull; });
+        sum = sum_over_wave(sum);
+        __syncthreads();
+        if (lane == 0) sm.sums[wave] = sum;
+        __syncthreads();
+        sum = 0;
+        for (int w = 0; w < kWaves; ++w) sum += sm.sums[w];
+        __syncthreads();
+        return sum;
+      };
+      if (s.top_k > 0) cut(sm, row, c.vocab, r, all, false, s.top_k);
+      if (s.top_p < 1.) {
+        const unsigned long long total = total_of();
+        // sums in front of a kept token are below p * total: whole numbers below its ceiling
+        const unsigned long long p64 = (unsigned long long)(s.top_p * 18446744073709551616.);
+        const unsigned long long target = __umul64hi(total, p64) + (total * p64 != 0);
+        cut(sm, row, c.vocab, r, all, true, target > 0 ? target : 1);
+      }
+    }
+  }
+  if (!listed) {
     unsigned long long sum = 0;
     each_token(row, 0, c.vocab, threadIdx.x, kThreads, [&](float x, int i) { sum += kept_weight(x, i); });
     sum = sum_over_wave(sum);
@@ -280,38 +753,81 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(SampleCall c, int bits
     sum = 0;
     for (int w = 0; w < kWaves; ++w) sum += sm.sums[w];
     __syncthreads();
-    return sum;
-  };
-  if (top_k > 0 && top_k < c.vocab) cut(sm, row, c.vocab, r, false, top_k);
-  if (top_p < 1.) {
-    const unsigned long long total = total_of();
-    // sums in front of a kept token are below p * total: whole numbers below its ceiling; the first token is kept always
-    const double p = top_p > 0. ? top_p : 0.;
-    const unsigned long long p64 = (unsigned long long)(p * 18446744073709551616.);
-    const unsigned long long target = __umul64hi(total, p64) + (total * p64 != 0);
-    cut(sm, row, c.vocab, r, true, target > 0 ? target : 1);
+    write(place_of(sm, row, 0, c.vocab, __umul64hi(sum, u64), kept_weight), (double)sum);
+    return;
   }
-  r.min_w = min_p > 0. ? (min_p < 1. ? min_p : 1.) : 0.;
-  const unsigned long long total = total_of();
-  const float u = c.uniforms[n];
-  const unsigned long long u64 = !(u > 0.f) ? 0 : u < 1.f ? (unsigned long long)((double)u * 18446744073709551616.) : ~0ull;
-  const int i = place_of(sm, row, 0, c.vocab, __umul64hi(total, u64), kept_weight);
-  if (threadIdx.x == 0) {
-    c.tokens[n] = i;
-    if (c.logprobs) c.logprobs[n] = (float)(((double)one_value(row[i]) - r.top) * r.inv_t - log((double)total / r.unit));
+  // what is kept of every part: what is above the list, and of the list
+  unsigned long long* of_part = sm.mass;
+  __syncthreads();
+  for (int p = threadIdx.x; p < kBins; p += kThreads) of_part[p] = p < space.n_parts ? parts[p].above : 0;
+  __syncthreads();
+  if (s.cut())
+    for (int j = threadIdx.x; j < space_of_row.cut.listed; j += kThreads) {
+      const unsigned long long e = space_of_row.list[j];
+      const uint32_t key = ~(uint32_t)(e >> 32);
+      const unsigned long long w = kept_weight(__uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key), (int)(uint32_t)e);
+      if (w) atomicAdd(&of_part[(uint32_t)e / (uint32_t)space.part], w);
+    }
+  for (int p = threadIdx.x; p < kBins; p += kThreads) sm.count[p] = 0;
+  __syncthreads();
+  unsigned long long total = 0;
+  for (int p = threadIdx.x; p < kBins; p += kThreads) total += of_part[p];
+  total = sum_over_wave(total);
+  if (lane == 0) sm.sums[wave] = total;
+  __syncthreads();
+  total = 0;
+  for (int w = 0; w < kWaves; ++w) total += sm.sums[w];
+  __syncthreads();
+  const unsigned long long target = __umul64hi(total, u64);
+  bin_of(sm, true, target);
+  const int lo = (int)sm.found * space.part;
+  const unsigned long long way = target - sm.found_before;
+  __syncthreads();
+  write(place_of(sm, row, lo, min(lo + space.part, c.vocab), way, kept_weight), (double)total);
+}
+
+Space space_of(const SampleCall& c, int64_t rows) {
+  Space s;
+  s.part = part_tokens(rows < kRowsAtOnce ? rows : kRowsAtOnce, c.vocab);
+  if ((int64_t)s.part * kBins < c.vocab) s.part = 8192;          // (a bin for every part)
+  s.n_parts = (c.vocab + s.part - 1) / s.part;
+  s.rows = static_cast<RowSpace*>(c.workspace);
+  s.parts = reinterpret_cast<Part*>(s.rows + (rows < kRowsAtOnce ? rows : kRowsAtOnce));
+  s.first_row = 0;
+  return s;
+}
+
+template <typename T>
+hipError_t launch_typed(const SampleCall& c, hipStream_t stream) {
+  Space s = space_of(c, c.rows);
+  const int bits = bits_of(c.vocab);
+  // (what is given one a row may be anything)
+  const bool cuts = c.top_ks || c.top_ps || (c.top_k > 0 && c.top_k < c.vocab) || c.top_p < 1., filters = cuts || c.min_ps || c.min_p > 0.;
+  for (; s.first_row < c.rows; s.first_row += kRowsAtOnce) {
+    const int64_t left = c.rows - s.first_row;
+    const dim3 grid((unsigned)s.n_parts, (unsigned)(left < kRowsAtOnce ? left : kRowsAtOnce));
+    if (s.part == 8192) parts_kernel<T, 4><<<grid, kPartThreads, 0, stream>>>(c, s, bits, cuts);
+    else parts_kernel<T, 1><<<grid, kPartThreads, 0, stream>>>(c, s, bits, cuts);
+    if (cuts) bins_kernel<T><<<grid, kPartThreads, 0, stream>>>(c, s, bits);
+    if (filters) collect_kernel<T><<<grid, kPartThreads, 0, stream>>>(c, s, bits);
+    draw_kernel<T><<<grid.y, kThreads, 0, stream>>>(c, s, bits);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
   }
+  return hipSuccess;
 }
 
 }  // namespace
 
-size_t sample_workspace(int, int) { return 0; }
+size_t sample_workspace(int rows, int vocab) {
+  SampleCall c = {};
+  c.vocab = vocab;
+  const Space s = space_of(c, rows);
+  return (size_t)(rows < kRowsAtOnce ? rows : kRowsAtOnce) * (sizeof(RowSpace) + (size_t)s.n_parts * sizeof(Part));
+}
 
 hipError_t launch_sample(const SampleCall& c, int dtype, hipStream_t stream) {
-  int bits = 62;
-  for (int64_t n = 1; n < c.vocab; n *= 2) --bits;
-  if (dtype == RLKV_F32) sample_kernel<float><<<(unsigned)c.rows, kThreads, 0, stream>>>(c, bits);
-  else sample_kernel<uint16_t><<<(unsigned)c.rows, kThreads, 0, stream>>>(c, bits);
-  return hipGetLastError();
+  return dtype == RLKV_F32 ? launch_typed<float>(c, stream) : launch_typed<uint16_t>(c, stream);
 }
 
 }  // namespace rlkv
