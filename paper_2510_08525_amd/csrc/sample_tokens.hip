@@ -7,23 +7,26 @@
 // order they are formed, so atomics and scans give the same token at every call, and borders between tokens are where the formula has them to 2^-39
 // of the weights (what sums in 32 bits leave, 2^-24 of a border's place, changes a token of 128k in one of hundred rows).
 //
-// A row is read by as many workgroups as it has parts of 2048 or 8192 tokens.  Launches, of which rows without filters need the first and the last:
+// A row is read by as many workgroups as it has parts of 8192 tokens.  Launches, of which rows without filters need the first and the last:
 //   parts    largest logit and, for rows whose sum is asked for, the sum of weights of a part
-//   bins     of rows with top_k or top_p: how many tokens, and what weight, lie in each of 2048 steps down from the largest logit
+//   bins     of rows with top_k or top_p: how many tokens, and what weight, lie in each of 4096 steps down from the largest logit
 //   collect  the step in which the cut falls: its tokens go into a list; the weight of a part's tokens above it
 //   draw     one workgroup a row: the cut among the list's tokens, the part that the number falls into, the token in it
 // A row whose list would be too long (thousands of like logits at the cut, a top_k of thousands) is cut by its last workgroup alone, in passes over the row.
 #include "sample_tokens.h"
+
+#include <type_traits>
+
 #include "token_ops.h"
 
 namespace rlkv {
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 2048;
-constexpr int kTileTokens = kThreads * 8;
-constexpr float kBinsPerUnit = 32.f;      // bins: the way from the largest logit over the temperature, 64 of it
+constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 4096;
+constexpr float kBinsPerUnit = 128.f;     // bins: the way from the largest logit over the temperature, 32 of it
 constexpr int kList = 2048;               // tokens of a row's list
-constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64;
+constexpr int kPart = 8192;               // tokens of a part
+constexpr int kFewThreads = 256;          // of the launches that many rows have many workgroups of
 constexpr int kRowsAtOnce = 512;          // rows that have a workspace
 
 // Ascending with x; zeros of either sign are the same.
@@ -36,38 +39,71 @@ __device__ __forceinline__ unsigned long long sum_over_wave(unsigned long long x
   return x;
 }
 
-// 2^(j / 32)
-__constant__ double kRoots[32] = {
-    0x1.0000000000000p+0, 0x1.059b0d3158574p+0, 0x1.0b5586cf9890fp+0, 0x1.11301d0125b51p+0,
-    0x1.172b83c7d517bp+0, 0x1.1d4873168b9aap+0, 0x1.2387a6e756238p+0, 0x1.29e9df51fdee1p+0,
-    0x1.306fe0a31b715p+0, 0x1.371a7373aa9cbp+0, 0x1.3dea64c123422p+0, 0x1.44e086061892dp+0,
-    0x1.4bfdad5362a27p+0, 0x1.5342b569d4f82p+0, 0x1.5ab07dd485429p+0, 0x1.6247eb03a5585p+0,
-    0x1.6a09e667f3bcdp+0, 0x1.71f75e8ec5f74p+0, 0x1.7a11473eb0187p+0, 0x1.82589994cce13p+0,
-    0x1.8ace5422aa0dbp+0, 0x1.93737b0cdc5e5p+0, 0x1.9c49182a3f090p+0, 0x1.a5503b23e255dp+0,
-    0x1.ae89f995ad3adp+0, 0x1.b7f76f2fb5e47p+0, 0x1.c199bdd85529cp+0, 0x1.cb720dcef9069p+0,
-    0x1.d5818dcfba487p+0, 0x1.dfc97337b9b5fp+0, 0x1.ea4afa2a490dap+0, 0x1.f50765b6e4540p+0};
+// 2^(j / 128)
+constexpr int kRootCount = 128;
+__constant__ double kRoots[kRootCount] = {
+    0x1.0000000000000p+0, 0x1.0163da9fb3335p+0, 0x1.02c9a3e778061p+0, 0x1.04315e86e7f85p+0,
+    0x1.059b0d3158574p+0, 0x1.0706b29ddf6dep+0, 0x1.0874518759bc8p+0, 0x1.09e3ecac6f383p+0,
+    0x1.0b5586cf9890fp+0, 0x1.0cc922b7247f7p+0, 0x1.0e3ec32d3d1a2p+0, 0x1.0fb66affed31bp+0,
+    0x1.11301d0125b51p+0, 0x1.12abdc06c31ccp+0, 0x1.1429aaea92de0p+0, 0x1.15a98c8a58e51p+0,
+    0x1.172b83c7d517bp+0, 0x1.18af9388c8deap+0, 0x1.1a35beb6fcb75p+0, 0x1.1bbe084045cd4p+0,
+    0x1.1d4873168b9aap+0, 0x1.1ed5022fcd91dp+0, 0x1.2063b88628cd6p+0, 0x1.21f49917ddc96p+0,
+    0x1.2387a6e756238p+0, 0x1.251ce4fb2a63fp+0, 0x1.26b4565e27cddp+0, 0x1.284dfe1f56381p+0,
+    0x1.29e9df51fdee1p+0, 0x1.2b87fd0dad990p+0, 0x1.2d285a6e4030bp+0, 0x1.2ecafa93e2f56p+0,
+    0x1.306fe0a31b715p+0, 0x1.32170fc4cd831p+0, 0x1.33c08b26416ffp+0, 0x1.356c55f929ff1p+0,
+    0x1.371a7373aa9cbp+0, 0x1.38cae6d05d866p+0, 0x1.3a7db34e59ff7p+0, 0x1.3c32dc313a8e5p+0,
+    0x1.3dea64c123422p+0, 0x1.3fa4504ac801cp+0, 0x1.4160a21f72e2ap+0, 0x1.431f5d950a897p+0,
+    0x1.44e086061892dp+0, 0x1.46a41ed1d0057p+0, 0x1.486a2b5c13cd0p+0, 0x1.4a32af0d7d3dep+0,
+    0x1.4bfdad5362a27p+0, 0x1.4dcb299fddd0dp+0, 0x1.4f9b2769d2ca7p+0, 0x1.516daa2cf6642p+0,
+    0x1.5342b569d4f82p+0, 0x1.551a4ca5d920fp+0, 0x1.56f4736b527dap+0, 0x1.58d12d497c7fdp+0,
+    0x1.5ab07dd485429p+0, 0x1.5c9268a5946b7p+0, 0x1.5e76f15ad2148p+0, 0x1.605e1b976dc09p+0,
+    0x1.6247eb03a5585p+0, 0x1.6434634ccc320p+0, 0x1.6623882552225p+0, 0x1.68155d44ca973p+0,
+    0x1.6a09e667f3bcdp+0, 0x1.6c012750bdabfp+0, 0x1.6dfb23c651a2fp+0, 0x1.6ff7df9519484p+0,
+    0x1.71f75e8ec5f74p+0, 0x1.73f9a48a58174p+0, 0x1.75feb564267c9p+0, 0x1.780694fde5d3fp+0,
+    0x1.7a11473eb0187p+0, 0x1.7c1ed0130c132p+0, 0x1.7e2f336cf4e62p+0, 0x1.80427543e1a12p+0,
+    0x1.82589994cce13p+0, 0x1.8471a4623c7adp+0, 0x1.868d99b4492edp+0, 0x1.88ac7d98a6699p+0,
+    0x1.8ace5422aa0dbp+0, 0x1.8cf3216b5448cp+0, 0x1.8f1ae99157736p+0, 0x1.9145b0b91ffc6p+0,
+    0x1.93737b0cdc5e5p+0, 0x1.95a44cbc8520fp+0, 0x1.97d829fde4e50p+0, 0x1.9a0f170ca07bap+0,
+    0x1.9c49182a3f090p+0, 0x1.9e86319e32323p+0, 0x1.a0c667b5de565p+0, 0x1.a309bec4a2d33p+0,
+    0x1.a5503b23e255dp+0, 0x1.a799e1330b358p+0, 0x1.a9e6b5579fdbfp+0, 0x1.ac36bbfd3f37ap+0,
+    0x1.ae89f995ad3adp+0, 0x1.b0e07298db666p+0, 0x1.b33a2b84f15fbp+0, 0x1.b59728de5593ap+0,
+    0x1.b7f76f2fb5e47p+0, 0x1.ba5b030a1064ap+0, 0x1.bcc1e904bc1d2p+0, 0x1.bf2c25bd71e09p+0,
+    0x1.c199bdd85529cp+0, 0x1.c40ab5fffd07ap+0, 0x1.c67f12e57d14bp+0, 0x1.c8f6d9406e7b5p+0,
+    0x1.cb720dcef9069p+0, 0x1.cdf0b555dc3fap+0, 0x1.d072d4a07897cp+0, 0x1.d2f87080d89f2p+0,
+    0x1.d5818dcfba487p+0, 0x1.d80e316c98398p+0, 0x1.da9e603db3285p+0, 0x1.dd321f301b460p+0,
+    0x1.dfc97337b9b5fp+0, 0x1.e264614f5a129p+0, 0x1.e502ee78b3ff6p+0, 0x1.e7a51fbc74c83p+0,
+    0x1.ea4afa2a490dap+0, 0x1.ecf482d8e67f1p+0, 0x1.efa1bee615a27p+0, 0x1.f252b376bba97p+0,
+    0x1.f50765b6e4540p+0, 0x1.f7bfdad9cbe14p+0, 0x1.fa7c1819e90d8p+0, 0x1.fd3c22b8f71f1p+0};
 
-// The weight of a logit: 2^bits exp((x - ref) / t), rounded to a whole number; 0 below a half and for what is masked.
-// With z = 32 log2(e) (x - ref) / t = 32 n + j + r, |r| <= 1/2:  2^n 2^(j / 32) (1 + a r + .. + (a r)^4 / 24), a = ln(2) / 32: the series ends 1.2e-12 of it.
+// The weight of a logit: 2^bits exp((x - ref) / t), rounded to a whole number.
+// With z = 128 log2(e) (x - ref) / t = 128 n + j + r, |r| <= 1/2:  2^n 2^(j / 128) (1 + a r + .. + (a r)^3 / 6), a = ln(2) / 128: the series ends 2.3e-12 of
+// it.  Eighteen instructions, which is what the launch over many rows is bound by.
 struct Weight {
-  const double* roots;       // in LDS: the lanes' places are in banks of their own
-  double ref, c;             // 32 log2(e) / t
-  int bits;
+  const uint64_t* roots;     // in LDS, times 2^bits
+  double ref, c;             // 128 log2(e) / t
+  double lowest;             // -128 (bits + 600): what is below it, or masked (a place of -infinity, or NaN at an infinite temperature), has 2^-600
   double least;              // least weight that counts, of 2^bits (min_p)
-  __device__ __forceinline__ unsigned long long operator()(float x) const {
-    const double z = ((double)x - ref) * c;
-    if (!(z >= -32. * (bits + 1))) return 0;             // (a masked logit's place is -infinity, or NaN where the temperature is infinite)
+  __device__ __forceinline__ double real(float x) const {
+    const double z = fmax(((double)x - ref) * c, lowest);
     const double shifted = z + 6755399441055744.;        // 1.5 * 2^52: the nearest whole number in the low bits
     const int k = (int)(uint32_t)__double_as_longlong(shifted);
     const double r = z - (shifted - 6755399441055744.);
-    constexpr double a = 0.69314718055994530942 / 32;
-    double p = __builtin_fma(r, a * a * a * a / 24, a * a * a / 6);
-    p = __builtin_fma(r, p, a * a / 2);
+    constexpr double a = 0.69314718055994530942 / kRootCount;
+    double p = __builtin_fma(r, a * a * a / 6, a * a / 2);
     p = __builtin_fma(r, p, a);
     p = __builtin_fma(r, p, 1.);
-    const double w = ldexp(roots[k & 31] * p, (k >> 5) + bits);
-    return w >= least ? (unsigned long long)__double_as_longlong(w + 4503599627370496.) - 0x4330000000000000ull : 0;      // 2^52
+    const uint64_t root = roots[k & (kRootCount - 1)];
+    const uint32_t high = (uint32_t)(root >> 32) + ((uint32_t)(k & ~(kRootCount - 1)) << 13);      // (k / 128 into the exponent)
+    return __longlong_as_double((long long)((uint64_t)high << 32 | (uint32_t)root)) * p;
   }
+  __device__ __forceinline__ unsigned long long rounded(double w) const {       // (by adding 2^52)
+    return (unsigned long long)__double_as_longlong(w + 4503599627370496.) - 0x4330000000000000ull;
+  }
+  __device__ __forceinline__ unsigned long long operator()(float x) const {
+    const double w = real(x);
+    return w >= least ? rounded(w) : 0;
+  }
+  __device__ __forceinline__ unsigned long long whole(float x) const { return rounded(real(x)); }      // without min_p
 };
 // (w below 2^51: bits is at most 50 then)
 __host__ __device__ inline int bits_of(int vocab) {
@@ -97,8 +133,8 @@ __device__ __forceinline__ Settings settings_of(const SampleCall& c, int64_t n) 
 }
 // (1 / t is at most 1e300: a way of 0 stays 0)
 __device__ __forceinline__ double inverse(double t) { return t > 1e-300 ? 1. / t : 1e300; }
-__device__ __forceinline__ Weight weight_of(const Settings& s, const double* roots, double ref, int bits, double least) {
-  return {roots, ref, inverse(s.t) * (32 * 1.4426950408889634074), bits, least};
+__device__ __forceinline__ Weight weight_of(const Settings& s, const uint64_t* roots, double ref, int bits, double least) {
+  return {roots, ref, inverse(s.t) * (kRootCount * 1.4426950408889634074), -1. * kRootCount * (bits + 600), least};
 }
 
 // Steps down from the largest logit; not decreasing as x falls.
@@ -115,7 +151,7 @@ __device__ __forceinline__ FirstBin first_bin(float top, const Settings& s) { re
 struct Part {
   float top;
   int32_t bad;                     // a NaN or +inf is there
-  unsigned long long sum;          // of weights with the part's largest logit for reference
+  double sum;                      // of weights with the part's largest logit for reference, of 2^bits
   unsigned long long above;        // of weights above the cut's bin that min_p keeps, with the row's largest for reference
 };
 struct RowCut {
@@ -129,15 +165,19 @@ struct RowSpace {
   unsigned long long list[kList];  // ~key, token: ascending is the order of the cut
   RowCut cut;
 };
-__host__ __device__ inline int part_tokens(int64_t rows, int64_t vocab) { return rows * ((vocab + 8191) / 8192) >= 512 ? 8192 : 2048; }
 struct Space {
   RowSpace* rows;
   Part* parts;                     // [rows][n_parts]
-  int32_t n_parts, part;
+  int32_t n_parts;
   int64_t first_row;               // of the launch
 };
 
+struct PlaceSmem {
+  unsigned long long sums[kWaves];
+  int32_t index;
+};
 struct Smem {
+  PlaceSmem place;
   unsigned long long mass[kBins];
   uint32_t count[kBins];
   unsigned long long sums[kWaves];
@@ -145,7 +185,7 @@ struct Smem {
   unsigned long long found_before, found_mass;
   uint32_t found, found_count;
   int32_t index;
-  double roots[32];
+  uint64_t roots[kRootCount];
 };
 
 // What is kept: keys above `key`, and `key` itself up to the place `last`.
@@ -172,11 +212,13 @@ __device__ __forceinline__ void each_token(const T* row, int lo, int hi, int t, 
   }
 }
 
-// First place in [lo, hi) where the running sum of f is above `target`, in all threads.  The sum over [lo, hi) has to be.
-template <typename T, typename F>
-__device__ int place_of(Smem& sm, const T* row, int lo, int hi, unsigned long long target, F f) {
+// First place in [lo, hi) where the running sum of f is above `target`, in all threads; where there is none, the last one where f is above 0 (one
+// there has to be).
+template <int THREADS, typename T, typename F>
+__device__ int place_of(PlaceSmem& sm, const T* row, int lo, int hi, unsigned long long target, F f) {
+  constexpr int kWaves = THREADS / 64;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  while (hi - lo > kTileTokens) {            // sixteen parts, one a wavefront
+  while (hi - lo > THREADS * 8) {            // a part for each wavefront
     const int part = ((hi - lo + kWaves - 1) / kWaves + 7) / 8 * 8;
     const int64_t a = lo + (int64_t)wave * part, b = a + part;
     unsigned long long sum = 0;
@@ -185,9 +227,17 @@ __device__ int place_of(Smem& sm, const T* row, int lo, int hi, unsigned long lo
     __syncthreads();
     if (lane == 0) sm.sums[wave] = sum;
     __syncthreads();
-    int w = 0;
-    for (; w < kWaves - 1 && target >= sm.sums[w]; ++w) target -= sm.sums[w];
-    lo += w * part;
+    int found = 0;
+    bool inside = false;
+    for (int w = 0; w < kWaves && !inside; ++w) {
+      const unsigned long long s = sm.sums[w];
+      if (s == 0) continue;
+      found = w;
+      inside = target < s;
+      if (!inside) target -= s;
+    }
+    if (!inside) target = ~0ull >> 1;        // (behind all sums that follow, too)
+    lo += found * part;
     hi = lo + part < hi ? lo + part : hi;
   }
   // eight tokens a thread
@@ -207,9 +257,15 @@ __device__ int place_of(Smem& sm, const T* row, int lo, int hi, unsigned long lo
   }
   __syncthreads();
   if (lane == 63) sm.sums[wave] = before;
+  if (threadIdx.x == 0) sm.index = -1;
   __syncthreads();
   before -= sum;
-  for (int w = 0; w < wave; ++w) before += sm.sums[w];
+  unsigned long long total = 0;
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) before += sm.sums[w];
+    total += sm.sums[w];
+  }
+  if (target >= total) target = total - 1;   // (the last token's share)
   if (before <= target && target < before + sum) {
     int i = 0;
     unsigned long long run = before;
@@ -222,23 +278,34 @@ __device__ int place_of(Smem& sm, const T* row, int lo, int hi, unsigned long lo
 
 // The bin in which the running sum (of counts, or of masses) passes `target`; found_before: the sum in front of it.
 __device__ void bin_of(Smem& sm, bool by_mass, unsigned long long target) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, b = threadIdx.x * 2;
-  const unsigned long long x = by_mass ? sm.mass[b] : sm.count[b], y = by_mass ? sm.mass[b + 1] : sm.count[b + 1];
-  unsigned long long run = x + y;
+  constexpr int kEach = kBins / kThreads;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, first = threadIdx.x * kEach;
+  unsigned long long v[kEach], own = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    v[i] = by_mass ? sm.mass[first + i] : sm.count[first + i];
+    own += v[i];
+  }
+  unsigned long long run = own;
   for (int d = 1; d < 64; d <<= 1) {
     const unsigned long long other = __shfl_up(run, d);
     if (lane >= d) run += other;
   }
   if (lane == 63) sm.sums[wave] = run;
   __syncthreads();
-  run -= x + y;
+  run -= own;
   for (int w = 0; w < wave; ++w) run += sm.sums[w];
-  if (run <= target && target < run + x + y) {
-    const bool second = target >= run + x;
-    sm.found = b + second;
-    sm.found_before = run + (second ? x : 0);
-    sm.found_mass = sm.mass[b + second];
-    sm.found_count = sm.count[b + second];
+  if (run <= target && target < run + own) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (run <= target && target < run + v[i]) {
+        sm.found = first + i;
+        sm.found_before = run;
+        sm.found_mass = sm.mass[first + i];
+        sm.found_count = sm.count[first + i];
+      }
+      run += v[i];
+    }
   }
   __syncthreads();
 }
@@ -320,14 +387,14 @@ __device__ void cut(Smem& sm, const T* row, int vocab, Row& r, const Weight& wei
   __syncthreads();
   const int32_t old_last = high == r.key ? r.last : 0x7fffffff;
   int32_t place = old_last;
-  if (need < count) place = place_of(sm, row, 0, vocab, need - 1, [&](float x, int i) { return (unsigned long long)(key_of(x) == high && i <= old_last); });
+  if (need < count) place = place_of<kThreads>(sm.place, row, 0, vocab, need - 1, [&](float x, int i) { return (unsigned long long)(key_of(x) == high && i <= old_last); });
   r.key = high;
   r.last = place;
 }
 
 // ---- the launches ------------------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ void load_roots(double* roots) {
-  if (threadIdx.x < 32) roots[threadIdx.x] = kRoots[threadIdx.x];
+__device__ __forceinline__ void load_roots(uint64_t* roots, int bits) {
+  if (threadIdx.x < kRootCount) roots[threadIdx.x] = (uint64_t)__double_as_longlong(kRoots[threadIdx.x]) + ((uint64_t)bits << 52);
 }
 // Largest logit of a row, from its parts (a few dozen); false where there is nothing to draw from.
 __device__ __forceinline__ bool top_of(const Part* parts, int n, float& top) {
@@ -341,32 +408,52 @@ __device__ __forceinline__ bool top_of(const Part* parts, int n, float& top) {
   return !__any(bad) && top != -INFINITY;
 }
 
-template <typename T, int PIECES>
-__global__ __launch_bounds__(kPartThreads) void parts_kernel(SampleCall c, Space space, int bits, int cuts) {
-  __shared__ double roots[32];
-  __shared__ float tops[kPartWaves];
-  __shared__ unsigned long long sums[kPartWaves];
+// The tokens of a part, all asked for at once; -infinity behind the row's end.
+template <typename T, int THREADS>
+struct PartTokens {
+  static constexpr int PIECES = kPart / 8 / THREADS;
+  float x[PIECES][8];
+  int lo;
+  __device__ __forceinline__ PartTokens(const T* row, int part, int vocab) : lo(part * kPart) {
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) {
+      const int at = place(k);
+      if (at + 8 <= vocab) {
+        widen(piece_at<false>(row + at), x[k]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[k][i] = at + i < vocab ? one_value(row[at + i]) : -INFINITY;
+      }
+    }
+  }
+  __device__ __forceinline__ int place(int k) const { return lo + (k * THREADS + (int)threadIdx.x) * 8; }
+  template <typename F>
+  __device__ __forceinline__ void each(int vocab, F f) const {
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (place(k) + i < vocab) f(x[k][i], place(k) + i);
+  }
+};
+
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void parts_kernel(SampleCall c, Space space, int bits, int cuts) {
+  constexpr int kWaves = THREADS / 64, PIECES = kPart / 8 / THREADS;
+  __shared__ uint64_t roots[kRootCount];
+  __shared__ float tops[kWaves];
+  __shared__ double sums[kWaves];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, p = blockIdx.x;
   const int64_t n = space.first_row + blockIdx.y;
   const T* row = static_cast<const T*>(c.logits) + n * c.stride;
-  const int lo = p * (PIECES * kPartThreads * 8);
-  float x[PIECES][8];
-#pragma unroll
-  for (int k = 0; k < PIECES; ++k) {
-    const int at = lo + (k * kPartThreads + (int)threadIdx.x) * 8;
-    if (at + 8 <= c.vocab) {
-      widen(piece_at<false>(row + at), x[k]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[k][i] = at + i < c.vocab ? one_value(row[at + i]) : -INFINITY;
-    }
-  }
+  const PartTokens<T, THREADS> part(row, p, c.vocab);
+  const auto& x = part.x;
   const Settings s = settings_of(c, n);
-  load_roots(roots);
+  load_roots(roots, bits);
   // (what the next launches add up starts at 0)
   if (cuts && s.cut()) {
     RowSpace& r = space.rows[blockIdx.y];
-    for (int b = p * kPartThreads + threadIdx.x; b < kBins; b += space.n_parts * kPartThreads) {
+    for (int b = p * THREADS + threadIdx.x; b < kBins; b += space.n_parts * THREADS) {
       r.mass[b] = 0;
       r.count[b] = 0;
     }
@@ -385,21 +472,21 @@ __global__ __launch_bounds__(kPartThreads) void parts_kernel(SampleCall c, Space
   if (lane == 0) tops[wave] = top;
   bad = __syncthreads_or(bad);
 #pragma unroll
-  for (int w = 0; w < kPartWaves; ++w) top = fmaxf(top, tops[w]);
-  unsigned long long sum = 0;
+  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, tops[w]);
+  double sum = 0.;
   // (a top_k's weights are those of its list, and what min_p alone keeps is summed later)
   if (!bad && top != -INFINITY && !s.greedy() && s.top_k == 0 && (s.top_p < 1. || !s.filter())) {
     const Weight weight = weight_of(s, roots, top, bits, 0.);
 #pragma unroll
     for (int k = 0; k < PIECES; ++k)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum += weight(x[k][i]);
-    sum = sum_over_wave(sum);
+      for (int i = 0; i < 8; ++i) sum += weight.real(x[k][i]);
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
     if (lane == 0) sums[wave] = sum;
     __syncthreads();
-    sum = 0;
+    sum = 0.;
 #pragma unroll
-    for (int w = 0; w < kPartWaves; ++w) sum += sums[w];
+    for (int w = 0; w < kWaves; ++w) sum += sums[w];
   }
   if (threadIdx.x == 0) space.parts[(int64_t)blockIdx.y * space.n_parts + p] = {top, bad, sum, 0};
 }
@@ -409,14 +496,14 @@ __device__ __forceinline__ double total_of_parts(const Part* parts, int n, float
   const double inv = inverse(s.t);
   double sum = 0.;
   for (int p = threadIdx.x & 63; p < n; p += 64)
-    if (parts[p].top != -INFINITY) sum += (double)parts[p].sum * exp(((double)parts[p].top - (double)top) * inv);
+    if (parts[p].top != -INFINITY) sum += parts[p].sum * exp(((double)parts[p].top - (double)top) * inv);
   for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
   return sum;
 }
 
 template <typename T>
-__global__ __launch_bounds__(kPartThreads) void bins_kernel(SampleCall c, Space space, int bits) {
-  __shared__ double roots[32];
+__global__ __launch_bounds__(kThreads, 8) void bins_kernel(SampleCall c, Space space, int bits) {
+  __shared__ uint64_t roots[kRootCount];
   __shared__ unsigned long long mass[kBins];
   __shared__ uint32_t count[kBins];
   const int64_t n = space.first_row + blockIdx.y;
@@ -424,8 +511,9 @@ __global__ __launch_bounds__(kPartThreads) void bins_kernel(SampleCall c, Space 
   const Settings s = settings_of(c, n);
   float top;
   if (!s.cut() || !top_of(space.parts + (int64_t)blockIdx.y * space.n_parts, space.n_parts, top)) return;
-  load_roots(roots);
-  for (int b = threadIdx.x; b < kBins; b += kPartThreads) {
+  const PartTokens<T, kThreads> part(row, blockIdx.x, c.vocab);
+  load_roots(roots, bits);
+  for (int b = threadIdx.x; b < kBins; b += kThreads) {
     mass[b] = 0;
     count[b] = 0;
   }
@@ -433,17 +521,16 @@ __global__ __launch_bounds__(kPartThreads) void bins_kernel(SampleCall c, Space 
   const FirstBin bin_at = first_bin(top, s);
   const Weight weight = weight_of(s, roots, top, bits, 0.);
   const bool by_mass = s.top_k == 0;
-  const int lo = blockIdx.x * space.part, hi = min(lo + space.part, c.vocab);
   // Tokens that top_p keeps for sure not: those of a weight below (1 - p) sum / vocab have less than 1 - p of the sum together.
   unsigned long long least = 0;
   if (by_mass) {
     const double sum = total_of_parts(space.parts + (int64_t)blockIdx.y * space.n_parts, space.n_parts, top, s);
     least = (unsigned long long)((1. - s.top_p) * sum * 0.99 / c.vocab);
   }
-  each_token(row, lo, hi, threadIdx.x, kPartThreads, [&](float x, int) {
+  part.each(c.vocab, [&](float x, int) {
     const int b = bin_at(x);
     if (by_mass) {
-      const unsigned long long w = weight(x);
+      const unsigned long long w = weight.whole(x);
       if (w < least || w == 0) return;
       atomicAdd(&mass[b], w);
     }
@@ -451,18 +538,18 @@ __global__ __launch_bounds__(kPartThreads) void bins_kernel(SampleCall c, Space 
   });
   __syncthreads();
   RowSpace& r = space.rows[blockIdx.y];
-  for (int b = threadIdx.x; b < kBins; b += kPartThreads) {
+  for (int b = threadIdx.x; b < kBins; b += kThreads) {
     if (count[b]) atomicAdd(&r.count[b], count[b]);
     if (mass[b]) atomicAdd(&r.mass[b], mass[b]);
   }
 }
 
 template <typename T>
-__global__ __launch_bounds__(kPartThreads) void collect_kernel(SampleCall c, Space space, int bits) {
-  __shared__ double roots[32];
-  __shared__ unsigned long long sums[kPartWaves];
-  __shared__ int32_t found, found_count;
-  __shared__ unsigned long long found_before;
+__global__ __launch_bounds__(kThreads, 8) void collect_kernel(SampleCall c, Space space, int bits) {
+  __shared__ uint64_t roots[kRootCount];
+  __shared__ unsigned long long sums[kWaves];
+  __shared__ int32_t found, found_count, here, at_list;
+  __shared__ unsigned long long found_before, list[kList];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int64_t n = space.first_row + blockIdx.y;
   const T* row = static_cast<const T*>(c.logits) + n * c.stride;
@@ -470,13 +557,14 @@ __global__ __launch_bounds__(kPartThreads) void collect_kernel(SampleCall c, Spa
   const Settings s = settings_of(c, n);
   float top;
   if (!s.filter() || !top_of(parts, space.n_parts, top)) return;
-  load_roots(roots);
+  const PartTokens<T, kThreads> part(row, blockIdx.x, c.vocab);
+  load_roots(roots, bits);
   RowSpace& r = space.rows[blockIdx.y];
   int first = kBins, last = kBins;                  // bins [first, last] are listed
   if (s.cut()) {
     const bool by_mass = s.top_k == 0;
     const double target = by_mass ? s.top_p * total_of_parts(parts, space.n_parts, top, s) : 0.;
-    constexpr int kEach = kBins / kPartThreads;
+    constexpr int kEach = kBins / kThreads;
     unsigned long long v[kEach], run = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -516,29 +604,99 @@ __global__ __launch_bounds__(kPartThreads) void collect_kernel(SampleCall c, Spa
     // (none reaches it, by the roundings of the target: nothing is cut)
     if (last < kBins && found_count > kList) return;
   }
+  if (threadIdx.x == 0) here = 0;
   __syncthreads();
   const FirstBin bin_at = first_bin(top, s);
   const Weight weight = weight_of(s, roots, top, bits, s.min_p * (double)(1ull << bits));
-  const int lo = blockIdx.x * space.part, hi = min(lo + space.part, c.vocab);
   unsigned long long sum = 0;
-  each_token(row, lo, hi, threadIdx.x, kPartThreads, [&](float x, int i) {
+  part.each(c.vocab, [&](float x, int i) {
     const int b = first == kBins ? 0 : bin_at(x);
     if (b < first) {
       sum += weight(x);
     } else if (b <= last) {
-      const int at = atomicAdd(&r.cut.listed, 1);
-      if (at < kList) r.list[at] = (unsigned long long)~key_of(x) << 32 | (uint32_t)i;
+      const int at = atomicAdd(&here, 1);
+      if (at < kList) list[at] = (unsigned long long)~key_of(x) << 32 | (uint32_t)i;
     }
   });
   sum = sum_over_wave(sum);
   __syncthreads();
   if (lane == 0) sums[wave] = sum;
+  if (threadIdx.x == 0 && here > 0) at_list = atomicAdd(&r.cut.listed, here);
   __syncthreads();
+  for (int j = threadIdx.x; j < here && at_list + j < kList; j += kThreads) r.list[at_list + j] = list[j];
   if (threadIdx.x == 0) {
     sum = 0;
 #pragma unroll
-    for (int w = 0; w < kPartWaves; ++w) sum += sums[w];
+    for (int w = 0; w < kWaves; ++w) sum += sums[w];
     parts[blockIdx.x].above = sum;
+  }
+}
+
+// The part that a row's number falls into where there are no filters: parts have references of their own, so their sums are added in 64-bit floating
+// point, in a fixed order.  One wavefront; part, way into it, sum of the row.
+struct PlainDraw {
+  double total;
+  unsigned long long way;
+  int32_t part;
+};
+__device__ PlainDraw plain_part(const Part* parts, int n, float top, double inv, float u) {
+  const int lane = threadIdx.x & 63;
+  double total = 0., run = 0., before = 0.;
+  int found = -1;
+  auto weight_at = [&](int p) { return p < n && parts[p].top != -INFINITY ? parts[p].sum * exp(((double)parts[p].top - (double)top) * inv) : 0.; };
+  for (int p0 = 0; p0 < n; p0 += 64) total += weight_at(p0 + lane);
+  for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
+  const double target = (u > 0.f ? u < 1.f ? (double)u : 1. - 1e-16 : 0.) * total;
+  for (int p0 = 0; p0 < n; p0 += 64) {
+    const double w = weight_at(p0 + lane);
+    double upto = w;
+    for (int d = 1; d < 64; d <<= 1) {
+      const double other = __shfl_up(upto, d);
+      if (lane >= d) upto += other;
+    }
+    upto += run;
+    run = __shfl(upto, 63);
+    // the first one past the target; by the roundings of the sums there may be none: the last with any weight
+    const unsigned long long past = __ballot(w > 0. && target < upto), any = __ballot(w > 0.);
+    if (!any) continue;
+    const int at = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(any);
+    found = p0 + at;
+    before = __shfl(upto - w, at);
+    if (past) break;
+  }
+  // (the way into the part, in its own unit; where the roundings of the sums lead behind the part's last token, that one is drawn)
+  const double way = (target - before) / exp(((double)parts[found].top - (double)top) * inv);
+  return {total, way > 0. ? (unsigned long long)way : 0, found};
+}
+
+// Rows without filters, the temperature the same for all and above 0.
+template <typename T>
+__global__ __launch_bounds__(kFewThreads) void draw_plain_kernel(SampleCall c, Space space, int bits) {
+  __shared__ PlaceSmem place;
+  __shared__ uint64_t roots[kRootCount];
+  const int64_t n = space.first_row + blockIdx.x;
+  const T* row = static_cast<const T*>(c.logits) + n * c.stride;
+  const Part* parts = space.parts + (int64_t)blockIdx.x * space.n_parts;
+  Settings s = {c.temperature, 1., 0., 0};
+  const float u = c.uniforms[n];
+  float top;
+  if (!top_of(parts, space.n_parts, top)) {             // nothing to draw from
+    if (threadIdx.x == 0) {
+      c.tokens[n] = -1;
+      if (c.logprobs) c.logprobs[n] = NAN;
+    }
+    return;
+  }
+  load_roots(roots, bits);
+  const double inv = inverse(s.t);
+  const PlainDraw d = plain_part(parts, space.n_parts, top, inv, u);      // (every wavefront for itself)
+  const Weight weight = weight_of(s, roots, parts[d.part].top, bits, 0.);
+  const int lo = d.part * kPart;
+  __syncthreads();
+  const int i = place_of<kFewThreads>(place, row, lo, min(lo + kPart, c.vocab), d.way, [&](float x, int) { return weight.whole(x); });
+  if (threadIdx.x == 0) {
+    c.tokens[n] = i;
+    if (c.logprobs) c.logprobs[n] = (float)(((double)one_value(row[i]) - (double)top) * inv - log(d.total / (double)(1ull << bits)));
   }
 }
 
@@ -562,7 +720,7 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
     }
     return;
   }
-  load_roots(sm.roots);
+  load_roots(sm.roots, bits);
   const double unit = (double)(1ull << bits), inv = inverse(s.t);
   const float u = c.uniforms[n];
   auto write = [&](int i, double total) {
@@ -576,72 +734,21 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
     for (int p = threadIdx.x; p < space.n_parts; p += kThreads)
       if (parts[p].top == r.top) atomicMin(&sm.index, p);
     __syncthreads();
-    const int lo = sm.index * space.part;
+    const int lo = sm.index * kPart;
     __syncthreads();
-    const int i = place_of(sm, row, lo, min(lo + space.part, c.vocab), 0, [&](float x, int) { return (unsigned long long)(x == r.top); });
+    const int i = place_of<kThreads>(sm.place, row, lo, min(lo + kPart, c.vocab), 0, [&](float x, int) { return (unsigned long long)(x == r.top); });
     if (threadIdx.x == 0) {
       c.tokens[n] = i;
       if (c.logprobs) c.logprobs[n] = 0.f;
     }
     return;
   }
-  // Parts of the whole: (weight of the parts in front, weight) of the part that the number falls into; parts in rounds of a thread each.
   const unsigned long long u64 = !(u > 0.f) ? 0 : u < 1.f ? (unsigned long long)((double)u * 18446744073709551616.) : ~0ull;
   if (!s.filter()) {
-    // every part has its own reference: sums in 64-bit floating point, in a fixed order
-    double total = 0.;
-    if (wave == 0) {
-      double run = 0.;
-      for (int turn = 0; turn < 2; ++turn) {                 // the sum, then the part
-        const double target = turn ? (u > 0.f ? (u < 1.f ? (double)u : 1. - 1e-16) : 0.) * total : 0.;
-        run = 0.;
-        int last = -1;
-        double before_last = 0.;
-        bool done = false;
-        for (int p0 = 0; p0 < space.n_parts && !done; p0 += 64) {
-          const int p = p0 + lane;
-          double w = 0.;
-          if (p < space.n_parts && parts[p].top != -INFINITY) w = (double)parts[p].sum * exp(((double)parts[p].top - (double)r.top) * inv);
-          double upto = w;
-          for (int d = 1; d < 64; d <<= 1) {
-            const double other = __shfl_up(upto, d);
-            if (lane >= d) upto += other;
-          }
-          upto += run;
-          if (turn) {
-            const double before = upto - w;
-            unsigned long long here = __ballot(w > 0.);
-            if (here) {
-              const int at = 63 - __builtin_clzll(here);
-              last = p0 + at;
-              before_last = __shfl(before, at);
-            }
-            here = __ballot(w > 0. && target < upto);
-            if (here) {
-              const int at = __builtin_ctzll(here);
-              last = p0 + at;
-              before_last = __shfl(before, at);
-              done = true;
-            }
-          }
-          run = __shfl(upto, 63);
-        }
-        if (!turn) total = run;
-        else if (lane == 0) {
-          // (the way into the part, in its own unit)
-          double way = (target - before_last) / exp(((double)parts[last].top - (double)r.top) * inv);
-          const unsigned long long most = parts[last].sum - 1;
-          sm.found = last;
-          sm.found_before = !(way > 0.) ? 0 : way < (double)most ? (unsigned long long)way : most;
-          sm.found_mass = (unsigned long long)__double_as_longlong(total);
-        }
-      }
-    }
-    __syncthreads();
-    const int p = sm.found, lo = p * space.part;
-    total = __longlong_as_double((long long)sm.found_mass);
+    const PlainDraw d = plain_part(parts, space.n_parts, r.top, inv, u);      // (every wavefront for itself)
+    const int p = d.part, lo = p * kPart;
     const Weight weight = weight_of(s, sm.roots, parts[p].top, bits, 0.);
-    write(place_of(sm, row, lo, min(lo + space.part, c.vocab), sm.found_before, [&](float x, int) { return weight(x); }), total);
+    write(place_of<kThreads>(sm.place, row, lo, min(lo + kPart, c.vocab), d.way, [&](float x, int) { return weight.whole(x); }), d.total);
     return;
   }
 
@@ -664,25 +771,43 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
         weights[j] = all(__uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key));
       }
       __syncthreads();
+      // (a token's comparisons are shared by as many threads as there are for each)
+      __shared__ unsigned long long in_front_of[kList];
+      __shared__ uint32_t ahead_of[kList];
+      int each = 64;
+      while (each < count && each < kThreads) each *= 2;
+      const int share = kThreads / each, len = (count + share - 1) / share, from = threadIdx.x / each * len, to = min(from + len, count);
+      for (int j = threadIdx.x; j < count; j += kThreads) {
+        in_front_of[j] = 0;
+        ahead_of[j] = 0;
+      }
+      __syncthreads();
+      for (int j = threadIdx.x % each; j < count; j += each) {
+        const unsigned long long mine = order[j];
+        uint32_t ahead = 0;
+        unsigned long long sum = 0;
+#pragma unroll 8
+        for (int i = from; i < to; ++i) {           // (without branches: the reads go out together)
+          const bool is = order[i] < mine;
+          ahead += is;
+          sum += is ? weights[i] : 0ull;
+        }
+        atomicAdd(&ahead_of[j], ahead);
+        atomicAdd(&in_front_of[j], sum);
+      }
+      __syncthreads();
       uint32_t rank[kList / kThreads];
       unsigned long long before[kList / kThreads], mine[kList / kThreads], total = 0;
 #pragma unroll
       for (int q = 0; q < kList / kThreads; ++q) {
         const int j = q * kThreads + threadIdx.x;
         rank[q] = 0xffffffffu;
-        before[q] = 0;
+        before[q] = mine[q] = 0;
         if (j >= count) continue;
         mine[q] = order[j];
-        uint32_t ahead = 0;
-        unsigned long long sum = 0;
-        for (int i = 0; i < count; ++i)
-          if (order[i] < mine[q]) {
-            ++ahead;
-            sum += weights[i];
-          }
-        rank[q] = ahead;
-        before[q] = sum;
-        if (s.top_k > 0 && ahead < (uint32_t)s.top_k) total += weights[j];
+        rank[q] = ahead_of[j];
+        before[q] = in_front_of[j];
+        if (s.top_k > 0 && rank[q] < (uint32_t)s.top_k) total += weights[j];
       }
       double target = INFINITY;
       if (s.top_p < 1.) {
@@ -753,7 +878,7 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
     sum = 0;
     for (int w = 0; w < kWaves; ++w) sum += sm.sums[w];
     __syncthreads();
-    write(place_of(sm, row, 0, c.vocab, __umul64hi(sum, u64), kept_weight), (double)sum);
+    write(place_of<kThreads>(sm.place, row, 0, c.vocab, __umul64hi(sum, u64), kept_weight), (double)sum);
     return;
   }
   // what is kept of every part: what is above the list, and of the list
@@ -766,7 +891,7 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
       const unsigned long long e = space_of_row.list[j];
       const uint32_t key = ~(uint32_t)(e >> 32);
       const unsigned long long w = kept_weight(__uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key), (int)(uint32_t)e);
-      if (w) atomicAdd(&of_part[(uint32_t)e / (uint32_t)space.part], w);
+      if (w) atomicAdd(&of_part[(uint32_t)e / kPart], w);
     }
   for (int p = threadIdx.x; p < kBins; p += kThreads) sm.count[p] = 0;
   __syncthreads();
@@ -780,17 +905,15 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
   __syncthreads();
   const unsigned long long target = __umul64hi(total, u64);
   bin_of(sm, true, target);
-  const int lo = (int)sm.found * space.part;
+  const int lo = (int)sm.found * kPart;
   const unsigned long long way = target - sm.found_before;
   __syncthreads();
-  write(place_of(sm, row, lo, min(lo + space.part, c.vocab), way, kept_weight), (double)total);
+  write(place_of<kThreads>(sm.place, row, lo, min(lo + kPart, c.vocab), way, kept_weight), (double)total);
 }
 
 Space space_of(const SampleCall& c, int64_t rows) {
   Space s;
-  s.part = part_tokens(rows < kRowsAtOnce ? rows : kRowsAtOnce, c.vocab);
-  if ((int64_t)s.part * kBins < c.vocab) s.part = 8192;          // (a bin for every part)
-  s.n_parts = (c.vocab + s.part - 1) / s.part;
+  s.n_parts = (c.vocab + kPart - 1) / kPart;                    // (at most kBins: vocab <= 2^24)
   s.rows = static_cast<RowSpace*>(c.workspace);
   s.parts = reinterpret_cast<Part*>(s.rows + (rows < kRowsAtOnce ? rows : kRowsAtOnce));
   s.first_row = 0;
@@ -806,11 +929,13 @@ hipError_t launch_typed(const SampleCall& c, hipStream_t stream) {
   for (; s.first_row < c.rows; s.first_row += kRowsAtOnce) {
     const int64_t left = c.rows - s.first_row;
     const dim3 grid((unsigned)s.n_parts, (unsigned)(left < kRowsAtOnce ? left : kRowsAtOnce));
-    if (s.part == 8192) parts_kernel<T, 4><<<grid, kPartThreads, 0, stream>>>(c, s, bits, cuts);
-    else parts_kernel<T, 1><<<grid, kPartThreads, 0, stream>>>(c, s, bits, cuts);
-    if (cuts) bins_kernel<T><<<grid, kPartThreads, 0, stream>>>(c, s, bits);
-    if (filters) collect_kernel<T><<<grid, kPartThreads, 0, stream>>>(c, s, bits);
-    draw_kernel<T><<<grid.y, kThreads, 0, stream>>>(c, s, bits);
+    // (eight tokens a thread where latency counts, 32 where there is enough to do)
+    if ((int64_t)grid.x * grid.y < 1024) parts_kernel<T, kThreads><<<grid, kThreads, 0, stream>>>(c, s, bits, cuts);
+    else parts_kernel<T, kFewThreads><<<grid, kFewThreads, 0, stream>>>(c, s, bits, cuts);
+    if (cuts) bins_kernel<T><<<grid, kThreads, 0, stream>>>(c, s, bits);
+    if (filters) collect_kernel<T><<<grid, kThreads, 0, stream>>>(c, s, bits);
+    if (!filters && !c.temperatures && c.temperature > 0.) draw_plain_kernel<T><<<grid.y, kFewThreads, 0, stream>>>(c, s, bits);
+    else draw_kernel<T><<<grid.y, kThreads, 0, stream>>>(c, s, bits);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;
   }
