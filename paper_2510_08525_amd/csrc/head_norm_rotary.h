@@ -22,7 +22,7 @@ struct HeadNormCall {
   void* grad;                      // backward: packed, rows grad_stride elements apart
   int64_t grad_stride;
   float *grad_q_weight, *grad_k_weight;      // backward, fp32 [kHeadDim]; null: not wanted
-  float* partials;                 // backward: [blocks][2][kHeadDim]
+  float* partials;                 // backward: [blocks][kHeadDim]
 };
 hipError_t launch_head_norm_rotary(const HeadNormCall& call, const RotaryTurns& turns, int dtype, hipStream_t stream);
 hipError_t launch_head_norm_rotary_grad(const HeadNormCall& call, const RotaryTurns& turns, int dtype, hipStream_t stream);

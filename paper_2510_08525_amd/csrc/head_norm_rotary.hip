@@ -28,97 +28,131 @@ __device__ __forceinline__ void angles_at(const RotaryTurns& turns, int j, int p
   for (int i = 0; i < 8; ++i) g.sine[i] *= direction;
 }
 
-// A part of a token's heads: token, first and last head.
-struct Part { int64_t token; int first, last; };
-__device__ __forceinline__ Part part_of(int64_t index, int parts, int heads_each, int heads) {
-  Part p;
-  p.token = index / parts;
-  p.first = (int)(index - p.token * parts) * heads_each;
-  p.last = p.first + heads_each < heads ? p.first + heads_each : heads;
-  return p;
+// Queries, keys and values of a token are dealt out in parts, heads of one kind that a thread takes one after the other.
+enum Kind { kQuery, kKey, kValue };
+struct Deal {
+  int32_t heads[3];              // of a token (0 of values: they stay where they are)
+  int32_t each[3], parts[3];     // heads of a part, at most; parts of a token
+};
+Deal deal_of(const HeadNormCall& c) {
+  Deal d;
+  d.heads[kQuery] = c.n_q_heads;
+  d.heads[kKey] = c.n_kv_heads;
+  d.heads[kValue] = c.v.p ? c.n_kv_heads : 0;
+  // (one head each where there are few rows)
+  const bool many = (int64_t)c.tokens * (c.n_q_heads + c.n_kv_heads) >= 65536;
+  for (int k = 0; k < 3; ++k) {
+    d.parts[k] = many ? (d.heads[k] + 7) / 8 : d.heads[k];
+    d.each[k] = d.parts[k] ? (d.heads[k] + d.parts[k] - 1) / d.parts[k] : 0;
+  }
+  return d;
+}
+
+// Two pieces of a row as they come from memory.
+template <typename T> struct TwoPieces { Piece<T> a, b; };
+template <bool STREAM, typename T>
+__device__ __forceinline__ TwoPieces<T> two_at(const T* row, int c0, int c1) {
+  return {piece_at<STREAM>(row + c0), piece_at<STREAM>(row + c1)};
+}
+template <typename T>
+__device__ __forceinline__ void load_weight(const void* w, int c0, int c1, float (&f)[16]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    f[i] = w ? one_value(static_cast<const T*>(w)[c0 + i]) : 1.f;
+    f[8 + i] = w ? one_value(static_cast<const T*>(w)[c1 + i]) : 1.f;
+  }
 }
 
 template <typename T, bool STREAM>
-__global__ __launch_bounds__(kBlock) void head_norm_rotary_kernel(HeadNormCall c, RotaryTurns turns, int heads, int heads_each) {
+__global__ __launch_bounds__(kBlock) void head_norm_rotary_kernel(HeadNormCall c, RotaryTurns turns, Deal deal) {
   const int j = threadIdx.x % kRowThreads, Hq = c.n_q_heads, H = c.n_kv_heads;
   const int c0 = first_piece(turns, j) * 8, c1 = second_piece(turns, j) * 8;
-  const bool turned = j < turns.pairs / 8;
-  const int parts = (heads + heads_each - 1) / heads_each;
-  const Part p = part_of((int64_t)blockIdx.x * kItems + threadIdx.x / kRowThreads, parts, heads_each, heads);
-  if (p.token >= c.tokens) return;
-  const T* row = static_cast<const T*>(c.qkv) + p.token * c.token_stride;
+  const uint32_t parts = deal.parts[0] + deal.parts[1] + deal.parts[2];
+  const uint32_t index = blockIdx.x * kItems + threadIdx.x / kRowThreads, token = index / parts;
+  int part = (int)(index - token * parts);
+  if (token >= (uint32_t)c.tokens) return;
+  const int kind = part < deal.parts[0] ? kQuery : part < deal.parts[0] + deal.parts[1] ? kKey : kValue;
+  part -= kind == kQuery ? 0 : kind == kKey ? deal.parts[0] : deal.parts[0] + deal.parts[1];
+  const int each = kind == kQuery ? deal.each[0] : kind == kKey ? deal.each[1] : deal.each[2], heads = kind == kQuery ? Hq : H;
+  const int first = part * each, last = min(first + each, heads);
+  const T* row = static_cast<const T*>(c.qkv) + token * c.token_stride + (int64_t)(kind == kQuery ? 0 : kind == kKey ? Hq : Hq + H) * kHeadDim;
+  const TokenHeads to = kind == kQuery ? c.q : kind == kKey ? c.k : c.v;
+  T* out = static_cast<T*>(to.p) + token * to.token;
+  if (first >= last) return;
+  TwoPieces<T> next = two_at<STREAM>(row + (int64_t)first * kHeadDim, c0, c1);
+  const bool turned = kind != kValue && j < turns.pairs / 8, normed = kind != kValue && c.norm;
+  float w[16];
+  if (normed) load_weight<T>(kind == kQuery ? c.q_weight : c.k_weight, c0, c1, w);
   Angles g = {};
-  if (turned && p.first < Hq + H) angles_at(turns, j, c.positions[p.token], 1.f, g);
-  float wq[16], wk[16];
-  auto weights = [&](const void* w, float (&f)[16]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      f[i] = w ? one_value(static_cast<const T*>(w)[c0 + i]) : 1.f;
-      f[8 + i] = w ? one_value(static_cast<const T*>(w)[c1 + i]) : 1.f;
-    }
-  };
-  if (c.norm && p.first < Hq) weights(c.q_weight, wq);
-  if (c.norm && p.last > Hq) weights(c.k_weight, wk);
-  for (int h = p.first; h < p.last; ++h) {
+  if (turned) angles_at(turns, j, c.positions[token], 1.f, g);
+  for (int h = first; h < last; ++h) {
     float x[8], y[8];
-    load_piece<STREAM>(row + (int64_t)h * kHeadDim, c0, kHeadDim, x);
-    load_piece<STREAM>(row + (int64_t)h * kHeadDim, c1, kHeadDim, y);
-    if (c.norm && h < Hq + H) {
+    widen(next.a, x);
+    widen(next.b, y);
+    if (h + 1 < last) next = two_at<STREAM>(row + (int64_t)(h + 1) * kHeadDim, c0, c1);
+    if (normed) {
       float squares = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) squares += x[i] * x[i] + y[i] * y[i];
       const float r = 1.f / sqrtf(sum_of_row(squares) * (1.f / kHeadDim) + c.eps);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[i] *= r * (h < Hq ? wq[i] : wk[i]);
-        y[i] *= r * (h < Hq ? wq[8 + i] : wk[8 + i]);
+        x[i] *= r * w[i];
+        y[i] *= r * w[8 + i];
       }
     }
-    if (turned && h < Hq + H) rotate(turns, g, x, y);
-    const TokenHeads& to = h < Hq ? c.q : h < Hq + H ? c.k : c.v;
-    T* out = static_cast<T*>(to.p) + p.token * to.token + (h < Hq ? h : h < Hq + H ? h - Hq : h - Hq - H) * to.head;
-    store_piece<STREAM>(out, c0, kHeadDim, x);
-    store_piece<STREAM>(out, c1, kHeadDim, y);
+    if (turned) rotate(turns, g, x, y);
+    store_piece<STREAM>(out + h * to.head, c0, kHeadDim, x);
+    store_piece<STREAM>(out + h * to.head, c1, kHeadDim, y);
   }
 }
 
-template <typename T, bool STREAM>
-__global__ __launch_bounds__(kBlock) void head_norm_rotary_grad_kernel(HeadNormCall c, RotaryTurns turns, int heads, int heads_each, int64_t items) {
+// Workgroups [first[k], first[k + 1]) take the parts of kind k, one after the other.
+struct GradGrid { int32_t first[4]; };
+
+template <typename T, bool NORM, bool STREAM>
+__global__ __launch_bounds__(kBlock) void head_norm_rotary_grad_kernel(HeadNormCall c, RotaryTurns turns, Deal deal, GradGrid grid) {
   const int j = threadIdx.x % kRowThreads, Hq = c.n_q_heads, H = c.n_kv_heads;
   const int c0 = first_piece(turns, j) * 8, c1 = second_piece(turns, j) * 8;
-  const bool turned = j < turns.pairs / 8;
-  const int parts = (heads + heads_each - 1) / heads_each;
-  float wq[16], wk[16], gq[16], gk[16];
-  auto weights = [&](const void* w, float (&f)[16]) {
+  const int kind = (int)blockIdx.x < grid.first[1] ? kQuery : (int)blockIdx.x < grid.first[2] ? kKey : kValue;
+  const int first_block = kind == kQuery ? 0 : kind == kKey ? grid.first[1] : grid.first[2];
+  const int blocks = (kind == kQuery ? grid.first[1] : kind == kKey ? grid.first[2] : grid.first[3]) - first_block;
+  const uint32_t parts = kind == kQuery ? deal.parts[0] : kind == kKey ? deal.parts[1] : deal.parts[2];
+  const int each = kind == kQuery ? deal.each[0] : kind == kKey ? deal.each[1] : deal.each[2], heads = kind == kQuery ? Hq : H;
+  const int64_t column = (int64_t)(kind == kQuery ? 0 : kind == kKey ? Hq : Hq + H) * kHeadDim;
+  const TokenHeads from = kind == kQuery ? c.q : kind == kKey ? c.k : c.v;
+  const bool turned = kind != kValue && j < turns.pairs / 8, normed = NORM && kind != kValue;
+  float w[16], sum[16];
+  if (normed) load_weight<T>(kind == kQuery ? c.q_weight : c.k_weight, c0, c1, w);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      f[i] = w ? one_value(static_cast<const T*>(w)[c0 + i]) : 1.f;
-      f[8 + i] = w ? one_value(static_cast<const T*>(w)[c1 + i]) : 1.f;
-    }
-  };
-  if (c.norm) {
-    weights(c.q_weight, wq);
-    weights(c.k_weight, wk);
-  }
-#pragma unroll
-  for (int i = 0; i < 16; ++i) gq[i] = gk[i] = 0.f;
-  for (int64_t index = (int64_t)blockIdx.x * kItems + threadIdx.x / kRowThreads; index < items; index += (int64_t)gridDim.x * kItems) {
-    const Part p = part_of(index, parts, heads_each, heads);
-    const T* row = static_cast<const T*>(c.qkv) + p.token * c.token_stride;
-    T* out = static_cast<T*>(c.grad) + p.token * c.grad_stride;
+  for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+  const uint32_t items = (uint32_t)c.tokens * parts;
+  for (uint32_t index = (blockIdx.x - first_block) * kItems + threadIdx.x / kRowThreads; index < items; index += blocks * kItems) {
+    const uint32_t token = index / parts;
+    const int first = (int)(index - token * parts) * each, last = min(first + each, heads);
+    const T* row = static_cast<const T*>(c.qkv) + token * c.token_stride + column;
+    const T* grad = static_cast<const T*>(from.p) + token * from.token;
+    T* out = static_cast<T*>(c.grad) + token * c.grad_stride + column;
+    if (first >= last) continue;
+    TwoPieces<T> next_g = two_at<STREAM>(grad + first * from.head, c0, c1), next_x = next_g;
+    if (normed) next_x = two_at<STREAM>(row + (int64_t)first * kHeadDim, c0, c1);
     Angles g = {};
-    if (turned && p.first < Hq + H) angles_at(turns, j, c.positions[p.token], -1.f, g);
-    for (int h = p.first; h < p.last; ++h) {
-      const TokenHeads& from = h < Hq ? c.q : h < Hq + H ? c.k : c.v;
-      const T* grad = static_cast<const T*>(from.p) + p.token * from.token + (h < Hq ? h : h < Hq + H ? h - Hq : h - Hq - H) * from.head;
-      float x[8], y[8];
-      load_piece<STREAM>(grad, c0, kHeadDim, x);
-      load_piece<STREAM>(grad, c1, kHeadDim, y);
-      if (turned && h < Hq + H) rotate(turns, g, x, y);
-      if (c.norm && h < Hq + H) {
-        float a[8], b[8], squares = 0.f, along = 0.f;
-        load_piece<STREAM>(row + (int64_t)h * kHeadDim, c0, kHeadDim, a);
-        load_piece<STREAM>(row + (int64_t)h * kHeadDim, c1, kHeadDim, b);
+    if (turned) angles_at(turns, j, c.positions[token], -1.f, g);
+    for (int h = first; h < last; ++h) {
+      float x[8], y[8], a[8], b[8];
+      widen(next_g.a, x);
+      widen(next_g.b, y);
+      if (normed) {
+        widen(next_x.a, a);
+        widen(next_x.b, b);
+      }
+      if (h + 1 < last) {
+        next_g = two_at<STREAM>(grad + (h + 1) * from.head, c0, c1);
+        if (normed) next_x = two_at<STREAM>(row + (int64_t)(h + 1) * kHeadDim, c0, c1);
+      }
+      if (turned) rotate(turns, g, x, y);
+      if (normed) {
+        float squares = 0.f, along = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) squares += a[i] * a[i] + b[i] * b[i];
         const float r = 1.f / sqrtf(sum_of_row(squares) * (1.f / kHeadDim) + c.eps);
@@ -126,15 +160,10 @@ __global__ __launch_bounds__(kBlock) void head_norm_rotary_grad_kernel(HeadNormC
         for (int i = 0; i < 8; ++i) {
           a[i] *= r;
           b[i] *= r;
-          if (h < Hq) {
-            gq[i] = __builtin_fmaf(x[i], a[i], gq[i]);
-            gq[8 + i] = __builtin_fmaf(y[i], b[i], gq[8 + i]);
-          } else {
-            gk[i] = __builtin_fmaf(x[i], a[i], gk[i]);
-            gk[8 + i] = __builtin_fmaf(y[i], b[i], gk[8 + i]);
-          }
-          x[i] *= h < Hq ? wq[i] : wk[i];
-          y[i] *= h < Hq ? wq[8 + i] : wk[8 + i];
+          sum[i] = __builtin_fmaf(x[i], a[i], sum[i]);
+          sum[8 + i] = __builtin_fmaf(y[i], b[i], sum[8 + i]);
+          x[i] *= w[i];
+          y[i] *= w[8 + i];
           along = __builtin_fmaf(x[i], a[i], along);
           along = __builtin_fmaf(y[i], b[i], along);
         }
@@ -149,91 +178,90 @@ __global__ __launch_bounds__(kBlock) void head_norm_rotary_grad_kernel(HeadNormC
       store_piece<STREAM>(out + (int64_t)h * kHeadDim, c1, kHeadDim, y);
     }
   }
-  if (!c.partials) return;
+  if (!NORM || !c.partials || kind == kValue) return;
   // over the rows side by side: first within the wavefront (lanes 8 apart), then over the wavefronts
-  __shared__ float sums[kBlock / 64][2][kHeadDim];
+  __shared__ float sums[kBlock / 64][kHeadDim];
   const int wave = threadIdx.x >> 6;
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
-    float q = gq[i], k = gk[i];
-    for (int d = 8; d < 64; d *= 2) {
-      q += __shfl_xor(q, d);
-      k += __shfl_xor(k, d);
-    }
-    if ((threadIdx.x & 63) < kRowThreads) {
-      const int col = i < 8 ? c0 + i : c1 + i - 8;
-      sums[wave][0][col] = q;
-      sums[wave][1][col] = k;
-    }
+    float s = sum[i];
+    for (int d = 8; d < 64; d *= 2) s += __shfl_xor(s, d);
+    if ((threadIdx.x & 63) < kRowThreads) sums[wave][i < 8 ? c0 + i : c1 + i - 8] = s;
   }
   __syncthreads();
+  if (threadIdx.x >= kHeadDim) return;
   float total = 0.f;
 #pragma unroll
-  for (int w = 0; w < kBlock / 64; ++w) total += sums[w][threadIdx.x >> 7][threadIdx.x & 127];
-  c.partials[(int64_t)blockIdx.x * 2 * kHeadDim + threadIdx.x] = total;
+  for (int v = 0; v < kBlock / 64; ++v) total += sums[v][threadIdx.x];
+  c.partials[(int64_t)blockIdx.x * kHeadDim + threadIdx.x] = total;
 }
-static_assert(kBlock == 2 * kHeadDim, "a thread of the last step has a column of one weight");
 
-// The workgroups' sums of 32 of the 256 columns, eight rows side by side, in 64 bits.
-__global__ __launch_bounds__(kBlock) void weight_grad_kernel(const float* __restrict__ partials, int blocks, float* __restrict__ grad_q,
-                                                             float* __restrict__ grad_k) {
-  __shared__ double sums[8][32];
-  const int col = blockIdx.x * 32 + (threadIdx.x & 31), part = threadIdx.x >> 5;
+// The workgroups' sums of 16 columns of one weight, 64 rows side by side, in 64 bits.
+constexpr int kSumThreads = 1024, kSumColumns = 16, kSumRows = kSumThreads / kSumColumns;
+__global__ __launch_bounds__(kSumThreads) void weight_grad_kernel(const float* __restrict__ partials, GradGrid grid, float* __restrict__ grad_q,
+                                                                  float* __restrict__ grad_k) {
+  __shared__ double sums[kSumRows][kSumColumns];
+  const int kind = blockIdx.y, col = blockIdx.x * kSumColumns + threadIdx.x % kSumColumns, part = threadIdx.x / kSumColumns;
+  float* out = kind == kQuery ? grad_q : grad_k;
+  if (!out) return;
+  const int first = kind == kQuery ? 0 : grid.first[1], last = kind == kQuery ? grid.first[1] : grid.first[2];
   double sum = 0.;
-  for (int b = part; b < blocks; b += 8) sum += partials[(int64_t)b * 2 * kHeadDim + col];
-  sums[part][threadIdx.x & 31] = sum;
+#pragma unroll 4
+  for (int b = first + part; b < last; b += kSumRows) sum += partials[(int64_t)b * kHeadDim + col];
+  sums[part][threadIdx.x % kSumColumns] = sum;
   __syncthreads();
-  if (part != 0) return;
-  for (int i = 1; i < 8; ++i) sum += sums[i][threadIdx.x];
-  float* out = col < kHeadDim ? grad_q : grad_k;
-  if (out) out[col & (kHeadDim - 1)] = (float)sum;
+  for (int n = kSumRows / 2; n; n /= 2) {
+    if (part < n) sums[part][threadIdx.x % kSumColumns] += sums[part + n][threadIdx.x % kSumColumns];
+    __syncthreads();
+  }
+  if (part == 0) out[col] = (float)sums[0][threadIdx.x];
 }
 
-// Heads a thread takes one after the other: few where there are few rows.
-int heads_each_of(int64_t rows) { return rows >= 65536 ? 8 : 1; }
-
-constexpr int kGradBlocks = 1024;
-int64_t grad_items(const HeadNormCall& c, int heads, int heads_each) { return (int64_t)c.tokens * ((heads + heads_each - 1) / heads_each); }
+constexpr int kGradBlocks = 1024;          // four a compute unit
 
 template <typename T>
 hipError_t launch_forward(const HeadNormCall& c, const RotaryTurns& turns, hipStream_t stream) {
-  const int heads = c.n_q_heads + c.n_kv_heads * (c.v.p ? 2 : 1);
-  const int heads_each = heads_each_of((int64_t)c.tokens * heads);
-  const int64_t blocks = (grad_items(c, heads, heads_each) + kItems - 1) / kItems;
-  const bool streams = (int64_t)c.tokens * heads * kHeadDim * 2 * (int64_t)sizeof(T) > kStreamBytes;
+  const Deal deal = deal_of(c);
+  const int64_t items = (int64_t)c.tokens * (deal.parts[0] + deal.parts[1] + deal.parts[2]);
+  const int64_t heads = deal.heads[0] + deal.heads[1] + deal.heads[2];
+  const bool streams = c.tokens * heads * kHeadDim * 2 * (int64_t)sizeof(T) > kStreamBytes;
   auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kBlock), 0, stream, c, turns, heads, heads_each);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((items + kItems - 1) / kItems)), dim3(kBlock), 0, stream, c, turns, deal);
     return hipGetLastError();
   };
   return streams ? launch(head_norm_rotary_kernel<T, true>) : launch(head_norm_rotary_kernel<T, false>);
 }
 template <typename T>
 hipError_t launch_backward(HeadNormCall c, const RotaryTurns& turns, hipStream_t stream) {
-  const int heads = c.n_q_heads + c.n_kv_heads * (c.v.p ? 2 : 1);
-  const int heads_each = heads_each_of((int64_t)c.tokens * heads);
-  const int64_t items = grad_items(c, heads, heads_each), all = (items + kItems - 1) / kItems;
+  const Deal deal = deal_of(c);
   const bool sums = c.grad_q_weight || c.grad_k_weight;
   if (!sums) c.partials = nullptr;
-  const int blocks = (int)(all < kGradBlocks ? all : kGradBlocks);
-  const bool streams = (int64_t)c.tokens * heads * kHeadDim * 3 * (int64_t)sizeof(T) > kStreamBytes;
+  const int64_t heads = deal.heads[0] + deal.heads[1] + deal.heads[2];
+  GradGrid grid = {};
+  for (int k = 0; k < 3; ++k) {
+    const int64_t all = ((int64_t)c.tokens * deal.parts[k] + kItems - 1) / kItems, share = (kGradBlocks * (int64_t)deal.heads[k] + heads - 1) / heads;
+    grid.first[k + 1] = grid.first[k] + (int)(all < share ? all : share);
+  }
+  const bool streams = c.tokens * heads * kHeadDim * 3 * (int64_t)sizeof(T) > kStreamBytes;
   auto launch = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kBlock), 0, stream, c, turns, heads, heads_each, items);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid.first[3]), dim3(kBlock), 0, stream, c, turns, deal, grid);
     return hipGetLastError();
   };
-  if (blocks > 0) {
-    const hipError_t err = streams ? launch(head_norm_rotary_grad_kernel<T, true>) : launch(head_norm_rotary_grad_kernel<T, false>);
+  if (c.tokens > 0) {
+    const hipError_t err = c.norm ? streams ? launch(head_norm_rotary_grad_kernel<T, true, true>) : launch(head_norm_rotary_grad_kernel<T, true, false>)
+                                  : streams ? launch(head_norm_rotary_grad_kernel<T, false, true>) : launch(head_norm_rotary_grad_kernel<T, false, false>);
     if (err != hipSuccess) return err;
   }
   if (!sums) return hipSuccess;
-  weight_grad_kernel<<<2 * kHeadDim / 32, kBlock, 0, stream>>>(c.partials, blocks, c.grad_q_weight, c.grad_k_weight);
+  weight_grad_kernel<<<dim3(kHeadDim / kSumColumns, 2), kSumThreads, 0, stream>>>(c.partials, grid, c.grad_q_weight, c.grad_k_weight);
   return hipGetLastError();
 }
 
 }  // namespace
 
 size_t head_norm_grad_workspace(int tokens, int n_q_heads, int n_kv_heads) {
-  const int64_t all = ((int64_t)tokens * (n_q_heads + 2 * (int64_t)n_kv_heads) + kItems - 1) / kItems;
-  return (size_t)(all < kGradBlocks ? all : kGradBlocks) * 2 * kHeadDim * sizeof(float);
+  const int64_t all = ((int64_t)tokens * (n_q_heads + 2 * (int64_t)n_kv_heads) + kItems - 1) / kItems + 2;      // (a share is rounded up for each kind)
+  return (size_t)(all < kGradBlocks + 3 ? all : kGradBlocks + 3) * kHeadDim * sizeof(float);
 }
 
 hipError_t launch_head_norm_rotary(const HeadNormCall& call, const RotaryTurns& turns, int dtype, hipStream_t stream) {
