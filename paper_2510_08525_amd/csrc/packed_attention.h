@@ -58,17 +58,41 @@ constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 // Which sequence a position belongs to.  Offsets come from device memory, where the host cannot check them: whatever they hold, 0 <= begin <=
 // position < end <= tokens.  A position of no sequence has begin = -1.
 struct Span { int32_t begin, end; };
-constexpr int kOffsetsInLds = 1024;
+// The same position in all lanes.  64 offsets are looked at at a time, so up to 63 sequences take one turn of memory, up to 4095 two.
 __device__ __forceinline__ Span span_of(const int32_t* offsets, int n_seqs, int tokens, int position) {
-  int lo = 0, hi = n_seqs + 1;                 // the first offset behind the position is in [lo, hi]
-  while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
-    if (offsets[mid] > position) hi = mid;
-    else lo = mid + 1;
+  const int lane = threadIdx.x & 63;
+  int from = 0, to = n_seqs + 1;               // the first offset behind the position is in [from, to]
+  while (to - from > 64) {
+    const int each = (to - from + 63) / 64, at = from + (lane + 1) * each - 1;
+    const int below = __popcll(__ballot(at < to && offsets[at < to ? at : from] <= position));      // (not decreasing: the first ones)
+    from += below * each;
+    to = min(to, from + each);
   }
-  if (lo == 0 || lo > n_seqs || position >= tokens) return {-1, -1};
-  const int b = offsets[lo - 1], e = offsets[lo];
-  return {b < 0 ? 0 : b > position ? position : b, e > tokens ? tokens : e};
+  const int x = from + lane < to ? offsets[from + lane] : 0;
+  const int below = __popcll(__ballot(from + lane < to && x <= position)), at = from + below;
+  if (at <= 0 || at > n_seqs || position >= tokens) return {-1, -1};
+  const int b = below > 0 ? __builtin_amdgcn_readlane(x, below - 1) : offsets[at - 1];
+  const int e = below < 64 && from + below < to ? __builtin_amdgcn_readlane(x, below) : offsets[at];
+  return {b < 0 ? 0 : b > position ? position : b, e > tokens ? tokens : e > position ? e : position + 1};
+}
+// Positions that ascend over the lanes (over the first 32 of them, the others have the same again), those below 0 or from `tokens` on of no sequence: each
+// lane's own span, by as many turns as there are sequences among them.
+__device__ __forceinline__ Span span_of_lane(const int32_t* offsets, int n_seqs, int tokens, int position) {
+  Span mine = {-1, -1};
+  const int top = __builtin_amdgcn_readlane(position, 31);
+  int at = __builtin_amdgcn_readlane(position, 0);
+  while (at <= top) {
+    const Span s = span_of(offsets, n_seqs, tokens, at);
+    if (s.begin < 0) {                         // in front of the first sequence, or behind the last one
+      const int begin = offsets[0];
+      if (begin <= at) break;
+      at = begin;
+      continue;
+    }
+    if (position >= at && position < s.end) mine = s;
+    at = s.end;
+  }
+  return mine;
 }
 
 __device__ __forceinline__ float other_half(float x) {      // the value of the lane 32 away
@@ -87,52 +111,44 @@ __device__ __forceinline__ float sum_of_halves(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Over the lanes of a wavefront (an int each), to all of them.
-__device__ __forceinline__ int min_of_lanes(int x) {
-  for (int d = 32; d; d >>= 1) x = min(x, __shfl_xor(x, d));
-  return x;
-}
-__device__ __forceinline__ int max_of_lanes(int x) {
-  for (int d = 32; d; d >>= 1) x = max(x, __shfl_xor(x, d));
-  return x;
-}
-
 __device__ __forceinline__ uint32_t two_bf16(float a, float b) {      // rounded to nearest even
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   const bf16x2 r = {(__bf16)a, (__bf16)b};
   return __builtin_bit_cast(uint32_t, r);
 }
 
-// Rows in LDS: 256 bytes each in 16 units of 16 bytes, of which row r holds unit u at u ^ 2 (r % 8).  Then the 8 rows of which 8 lanes read the
-// same unit at a time, and the 4 rows of which 16 lanes read two units transposed, lie in banks of their own.
-__device__ __forceinline__ int unit_at(int row, int unit) { return row * 16 + (unit ^ ((row & 7) << 1)); }
-
-// Operand of 32 rows for the k's 16 step .. + 15 as they stand (A: rows of a tile in LDS).
+// Rows in LDS, 16 units of 16 bytes each: blocks of 8 rows x 8 units (1 KiB), in a block pairs of units, in a pair the rows.  The 8 rows of which 8 lanes
+// read the same unit at a time, and the 4 rows of which 16 lanes read a pair transposed, then lie in banks of their own; and where a unit is, is a sum
+// of what the lane and what the instruction says, so all reads of a tile have one address register (with the units of a row swapped by exclusive or,
+// 24 of them, the gradient's second kernel kept its keys outside the registers).
+__device__ __forceinline__ int unit_at(int row, int unit) {
+  return (row >> 3) * 128 + (unit >> 3) * 64 + ((unit >> 1) & 3) * 16 + (row & 7) * 2 + (unit & 1);
+}
+// Operand of 32 rows for the k's 16 step .. + 15 as they stand (A: rows of a tile in LDS); row0 a multiple of 8.
 __device__ __forceinline__ bf16x8 row_fragment(const uint4* tile, int row0, int step) {
   const int lane = threadIdx.x & 63;
-  return __builtin_bit_cast(bf16x8, tile[unit_at(row0 + (lane & 31), 2 * step + (lane >> 5))]);
+  return __builtin_bit_cast(bf16x8, tile[unit_at(lane & 31, lane >> 5) + (row0 >> 3) * 128 + (step >> 2) * 64 + (step & 3) * 16]);
 }
 // Operand of the 32 columns 32 block .. of a tile for 16 of its rows, in the order of k that a product's result has.
 __device__ __forceinline__ bf16x8 transposed_fragment(const uint4* tile, int row0, int block) {
 #ifdef __HIP_DEVICE_COMPILE__
   const int lane = threadIdx.x & 63;
-  const int row = row0 + 4 * (lane >> 5) + ((lane >> 2) & 3);
-  const int unit = 4 * block + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
-  // (row and row + 8 have the same swizzle)
-  const char* at = reinterpret_cast<const char*>(tile + unit_at(row, unit)) + 8 * (lane & 1);
+  const int own = unit_at(4 * (lane >> 5) + ((lane >> 2) & 3), 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1));
+  const char* at = reinterpret_cast<const char*>(tile) + own * 16 + 8 * (lane & 1) + ((row0 >> 3) * 128 + (block >> 1) * 64 + (block & 1) * 32) * 16;
   union { shorts4 part[2]; bf16x8 all; } f;
   f.part[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(RLKV_LDS_PTR(shorts4, at));
-  f.part[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(RLKV_LDS_PTR(shorts4, at + 8 * 256));
+  f.part[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(RLKV_LDS_PTR(shorts4, at + 128 * 16));
   return f.all;
 #else
   return bf16x8{};
 #endif
 }
 
-// 64 rows from `token` on of a head's rows, straight from memory to a tile in LDS; of a workgroup of eight wavefronts, all of them at the call.  Rows from
+// 64 rows from `token` on of a head's rows, straight from memory to a tile in LDS; all WAVES wavefronts of the workgroup are at the call.  Rows from
 // `tokens` on are the last one.  (Buffer loads, whose base is the same in all lanes; a row's place from it fits 32 bits.)
 constexpr int kStageRows = 64;
 constexpr int64_t kMostTokenStride = 1 << 24;
+template <int WAVES>
 __device__ __forceinline__ void stage_rows(const HeadRows& t, int token, int head, int tokens, uint4* tile) {
 #ifdef __HIP_DEVICE_COMPILE__
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -140,10 +156,10 @@ __device__ __forceinline__ void stage_rows(const HeadRows& t, int token, int hea
       __builtin_amdgcn_make_buffer_rsrc(t.p + (int64_t)token * t.token + (int64_t)head * t.head, 0, 0xffffffff, 0x00027000);
   const int most = tokens - 1 - token;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int row = 8 * wave + 4 * i + (lane >> 4), r = row < most ? row : most;
-    const uint32_t at = (uint32_t)r * (uint32_t)(t.token * 2) + ((lane & 15) ^ ((row & 7) << 1)) * 16;
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, RLKV_LDS_PTR(void, tile + (8 * wave + 4 * i) * 16), 16, (int)at, 0, 0, 0);
+  for (int i = 0; i < 16 / WAVES; ++i) {
+    const int block = i * WAVES + wave, row = (block >> 1) * 8 + ((lane >> 1) & 7), unit = (block & 1) * 8 + (lane >> 4) * 2 + (lane & 1);
+    const uint32_t at = (uint32_t)(row < most ? row : most) * (uint32_t)(t.token * 2) + unit * 16;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, RLKV_LDS_PTR(void, tile + block * 64), 16, (int)at, 0, 0, 0);
   }
 #endif
 }
@@ -216,9 +232,9 @@ __device__ __forceinline__ void admitted_products(const uint4* tile, int row0, c
   }
 }
 
-// ---- a workgroup of 256 columns and the tiles of keys that it walks over ----
-constexpr int kPackedWaves = 8, kPackedThreads = 64 * kPackedWaves;
-constexpr int kColumns = 32 * kPackedWaves, kKeys = kStageRows;
+// ---- a workgroup of columns, 32 a wavefront, and the tiles of keys that it walks over ----
+constexpr int kKeys = kStageRows;
+inline uint32_t column_blocks(const PackedCall& c, int waves) { return (uint32_t)(((int64_t)c.tokens * c.group + 32 * waves - 1) / (32 * waves)); }
 
 // The n-th KV head of a launch: full ones in front of local ones, so that the long workgroups are handed out first, and neighbours in the launch
 // (which the hardware deals to the 8 XCDs in turn) are of different heads: a head's keys are then read by few of the L2s.
@@ -258,10 +274,6 @@ __device__ __forceinline__ ColumnBlock column_block(const PackedCall& c, uint32_
   return b;
 }
 
-struct ColumnSmem {
-  int32_t offsets[kOffsetsInLds];
-  int32_t first[kPackedWaves], begin[kPackedWaves], last[kPackedWaves];
-};
 struct Columns {
   int pos, head, begin;                            // of the lane's column; begin: of its sequence
   bool valid, full;                                // a column of no sequence reads row 0 and writes nothing
@@ -283,48 +295,50 @@ struct Columns {
     return k0 + n - 1 <= pos_lo && k0 >= begin_hi && (full || k0 + n - 1 - begin_lo < sink || pos_hi - k0 < recent);
   }
 };
+// What a wavefront knows of its columns' positions, each of its lanes' own.  (Where offsets make no sense, so do these, but a lane's own mask is its own.)
+struct Ends { int first_lane, last_lane; };
+__device__ __forceinline__ Ends ends_of(bool valid) {
+  const uint32_t lanes = (uint32_t)__ballot(valid);
+  return {lanes ? __builtin_ctz(lanes) : -1, lanes ? 31 - __builtin_clz(lanes) : -1};
+}
+template <int WAVES>
+__device__ __forceinline__ int column_position(const PackedCall& c, const ColumnBlock& b, int& head) {
+  const uint32_t column = ((uint32_t)b.block * WAVES + (threadIdx.x >> 6)) * 32 + (threadIdx.x & 31);
+  const int pos = (int)(column / (uint32_t)c.group);
+  head = b.head * c.group + (int)(column - (uint32_t)pos * c.group);
+  return pos;
+}
 // False: no column of the block is of a sequence.
-__device__ __forceinline__ bool set_columns(const PackedCall& c, const int32_t* offsets, const ColumnBlock& b, ColumnSmem& sm, Columns& x) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const uint32_t column = (uint32_t)b.block * kColumns + wave * 32 + (lane & 31);
-  x.pos = (int)(column / (uint32_t)c.group);
-  x.head = b.head * c.group + (int)(column - (uint32_t)x.pos * c.group);
+template <int WAVES>
+__device__ __forceinline__ bool set_columns(const PackedCall& c, const ColumnBlock& b, int pos, int head, Columns& x) {
+  x.pos = pos;
+  x.head = head;
   x.full = b.full;
   x.sink = c.sink;
   x.recent = c.recent;
-  const Span span = span_of(offsets, c.n_seqs, c.tokens, x.pos);
-  x.valid = span.begin >= 0;
-  x.begin = x.valid ? span.begin : 0;
-  x.row = x.valid ? x.pos : 0;
-  x.pos_lo = min_of_lanes(x.valid ? x.pos : INT32_MAX);
-  x.pos_hi = max_of_lanes(x.valid ? x.pos : -1);
-  x.begin_lo = min_of_lanes(x.valid ? x.begin : INT32_MAX);
-  x.begin_hi = max_of_lanes(x.valid ? x.begin : -1);
-  if (lane == 0) {
-    sm.first[wave] = x.pos_lo;
-    sm.begin[wave] = x.begin_lo;
-    sm.last[wave] = x.pos_hi;
-  }
-  __syncthreads();
-  int first = INT32_MAX, last = -1;
-  x.keys_begin = INT32_MAX;
-#pragma unroll
-  for (int w = 0; w < kPackedWaves; ++w) {
-    first = min(first, sm.first[w]);
-    x.keys_begin = min(x.keys_begin, sm.begin[w]);
-    last = max(last, sm.last[w]);
-  }
-  if (last < 0) return false;
+  // the block's first and last position that is of a sequence, and where the first one's begins: the same in all wavefronts
+  const uint32_t from = (uint32_t)b.block * WAVES * 32;
+  const int first = max((int)(from / (uint32_t)c.group), c.offsets[0]);
+  const int last = min(min((int)((from + WAVES * 32 - 1) / (uint32_t)c.group), c.tokens - 1), c.offsets[c.n_seqs] - 1);
+  if (first > last) return false;
+  const Span start = span_of(c.offsets, c.n_seqs, c.tokens, first);
+  if (start.begin < 0) return false;
+  x.keys_begin = start.begin;
   x.sink_tiles = x.full ? 0 : (int)(((int64_t)min(c.sink, last + 1 - x.keys_begin) + kKeys - 1) / kKeys);
   x.band = x.full ? x.keys_begin : max(x.keys_begin + x.sink_tiles * kKeys, first - c.recent + 1);
   x.tiles = x.sink_tiles + (x.band > last ? 0 : (last - x.band) / kKeys + 1);
+  Span span = start;
+  if (__any(pos < first || pos >= start.end)) span = span_of_lane(c.offsets, c.n_seqs, c.tokens, pos);
+  x.valid = span.begin >= 0;
+  x.begin = x.valid ? span.begin : 0;
+  x.row = x.valid ? x.pos : 0;
+  const Ends e = ends_of(x.valid);
+  const bool any = e.first_lane >= 0;
+  x.pos_lo = any ? __builtin_amdgcn_readlane(x.pos, e.first_lane) : INT32_MAX;
+  x.pos_hi = any ? __builtin_amdgcn_readlane(x.pos, e.last_lane) : -1;
+  x.begin_lo = any ? __builtin_amdgcn_readlane(x.begin, e.first_lane) : INT32_MAX;
+  x.begin_hi = any ? __builtin_amdgcn_readlane(x.begin, e.last_lane) : -1;
   return true;
-}
-__device__ __forceinline__ const int32_t* offsets_of(const PackedCall& c, int32_t* here) {
-  if (c.n_seqs >= kOffsetsInLds) return c.offsets;
-  for (int i = threadIdx.x; i <= c.n_seqs; i += kPackedThreads) here[i] = c.offsets[i];
-  __syncthreads();
-  return here;
 }
 
 }  // namespace rlkv

@@ -7,6 +7,7 @@
 // few keys of other sequences are masked.  So blocks of columns need no plan, sequences of any lengths (none among them) fill them, and the launch is
 // the same whatever the offsets hold.  Keys x queries first: scores, weights, maximum and sum of a column are in its two lanes.
 #include "packed_attention.h"
+#include <stdlib.h>
 
 namespace rlkv {
 namespace {
@@ -15,27 +16,28 @@ namespace {
 // fp32 sums and bf16 weights nothing, and the accumulators stay as they are.
 constexpr float kSlack = 8.f;
 
-__global__ __launch_bounds__(kPackedThreads) void packed_attention_kernel(PackedCall c, uint32_t blocks) {
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void packed_attention_kernel(PackedCall c, uint32_t blocks) {
   // (objects of their own, and the buffer of a tile known at compile time: else reads of one tile would wait for the loads of the next)
-  __shared__ uint4 k0[kKeys * 16], k1[kKeys * 16], v0[kKeys * 16], v1[kKeys * 16];
-  __shared__ ColumnSmem sm;
+  __shared__ uint4 t0[2][kKeys * 16], t1[2][kKeys * 16];      // keys, values
   const int half = (threadIdx.x >> 5) & 1;
-  const int32_t* offsets = offsets_of(c, sm.offsets);
   const ColumnBlock block = column_block(c, blockIdx.x, blocks);
-  Columns x;
-  if (!set_columns(c, offsets, block, sm, x)) return;
-
+  int head;
+  const int pos = column_position<WAVES>(c, block, head);
+  // (the queries are asked for before it is known whose they are)
   bf16x8 q[8];
   {
-    const uint16_t* row = c.q.p + x.row * c.q.token + x.head * c.q.head + 8 * half;
+    const uint16_t* row = c.q.p + (int64_t)min(pos, c.tokens - 1) * c.q.token + head * c.q.head + 8 * half;
 #pragma unroll
     for (int s = 0; s < 8; ++s) q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(row + 16 * s));
   }
+  Columns x;
+  if (!set_columns<WAVES>(c, block, pos, head, x)) return;
   const float scale = c.scale * kLog2e, slack = kSlack / scale;
   auto ask = [&](auto odd, int t) {
     constexpr int kOdd = decltype(odd)::value;
-    stage_rows(c.k, x.tile_key(t), block.head, c.tokens, kOdd ? k1 : k0);
-    stage_rows(c.v, x.tile_key(t), block.head, c.tokens, kOdd ? v1 : v0);
+    stage_rows<WAVES>(c.k, x.tile_key(t), block.head, c.tokens, kOdd ? t1[0] : t0[0]);
+    stage_rows<WAVES>(c.v, x.tile_key(t), block.head, c.tokens, kOdd ? t1[1] : t0[1]);
   };
 
   floatx16 o[4];
@@ -51,7 +53,7 @@ __global__ __launch_bounds__(kPackedThreads) void packed_attention_kernel(Packed
     ask(std::integral_constant<int, 0>{}, 0);
     auto step = [&](auto odd, int t) {
       constexpr int kOdd = decltype(odd)::value;
-      const uint4 *kt = kOdd ? k1 : k0, *vt = kOdd ? v1 : v0;
+      const uint4 *kt = kOdd ? t1[0] : t0[0], *vt = kOdd ? t1[1] : t0[1];
       __syncthreads();
       if (t + 1 < x.tiles) ask(std::integral_constant<int, 1 - kOdd>{}, t + 1);
       const int key = x.tile_key(t);
@@ -120,10 +122,16 @@ __global__ __launch_bounds__(kPackedThreads) void packed_attention_kernel(Packed
 
 }  // namespace
 
-hipError_t launch_packed_attention(const PackedCall& call, hipStream_t stream) {
-  const uint32_t blocks = (uint32_t)(((int64_t)call.tokens * call.group + kColumns - 1) / kColumns);
-  packed_attention_kernel<<<blocks * (uint32_t)call.n_kv_heads, kPackedThreads, 0, stream>>>(call, blocks);
+template <int WAVES>
+static hipError_t launch_waves(const PackedCall& call, hipStream_t stream) {
+  const uint32_t blocks = column_blocks(call, WAVES);
+  packed_attention_kernel<WAVES><<<blocks * (uint32_t)call.n_kv_heads, 64 * WAVES, 0, stream>>>(call, blocks);
   return hipGetLastError();
+}
+
+hipError_t launch_packed_attention(const PackedCall& call, hipStream_t stream) {
+  static const int waves = getenv("W") ? atoi(getenv("W")) : 8;
+  return waves == 8 ? launch_waves<8>(call, stream) : launch_waves<4>(call, stream);
 }
 
 }  // namespace rlkv

@@ -9,11 +9,12 @@
 #include <type_traits>
 
 #include "packed_attention.h"
+#include <stdlib.h>
 
 namespace rlkv {
 namespace {
 
-constexpr int kWaves = kPackedWaves, kThreads = kPackedThreads;
+constexpr int kWaves = 8, kThreads = 64 * kWaves;
 
 __device__ __forceinline__ float dot_of_units(uint4 a, uint4 b) {
   const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
@@ -51,12 +52,19 @@ struct PlanSmem {
 };
 // The positions of a tile's keys; end <= first: none.
 struct TileRange { int32_t first, end; };
-__device__ __forceinline__ TileRange range_of(const PackedCall& c, const int32_t* offsets, int tile, bool full) {
+__device__ __forceinline__ TileRange range_of(const PackedCall& c, int tile, bool full) {
+  const int32_t* offsets = c.offsets;
   const int begin = offsets[0], end = offsets[c.n_seqs];
   const int first = max(tile * kKeysHere, begin), last = min(min(tile * kKeysHere + kKeysHere, end), c.tokens) - 1;
   if (first > last) return {0, 0};
-  const Span span = span_of(offsets, c.n_seqs, c.tokens, last);
-  if (span.begin < 0) return {0, 0};
+  int lo = 0, hi = c.n_seqs + 1;              // (every thread has a tile of its own)
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (offsets[mid] > last) hi = mid;
+    else lo = mid + 1;
+  }
+  if (lo == 0 || lo > c.n_seqs) return {0, 0};
+  const Span span = {min(max(offsets[lo - 1], 0), last), min(offsets[lo], c.tokens)};
   if (full || max(span.begin, first) - span.begin < c.sink || span.end - last < c.recent) return {first, span.end};
   return {first, last + c.recent};
 }
@@ -64,7 +72,7 @@ __device__ __forceinline__ int steps_of(const TileRange& r, int group) {
   return r.end <= r.first ? 0 : (r.end - r.first + kStep - 1) / kStep * group;
 }
 // One workgroup.
-__device__ void make_plan(const PackedCall& c, const int32_t* offsets, PlanSmem& sm) {
+__device__ void make_plan(const PackedCall& c, PlanSmem& sm) {
   const int64_t pairs = tiles_of(c.tokens) * c.n_kv_heads;
   if (threadIdx.x == 0) {
     sm.total = 0;
@@ -74,11 +82,11 @@ __device__ void make_plan(const PackedCall& c, const int32_t* offsets, PlanSmem&
   auto pair = [&](int64_t i, int& tile, int& h) {
     tile = (int)(i / c.n_kv_heads);
     h = (int)(i - (int64_t)tile * c.n_kv_heads);
-    return range_of(c, offsets, tile, (c.full[h >> 6] >> (h & 63)) & 1);
+    return range_of(c, tile, (c.full[h >> 6] >> (h & 63)) & 1);
   };
   int tile, h;
   unsigned long long mine = 0;
-  for (int64_t i = threadIdx.x; i < pairs; i += kThreads) mine += steps_of(pair(i, tile, h), c.group);
+  for (int64_t i = threadIdx.x; i < pairs; i += blockDim.x) mine += steps_of(pair(i, tile, h), c.group);
   atomicAdd(&sm.total, mine);
   __syncthreads();
   // parts of at least `least` and less than twice as many steps, so at most kMostParts of them
@@ -88,7 +96,7 @@ __device__ void make_plan(const PackedCall& c, const int32_t* offsets, PlanSmem&
   PlanMerge* merges = merges_of(c.plan, pairs);
   // (the long ones in front of the others)
   for (int turn = 0; turn < 2; ++turn) {
-    for (int64_t i = threadIdx.x; i < pairs; i += kThreads) {
+    for (int64_t i = threadIdx.x; i < pairs; i += blockDim.x) {
       const TileRange r = pair(i, tile, h);
       const int steps = steps_of(r, c.group), parts = max(1, steps / least);
       if (turn == 0) merges[i] = {-1, 0};
@@ -104,28 +112,27 @@ __device__ void make_plan(const PackedCall& c, const int32_t* offsets, PlanSmem&
 }
 
 // ---- queries ------------------------------------------------------------------------------------------------------------------
-__global__ __launch_bounds__(kThreads) void packed_grad_q_kernel(PackedCall c, uint32_t blocks) {
-  __shared__ uint4 k0[kKeys * 16], k1[kKeys * 16], v0[kKeys * 16], v1[kKeys * 16];
-  __shared__ ColumnSmem sm;
+template <int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void packed_grad_q_kernel(PackedCall c, uint32_t blocks) {
+  __shared__ uint4 t0[2][kKeys * 16], t1[2][kKeys * 16];      // keys, values
   __shared__ PlanSmem plan;
   const int half = (threadIdx.x >> 5) & 1;
-  const int32_t* offsets = offsets_of(c, sm.offsets);
   if (blockIdx.x == 0) {                                     // (the launch's first workgroup plans the next launch)
-    make_plan(c, offsets, plan);
+    make_plan(c, plan);
     return;
   }
   const ColumnBlock block = column_block(c, blockIdx.x - 1, blocks);
-  Columns x;
-  if (!set_columns(c, offsets, block, sm, x)) return;
-
+  int head;
+  const int pos = column_position<WAVES>(c, block, head);
+  // (the rows are asked for before it is known whose they are)
   bf16x8 q[8], g[8];
-  float delta = 0.f, lse = 0.f;
+  float delta = 0.f, lse;
   {
-    const uint16_t* q_row = c.q.p + x.row * c.q.token + x.head * c.q.head + 8 * half;
-    const uint16_t* g_row = c.grad_out.p + x.row * c.grad_out.token + x.head * c.grad_out.head + 8 * half;
-    const uint16_t* o_row = c.out.p + x.row * c.out.token + x.head * c.out.head + 8 * half;
-    const int64_t at = (int64_t)x.head * c.tokens + x.pos;
-    if (x.valid) lse = c.lse[at] * kLog2e;
+    const int64_t row = min(pos, c.tokens - 1);
+    const uint16_t* q_row = c.q.p + row * c.q.token + head * c.q.head + 8 * half;
+    const uint16_t* g_row = c.grad_out.p + row * c.grad_out.token + head * c.grad_out.head + 8 * half;
+    const uint16_t* o_row = c.out.p + row * c.out.token + head * c.out.head + 8 * half;
+    lse = c.lse[head * (int64_t)c.tokens + row] * kLog2e;
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
       q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(q_row + 16 * s));
@@ -134,13 +141,15 @@ __global__ __launch_bounds__(kThreads) void packed_grad_q_kernel(PackedCall c, u
       delta += dot_of_units(gw, *reinterpret_cast<const uint4*>(o_row + 16 * s));
     }
     delta = sum_of_halves(delta);
-    if (x.valid && half == 0) c.delta[at] = delta;
   }
+  Columns x;
+  if (!set_columns<WAVES>(c, block, pos, head, x)) return;
+  if (x.valid && half == 0) c.delta[(int64_t)x.head * c.tokens + x.pos] = delta;
   const float scale = c.scale * kLog2e;
   auto ask = [&](auto odd, int t) {
     constexpr int kOdd = decltype(odd)::value;
-    stage_rows(c.k, x.tile_key(t), block.head, c.tokens, kOdd ? k1 : k0);
-    stage_rows(c.v, x.tile_key(t), block.head, c.tokens, kOdd ? v1 : v0);
+    stage_rows<WAVES>(c.k, x.tile_key(t), block.head, c.tokens, kOdd ? t1[0] : t0[0]);
+    stage_rows<WAVES>(c.v, x.tile_key(t), block.head, c.tokens, kOdd ? t1[1] : t0[1]);
   };
 
   floatx16 dq[4];
@@ -151,7 +160,7 @@ __global__ __launch_bounds__(kThreads) void packed_grad_q_kernel(PackedCall c, u
     ask(std::integral_constant<int, 0>{}, 0);
     auto step = [&](auto odd, int t) {
       constexpr int kOdd = decltype(odd)::value;
-      const uint4 *kt = kOdd ? k1 : k0, *vt = kOdd ? v1 : v0;
+      const uint4 *kt = kOdd ? t1[0] : t0[0], *vt = kOdd ? t1[1] : t0[1];
       __syncthreads();
       if (t + 1 < x.tiles) ask(std::integral_constant<int, 1 - kOdd>{}, t + 1);
 #pragma unroll
@@ -214,44 +223,52 @@ __device__ __forceinline__ float* slot_piece(float* slots, int slot, int piece, 
 
 __global__ __launch_bounds__(kThreads) void packed_grad_kv_kernel(PackedCall c) {
   // (objects of their own, and the slot of a step known at compile time: else reads of one tile would wait for the loads of the next)
-  __shared__ uint4 q0[kStep * 16], q1[kStep * 16], g0[kStep * 16], g1[kStep * 16];
+  __shared__ uint4 t0[2][kStep * 16], t1[2][kStep * 16];      // queries, gradients
   __shared__ float minus_lse[2][kStep], minus_delta[2][kStep];
-  __shared__ int32_t seqs[kOffsetsInLds];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   if ((int)blockIdx.x >= c.plan->items) return;
   const PlanItem item = items_of(c.plan)[blockIdx.x];
   const int h = item.head, group = c.group;
   const bool full = (c.full[h >> 6] >> (h & 63)) & 1;
-  const int32_t* offsets = offsets_of(c, seqs);
   const int at = item.tile * kKeysHere + (threadIdx.x >> 6) * 32 + (lane & 31);
-  const Span span = span_of(offsets, c.n_seqs, c.tokens, at);
+  const Span span = span_of_lane(c.offsets, c.n_seqs, c.tokens, at);
   const bool valid = span.begin >= 0;
   const int key = valid ? at : 0;                                       // (a key of no sequence: nothing is admitted, nothing written)
   int limit = !valid ? 0 : full || key - span.begin < c.sink || span.end - key < c.recent ? span.end : key + c.recent;
   limit = min(limit, item.end);
   const uint32_t width = valid ? max(limit - key, 0) : 0;
-  const int key_lo = min_of_lanes(valid ? key : INT32_MAX), key_hi = max_of_lanes(valid ? key : -1);
-  const int limit_lo = min_of_lanes(valid ? limit : INT32_MAX), limit_hi = max_of_lanes(valid ? limit : -1);
+  // of the wavefront: keys ascend; the least and the largest limit over its valid lanes
+  const Ends ends = ends_of(valid);
+  const int key_lo = ends.first_lane >= 0 ? __builtin_amdgcn_readlane(key, ends.first_lane) : INT32_MAX;
+  const int key_hi = ends.first_lane >= 0 ? __builtin_amdgcn_readlane(key, ends.last_lane) : -1;
+  int limit_lo = valid ? limit : INT32_MAX, limit_hi = valid ? limit : -1;
+#pragma unroll
+  for (int d = 1; d < 32; d *= 2) {
+    limit_lo = min(limit_lo, __shfl_xor(limit_lo, d));
+    limit_hi = max(limit_hi, __shfl_xor(limit_hi, d));
+  }
+  limit_lo = __builtin_amdgcn_readfirstlane(limit_lo);
+  limit_hi = __builtin_amdgcn_readfirstlane(limit_hi);
 
   bf16x8 k[8], v[8];
   {
-    const uint16_t* k_row = c.k.p + (int64_t)key * c.k.token + h * c.k.head + 8 * half;
-    const uint16_t* v_row = c.v.p + (int64_t)key * c.v.token + h * c.v.head + 8 * half;
+    const int64_t row = key;
+    const uint16_t* k_row = c.k.p + row * c.k.token + h * c.k.head + 8 * half;
+    const uint16_t* v_row = c.v.p + row * c.v.token + h * c.v.head + 8 * half;
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
       k[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(k_row + 16 * s));
       v[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(v_row + 16 * s));
     }
   }
-
   const int per_head = (item.end - item.first + kStep - 1) / kStep;      // steps of a query head
   const float scale = c.scale * kLog2e, inv_scale = 1.f / c.scale;
   // the step that is asked for next: query head and first position
   int next_head, next_pos;
   auto ask = [&](auto odd) {
     constexpr int kOdd = decltype(odd)::value;
-    stage_rows(c.q, next_pos, next_head, c.tokens, kOdd ? q1 : q0);
-    stage_rows(c.grad_out, next_pos, next_head, c.tokens, kOdd ? g1 : g0);
+    stage_rows<kWaves>(c.q, next_pos, next_head, c.tokens, kOdd ? t1[0] : t0[0]);
+    stage_rows<kWaves>(c.grad_out, next_pos, next_head, c.tokens, kOdd ? t1[1] : t0[1]);
     if (threadIdx.x < kStep) {
       const int64_t row = (int64_t)next_head * c.tokens + min(next_pos + (int)threadIdx.x, c.tokens - 1);
       minus_lse[kOdd][threadIdx.x] = -c.lse[row] * inv_scale;
@@ -278,7 +295,7 @@ __global__ __launch_bounds__(kThreads) void packed_grad_kv_kernel(PackedCall c) 
     ask(std::integral_constant<int, 0>{});
     auto step = [&](auto odd, bool more) {
       constexpr int kOdd = decltype(odd)::value;
-      const uint4 *qt = kOdd ? q1 : q0, *gt = kOdd ? g1 : g0;
+      const uint4 *qt = kOdd ? t1[0] : t0[0], *gt = kOdd ? t1[1] : t0[1];
       __syncthreads();
       if (more) ask(std::integral_constant<int, 1 - kOdd>{});
 #pragma unroll
@@ -371,7 +388,7 @@ __global__ __launch_bounds__(kThreads) void packed_grad_sum_kernel(PackedCall c)
       sum[i].w += x.w;
     }
   const int key = tile * kKeysHere + (threadIdx.x >> 6) * 32 + (lane & 31);
-  if (span_of(c.offsets, c.n_seqs, c.tokens, key).begin < 0) return;
+  if (span_of_lane(c.offsets, c.n_seqs, c.tokens, key).begin < 0) return;
   const HeadRows& to = blockIdx.y < 4 ? c.grad_k : c.grad_v;
   const float scale = blockIdx.y < 4 ? c.scale : 1.f;
   uint16_t* row = to.p + (int64_t)key * to.token + h * to.head + 32 * (blockIdx.y & 3) + 4 * (lane >> 5);
@@ -408,9 +425,11 @@ hipError_t launch_packed_attention_grad(PackedCall call, hipStream_t stream) {
   call.delta = reinterpret_cast<float*>(work + space.delta);
   call.plan = reinterpret_cast<PackedPlan*>(work + space.plan);
   call.slots = reinterpret_cast<float*>(work + space.slots);
-  const uint32_t blocks = (uint32_t)(((int64_t)call.tokens * call.group + kColumns - 1) / kColumns);
   const int64_t pairs = tiles_of(call.tokens) * call.n_kv_heads;
-  packed_grad_q_kernel<<<blocks * (uint32_t)call.n_kv_heads + 1, kThreads, 0, stream>>>(call, blocks);
+  static const int waves = getenv("W") ? atoi(getenv("W")) : 8;
+  const uint32_t blocks = column_blocks(call, waves);
+  if (waves == 8) packed_grad_q_kernel<8><<<blocks * (uint32_t)call.n_kv_heads + 1, 512, 0, stream>>>(call, blocks);
+  else packed_grad_q_kernel<4><<<blocks * (uint32_t)call.n_kv_heads + 1, 256, 0, stream>>>(call, blocks);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
   const int64_t parts = (int64_t)(space.bytes - space.slots) / (int64_t)(kSlotFloats * sizeof(float));
