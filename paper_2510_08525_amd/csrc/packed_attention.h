@@ -32,6 +32,16 @@ struct HeadRows {
   int64_t token, head;
 };
 struct PackedPlan { int32_t items, pad[3]; };      // of the gradient's second launch (packed_attention_grad.hip)
+// Division of numbers below 2^31 by one that the host knows: x / d = x * mul >> (31 + shift), mul = ceil(2^(31 + shift) / d), shift = ceil(log2 d).
+struct Divisor {
+  uint32_t mul, shift;
+  static Divisor by(uint32_t d) {
+    uint32_t s = 0;
+    while ((1ull << s) < d) ++s;
+    return {(uint32_t)(((1ull << (31 + s)) + d - 1) / d), s};
+  }
+  __device__ __forceinline__ uint32_t of(uint32_t x) const { return (uint32_t)(((uint64_t)x * mul) >> (31 + shift)); }
+};
 struct PackedCall {
   HeadRows q, k, v, out, grad_out, grad_q, grad_k, grad_v;
   float* lse;                       // [n_q_heads][tokens]
@@ -41,6 +51,8 @@ struct PackedCall {
   void* workspace;                  // gradient only
   const int32_t* offsets;           // [n_seqs + 1]
   int32_t n_seqs, tokens, n_q_heads, n_kv_heads, group;
+  int32_t n_full;                   // KV heads that are
+  Divisor by_group, by_full, by_local;      // the numbers of query heads of a KV head, of full and of local KV heads (1 where there are none)
   int32_t sink, recent;
   float scale;
   uint64_t full[kPackedMaskWords];  // a bit for each KV head
@@ -58,42 +70,63 @@ constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 // Which sequence a position belongs to.  Offsets come from device memory, where the host cannot check them: whatever they hold, 0 <= begin <=
 // position < end <= tokens.  A position of no sequence has begin = -1.
 struct Span { int32_t begin, end; };
-// The same position in all lanes.  64 offsets are looked at at a time, so up to 63 sequences take one turn of memory, up to 4095 two.
-__device__ __forceinline__ Span span_of(const int32_t* offsets, int n_seqs, int tokens, int position) {
-  const int lane = threadIdx.x & 63;
-  int from = 0, to = n_seqs + 1;               // the first offset behind the position is in [from, to]
-  while (to - from > 64) {
-    const int each = (to - from + 63) / 64, at = from + (lane + 1) * each - 1;
-    const int below = __popcll(__ballot(at < to && offsets[at < to ? at : from] <= position));      // (not decreasing: the first ones)
-    from += below * each;
-    to = min(to, from + each);
-  }
-  const int x = from + lane < to ? offsets[from + lane] : 0;
-  const int below = __popcll(__ballot(from + lane < to && x <= position)), at = from + below;
-  if (at <= 0 || at > n_seqs || position >= tokens) return {-1, -1};
-  const int b = below > 0 ? __builtin_amdgcn_readlane(x, below - 1) : offsets[at - 1];
-  const int e = below < 64 && from + below < to ? __builtin_amdgcn_readlane(x, below) : offsets[at];
+__device__ __forceinline__ Span clamped(int b, int e, int position, int tokens) {
   return {b < 0 ? 0 : b > position ? position : b, e > tokens ? tokens : e > position ? e : position + 1};
 }
-// Positions that ascend over the lanes (over the first 32 of them, the others have the same again), those below 0 or from `tokens` on of no sequence: each
-// lane's own span, by as many turns as there are sequences among them.
-__device__ __forceinline__ Span span_of_lane(const int32_t* offsets, int n_seqs, int tokens, int position) {
-  Span mine = {-1, -1};
-  const int top = __builtin_amdgcn_readlane(position, 31);
-  int at = __builtin_amdgcn_readlane(position, 0);
-  while (at <= top) {
-    const Span s = span_of(offsets, n_seqs, tokens, at);
-    if (s.begin < 0) {                         // in front of the first sequence, or behind the last one
-      const int begin = offsets[0];
-      if (begin <= at) break;
-      at = begin;
-      continue;
+// The offsets as a wavefront has them: up to 63 sequences in its lanes, one turn of memory for everything that is asked of them; more stay in memory.
+struct Offsets {
+  const int32_t* p;
+  int32_t n_seqs, tokens, lanes;
+  int32_t first, last;                         // offsets[0], offsets[n_seqs]
+  __device__ __forceinline__ explicit Offsets(const PackedCall& c) : p(c.offsets), n_seqs(c.n_seqs), tokens(c.tokens) {
+    const int lane = threadIdx.x & 63;
+    if (n_seqs < 64) {
+      lanes = p[lane < n_seqs ? lane : n_seqs];
+      first = __builtin_amdgcn_readlane(lanes, 0);
+      last = __builtin_amdgcn_readlane(lanes, n_seqs);
+    } else {
+      first = p[0];
+      last = p[n_seqs];
     }
-    if (position >= at && position < s.end) mine = s;
-    at = s.end;
   }
-  return mine;
-}
+  // of a position that is the same in all lanes
+  __device__ __forceinline__ Span of(int position) const {
+    const int lane = threadIdx.x & 63;
+    if (position >= tokens) return {-1, -1};
+    if (n_seqs < 64) {
+      const int at = __popcll(__ballot(lane <= n_seqs && lanes <= position));      // the first offset behind the position
+      if (at <= 0 || at > n_seqs) return {-1, -1};
+      return clamped(__builtin_amdgcn_readlane(lanes, at - 1), __builtin_amdgcn_readlane(lanes, at), position, tokens);
+    }
+    int from = 0, to = n_seqs + 1;               // the first offset behind the position is in [from, to]; 64 are looked at at a time
+    while (to - from > 0) {
+      const int each = (to - from + 63) / 64, at = from + (lane + 1) * each - 1;
+      const int below = __popcll(__ballot(at < to && p[at < to ? at : from] <= position));      // (not decreasing: the first ones)
+      from += below * each;
+      to = min(to, from + each - 1);
+    }
+    if (from <= 0 || from > n_seqs) return {-1, -1};
+    return clamped(p[from - 1], p[from], position, tokens);
+  }
+  // Positions that ascend over the lanes (over the first 32 of them, the others have the same again): each lane's own span, by as many turns as there are
+  // sequences among them.
+  __device__ __forceinline__ Span of_lane(int position) const {
+    Span mine = {-1, -1};
+    const int top = __builtin_amdgcn_readlane(position, 31);
+    int at = __builtin_amdgcn_readlane(position, 0);
+    while (at <= top) {
+      const Span s = of(at);
+      if (s.begin < 0) {                         // in front of the first sequence, or behind the last one
+        if (first <= at) break;
+        at = first;
+        continue;
+      }
+      if (position >= at && position < s.end) mine = s;
+      at = s.end;
+    }
+    return mine;
+  }
+};
 
 __device__ __forceinline__ float other_half(float x) {      // the value of the lane 32 away
   typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
@@ -162,6 +195,13 @@ __device__ __forceinline__ void stage_rows(const HeadRows& t, int token, int hea
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, RLKV_LDS_PTR(void, tile + block * 64), 16, (int)at, 0, 0, 0);
   }
 #endif
+}
+
+// All of the workgroup's loads to LDS have arrived.  (The compiler makes a wavefront wait for its own before it reads them, which may be behind the
+// barrier: what another wavefront reads has to be waited for in front of it.)
+__device__ __forceinline__ void tile_arrived() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
 }
 
 // Results of 16 rows as the operand of the next product: rounded to bf16 (half a step of 2^-8 each, independent of each other: less than what the
@@ -234,44 +274,31 @@ __device__ __forceinline__ void admitted_products(const uint4* tile, int row0, c
 
 // ---- a workgroup of columns, 32 a wavefront, and the tiles of keys that it walks over ----
 constexpr int kKeys = kStageRows;
+constexpr int kPackedWaves = 8;      // (with four, two workgroups a compute unit, every tile is fetched twice as often: 16384 tokens 3265 us against 2006)
 inline uint32_t column_blocks(const PackedCall& c, int waves) { return (uint32_t)(((int64_t)c.tokens * c.group + 32 * waves - 1) / (32 * waves)); }
 
-// The n-th KV head of a launch: full ones in front of local ones, so that the long workgroups are handed out first, and neighbours in the launch
-// (which the hardware deals to the 8 XCDs in turn) are of different heads: a head's keys are then read by few of the L2s.
-__device__ __forceinline__ int head_in_order(const PackedCall& c, int n, bool& full) {
-  int n_full = 0;
-  for (int w = 0; w < kPackedMaskWords; ++w) n_full += __popcll(c.full[w]);
-  full = n < n_full;
-  if (!full) n -= n_full;
+// Block and head of the launch's workgroup `index`: of all full heads the last blocks first, then of the local ones, so that the long workgroups are
+// handed out first; and neighbours in the launch, which the hardware deals to the 8 XCDs in turn, are of different heads: a head's keys are then read by
+// few of the L2s.
+struct ColumnBlock { int block, head; bool full; };
+__device__ __forceinline__ ColumnBlock column_block(const PackedCall& c, uint32_t index, uint32_t blocks) {
+  ColumnBlock b;
+  b.full = index < blocks * c.n_full;
+  if (!b.full) index -= blocks * c.n_full;
+  const uint32_t turn = b.full ? c.by_full.of(index) : c.by_local.of(index);
+  b.block = blocks - 1 - turn;
+  int n = index - turn * (b.full ? c.n_full : c.n_kv_heads - c.n_full);      // the n-th of its kind
   for (int w = 0;; ++w) {
-    uint64_t bits = full ? c.full[w] : ~c.full[w];
+    uint64_t bits = b.full ? c.full[w] : ~c.full[w];
     const int here = __popcll(bits);
     if (n >= here) {
       n -= here;
       continue;
     }
     for (; n; --n) bits &= bits - 1;
-    return w * 64 + __builtin_ctzll(bits);
+    b.head = w * 64 + __builtin_ctzll(bits);
+    return b;
   }
-}
-// Block and head of the launch's workgroup `index`: of all full heads the last blocks first, then of the local ones.
-struct ColumnBlock { int block, head; bool full; };
-__device__ __forceinline__ ColumnBlock column_block(const PackedCall& c, uint32_t index, uint32_t blocks) {
-  int n_full = 0;
-  for (int w = 0; w < kPackedMaskWords; ++w) n_full += __popcll(c.full[w]);
-  ColumnBlock b;
-  uint32_t n;
-  if (index < blocks * n_full) {
-    b.block = blocks - 1 - index / n_full;
-    n = index % n_full;
-  } else {
-    index -= blocks * n_full;
-    const uint32_t n_local = c.n_kv_heads - n_full;
-    b.block = blocks - 1 - index / n_local;
-    n = n_full + index % n_local;
-  }
-  b.head = head_in_order(c, n, b.full);
-  return b;
 }
 
 struct Columns {
@@ -301,34 +328,27 @@ __device__ __forceinline__ Ends ends_of(bool valid) {
   const uint32_t lanes = (uint32_t)__ballot(valid);
   return {lanes ? __builtin_ctz(lanes) : -1, lanes ? 31 - __builtin_clz(lanes) : -1};
 }
-template <int WAVES>
-__device__ __forceinline__ int column_position(const PackedCall& c, const ColumnBlock& b, int& head) {
-  const uint32_t column = ((uint32_t)b.block * WAVES + (threadIdx.x >> 6)) * 32 + (threadIdx.x & 31);
-  const int pos = (int)(column / (uint32_t)c.group);
-  head = b.head * c.group + (int)(column - (uint32_t)pos * c.group);
-  return pos;
-}
 // False: no column of the block is of a sequence.
 template <int WAVES>
-__device__ __forceinline__ bool set_columns(const PackedCall& c, const ColumnBlock& b, int pos, int head, Columns& x) {
-  x.pos = pos;
-  x.head = head;
+__device__ __forceinline__ bool set_columns(const PackedCall& c, const Offsets& offsets, const ColumnBlock& b, Columns& x) {
+  const uint32_t from = (uint32_t)b.block * (WAVES * 32), column = from + (threadIdx.x >> 6) * 32 + (threadIdx.x & 31);
+  x.pos = (int)c.by_group.of(column);
+  x.head = b.head * c.group + (int)(column - (uint32_t)x.pos * c.group);
   x.full = b.full;
   x.sink = c.sink;
   x.recent = c.recent;
   // the block's first and last position that is of a sequence, and where the first one's begins: the same in all wavefronts
-  const uint32_t from = (uint32_t)b.block * WAVES * 32;
-  const int first = max((int)(from / (uint32_t)c.group), c.offsets[0]);
-  const int last = min(min((int)((from + WAVES * 32 - 1) / (uint32_t)c.group), c.tokens - 1), c.offsets[c.n_seqs] - 1);
+  const int first = max((int)c.by_group.of(from), offsets.first);
+  const int last = min(min((int)c.by_group.of(from + WAVES * 32 - 1) + 1, c.tokens), max(offsets.last, 0)) - 1;
   if (first > last) return false;
-  const Span start = span_of(c.offsets, c.n_seqs, c.tokens, first);
+  const Span start = offsets.of(first);
   if (start.begin < 0) return false;
   x.keys_begin = start.begin;
   x.sink_tiles = x.full ? 0 : (int)(((int64_t)min(c.sink, last + 1 - x.keys_begin) + kKeys - 1) / kKeys);
   x.band = x.full ? x.keys_begin : max(x.keys_begin + x.sink_tiles * kKeys, first - c.recent + 1);
   x.tiles = x.sink_tiles + (x.band > last ? 0 : (last - x.band) / kKeys + 1);
   Span span = start;
-  if (__any(pos < first || pos >= start.end)) span = span_of_lane(c.offsets, c.n_seqs, c.tokens, pos);
+  if (__any(x.pos < first || x.pos >= start.end)) span = offsets.of_lane(x.pos);
   x.valid = span.begin >= 0;
   x.begin = x.valid ? span.begin : 0;
   x.row = x.valid ? x.pos : 0;
@@ -339,6 +359,12 @@ __device__ __forceinline__ bool set_columns(const PackedCall& c, const ColumnBlo
   x.begin_lo = any ? __builtin_amdgcn_readlane(x.begin, e.first_lane) : INT32_MAX;
   x.begin_hi = any ? __builtin_amdgcn_readlane(x.begin, e.last_lane) : -1;
   return true;
+}
+// Whether any lane of the workgroup says so.  `flag`, in LDS, has been 0 since before the last barrier.
+__device__ __forceinline__ bool any_of_workgroup(bool x, int32_t& flag) {
+  if (__any(x) && (threadIdx.x & 63) == 0) flag = 1;
+  __syncthreads();
+  return flag != 0;
 }
 
 }  // namespace rlkv

@@ -7,7 +7,6 @@
 // few keys of other sequences are masked.  So blocks of columns need no plan, sequences of any lengths (none among them) fill them, and the launch is
 // the same whatever the offsets hold.  Keys x queries first: scores, weights, maximum and sum of a column are in its two lanes.
 #include "packed_attention.h"
-#include <stdlib.h>
 
 namespace rlkv {
 namespace {
@@ -20,19 +19,20 @@ template <int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void packed_attention_kernel(PackedCall c, uint32_t blocks) {
   // (objects of their own, and the buffer of a tile known at compile time: else reads of one tile would wait for the loads of the next)
   __shared__ uint4 t0[2][kKeys * 16], t1[2][kKeys * 16];      // keys, values
+  __shared__ int32_t lost;
   const int half = (threadIdx.x >> 5) & 1;
+  const Offsets offsets(c);
   const ColumnBlock block = column_block(c, blockIdx.x, blocks);
-  int head;
-  const int pos = column_position<WAVES>(c, block, head);
-  // (the queries are asked for before it is known whose they are)
+  Columns x;
+  if (!set_columns<WAVES>(c, offsets, block, x)) return;
+  if (threadIdx.x == 0) lost = 0;
+
   bf16x8 q[8];
   {
-    const uint16_t* row = c.q.p + (int64_t)min(pos, c.tokens - 1) * c.q.token + head * c.q.head + 8 * half;
+    const uint16_t* row = c.q.p + x.row * c.q.token + x.head * c.q.head + 8 * half;
 #pragma unroll
     for (int s = 0; s < 8; ++s) q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(row + 16 * s));
   }
-  Columns x;
-  if (!set_columns<WAVES>(c, block, pos, head, x)) return;
   const float scale = c.scale * kLog2e, slack = kSlack / scale;
   auto ask = [&](auto odd, int t) {
     constexpr int kOdd = decltype(odd)::value;
@@ -54,7 +54,7 @@ __global__ __launch_bounds__(64 * WAVES) void packed_attention_kernel(PackedCall
     auto step = [&](auto odd, int t) {
       constexpr int kOdd = decltype(odd)::value;
       const uint4 *kt = kOdd ? t1[0] : t0[0], *vt = kOdd ? t1[1] : t0[1];
-      __syncthreads();
+      tile_arrived();
       if (t + 1 < x.tiles) ask(std::integral_constant<int, 1 - kOdd>{}, t + 1);
       const int key = x.tile_key(t);
       if (!x.any_of(key, kKeys)) return;
@@ -113,25 +113,19 @@ __global__ __launch_bounds__(64 * WAVES) void packed_attention_kernel(PackedCall
     if (t < x.tiles) step(std::integral_constant<int, 0>{}, t);
   };
   walk(std::false_type{});
-  if (__syncthreads_or(x.valid && zero_or_nan(o) != 0.f)) walk(std::true_type{});
+  if (any_of_workgroup(x.valid && zero_or_nan(o) != 0.f, lost)) walk(std::true_type{});
 
   l = sum_of_halves(l);
-  store_rows(c.out.p + x.row * c.out.token + x.head * c.out.head, o, 1.f / l, x.valid);
-  if (c.lse && x.valid && half == 0) c.lse[(int64_t)x.head * c.tokens + x.pos] = m * c.scale + logf(l);
+  store_rows(c.out.p + x.row * c.out.token + x.head * c.out.head, o, __builtin_amdgcn_rcpf(l), x.valid);
+  if (c.lse && x.valid && half == 0) c.lse[(int64_t)x.head * c.tokens + x.pos] = m * c.scale + __builtin_amdgcn_logf(l) * kLn2;
 }
 
 }  // namespace
 
-template <int WAVES>
-static hipError_t launch_waves(const PackedCall& call, hipStream_t stream) {
-  const uint32_t blocks = column_blocks(call, WAVES);
-  packed_attention_kernel<WAVES><<<blocks * (uint32_t)call.n_kv_heads, 64 * WAVES, 0, stream>>>(call, blocks);
-  return hipGetLastError();
-}
-
 hipError_t launch_packed_attention(const PackedCall& call, hipStream_t stream) {
-  static const int waves = getenv("W") ? atoi(getenv("W")) : 8;
-  return waves == 8 ? launch_waves<8>(call, stream) : launch_waves<4>(call, stream);
+  const uint32_t blocks = column_blocks(call, kPackedWaves);
+  packed_attention_kernel<kPackedWaves><<<blocks * (uint32_t)call.n_kv_heads, 64 * kPackedWaves, 0, stream>>>(call, blocks);
+  return hipGetLastError();
 }
 
 }  // namespace rlkv

@@ -9,12 +9,11 @@
 #include <type_traits>
 
 #include "packed_attention.h"
-#include <stdlib.h>
 
 namespace rlkv {
 namespace {
 
-constexpr int kWaves = 8, kThreads = 64 * kWaves;
+constexpr int kWaves = kPackedWaves, kThreads = 64 * kWaves;
 
 __device__ __forceinline__ float dot_of_units(uint4 a, uint4 b) {
   const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w};
@@ -121,30 +120,29 @@ __global__ __launch_bounds__(64 * WAVES) void packed_grad_q_kernel(PackedCall c,
     make_plan(c, plan);
     return;
   }
+  __shared__ int32_t lost;
+  const Offsets offsets(c);
   const ColumnBlock block = column_block(c, blockIdx.x - 1, blocks);
-  int head;
-  const int pos = column_position<WAVES>(c, block, head);
-  // (the rows are asked for before it is known whose they are)
+  Columns x;
+  if (!set_columns<WAVES>(c, offsets, block, x)) return;
+  if (threadIdx.x == 0) lost = 0;
+
   bf16x8 q[8], g[8];
-  float delta = 0.f, lse;
+  uint4 out[8];
+  const int64_t stat = (int64_t)x.head * c.tokens + x.row;
+  const float lse = c.lse[stat] * kLog2e;
   {
-    const int64_t row = min(pos, c.tokens - 1);
-    const uint16_t* q_row = c.q.p + row * c.q.token + head * c.q.head + 8 * half;
-    const uint16_t* g_row = c.grad_out.p + row * c.grad_out.token + head * c.grad_out.head + 8 * half;
-    const uint16_t* o_row = c.out.p + row * c.out.token + head * c.out.head + 8 * half;
-    lse = c.lse[head * (int64_t)c.tokens + row] * kLog2e;
+    const uint16_t* q_row = c.q.p + x.row * c.q.token + x.head * c.q.head + 8 * half;
+    const uint16_t* g_row = c.grad_out.p + x.row * c.grad_out.token + x.head * c.grad_out.head + 8 * half;
+    const uint16_t* o_row = c.out.p + x.row * c.out.token + x.head * c.out.head + 8 * half;
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
-      q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(q_row + 16 * s));
-      const uint4 gw = *reinterpret_cast<const uint4*>(g_row + 16 * s);
-      g[s] = __builtin_bit_cast(bf16x8, gw);
-      delta += dot_of_units(gw, *reinterpret_cast<const uint4*>(o_row + 16 * s));
+      g[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(g_row + 16 * s));
+      out[s] = *reinterpret_cast<const uint4*>(o_row + 16 * s);
     }
-    delta = sum_of_halves(delta);
+#pragma unroll
+    for (int s = 0; s < 8; ++s) q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(q_row + 16 * s));
   }
-  Columns x;
-  if (!set_columns<WAVES>(c, block, pos, head, x)) return;
-  if (x.valid && half == 0) c.delta[(int64_t)x.head * c.tokens + x.pos] = delta;
   const float scale = c.scale * kLog2e;
   auto ask = [&](auto odd, int t) {
     constexpr int kOdd = decltype(odd)::value;
@@ -152,16 +150,24 @@ __global__ __launch_bounds__(64 * WAVES) void packed_grad_q_kernel(PackedCall c,
     stage_rows<WAVES>(c.v, x.tile_key(t), block.head, c.tokens, kOdd ? t1[1] : t0[1]);
   };
 
+  // (while the first tile is under way)
+  ask(std::integral_constant<int, 0>{}, 0);
+  float delta = 0.f;
+#pragma unroll
+  for (int s = 0; s < 8; ++s) delta += dot_of_units(__builtin_bit_cast(uint4, g[s]), out[s]);
+  delta = sum_of_halves(delta);
+  if (x.valid && half == 0) c.delta[stat] = delta;
+
   floatx16 dq[4];
   auto walk = [&](auto careful) {
     constexpr bool kCareful = decltype(careful)::value;
 #pragma unroll
     for (int b = 0; b < 4; ++b) clear(dq[b]);
-    ask(std::integral_constant<int, 0>{}, 0);
+    if (kCareful) ask(std::integral_constant<int, 0>{}, 0);
     auto step = [&](auto odd, int t) {
       constexpr int kOdd = decltype(odd)::value;
       const uint4 *kt = kOdd ? t1[0] : t0[0], *vt = kOdd ? t1[1] : t0[1];
-      __syncthreads();
+      tile_arrived();
       if (t + 1 < x.tiles) ask(std::integral_constant<int, 1 - kOdd>{}, t + 1);
 #pragma unroll
       for (int b = 0; b < kKeys; b += 32) {
@@ -203,7 +209,7 @@ __global__ __launch_bounds__(64 * WAVES) void packed_grad_q_kernel(PackedCall c,
     if (t < x.tiles) step(std::integral_constant<int, 0>{}, t);
   };
   walk(std::false_type{});
-  if (__syncthreads_or(x.valid && zero_or_nan(dq) != 0.f)) walk(std::true_type{});
+  if (any_of_workgroup(x.valid && zero_or_nan(dq) != 0.f, lost)) walk(std::true_type{});
   store_rows(c.grad_q.p + x.row * c.grad_q.token + x.head * c.grad_q.head, dq, c.scale, x.valid);
 }
 
@@ -226,12 +232,15 @@ __global__ __launch_bounds__(kThreads) void packed_grad_kv_kernel(PackedCall c) 
   __shared__ uint4 t0[2][kStep * 16], t1[2][kStep * 16];      // queries, gradients
   __shared__ float minus_lse[2][kStep], minus_delta[2][kStep];
   const int lane = threadIdx.x & 63, half = lane >> 5;
+  __shared__ int32_t lost;
   if ((int)blockIdx.x >= c.plan->items) return;
+  const Offsets offsets(c);
+  if (threadIdx.x == 0) lost = 0;
   const PlanItem item = items_of(c.plan)[blockIdx.x];
   const int h = item.head, group = c.group;
   const bool full = (c.full[h >> 6] >> (h & 63)) & 1;
   const int at = item.tile * kKeysHere + (threadIdx.x >> 6) * 32 + (lane & 31);
-  const Span span = span_of_lane(c.offsets, c.n_seqs, c.tokens, at);
+  const Span span = offsets.of_lane(at);
   const bool valid = span.begin >= 0;
   const int key = valid ? at : 0;                                       // (a key of no sequence: nothing is admitted, nothing written)
   int limit = !valid ? 0 : full || key - span.begin < c.sink || span.end - key < c.recent ? span.end : key + c.recent;
@@ -296,7 +305,7 @@ __global__ __launch_bounds__(kThreads) void packed_grad_kv_kernel(PackedCall c) 
     auto step = [&](auto odd, bool more) {
       constexpr int kOdd = decltype(odd)::value;
       const uint4 *qt = kOdd ? t1[0] : t0[0], *gt = kOdd ? t1[1] : t0[1];
-      __syncthreads();
+      tile_arrived();
       if (more) ask(std::integral_constant<int, 1 - kOdd>{});
 #pragma unroll
       for (int sub = 0; sub < kStep; sub += 32) {
@@ -354,7 +363,7 @@ __global__ __launch_bounds__(kThreads) void packed_grad_kv_kernel(PackedCall c) 
   };
   walk(std::false_type{});
   // (a weight of 0 does not keep an infinity or a NaN of a row that is not admitted out of the products)
-  if (__syncthreads_or(valid && (zero_or_nan(dk) != 0.f || zero_or_nan(dv) != 0.f))) walk(std::true_type{});
+  if (any_of_workgroup(valid && (zero_or_nan(dk) != 0.f || zero_or_nan(dv) != 0.f), lost)) walk(std::true_type{});
   if (item.slot >= 0) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -388,7 +397,7 @@ __global__ __launch_bounds__(kThreads) void packed_grad_sum_kernel(PackedCall c)
       sum[i].w += x.w;
     }
   const int key = tile * kKeysHere + (threadIdx.x >> 6) * 32 + (lane & 31);
-  if (span_of_lane(c.offsets, c.n_seqs, c.tokens, key).begin < 0) return;
+  if (Offsets(c).of_lane(key).begin < 0) return;
   const HeadRows& to = blockIdx.y < 4 ? c.grad_k : c.grad_v;
   const float scale = blockIdx.y < 4 ? c.scale : 1.f;
   uint16_t* row = to.p + (int64_t)key * to.token + h * to.head + 32 * (blockIdx.y & 3) + 4 * (lane >> 5);
@@ -426,10 +435,8 @@ hipError_t launch_packed_attention_grad(PackedCall call, hipStream_t stream) {
   call.plan = reinterpret_cast<PackedPlan*>(work + space.plan);
   call.slots = reinterpret_cast<float*>(work + space.slots);
   const int64_t pairs = tiles_of(call.tokens) * call.n_kv_heads;
-  static const int waves = getenv("W") ? atoi(getenv("W")) : 8;
-  const uint32_t blocks = column_blocks(call, waves);
-  if (waves == 8) packed_grad_q_kernel<8><<<blocks * (uint32_t)call.n_kv_heads + 1, 512, 0, stream>>>(call, blocks);
-  else packed_grad_q_kernel<4><<<blocks * (uint32_t)call.n_kv_heads + 1, 256, 0, stream>>>(call, blocks);
+  const uint32_t blocks = column_blocks(call, kWaves);
+  packed_grad_q_kernel<kWaves><<<blocks * (uint32_t)call.n_kv_heads + 1, kThreads, 0, stream>>>(call, blocks);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
   const int64_t parts = (int64_t)(space.bytes - space.slots) / (int64_t)(kSlotFloats * sizeof(float));

@@ -60,7 +60,13 @@ PackedCall packed_call(const rlkv_packed_t* s) {
   c.recent = s->recent;
   c.scale = s->softmax_scale;
   for (int h = 0; h < s->n_kv_heads; ++h)
-    if (!s->full_mask || s->full_mask[h]) c.full[h >> 6] |= (uint64_t)1 << (h & 63);
+    if (!s->full_mask || s->full_mask[h]) {
+      c.full[h >> 6] |= (uint64_t)1 << (h & 63);
+      ++c.n_full;
+    }
+  c.by_group = Divisor::by(c.group);
+  c.by_full = Divisor::by(c.n_full ? c.n_full : 1);
+  c.by_local = Divisor::by(c.n_full < c.n_kv_heads ? c.n_kv_heads - c.n_full : 1);
   return c;
 }
 
