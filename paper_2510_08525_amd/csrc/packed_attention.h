@@ -204,6 +204,20 @@ __device__ __forceinline__ void tile_arrived() {
   __syncthreads();
 }
 
+// Order of a stretch of instructions: `first` reads of LDS, then with every matrix instruction EACH more, so that a fragment's way (some 100 clocks)
+// passes behind the products in front of it.
+template <int PRODUCTS, int READS, int FIRST, int EACH>
+__device__ __forceinline__ void reads_ahead() {
+#ifdef __HIP_DEVICE_COMPILE__
+  __builtin_amdgcn_sched_group_barrier(0x100, FIRST, 0);
+#pragma unroll
+  for (int i = 0; i < PRODUCTS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if (FIRST + i * EACH < READS) __builtin_amdgcn_sched_group_barrier(0x100, EACH, 0);
+  }
+#endif
+}
+
 // Results of 16 rows as the operand of the next product: rounded to bf16 (half a step of 2^-8 each, independent of each other: less than what the
 // rounding of the output leaves).
 __device__ __forceinline__ bf16x8 weights_fragment(const floatx16& x, int step) {
@@ -304,15 +318,32 @@ __device__ __forceinline__ ColumnBlock column_block(const PackedCall& c, uint32_
 struct Columns {
   int pos, head, begin;                            // of the lane's column; begin: of its sequence
   bool valid, full;                                // a column of no sequence reads row 0 and writes nothing
-  int64_t row;
   int pos_lo, pos_hi, begin_lo, begin_hi;          // of the wavefront's
   int sink, recent;
   int keys_begin, band, sink_tiles, tiles;         // of the workgroup: tiles of a full head from keys_begin on; of a local one those of the sinks
                                                    // of the first sequence, then from the first position's band on (the block's later sequences
                                                    // begin behind its first position)
   __device__ __forceinline__ int tile_key(int t) const { return t < sink_tiles ? keys_begin + t * kKeys : band + (t - sink_tiles) * kKeys; }
+  int64_t row;
+  int mask_begin, mask_span, mask_near;            // of the lane: admitted are mask_begin + a, 0 <= a <= mask_span and (a < sink or a > mask_near)
+  // (without branches; LOCAL false: of a full head)
+  template <bool LOCAL>
   __device__ __forceinline__ bool admits(int key) const {
-    return key <= pos && key >= begin && (full || key - begin < sink || pos - key < recent);
+    const int a = key - mask_begin;
+    const bool in = (uint32_t)a <= (uint32_t)mask_span;
+    return LOCAL ? in & ((a < sink) | (a > mask_near)) : in;
+  }
+  __device__ __forceinline__ bool admits(int key) const { return full ? admits<false>(key) : admits<true>(key); }
+  // x of the keys that are not admitted becomes `otherwise`: results of 32 keys from k0 on
+  __device__ __forceinline__ void mask(floatx16& x, int k0, float otherwise) const {
+    const int first = k0 + 4 * ((threadIdx.x >> 5) & 1);
+    if (full) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = admits<false>(first + 8 * (r >> 2) + (r & 3)) ? x[r] : otherwise;
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[r] = admits<true>(first + 8 * (r >> 2) + (r & 3)) ? x[r] : otherwise;
+    }
   }
   // whether any, and whether all columns of the wavefront admit any, all of `n` keys from k0 on
   __device__ __forceinline__ bool any_of(int k0, int n) const {
@@ -352,6 +383,9 @@ __device__ __forceinline__ bool set_columns(const PackedCall& c, const Offsets& 
   x.valid = span.begin >= 0;
   x.begin = x.valid ? span.begin : 0;
   x.row = x.valid ? x.pos : 0;
+  x.mask_begin = x.valid ? x.begin : INT32_MAX;      // (none)
+  x.mask_span = x.valid ? x.pos - x.begin : 0;
+  x.mask_near = x.mask_span - c.recent;
   const Ends e = ends_of(x.valid);
   const bool any = e.first_lane >= 0;
   x.pos_lo = any ? __builtin_amdgcn_readlane(x.pos, e.first_lane) : INT32_MAX;

@@ -66,12 +66,10 @@ __global__ __launch_bounds__(64 * WAVES) void packed_attention_kernel(PackedCall
       for (int s = 0; s < 8; ++s)
 #pragma unroll
         for (int b = 0; b < 2; ++b) w[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(kt, 32 * b, s), q[s], w[b], 0, 0, 0);
+      reads_ahead<16, 16, 6, 1>();
       if (!all) {
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (!x.admits(key + 32 * b + 8 * (r >> 2) + 4 * half + (r & 3))) w[b][r] = -INFINITY;
+        x.mask(w[0], key, -INFINITY);
+        x.mask(w[1], key + 32, -INFINITY);
       }
       float mx = fmaxf(w[0][0], w[1][0]);
 #pragma unroll
@@ -103,6 +101,7 @@ __global__ __launch_bounds__(64 * WAVES) void packed_attention_kernel(PackedCall
 #pragma unroll
           for (int b = 0; b < 4; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_fragment(vt, 16 * s, b), p, o[b], 0, 0, 0);
         }
+        reads_ahead<16, 32, 8, 2>();
       }
     };
     int t = 0;

@@ -184,11 +184,7 @@ __global__ __launch_bounds__(64 * WAVES) void packed_grad_q_kernel(PackedCall c,
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) z[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(w[r], scale, -lse)) * (z[r] - delta);
-        if (!all) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (!x.admits(key + 8 * (r >> 2) + 4 * half + (r & 3))) z[r] = 0.f;
-        }
+        if (!all) x.mask(z, key, 0.f);
         if (kCareful && !all) {
           admitted_products(kt, b, z, dq, [&](int r) { return x.admits(key + r); });
         } else {
