@@ -29,7 +29,7 @@ __device__ __forceinline__ float dot_of_units(uint4 a, uint4 b) {
 // ---- the plan: what every workgroup of the second launch does ----
 constexpr int kKeysHere = 32 * kWaves, kStep = kStageRows;      // keys of a workgroup, positions of a step (below)
 constexpr int kMostParts = 512;           // workgroups that share keys, at most: two a compute unit
-constexpr int kLeastSteps = 4;            // steps that are worth a workgroup with a slot to write and to add up
+constexpr int kLeastSteps = 4, kEnoughSteps = 16;      // steps that are worth a workgroup with a slot to write and to add up where others idle; that are in any case
 constexpr int kSlotFloats = 2 * kHeadDim * kKeysHere;
 
 struct PlanItem {
@@ -88,9 +88,9 @@ __device__ void make_plan(const PackedCall& c, PlanSmem& sm) {
   for (int64_t i = threadIdx.x; i < pairs; i += blockDim.x) mine += steps_of(pair(i, tile, h), c.group);
   atomicAdd(&sm.total, mine);
   __syncthreads();
-  // parts of at least `least` and less than twice as many steps, so at most kMostParts of them
+  // parts of at least `least` and less than twice as many steps, so at most kMostParts of them; half as many where they are short
   const int64_t share = (int64_t)((sm.total + kMostParts - 1) / kMostParts);
-  const int least = (int)(share < kLeastSteps ? kLeastSteps : share);
+  const int least = (int)max(max(share, min(2 * share, (int64_t)kEnoughSteps)), (int64_t)kLeastSteps);
   PlanItem* items = items_of(c.plan);
   PlanMerge* merges = merges_of(c.plan, pairs);
   // (the long ones in front of the others)
@@ -182,6 +182,7 @@ __global__ __launch_bounds__(64 * WAVES) void packed_grad_q_kernel(PackedCall c,
           w = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(kt, b, s), q[s], w, 0, 0, 0);
           z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(vt, b, s), g[s], z, 0, 0, 0);
         }
+        reads_ahead<16, 16, 4, 1>();
 #pragma unroll
         for (int r = 0; r < 16; ++r) z[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(w[r], scale, -lse)) * (z[r] - delta);
         if (!all) x.mask(z, key, 0.f);
@@ -194,6 +195,7 @@ __global__ __launch_bounds__(64 * WAVES) void packed_grad_q_kernel(PackedCall c,
 #pragma unroll
             for (int d = 0; d < 4; ++d) dq[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_fragment(kt, b + 16 * s, d), p, dq[d], 0, 0, 0);
           }
+          reads_ahead<8, 16, 6, 2>();
         }
       }
     };
@@ -345,6 +347,7 @@ __global__ __launch_bounds__(kThreads) void packed_grad_kv_kernel(PackedCall c) 
               dk[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_fragment(qt, sub + 16 * s, d), z, dk[d], 0, 0, 0);
             }
           }
+          reads_ahead<16, 32, 6, 2>();
         }
       }
       pos += kStep;
