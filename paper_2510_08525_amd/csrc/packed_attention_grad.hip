@@ -228,6 +228,7 @@ __device__ __forceinline__ float* slot_piece(float* slots, int slot, int piece, 
 __global__ __launch_bounds__(kThreads) void packed_grad_kv_kernel(PackedCall c) {
   // (objects of their own, and the slot of a step known at compile time: else reads of one tile would wait for the loads of the next)
   __shared__ uint4 t0[2][kStep * 16], t1[2][kStep * 16];      // queries, gradients
+  __shared__ uint4 values[kKeysHere * 16];
   __shared__ float minus_lse[2][kStep], minus_delta[2][kStep];
   const int lane = threadIdx.x & 63, half = lane >> 5;
   __shared__ int32_t lost;
@@ -257,17 +258,18 @@ __global__ __launch_bounds__(kThreads) void packed_grad_kv_kernel(PackedCall c) 
   limit_lo = __builtin_amdgcn_readfirstlane(limit_lo);
   limit_hi = __builtin_amdgcn_readfirstlane(limit_hi);
 
-  bf16x8 k[8], v[8];
-  {
-    const int64_t row = key;
-    const uint16_t* k_row = c.k.p + row * c.k.token + h * c.k.head + 8 * half;
-    const uint16_t* v_row = c.v.p + row * c.v.token + h * c.v.head + 8 * half;
+  // Keys stay in registers; values, which would leave no room to read ahead, in LDS.
 #pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      k[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(k_row + 16 * s));
-      v[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(v_row + 16 * s));
-    }
+  for (int i = 0; i < kKeysHere; i += kStageRows)
+    if (item.tile * kKeysHere + i < c.tokens) stage_rows<kWaves>(c.v, item.tile * kKeysHere + i, h, c.tokens, values + i * 16);
+  bf16x8 k[8];
+  {
+    const uint16_t* k_row = c.k.p + (int64_t)key * c.k.token + h * c.k.head + 8 * half;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) k[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(k_row + 16 * s));
   }
+  const uint4* own_values = values + (threadIdx.x >> 6) * 32 * 16;
+
   const int per_head = (item.end - item.first + kStep - 1) / kStep;      // steps of a query head
   const float scale = c.scale * kLog2e, inv_scale = 1.f / c.scale;
   // the step that is asked for next: query head and first position
@@ -320,8 +322,9 @@ __global__ __launch_bounds__(kThreads) void packed_grad_kv_kernel(PackedCall c) 
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
           x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(qt, sub, s), k[s], x, 0, 0, 0);
-          y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(gt, sub, s), v[s], y, 0, 0, 0);
+          y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(gt, sub, s), row_fragment(own_values, 0, s), y, 0, 0, 0);
         }
+        reads_ahead<16, 24, 5, 2>();
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           x[r] = __builtin_amdgcn_exp2f(x[r] * scale);
