@@ -150,27 +150,37 @@ __device__ __forceinline__ uint32_t two_bf16(float a, float b) {      // rounded
   return __builtin_bit_cast(uint32_t, r);
 }
 
-// Rows in LDS, 16 units of 16 bytes each: blocks of 8 rows x 8 units (1 KiB), in a block pairs of units, in a pair the rows.  The 8 rows of which 8 lanes
-// read the same unit at a time, and the 4 rows of which 16 lanes read a pair transposed, then lie in banks of their own; and where a unit is, is a sum
-// of what the lane and what the instruction says, so all reads of a tile have one address register (with the units of a row swapped by exclusive or,
-// 24 of them, the gradient's second kernel kept its keys outside the registers).
+// Rows in LDS, 16 units of 16 bytes each: blocks of 8 rows x 8 units (1 KiB).  Where a unit is, is a sum of what the lane and what the instruction says, so
+// the reads of a tile have one to four address registers (with the units of a row permuted by its number, 24 of them, the gradient's second kernel
+// kept its keys outside the registers).
+//   kQuads  in a block quads of units, in a quad the rows, every fourth row's quad permuted: the 16 rows of which 16 lanes read the same unit at a time,
+//           and the 4 rows x 4 units of which 32 lanes read 8 bytes each transposed, lie in banks of their own
+//   kPairs  in a block pairs of units, in a pair the rows: half of the reads' time is conflicts.  Yet the forward kernel is the faster with it, for
+//           reasons that its counters do not tell (16384 tokens of 32 / 8 heads 1925 us and 1995 with quads), and the gradient's slower
+//           (2 x 8192 2415 us and 2227)
+enum Layout { kQuads, kPairs };
+template <Layout L>
 __device__ __forceinline__ int unit_at(int row, int unit) {
-  return (row >> 3) * 128 + (unit >> 3) * 64 + ((unit >> 1) & 3) * 16 + (row & 7) * 2 + (unit & 1);
+  if (L == kQuads) return (row >> 3) * 128 + (unit >> 2) * 32 + (row & 7) * 4 + ((unit ^ (row >> 2)) & 3);
+  return (row >> 3) * 128 + (unit >> 1) * 16 + (row & 7) * 2 + (unit & 1);
 }
-// Operand of 32 rows for the k's 16 step .. + 15 as they stand (A: rows of a tile in LDS); row0 a multiple of 8.
+// Operand of 32 rows for the k's 16 step .. + 15 as they stand (A: rows of a tile in LDS); row0 a multiple of 32.
+template <Layout L>
 __device__ __forceinline__ bf16x8 row_fragment(const uint4* tile, int row0, int step) {
   const int lane = threadIdx.x & 63;
-  return __builtin_bit_cast(bf16x8, tile[unit_at(lane & 31, lane >> 5) + (row0 >> 3) * 128 + (step >> 2) * 64 + (step & 3) * 16]);
+  return __builtin_bit_cast(bf16x8, tile[unit_at<L>(lane & 31, 2 * (step & 1) + (lane >> 5)) + (row0 >> 3) * 128 + (step >> 2) * 64 + (step & 2) * 16]);
 }
-// Operand of the 32 columns 32 block .. of a tile for 16 of its rows, in the order of k that a product's result has.
+// Operand of the 32 columns 32 block .. of a tile for 16 of its rows (row0 a multiple of 16), in the order of k that a product's result has.
+template <Layout L>
 __device__ __forceinline__ bf16x8 transposed_fragment(const uint4* tile, int row0, int block) {
 #ifdef __HIP_DEVICE_COMPILE__
   const int lane = threadIdx.x & 63;
-  const int own = unit_at(4 * (lane >> 5) + ((lane >> 2) & 3), 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1));
-  const char* at = reinterpret_cast<const char*>(tile) + own * 16 + 8 * (lane & 1) + ((row0 >> 3) * 128 + (block >> 1) * 64 + (block & 1) * 32) * 16;
+  const int row = 4 * (lane >> 5) + ((lane >> 2) & 3), unit = 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+  const int more = (row0 >> 3) * 128 + (block >> 1) * 64 + (block & 1) * 32;
+  const char* at = reinterpret_cast<const char*>(tile + more) + 8 * (lane & 1);
   union { shorts4 part[2]; bf16x8 all; } f;
-  f.part[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(RLKV_LDS_PTR(shorts4, at));
-  f.part[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(RLKV_LDS_PTR(shorts4, at + 128 * 16));
+  f.part[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(RLKV_LDS_PTR(shorts4, at + unit_at<L>(row, unit) * 16));
+  f.part[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(RLKV_LDS_PTR(shorts4, at + unit_at<L>(row + 8, unit) * 16));
   return f.all;
 #else
   return bf16x8{};
@@ -181,7 +191,7 @@ __device__ __forceinline__ bf16x8 transposed_fragment(const uint4* tile, int row
 // `tokens` on are the last one.  (Buffer loads, whose base is the same in all lanes; a row's place from it fits 32 bits.)
 constexpr int kStageRows = 64;
 constexpr int64_t kMostTokenStride = 1 << 24;
-template <int WAVES>
+template <Layout L, int WAVES>
 __device__ __forceinline__ void stage_rows(const HeadRows& t, int token, int head, int tokens, uint4* tile) {
 #ifdef __HIP_DEVICE_COMPILE__
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -190,7 +200,8 @@ __device__ __forceinline__ void stage_rows(const HeadRows& t, int token, int hea
   const int most = tokens - 1 - token;
 #pragma unroll
   for (int i = 0; i < 16 / WAVES; ++i) {
-    const int block = i * WAVES + wave, row = (block >> 1) * 8 + ((lane >> 1) & 7), unit = (block & 1) * 8 + (lane >> 4) * 2 + (lane & 1);
+    const int block = i * WAVES + wave, row = (block >> 1) * 8 + (L == kQuads ? (lane >> 2) & 7 : (lane >> 1) & 7);
+    const int unit = (block & 1) * 8 + (L == kQuads ? (lane >> 5) * 4 + ((lane ^ (row >> 2)) & 3) : (lane >> 4) * 2 + (lane & 1));
     const uint32_t at = (uint32_t)(row < most ? row : most) * (uint32_t)(t.token * 2) + unit * 16;
     __builtin_amdgcn_raw_ptr_buffer_load_lds(from, RLKV_LDS_PTR(void, tile + block * 64), 16, (int)at, 0, 0, 0);
   }
@@ -263,7 +274,7 @@ __device__ __forceinline__ void clear(floatx16& x) {
 }
 // acc[d][column] += sum over the rows of a 32-row tile of tile[row][d] * w[row][column] of admitted pairs, without the matrix instruction: a
 // weight of 0 does not keep an infinity or a NaN in the tile out of its products.
-template <typename F>
+template <Layout L, typename F>
 __device__ __forceinline__ void admitted_products(const uint4* tile, int row0, const floatx16& w, floatx16 (&acc)[4], F admits) {
   const int half = (threadIdx.x >> 5) & 1;
   for (int row = 0; row < 32; ++row) {
@@ -279,7 +290,7 @@ __device__ __forceinline__ void admitted_products(const uint4* tile, int row0, c
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const int d = 32 * b + 8 * g + 4 * half;
-        const words2 two = *reinterpret_cast<const words2*>(reinterpret_cast<const char*>(tile + unit_at(row0 + row, d >> 3)) + 2 * (d & 7));
+        const words2 two = *reinterpret_cast<const words2*>(reinterpret_cast<const char*>(tile + unit_at<L>(row0 + row, d >> 3)) + 2 * (d & 7));
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[b][4 * g + e] += x * __uint_as_float(e & 1 ? two[e >> 1] & 0xffff0000u : two[e >> 1] << 16);
       }

@@ -36,8 +36,8 @@ __global__ __launch_bounds__(64 * WAVES) void packed_attention_kernel(PackedCall
   const float scale = c.scale * kLog2e, slack = kSlack / scale;
   auto ask = [&](auto odd, int t) {
     constexpr int kOdd = decltype(odd)::value;
-    stage_rows<WAVES>(c.k, x.tile_key(t), block.head, c.tokens, kOdd ? t1[0] : t0[0]);
-    stage_rows<WAVES>(c.v, x.tile_key(t), block.head, c.tokens, kOdd ? t1[1] : t0[1]);
+    stage_rows<kPairs, WAVES>(c.k, x.tile_key(t), block.head, c.tokens, kOdd ? t1[0] : t0[0]);
+    stage_rows<kPairs, WAVES>(c.v, x.tile_key(t), block.head, c.tokens, kOdd ? t1[1] : t0[1]);
   };
 
   floatx16 o[4];
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(64 * WAVES) void packed_attention_kernel(PackedCall
 #pragma unroll
       for (int s = 0; s < 8; ++s)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) w[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(kt, 32 * b, s), q[s], w[b], 0, 0, 0);
+        for (int b = 0; b < 2; ++b) w[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment<kPairs>(kt, 32 * b, s), q[s], w[b], 0, 0, 0);
       reads_ahead<16, 16, 6, 1>();
       if (!all) {
         x.mask(w[0], key, -INFINITY);
@@ -93,13 +93,13 @@ __global__ __launch_bounds__(64 * WAVES) void packed_attention_kernel(PackedCall
         }
       if (kCareful && !all) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b) admitted_products(vt, 32 * b, w[b], o, [&](int r) { return x.admits(key + 32 * b + r); });
+        for (int b = 0; b < 2; ++b) admitted_products<kPairs>(vt, 32 * b, w[b], o, [&](int r) { return x.admits(key + 32 * b + r); });
       } else {
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
           const bf16x8 p = weights_fragment(w[s >> 1], s & 1);
 #pragma unroll
-          for (int b = 0; b < 4; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_fragment(vt, 16 * s, b), p, o[b], 0, 0, 0);
+          for (int b = 0; b < 4; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_fragment<kPairs>(vt, 16 * s, b), p, o[b], 0, 0, 0);
         }
         reads_ahead<16, 32, 8, 2>();
       }

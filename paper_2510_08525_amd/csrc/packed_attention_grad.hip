@@ -146,8 +146,8 @@ __global__ __launch_bounds__(64 * WAVES) void packed_grad_q_kernel(PackedCall c,
   const float scale = c.scale * kLog2e;
   auto ask = [&](auto odd, int t) {
     constexpr int kOdd = decltype(odd)::value;
-    stage_rows<WAVES>(c.k, x.tile_key(t), block.head, c.tokens, kOdd ? t1[0] : t0[0]);
-    stage_rows<WAVES>(c.v, x.tile_key(t), block.head, c.tokens, kOdd ? t1[1] : t0[1]);
+    stage_rows<kQuads, WAVES>(c.k, x.tile_key(t), block.head, c.tokens, kOdd ? t1[0] : t0[0]);
+    stage_rows<kQuads, WAVES>(c.v, x.tile_key(t), block.head, c.tokens, kOdd ? t1[1] : t0[1]);
   };
 
   // (while the first tile is under way)
@@ -179,21 +179,21 @@ __global__ __launch_bounds__(64 * WAVES) void packed_grad_q_kernel(PackedCall c,
         clear(z);
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
-          w = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(kt, b, s), q[s], w, 0, 0, 0);
-          z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(vt, b, s), g[s], z, 0, 0, 0);
+          w = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment<kQuads>(kt, b, s), q[s], w, 0, 0, 0);
+          z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment<kQuads>(vt, b, s), g[s], z, 0, 0, 0);
         }
         reads_ahead<16, 16, 4, 1>();
 #pragma unroll
         for (int r = 0; r < 16; ++r) z[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(w[r], scale, -lse)) * (z[r] - delta);
         if (!all) x.mask(z, key, 0.f);
         if (kCareful && !all) {
-          admitted_products(kt, b, z, dq, [&](int r) { return x.admits(key + r); });
+          admitted_products<kQuads>(kt, b, z, dq, [&](int r) { return x.admits(key + r); });
         } else {
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
             const bf16x8 p = weights_fragment(z, s);
 #pragma unroll
-            for (int d = 0; d < 4; ++d) dq[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_fragment(kt, b + 16 * s, d), p, dq[d], 0, 0, 0);
+            for (int d = 0; d < 4; ++d) dq[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_fragment<kQuads>(kt, b + 16 * s, d), p, dq[d], 0, 0, 0);
           }
           reads_ahead<8, 16, 6, 2>();
         }
@@ -261,7 +261,7 @@ __global__ __launch_bounds__(kThreads) void packed_grad_kv_kernel(PackedCall c) 
   // Keys stay in registers; values, which would leave no room to read ahead, in LDS.
 #pragma unroll
   for (int i = 0; i < kKeysHere; i += kStageRows)
-    if (item.tile * kKeysHere + i < c.tokens) stage_rows<kWaves>(c.v, item.tile * kKeysHere + i, h, c.tokens, values + i * 16);
+    if (item.tile * kKeysHere + i < c.tokens) stage_rows<kQuads, kWaves>(c.v, item.tile * kKeysHere + i, h, c.tokens, values + i * 16);
   bf16x8 k[8];
   {
     const uint16_t* k_row = c.k.p + (int64_t)key * c.k.token + h * c.k.head + 8 * half;
@@ -276,8 +276,8 @@ __global__ __launch_bounds__(kThreads) void packed_grad_kv_kernel(PackedCall c) 
   int next_head, next_pos;
   auto ask = [&](auto odd) {
     constexpr int kOdd = decltype(odd)::value;
-    stage_rows<kWaves>(c.q, next_pos, next_head, c.tokens, kOdd ? t1[0] : t0[0]);
-    stage_rows<kWaves>(c.grad_out, next_pos, next_head, c.tokens, kOdd ? t1[1] : t0[1]);
+    stage_rows<kQuads, kWaves>(c.q, next_pos, next_head, c.tokens, kOdd ? t1[0] : t0[0]);
+    stage_rows<kQuads, kWaves>(c.grad_out, next_pos, next_head, c.tokens, kOdd ? t1[1] : t0[1]);
     if (threadIdx.x < kStep) {
       const int64_t row = (int64_t)next_head * c.tokens + min(next_pos + (int)threadIdx.x, c.tokens - 1);
       minus_lse[kOdd][threadIdx.x] = -c.lse[row] * inv_scale;
@@ -321,8 +321,8 @@ __global__ __launch_bounds__(kThreads) void packed_grad_kv_kernel(PackedCall c) 
         }
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
-          x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(qt, sub, s), k[s], x, 0, 0, 0);
-          y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment(gt, sub, s), row_fragment(own_values, 0, s), y, 0, 0, 0);
+          x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment<kQuads>(qt, sub, s), k[s], x, 0, 0, 0);
+          y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(row_fragment<kQuads>(gt, sub, s), row_fragment<kQuads>(own_values, 0, s), y, 0, 0, 0);
         }
         reads_ahead<16, 24, 5, 2>();
 #pragma unroll
@@ -338,16 +338,16 @@ __global__ __launch_bounds__(kThreads) void packed_grad_kv_kernel(PackedCall c) 
         }
         if (kCareful && !all) {
           auto admits = [&](int col) { return (uint32_t)(p0 + col - key) < width; };
-          admitted_products(gt, sub, x, dv, admits);
-          admitted_products(qt, sub, y, dk, admits);
+          admitted_products<kQuads>(gt, sub, x, dv, admits);
+          admitted_products<kQuads>(qt, sub, y, dk, admits);
         } else {
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
             const bf16x8 w = weights_fragment(x, s), z = weights_fragment(y, s);
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-              dv[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_fragment(gt, sub + 16 * s, d), w, dv[d], 0, 0, 0);
-              dk[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_fragment(qt, sub + 16 * s, d), z, dk[d], 0, 0, 0);
+              dv[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_fragment<kQuads>(gt, sub + 16 * s, d), w, dv[d], 0, 0, 0);
+              dk[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(transposed_fragment<kQuads>(qt, sub + 16 * s, d), z, dk[d], 0, 0, 0);
             }
           }
           reads_ahead<16, 32, 6, 2>();
