@@ -396,17 +396,35 @@ __device__ void cut(Smem& sm, const T* row, int vocab, Row& r, const Weight& wei
 __device__ __forceinline__ void load_roots(uint64_t* roots, int bits) {
   if (threadIdx.x < kRootCount) roots[threadIdx.x] = (uint64_t)__double_as_longlong(kRoots[threadIdx.x]) + ((uint64_t)bits << 52);
 }
-// Largest logit of a row, from its parts (a few dozen); false where there is nothing to draw from.
-__device__ __forceinline__ bool top_of(const Part* parts, int n, float& top) {
-  bool bad = false;
-  top = -INFINITY;
-  for (int p = threadIdx.x & 63; p < n; p += 64) {
-    top = fmaxf(top, parts[p].top);
-    bad |= parts[p].bad != 0;
+// What a row's parts (a few dozen) come to, in every wavefront that asks: lane l reads the parts l, l + 64, ..
+struct RowParts {
+  const Part* parts;
+  int n;
+  Part first;                      // of this lane
+  float top;                       // the row's largest logit
+  bool drawn;                      // there is something to draw from
+  __device__ __forceinline__ RowParts(const Part* parts, int n) : parts(parts), n(n) {
+    const int lane = threadIdx.x & 63;
+    first = parts[lane < n ? lane : 0];
+    top = first.top;
+    bool bad = first.bad != 0;
+    for (int p = lane + 64; p < n; p += 64) {
+      top = fmaxf(top, parts[p].top);
+      bad |= parts[p].bad != 0;
+    }
+    top = max_of_wave(top);
+    drawn = !__any(bad) && top != -INFINITY;
   }
-  top = max_of_wave(top);
-  return !__any(bad) && top != -INFINITY;
-}
+  // Sum of the row's weights with `top` for reference, of 2^bits: parts in a fixed order.
+  __device__ __forceinline__ double total(double inv) const {
+    const int lane = threadIdx.x & 63;
+    double sum = lane < n && first.top != -INFINITY ? first.sum * exp(((double)first.top - (double)top) * inv) : 0.;
+    for (int p = lane + 64; p < n; p += 64)
+      if (parts[p].top != -INFINITY) sum += parts[p].sum * exp(((double)parts[p].top - (double)top) * inv);
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+    return sum;
+  }
+};
 
 // The tokens of a part, all asked for at once; -infinity behind the row's end.
 template <typename T, int THREADS>
@@ -491,16 +509,6 @@ __global__ __launch_bounds__(THREADS) void parts_kernel(SampleCall c, Space spac
   if (threadIdx.x == 0) space.parts[(int64_t)blockIdx.y * space.n_parts + p] = {top, bad, sum, 0};
 }
 
-// Sum of a row's weights with its largest logit for reference, of 2^bits: parts in their order, the same in every wavefront that asks.
-__device__ __forceinline__ double total_of_parts(const Part* parts, int n, float top, const Settings& s) {
-  const double inv = inverse(s.t);
-  double sum = 0.;
-  for (int p = threadIdx.x & 63; p < n; p += 64)
-    if (parts[p].top != -INFINITY) sum += parts[p].sum * exp(((double)parts[p].top - (double)top) * inv);
-  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-  return sum;
-}
-
 template <typename T>
 __global__ __launch_bounds__(kThreads, 8) void bins_kernel(SampleCall c, Space space, int bits) {
   __shared__ uint64_t roots[kRootCount];
@@ -509,10 +517,12 @@ __global__ __launch_bounds__(kThreads, 8) void bins_kernel(SampleCall c, Space s
   const int64_t n = space.first_row + blockIdx.y;
   const T* row = static_cast<const T*>(c.logits) + n * c.stride;
   const Settings s = settings_of(c, n);
-  float top;
-  if (!s.cut() || !top_of(space.parts + (int64_t)blockIdx.y * space.n_parts, space.n_parts, top)) return;
-  const PartTokens<T, kThreads> part(row, blockIdx.x, c.vocab);
+  if (!s.cut()) return;
+  const PartTokens<T, kThreads> part(row, blockIdx.x, c.vocab);      // (asked for before anything is waited for)
   load_roots(roots, bits);
+  const RowParts all(space.parts + (int64_t)blockIdx.y * space.n_parts, space.n_parts);
+  if (!all.drawn) return;
+  const float top = all.top;
   for (int b = threadIdx.x; b < kBins; b += kThreads) {
     mass[b] = 0;
     count[b] = 0;
@@ -524,8 +534,7 @@ __global__ __launch_bounds__(kThreads, 8) void bins_kernel(SampleCall c, Space s
   // Tokens that top_p keeps for sure not: those of a weight below (1 - p) sum / vocab have less than 1 - p of the sum together.
   unsigned long long least = 0;
   if (by_mass) {
-    const double sum = total_of_parts(space.parts + (int64_t)blockIdx.y * space.n_parts, space.n_parts, top, s);
-    least = (unsigned long long)((1. - s.top_p) * sum * 0.99 / c.vocab);
+    least = (unsigned long long)((1. - s.top_p) * all.total(inverse(s.t)) * 0.99 / c.vocab);
   }
   part.each(c.vocab, [&](float x, int) {
     const int b = bin_at(x);
@@ -555,22 +564,25 @@ __global__ __launch_bounds__(kThreads, 8) void collect_kernel(SampleCall c, Spac
   const T* row = static_cast<const T*>(c.logits) + n * c.stride;
   Part* parts = space.parts + (int64_t)blockIdx.y * space.n_parts;
   const Settings s = settings_of(c, n);
-  float top;
-  if (!s.filter() || !top_of(parts, space.n_parts, top)) return;
+  if (!s.filter()) return;
+  // (all of it asked for before anything is waited for)
   const PartTokens<T, kThreads> part(row, blockIdx.x, c.vocab);
-  load_roots(roots, bits);
   RowSpace& r = space.rows[blockIdx.y];
+  constexpr int kEach = kBins / kThreads;
+  const bool by_mass = s.top_k == 0;
+  unsigned long long v[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) v[i] = !s.cut() ? 0 : by_mass ? r.mass[threadIdx.x * kEach + i] : r.count[threadIdx.x * kEach + i];
+  load_roots(roots, bits);
+  const RowParts all(parts, space.n_parts);
+  if (!all.drawn) return;
+  const float top = all.top;
   int first = kBins, last = kBins;                  // bins [first, last] are listed
   if (s.cut()) {
-    const bool by_mass = s.top_k == 0;
-    const double target = by_mass ? s.top_p * total_of_parts(parts, space.n_parts, top, s) : 0.;
-    constexpr int kEach = kBins / kThreads;
-    unsigned long long v[kEach], run = 0;
+    const double target = by_mass ? s.top_p * all.total(inverse(s.t)) : 0.;
+    unsigned long long run = 0;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      v[i] = by_mass ? r.mass[threadIdx.x * kEach + i] : r.count[threadIdx.x * kEach + i];
-      run += v[i];
-    }
+    for (int i = 0; i < kEach; ++i) run += v[i];
     const unsigned long long own = run;
     for (int d = 1; d < 64; d <<= 1) {
       const unsigned long long other = __shfl_up(run, d);
@@ -639,13 +651,15 @@ struct PlainDraw {
   unsigned long long way;
   int32_t part;
 };
-__device__ PlainDraw plain_part(const Part* parts, int n, float top, double inv, float u) {
+__device__ PlainDraw plain_part(const RowParts& all, double inv, float u) {
+  const Part* parts = all.parts;
+  const int n = all.n;
+  const float top = all.top;
   const int lane = threadIdx.x & 63;
-  double total = 0., run = 0., before = 0.;
+  double run = 0., before = 0.;
   int found = -1;
   auto weight_at = [&](int p) { return p < n && parts[p].top != -INFINITY ? parts[p].sum * exp(((double)parts[p].top - (double)top) * inv) : 0.; };
-  for (int p0 = 0; p0 < n; p0 += 64) total += weight_at(p0 + lane);
-  for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
+  const double total = all.total(inv);
   const double target = (u > 0.f ? u < 1.f ? (double)u : 1. - 1e-16 : 0.) * total;
   for (int p0 = 0; p0 < n; p0 += 64) {
     const double w = weight_at(p0 + lane);
@@ -679,8 +693,9 @@ __global__ __launch_bounds__(kFewThreads) void draw_plain_kernel(SampleCall c, S
   const Part* parts = space.parts + (int64_t)blockIdx.x * space.n_parts;
   Settings s = {c.temperature, 1., 0., 0};
   const float u = c.uniforms[n];
-  float top;
-  if (!top_of(parts, space.n_parts, top)) {             // nothing to draw from
+  const RowParts all(parts, space.n_parts);
+  const float top = all.top;
+  if (!all.drawn) {                                     // nothing to draw from
     if (threadIdx.x == 0) {
       c.tokens[n] = -1;
       if (c.logprobs) c.logprobs[n] = NAN;
@@ -689,7 +704,7 @@ __global__ __launch_bounds__(kFewThreads) void draw_plain_kernel(SampleCall c, S
   }
   load_roots(roots, bits);
   const double inv = inverse(s.t);
-  const PlainDraw d = plain_part(parts, space.n_parts, top, inv, u);      // (every wavefront for itself)
+  const PlainDraw d = plain_part(all, inv, u);      // (every wavefront for itself)
   const Weight weight = weight_of(s, roots, parts[d.part].top, bits, 0.);
   const int lo = d.part * kPart;
   __syncthreads();
@@ -713,7 +728,18 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
   r.key = 0;
   r.last = 0x7fffffff;
   const Settings& s = r.how;
-  if (!top_of(parts, space.n_parts, r.top)) {             // nothing to draw from
+  // (what the last launch left, asked for before anything is waited for; behind the list's end it is not used)
+  const float u = c.uniforms[n];
+  RowCut cut_of_row = {};
+  unsigned long long listed_here[kList / kThreads] = {};
+  if (s.cut()) {
+    cut_of_row = space_of_row.cut;
+#pragma unroll
+    for (int q = 0; q < kList / kThreads; ++q) listed_here[q] = space_of_row.list[q * kThreads + threadIdx.x];
+  }
+  const RowParts row_parts(parts, space.n_parts);
+  r.top = row_parts.top;
+  if (!row_parts.drawn) {                               // nothing to draw from
     if (threadIdx.x == 0) {
       c.tokens[n] = -1;
       if (c.logprobs) c.logprobs[n] = NAN;
@@ -722,7 +748,6 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
   }
   load_roots(sm.roots, bits);
   const double unit = (double)(1ull << bits), inv = inverse(s.t);
-  const float u = c.uniforms[n];
   auto write = [&](int i, double total) {
     if (threadIdx.x != 0) return;
     c.tokens[n] = i;
@@ -745,7 +770,7 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
   }
   const unsigned long long u64 = !(u > 0.f) ? 0 : u < 1.f ? (unsigned long long)((double)u * 18446744073709551616.) : ~0ull;
   if (!s.filter()) {
-    const PlainDraw d = plain_part(parts, space.n_parts, r.top, inv, u);      // (every wavefront for itself)
+    const PlainDraw d = plain_part(row_parts, inv, u);      // (every wavefront for itself)
     const int p = d.part, lo = p * kPart;
     const Weight weight = weight_of(s, sm.roots, parts[p].top, bits, 0.);
     write(place_of<kThreads>(sm.place, row, lo, min(lo + kPart, c.vocab), d.way, [&](float x, int) { return weight.whole(x); }), d.total);
@@ -757,15 +782,17 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
   bool listed = true;
   __syncthreads();
   if (s.cut()) {
-    const RowCut cut_of_row = space_of_row.cut;
     listed = cut_of_row.listed <= kList;
     if (listed && cut_of_row.listed > 0) {
       // every token of the list by how many, and what weight, stand in front of it
       const int count = cut_of_row.listed;
       unsigned long long* order = sm.mass;                 // (2048 of each)
       __shared__ unsigned long long weights[kList];
-      for (int j = threadIdx.x; j < count; j += kThreads) {
-        const unsigned long long e = space_of_row.list[j];
+#pragma unroll
+      for (int q = 0; q < kList / kThreads; ++q) {
+        const int j = q * kThreads + threadIdx.x;
+        if (j >= count) continue;
+        const unsigned long long e = listed_here[q];
         order[j] = e;
         const uint32_t key = ~(uint32_t)(e >> 32);
         weights[j] = all(__uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key));
@@ -819,7 +846,7 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
           for (int w = 0; w < kWaves; ++w) total += sm.sums[w];
           target = s.top_p * (double)total;
         } else {
-          target = s.top_p * total_of_parts(parts, space.n_parts, r.top, s);
+          target = s.top_p * row_parts.total(inv);
         }
       }
       if (threadIdx.x == 0) sm.found = 0;
@@ -884,30 +911,43 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
   // what is kept of every part: what is above the list, and of the list
   unsigned long long* of_part = sm.mass;
   __syncthreads();
-  for (int p = threadIdx.x; p < kBins; p += kThreads) of_part[p] = p < space.n_parts ? parts[p].above : 0;
+  for (int p = threadIdx.x; p < (space.n_parts + 63) / 64 * 64; p += kThreads) of_part[p] = p < space.n_parts ? parts[p].above : 0;
   __syncthreads();
-  if (s.cut())
-    for (int j = threadIdx.x; j < space_of_row.cut.listed; j += kThreads) {
-      const unsigned long long e = space_of_row.list[j];
+  if (s.cut()) {
+#pragma unroll
+    for (int q = 0; q < kList / kThreads; ++q) {
+      const int j = q * kThreads + threadIdx.x;
+      if (j >= cut_of_row.listed) continue;
+      const unsigned long long e = listed_here[q];
       const uint32_t key = ~(uint32_t)(e >> 32);
       const unsigned long long w = kept_weight(__uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key), (int)(uint32_t)e);
       if (w) atomicAdd(&of_part[(uint32_t)e / kPart], w);
     }
-  for (int p = threadIdx.x; p < kBins; p += kThreads) sm.count[p] = 0;
+  }
   __syncthreads();
+  // (every wavefront for itself)
   unsigned long long total = 0;
-  for (int p = threadIdx.x; p < kBins; p += kThreads) total += of_part[p];
+  for (int p = lane; p < space.n_parts; p += 64) total += of_part[p];
   total = sum_over_wave(total);
-  if (lane == 0) sm.sums[wave] = total;
-  __syncthreads();
-  total = 0;
-  for (int w = 0; w < kWaves; ++w) total += sm.sums[w];
-  __syncthreads();
-  const unsigned long long target = __umul64hi(total, u64);
-  bin_of(sm, true, target);
-  const int lo = (int)sm.found * kPart;
-  const unsigned long long way = target - sm.found_before;
-  __syncthreads();
+  unsigned long long way = __umul64hi(total, u64);
+  int found = 0;
+  for (int p0 = 0; p0 < space.n_parts; p0 += 64) {
+    const unsigned long long own = of_part[p0 + lane];
+    unsigned long long upto = own;
+    for (int d = 1; d < 64; d <<= 1) {
+      const unsigned long long other = __shfl_up(upto, d);
+      if (lane >= d) upto += other;
+    }
+    const unsigned long long past = __ballot(way < upto);
+    if (past) {
+      const int at = __builtin_ctzll(past);
+      found = p0 + at;
+      way -= __shfl(upto - own, at);
+      break;
+    }
+    way -= __shfl(upto, 63);
+  }
+  const int lo = found * kPart;
   write(place_of<kThreads>(sm.place, row, lo, min(lo + kPart, c.vocab), way, kept_weight), (double)total);
 }
 
