@@ -105,17 +105,23 @@ class Decoder:
         rl.token_logprobs(logits, tokens, logprob, entropy=entropy, lse=lse, top=best)
         return logprob, entropy, lse, best
 
-    def rollout(self, prompts, counts, steps):
-        """Greedy answers to ragged prompts: tokens, their log probabilities, entropies [batch, steps] and the logits they came from."""
+    def rollout(self, prompts, counts, steps, sampling=None, seed=0):
+        """Answers to ragged prompts: tokens, their log probabilities, entropies [batch, steps] and the logits they came from.  Greedy, or drawn
+        with the arguments of `sample_tokens` in `sampling`."""
         B = self.batch
         logits = self.forward(prompts, counts)
         last = logits[torch.arange(B, device="cuda"), torch.tensor(counts, device="cuda") - 1].contiguous()
         said = []
+        uniforms = torch.rand(steps, B, generator=torch.Generator().manual_seed(seed)).cuda()
         for step in range(steps):
             if step:
                 last = self.forward(said[-1][0].long().view(B, 1)).view(B, -1)
-            _, _, _, (_, ids) = self.score(last, torch.full((B,), -1, dtype=torch.int32, device="cuda"), top=3)
-            token = ids[:, 0].contiguous()
+            if sampling is None:
+                _, _, _, (_, ids) = self.score(last, torch.full((B,), -1, dtype=torch.int32, device="cuda"), top=3)
+                token = ids[:, 0].contiguous()
+            else:
+                token = torch.empty(B, dtype=torch.int32, device="cuda")
+                rl.sample_tokens(last, uniforms[step], token, **sampling)
             logprob, entropy, lse, _ = self.score(last, token)
             said.append((token, logprob, entropy, lse, last))
         return [torch.stack(v, 1) for v in zip(*said)]

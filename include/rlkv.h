@@ -621,8 +621,9 @@ rlkv_status_t rlkv_head_norm_rotary_grad(const void* qkv /* device */, int64_t t
  *               Calls that may overlap in time need one each.
  * A filter is off at top_k = 0, top_p >= 1, min_p = 0; the most likely token is kept by all.  A temperature of 0 draws the most likely token (the lowest
  * of equal ones, log probability 0), whatever the filters are.  Masked logits (-inf) are never drawn.  A row with a NaN or +inf, or of masked logits
- * only, gets token -1 and log probability NaN.  Weights are whole numbers of 2^-b, b = 62 - log2(vocab), summed exactly: equal calls give equal
- * tokens, and a token less likely than 2^-b of the most likely one is never drawn. */
+ * only, gets token -1 and log probability NaN.  Weights come from an exponential in 64 bits that is good to 2^-38 and are whole numbers of 2^-b,
+ * b = min(50, 62 - log2(vocab)), of the most likely token's (without filters: of the most likely one's of the 8192 tokens that they are among); what is
+ * below 2^-b of it may not be drawn.  Sums are exact, or in 64-bit floating point in a fixed order: equal calls give equal tokens. */
 typedef struct {
   double temperature, top_p, min_p; /* temperature finite, >= 0; top_p >= 0; min_p in [0, 1] */
   int32_t top_k;                    /* >= 0                                          */

@@ -3,9 +3,9 @@
 //   w[i] = exp((x[i] - max x) / temperature);  in order of x (equal ones by the lower token) the first top_k are kept, of those the first whose
 //   weights reach top_p of their sum, of those the ones with w >= min_p;  token = first kept i with  sum of kept w[0 .. i] > u * sum of kept w
 //
-// Weights are whole numbers of 2^-bits, bits = 62 - log2(vocab), from an exponential in 64 bits: their sums are exact in 64-bit integers, in whatever
-// order they are formed, so atomics and scans give the same token at every call, and borders between tokens are where the formula has them to 2^-39
-// of the weights (what sums in 32 bits leave, 2^-24 of a border's place, changes a token of 128k in one of hundred rows).
+// Weights are whole numbers of 2^-bits, bits = min(50, 62 - log2(vocab)), from an exponential in 64 bits: their sums are exact in 64-bit integers, in
+// whatever order they are formed, so atomics and scans give the same token at every call, and borders between tokens are where the formula has
+// them to 2^-38 of the weights (what sums in 32 bits leave, 2^-24 of a border's place, changes a token of 128k in one of hundred rows).
 //
 // A row is read by as many workgroups as it has parts of 8192 tokens.  Launches, of which rows without filters need the first and the last:
 //   parts    largest logit and, for rows whose sum is asked for, the sum of weights of a part

@@ -1,7 +1,8 @@
 """Tokens drawn by given random numbers, against the definition in 64 bits.
 
-Weights are whole numbers of 2^-b, b = 62 - log2(vocab), so a border between two tokens lies within vocab * 2^-b of the sum of weights (at least 1) of
-where 64 bits have it: the reference names the token, and its neighbour where u lies that close to a border (and the cut by top_p its own neighbours)."""
+Weights are off by 2^-38 of themselves (the exponential) and, as whole numbers of 2^-b, b = min(50, 62 - log2(vocab)), by 2^-(b + 1): a border between two
+tokens lies within 2^-37 + vocab * 2^-b of the sum of weights (at least 1) of where 64 bits have it.  The reference names the token, and its neighbour
+where u lies that close to a border (and the cut by top_p its own neighbours)."""
 import math
 
 import pytest
@@ -39,7 +40,8 @@ def draw(x, u, T, k, p, m):
     cum = torch.cumsum(w, 0)
     i = int((cum <= u * cum[-1]).sum())
     i = min(i, int(w.nonzero()[-1]))
-    near = (cum / cum[-1] - u).abs().min() < x.numel() * 2.0 ** (math.ceil(math.log2(x.numel())) - 61)
+    bits = min(50, 62 - math.ceil(math.log2(x.numel()))) if x.numel() > 1 else 50
+    near = (cum / cum[-1] - u).abs().min() < 2.0 ** -37 + x.numel() * 2.0 ** -bits
     exact = (w[w > 0] == 1).all()                  # (equal logits: weights of 1 and their sums are whole numbers on both sides, borders the same)
     return i, math.log(w[i] / cum[-1]), bool(exact or not near)
 
