@@ -9,9 +9,12 @@
 //
 // A row is read by as many workgroups as it has parts of 8192 tokens.  Launches, of which rows without filters need the first and the last:
 //   parts    largest logit and, for rows whose sum is asked for, the sum of weights of a part
-//   bins     of rows with top_k or top_p: how many tokens, and what weight, lie in each of 4096 steps down from the largest logit
+//   bins     how many tokens, and what weight, lie in each of 4096 steps down from the largest logit
 //   collect  the step in which the cut falls: its tokens go into a list; the weight of a part's tokens above it
 //   draw     one workgroup a row: the cut among the list's tokens, the part that the number falls into, the token in it
+// Of rows with top_k the two in the middle do nothing where a logit that top_k tokens reach is found among the largest ones of each 128 tokens: the
+// last launch makes the list, from the chunks that reach it, and finds the token in the list (48 rows of 128011 in float32, most with a
+// top_k: 45 us, with bins for all of them 57).
 // A row whose list would be too long (thousands of like logits at the cut, a top_k of thousands) is cut by its last workgroup alone, in passes over the row.
 #include "sample_tokens.h"
 
@@ -26,6 +29,9 @@ constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 4096;
 constexpr float kBinsPerUnit = 128.f;     // bins: the way from the largest logit over the temperature, 32 of it
 constexpr int kList = 2048;               // tokens of a row's list
 constexpr int kPart = 8192;               // tokens of a part
+constexpr int kChunks = 64;               // of a part, of 128 tokens, eight in each of 16 lanes: their largest logits are kept
+constexpr int kSums = kWaves;             // of a part, of 512 tokens: the weights above the list's
+constexpr int kMostGroups = 256;          // groups of chunks whose largest logits are ranked
 constexpr int kFewThreads = 256;          // of the launches that many rows have many workgroups of
 constexpr int kRowsAtOnce = 512;          // rows that have a workspace
 
@@ -34,9 +40,37 @@ __device__ __forceinline__ uint32_t key_of(float x) {
   const uint32_t b = __float_as_uint(x + 0.f);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ unsigned long long sum_over_wave(unsigned long long x) {
-  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
+template <int CTRL, typename T>
+__device__ __forceinline__ T turned(T x) {
+  const unsigned long long b = __builtin_bit_cast(unsigned long long, x);
+  const uint32_t low = __builtin_amdgcn_update_dpp(0, (uint32_t)b, CTRL, 0xf, 0xf, false), high = __builtin_amdgcn_update_dpp(0, (uint32_t)(b >> 32), CTRL, 0xf, 0xf, false);
+  return __builtin_bit_cast(T, (unsigned long long)high << 32 | low);
+}
+// Largest of each 16 lanes.
+__device__ __forceinline__ float max_of_16(float x) {
+  auto step = [&](auto ctrl) {
+    x = fmaxf(x, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), decltype(ctrl)::value, 0xf, 0xf, false)));
+  };
+  step(std::integral_constant<int, 0xb1>{});
+  step(std::integral_constant<int, 0x4e>{});
+  step(std::integral_constant<int, 0x141>{});
+  step(std::integral_constant<int, 0x140>{});
   return x;
+}
+template <typename T>
+__device__ __forceinline__ T lane_of(T x, int lane) {
+  const unsigned long long b = __builtin_bit_cast(unsigned long long, x);
+  const uint32_t low = __builtin_amdgcn_readlane((uint32_t)b, lane), high = __builtin_amdgcn_readlane((uint32_t)(b >> 32), lane);
+  return __builtin_bit_cast(T, (unsigned long long)high << 32 | low);
+}
+// In the registers (neighbours, pairs, the halves and the whole of 16 lanes mirrored, the four rows of 16), the same in all lanes; all have to be there.
+template <typename T>
+__device__ __forceinline__ T sum_over_wave(T x) {
+  x += turned<0xb1>(x);
+  x += turned<0x4e>(x);
+  x += turned<0x141>(x);
+  x += turned<0x140>(x);
+  return (lane_of(x, 0) + lane_of(x, 16)) + (lane_of(x, 32) + lane_of(x, 48));
 }
 
 // 2^(j / 128)
@@ -112,6 +146,9 @@ __host__ __device__ inline int bits_of(int vocab) {
   return bits < 50 ? bits : 50;
 }
 
+// The share of a sum of weights that is to be reached: whole weights reach it where they reach the next whole number.
+__device__ __forceinline__ unsigned long long whole_share(double p, double total) { return (unsigned long long)ceil(p * total); }
+
 struct Settings {
   double t, top_p, min_p;
   int top_k;                 // 0: off, and so where it is no less than vocab
@@ -152,11 +189,11 @@ struct Part {
   float top;
   int32_t bad;                     // a NaN or +inf is there
   double sum;                      // of weights with the part's largest logit for reference, of 2^bits
-  unsigned long long above;        // of weights above the cut's bin that min_p keeps, with the row's largest for reference
+  unsigned long long above;        // of weights above the list's that min_p keeps, with the row's largest for reference
 };
 struct RowCut {
   int32_t listed;                  // tokens of the list; more than kList: there is no list
-  int32_t pad;
+  uint32_t by_tops;                // the list is made by the last launch
   unsigned long long before;       // weight of the tokens above the list's
 };
 struct RowSpace {
@@ -168,6 +205,8 @@ struct RowSpace {
 struct Space {
   RowSpace* rows;
   Part* parts;                     // [rows][n_parts]
+  unsigned long long* sums;        // [rows][n_parts][kSums]
+  float* tops;                     // [rows][n_parts][kChunks]
   int32_t n_parts;
   int64_t first_row;               // of the launch
 };
@@ -400,14 +439,15 @@ __device__ __forceinline__ void load_roots(uint64_t* roots, int bits) {
 struct RowParts {
   const Part* parts;
   int n;
-  Part first;                      // of this lane
+  struct { float top; double sum; } first;      // of this lane
   float top;                       // the row's largest logit
   bool drawn;                      // there is something to draw from
   __device__ __forceinline__ RowParts(const Part* parts, int n) : parts(parts), n(n) {
     const int lane = threadIdx.x & 63;
-    first = parts[lane < n ? lane : 0];
+    const Part& part = parts[lane < n ? lane : 0];
+    first = {part.top, part.sum};
     top = first.top;
-    bool bad = first.bad != 0;
+    bool bad = part.bad != 0;
     for (int p = lane + 64; p < n; p += 64) {
       top = fmaxf(top, parts[p].top);
       bad |= parts[p].bad != 0;
@@ -421,8 +461,7 @@ struct RowParts {
     double sum = lane < n && first.top != -INFINITY ? first.sum * exp(((double)first.top - (double)top) * inv) : 0.;
     for (int p = lane + 64; p < n; p += 64)
       if (parts[p].top != -INFINITY) sum += parts[p].sum * exp(((double)parts[p].top - (double)top) * inv);
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-    return sum;
+    return sum_over_wave(sum);
   }
 };
 
@@ -475,17 +514,28 @@ __global__ __launch_bounds__(THREADS) void parts_kernel(SampleCall c, Space spac
       r.mass[b] = 0;
       r.count[b] = 0;
     }
-    if (p == 0 && threadIdx.x == 0) r.cut.listed = 0;
+    if (p == 0 && threadIdx.x == 0) {
+      r.cut.listed = 0;
+      r.cut.by_tops = 0;
+    }
   }
+  Part& result = space.parts[(int64_t)blockIdx.y * space.n_parts + p];
   float top = -INFINITY;
   bool bad = false;
 #pragma unroll
-  for (int k = 0; k < PIECES; ++k)
+  for (int k = 0; k < PIECES; ++k) {
+    float here = x[k][0];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      top = fmaxf(top, x[k][i]);
+      here = fmaxf(here, x[k][i]);
       bad |= !(x[k][i] < INFINITY);
     }
+    if (cuts) {
+      here = max_of_16(here);
+      if (lane % 16 == 0) space.tops[((int64_t)blockIdx.y * space.n_parts + p) * kChunks + (k * THREADS + threadIdx.x) / 16] = here;
+    }
+    top = fmaxf(top, here);
+  }
   top = max_of_wave(top);
   if (lane == 0) tops[wave] = top;
   bad = __syncthreads_or(bad);
@@ -499,15 +549,39 @@ __global__ __launch_bounds__(THREADS) void parts_kernel(SampleCall c, Space spac
     for (int k = 0; k < PIECES; ++k)
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum += weight.real(x[k][i]);
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+    sum = sum_over_wave(sum);
     if (lane == 0) sums[wave] = sum;
     __syncthreads();
     sum = 0.;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) sum += sums[w];
   }
-  if (threadIdx.x == 0) space.parts[(int64_t)blockIdx.y * space.n_parts + p] = {top, bad, sum, 0};
+  if (threadIdx.x == 0) {
+    result.top = top;
+    result.bad = bad;
+    result.sum = sum;
+    result.above = 0;
+  }
 }
+
+// The rule by which a row's top_k is found among the largest logits of groups of chunks: the k-th largest of n of them is reached by k tokens at
+// least and by some n ln(n / (n - k)) where tokens lie in no order, 1.4 n for the largest k, three quarters of n: the list has room.  A row of 128k tokens
+// that wants 50 lists 53.
+struct Groups {
+  int each, n;                     // chunks of a group, groups
+  __device__ __forceinline__ Groups(int n_parts, int vocab) {
+    each = (n_parts * kChunks + kMostGroups - 1) / kMostGroups;
+    n = vocab < 8 ? 0 : (n_parts * kChunks + each - 1) / each;      // (the list is made from eight tokens at a time)
+  }
+  __device__ __forceinline__ bool serve(int top_k) const { return top_k > 0 && 4 * (int64_t)top_k <= 3 * (int64_t)n; }
+  // of this thread's group, -infinity for what is none
+  __device__ __forceinline__ float top(const float* tops, int n_parts) const {
+    float most = -INFINITY;
+    if ((int)threadIdx.x < n)
+      for (int i = threadIdx.x * each; i < min(((int)threadIdx.x + 1) * each, n_parts * kChunks); ++i) most = fmaxf(most, tops[i]);
+    return most;
+  }
+};
 
 template <typename T>
 __global__ __launch_bounds__(kThreads, 8) void bins_kernel(SampleCall c, Space space, int bits) {
@@ -518,9 +592,19 @@ __global__ __launch_bounds__(kThreads, 8) void bins_kernel(SampleCall c, Space s
   const T* row = static_cast<const T*>(c.logits) + n * c.stride;
   const Settings s = settings_of(c, n);
   if (!s.cut()) return;
+  const Part* parts = space.parts + (int64_t)blockIdx.y * space.n_parts;
+  const Groups groups(space.n_parts, c.vocab);
+  if (groups.serve(s.top_k)) {
+    const float most = groups.top(space.tops + (int64_t)blockIdx.y * space.n_parts * kChunks, space.n_parts);
+    // (of tokens masked nearly everywhere there are too few groups to rank)
+    if (__syncthreads_count(most != -INFINITY) >= s.top_k) {
+      if (blockIdx.x == 0 && threadIdx.x == 0) space.rows[blockIdx.y].cut.by_tops = 1;
+      return;
+    }
+  }
   const PartTokens<T, kThreads> part(row, blockIdx.x, c.vocab);      // (asked for before anything is waited for)
   load_roots(roots, bits);
-  const RowParts all(space.parts + (int64_t)blockIdx.y * space.n_parts, space.n_parts);
+  const RowParts all(parts, space.n_parts);
   if (!all.drawn) return;
   const float top = all.top;
   for (int b = threadIdx.x; b < kBins; b += kThreads) {
@@ -564,10 +648,10 @@ __global__ __launch_bounds__(kThreads, 8) void collect_kernel(SampleCall c, Spac
   const T* row = static_cast<const T*>(c.logits) + n * c.stride;
   Part* parts = space.parts + (int64_t)blockIdx.y * space.n_parts;
   const Settings s = settings_of(c, n);
-  if (!s.filter()) return;
+  RowSpace& r = space.rows[blockIdx.y];
+  if (!s.filter() || (s.cut() && s.top_k > 0 && r.cut.by_tops)) return;
   // (all of it asked for before anything is waited for)
   const PartTokens<T, kThreads> part(row, blockIdx.x, c.vocab);
-  RowSpace& r = space.rows[blockIdx.y];
   constexpr int kEach = kBins / kThreads;
   const bool by_mass = s.top_k == 0;
   unsigned long long v[kEach];
@@ -579,7 +663,7 @@ __global__ __launch_bounds__(kThreads, 8) void collect_kernel(SampleCall c, Spac
   const float top = all.top;
   int first = kBins, last = kBins;                  // bins [first, last] are listed
   if (s.cut()) {
-    const double target = by_mass ? s.top_p * all.total(inverse(s.t)) : 0.;
+    const unsigned long long target = by_mass ? whole_share(s.top_p, all.total(inverse(s.t))) : 0;
     unsigned long long run = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) run += v[i];
@@ -594,7 +678,7 @@ __global__ __launch_bounds__(kThreads, 8) void collect_kernel(SampleCall c, Spac
     run -= own;
     for (int w = 0; w < wave; ++w) run += sums[w];
     // the bin that reaches the target (the first with any weight, where the target is 0)
-    auto reached = [&](unsigned long long x) { return by_mass ? x > 0 && (double)x >= target : x >= (unsigned long long)s.top_k; };
+    auto reached = [&](unsigned long long x) { return by_mass ? x > 0 && x >= target : x >= (unsigned long long)s.top_k; };
     if (!reached(run)) {
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
@@ -632,7 +716,10 @@ __global__ __launch_bounds__(kThreads, 8) void collect_kernel(SampleCall c, Spac
   });
   sum = sum_over_wave(sum);
   __syncthreads();
-  if (lane == 0) sums[wave] = sum;
+  if (lane == 0) {
+    sums[wave] = sum;
+    space.sums[((int64_t)blockIdx.y * space.n_parts + blockIdx.x) * kSums + wave] = sum;
+  }
   if (threadIdx.x == 0 && here > 0) at_list = atomicAdd(&r.cut.listed, here);
   __syncthreads();
   for (int j = threadIdx.x; j < here && at_list + j < kList; j += kThreads) r.list[at_list + j] = list[j];
@@ -715,6 +802,78 @@ __global__ __launch_bounds__(kFewThreads) void draw_plain_kernel(SampleCall c, S
   }
 }
 
+// The list of a row that is cut by top_k, made from the chunks that reach the top_k-th largest of the groups' largest logits; its length, which may be
+// more than kList (then there is no list).
+template <typename T>
+__device__ int list_by_tops(Smem& sm, unsigned long long* list, const T* row, int vocab, const float* tops, int n_parts, const Groups& groups, float most, int top_k) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n = groups.n;
+  uint32_t *keys = sm.count, *chunks = keys + kMostGroups;
+  if ((int)threadIdx.x < kMostGroups) keys[threadIdx.x] = (int)threadIdx.x < n ? key_of(most) : 0;
+  if (threadIdx.x == 0) {
+    sm.found_count = 0;
+    sm.index = 0;
+  }
+  __syncthreads();
+  // the largest key that top_k of them reach, two bits at a time: one wavefront (comparing all with all took ten times as long)
+  if (wave == 0) {
+    uint32_t key[kMostGroups / 64], reached = 0;
+#pragma unroll
+    for (int i = 0; i < kMostGroups / 64; ++i) key[i] = keys[64 * i + lane];
+#pragma unroll 1
+    for (int shift = 30; shift >= 0; shift -= 2) {
+      int count[4] = {};
+#pragma unroll
+      for (int i = 0; i < kMostGroups / 64; ++i)
+#pragma unroll
+        for (int d = 1; d < 4; ++d) count[d] += __popcll(__ballot(key[i] >= (reached | (uint32_t)d << shift)));
+      reached |= (uint32_t)((count[1] >= top_k) + (count[2] >= top_k) + (count[3] >= top_k)) << shift;
+    }
+    if (lane == 0) sm.found = reached;
+  }
+  __syncthreads();
+  const uint32_t bound = sm.found;
+  for (int i = threadIdx.x; i < n_parts * kChunks; i += kThreads)
+    if (key_of(tops[i]) >= bound) {
+      const uint32_t at = atomicAdd(&sm.found_count, 1u);
+      if (at < kList) chunks[at] = i;
+    }
+  __syncthreads();
+  const int hit = sm.found_count;
+  if (hit > kList) return hit;
+  constexpr int kAtOnce = 2, kHere = 64 / (kPart / kChunks / 8);      // pieces of a lane asked for together; chunks of a wavefront's piece
+  for (int c = wave * kAtOnce * kHere; c < hit; c += kWaves * kAtOnce * kHere) {
+    // (the last lanes of a row read its last eight tokens and take their own of them: no branches, the loads go out together)
+    float x[kAtOnce][8];
+    int at[kAtOnce], first[kAtOnce];
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) {
+      const int chunk = c + q * kHere + lane / (64 / kHere);
+      at[q] = chunk < hit ? (int)chunks[chunk] * (kPart / kChunks) + lane % (64 / kHere) * 8 : vocab;
+      first[q] = min(at[q], vocab - 8);
+      widen(piece_at<false>(row + first[q]), x[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < kAtOnce; ++q) {
+      uint32_t reach = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) reach |= (uint32_t)(first[q] + i >= at[q] && key_of(x[q][i]) >= bound) << i;
+      if (reach == 0) continue;
+      int slot = atomicAdd(&sm.index, __popc(reach));
+      for (; reach; reach &= reach - 1, ++slot) {
+        const int which = __builtin_ctz(reach);
+        float v = x[q][0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) v = which == i ? x[q][i] : v;
+        if (slot < kList) list[slot] = (unsigned long long)~key_of(v) << 32 | (uint32_t)(first[q] + which);
+      }
+    }
+  }
+  __syncthreads();
+  const int listed = sm.index;
+  __syncthreads();
+  return listed;
+}
+
 template <typename T>
 __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space space, int bits) {
   __shared__ Smem sm;
@@ -723,6 +882,7 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
   const T* row = static_cast<const T*>(c.logits) + n * c.stride;
   const Part* parts = space.parts + (int64_t)blockIdx.x * space.n_parts;
   RowSpace& space_of_row = space.rows[blockIdx.x];
+  const float* tops = space.tops + (int64_t)blockIdx.x * space.n_parts * kChunks;
   Row r;
   r.how = settings_of(c, n);
   r.key = 0;
@@ -737,6 +897,8 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
 #pragma unroll
     for (int q = 0; q < kList / kThreads; ++q) listed_here[q] = space_of_row.list[q * kThreads + threadIdx.x];
   }
+  const Groups groups(space.n_parts, c.vocab);
+  const float most = s.cut() && groups.serve(s.top_k) ? groups.top(tops, space.n_parts) : -INFINITY;
   const RowParts row_parts(parts, space.n_parts);
   r.top = row_parts.top;
   if (!row_parts.drawn) {                               // nothing to draw from
@@ -782,11 +944,17 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
   bool listed = true;
   __syncthreads();
   if (s.cut()) {
+    unsigned long long* order = sm.mass;                   // (2048 of each)
+    if (cut_of_row.by_tops && s.top_k > 0) {
+      cut_of_row.listed = list_by_tops(sm, order, row, c.vocab, tops, space.n_parts, groups, most, s.top_k);
+      cut_of_row.before = 0;
+#pragma unroll
+      for (int q = 0; q < kList / kThreads; ++q) listed_here[q] = order[q * kThreads + threadIdx.x];
+    }
     listed = cut_of_row.listed <= kList;
     if (listed && cut_of_row.listed > 0) {
       // every token of the list by how many, and what weight, stand in front of it
       const int count = cut_of_row.listed;
-      unsigned long long* order = sm.mass;                 // (2048 of each)
       __shared__ unsigned long long weights[kList];
 #pragma unroll
       for (int q = 0; q < kList / kThreads; ++q) {
@@ -836,7 +1004,7 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
         before[q] = in_front_of[j];
         if (s.top_k > 0 && rank[q] < (uint32_t)s.top_k) total += weights[j];
       }
-      double target = INFINITY;
+      unsigned long long target = ~0ull;
       if (s.top_p < 1.) {
         if (s.top_k > 0) {
           total = sum_over_wave(total);
@@ -844,9 +1012,9 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
           __syncthreads();
           total = 0;
           for (int w = 0; w < kWaves; ++w) total += sm.sums[w];
-          target = s.top_p * (double)total;
+          target = whole_share(s.top_p, (double)total);
         } else {
-          target = s.top_p * row_parts.total(inv);
+          target = whole_share(s.top_p, row_parts.total(inv));
         }
       }
       if (threadIdx.x == 0) sm.found = 0;
@@ -857,7 +1025,7 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
       for (int q = 0; q < kList / kThreads; ++q) {
         if (rank[q] == 0xffffffffu || (s.top_k > 0 && rank[q] >= (uint32_t)s.top_k)) continue;
         const unsigned long long in_front = cut_of_row.before + before[q];
-        if (in_front == 0 ? rank[q] != 0 : !((double)in_front < target)) continue;
+        if (in_front == 0 ? rank[q] != 0 : in_front >= target) continue;
         keep = max(keep, (int)rank[q]);
       }
       if (keep >= 0) atomicMax(&sm.found, (uint32_t)keep);
@@ -872,6 +1040,45 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
       r.key = sm.low[0];
       r.last = sm.index;
       __syncthreads();
+      if (s.top_k > 0) {
+        // all that is kept is in the list: the weight of the kept tokens with lower numbers in front of each
+        unsigned long long own[kList / kThreads], sum = 0;
+#pragma unroll
+        for (int q = 0; q < kList / kThreads; ++q) {
+          const int j = q * kThreads + threadIdx.x;
+          own[q] = 0;
+          if (j >= count) continue;
+          const uint32_t key = ~(uint32_t)(mine[q] >> 32);
+          own[q] = kept_weight(__uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key), (int)(uint32_t)mine[q]);
+          weights[j] = own[q];
+          in_front_of[j] = 0;
+          sum += own[q];
+        }
+        sum = sum_over_wave(sum);
+        if (lane == 0) sm.sums[wave] = sum;
+        __syncthreads();
+        sum = 0;
+        for (int w = 0; w < kWaves; ++w) sum += sm.sums[w];
+        const unsigned long long target = __umul64hi(sum, u64);
+        for (int j = threadIdx.x % each; j < count; j += each) {
+          const uint32_t number = (uint32_t)order[j];
+          unsigned long long less = 0;
+#pragma unroll 8
+          for (int i = from; i < to; ++i) less += (uint32_t)order[i] < number ? weights[i] : 0ull;
+          atomicAdd(&in_front_of[j], less);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < kList / kThreads; ++q) {
+          const int j = q * kThreads + threadIdx.x;
+          if (j >= count || own[q] == 0 || target < in_front_of[j] || target >= in_front_of[j] + own[q]) continue;
+          const uint32_t key = ~(uint32_t)(mine[q] >> 32);
+          const float x = __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
+          c.tokens[n] = (int)(uint32_t)mine[q];
+          if (c.logprobs) c.logprobs[n] = (float)(((double)x - (double)r.top) * inv - log((double)sum / unit));
+        }
+        return;
+      }
     } else if (!listed) {
       auto total_of = [&]() {
         unsigned long long sum = 0;
@@ -888,9 +1095,7 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
       if (s.top_k > 0) cut(sm, row, c.vocab, r, all, false, s.top_k);
       if (s.top_p < 1.) {
         const unsigned long long total = total_of();
-        // sums in front of a kept token are below p * total: whole numbers below its ceiling
-        const unsigned long long p64 = (unsigned long long)(s.top_p * 18446744073709551616.);
-        const unsigned long long target = __umul64hi(total, p64) + (total * p64 != 0);
+        const unsigned long long share = whole_share(s.top_p, (double)total), target = share < total ? share : total;
         cut(sm, row, c.vocab, r, all, true, target > 0 ? target : 1);
       }
     }
@@ -913,6 +1118,9 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
   __syncthreads();
   for (int p = threadIdx.x; p < (space.n_parts + 63) / 64 * 64; p += kThreads) of_part[p] = p < space.n_parts ? parts[p].above : 0;
   __syncthreads();
+  unsigned long long* of_sum = sm.place.sums;
+  if (threadIdx.x < kSums) of_sum[threadIdx.x] = 0;
+  unsigned long long kept_here[kList / kThreads] = {};
   if (s.cut()) {
 #pragma unroll
     for (int q = 0; q < kList / kThreads; ++q) {
@@ -920,8 +1128,8 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
       if (j >= cut_of_row.listed) continue;
       const unsigned long long e = listed_here[q];
       const uint32_t key = ~(uint32_t)(e >> 32);
-      const unsigned long long w = kept_weight(__uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key), (int)(uint32_t)e);
-      if (w) atomicAdd(&of_part[(uint32_t)e / kPart], w);
+      kept_here[q] = kept_weight(__uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key), (int)(uint32_t)e);
+      if (kept_here[q]) atomicAdd(&of_part[(uint32_t)e / kPart], kept_here[q]);
     }
   }
   __syncthreads();
@@ -947,15 +1155,33 @@ __global__ __launch_bounds__(kThreads) void draw_kernel(SampleCall c, Space spac
     }
     way -= __shfl(upto, 63);
   }
-  const int lo = found * kPart;
-  write(place_of<kThreads>(sm.place, row, lo, min(lo + kPart, c.vocab), way, kept_weight), (double)total);
+  // the same in the part, whose sums the launch in front left, too
+#pragma unroll
+  for (int q = 0; q < kList / kThreads; ++q)
+    if (kept_here[q] && (int)((uint32_t)listed_here[q] / kPart) == found) atomicAdd(&of_sum[(uint32_t)listed_here[q] % kPart / (kPart / kSums)], kept_here[q]);
+  unsigned long long upto = lane < kSums ? space.sums[((int64_t)blockIdx.x * space.n_parts + found) * kSums + lane] : 0;
+  __syncthreads();
+  if (lane < kSums) upto += of_sum[lane];
+  const unsigned long long own = upto;
+  for (int d = 1; d < kSums; d <<= 1) {
+    const unsigned long long other = __shfl_up(upto, d);
+    if (lane >= d) upto += other;
+  }
+  const int at = __builtin_ctzll(__ballot(lane < kSums && way < upto) | 1ull << (kSums - 1));
+  way -= __shfl(upto - own, at);
+  const int lo = found * kPart + at * (kPart / kSums);
+  __syncthreads();
+  write(place_of<kThreads>(sm.place, row, lo, min(lo + kPart / kSums, c.vocab), way, kept_weight), (double)total);
 }
 
 Space space_of(const SampleCall& c, int64_t rows) {
   Space s;
   s.n_parts = (c.vocab + kPart - 1) / kPart;                    // (at most kBins: vocab <= 2^24)
   s.rows = static_cast<RowSpace*>(c.workspace);
-  s.parts = reinterpret_cast<Part*>(s.rows + (rows < kRowsAtOnce ? rows : kRowsAtOnce));
+  const int64_t held = rows < kRowsAtOnce ? rows : kRowsAtOnce;
+  s.parts = reinterpret_cast<Part*>(s.rows + held);
+  s.sums = reinterpret_cast<unsigned long long*>(s.parts + held * s.n_parts);
+  s.tops = reinterpret_cast<float*>(s.sums + held * s.n_parts * kSums);
   s.first_row = 0;
   return s;
 }
@@ -988,7 +1214,7 @@ size_t sample_workspace(int rows, int vocab) {
   SampleCall c = {};
   c.vocab = vocab;
   const Space s = space_of(c, rows);
-  return (size_t)(rows < kRowsAtOnce ? rows : kRowsAtOnce) * (sizeof(RowSpace) + (size_t)s.n_parts * sizeof(Part));
+  return (size_t)(rows < kRowsAtOnce ? rows : kRowsAtOnce) * (sizeof(RowSpace) + (size_t)s.n_parts * (sizeof(Part) + kSums * sizeof(unsigned long long) + kChunks * sizeof(float)));
 }
 
 hipError_t launch_sample(const SampleCall& c, int dtype, hipStream_t stream) {

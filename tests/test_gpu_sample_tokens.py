@@ -209,3 +209,36 @@ def test_recorded_calls_draw_by_the_numbers_of_the_replay():
     with torch.cuda.stream(torch.cuda.Stream()):
         other = call(x, u, temperature=0.9, top_k=300, top_p=0.9)
     assert torch.equal(other[0], tokens.cpu())
+
+
+@pytest.mark.parametrize("k", [1, 2, 5, 12, 13, 191, 192, 193, 384, 500, 1000])
+@pytest.mark.parametrize("vocab", [7, 8, 130, 8193, 30000, 131071])
+def test_top_k_of_any_number(vocab, k):
+    """Around the numbers up to which a top_k is found among the largest logits of groups of tokens."""
+    x, u = logits(6, vocab, F32, seed=vocab + k)
+    check(x, u, T=0.9, k=k, p=0.97, m=1e-3)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_top_k_where_most_tokens_are_masked(dtype):
+    """Tokens of a few chunks only, of one chunk, every 500th, fewer than top_k; and many equal ones where the cut falls."""
+    x, u = logits(6, 100003, dtype, seed=11)
+    x[0, 4000:] = -math.inf
+    x[1, :70000] = x[1, 70090:] = -math.inf
+    x[2, torch.arange(100003) % 500 != 3] = -math.inf
+    x[3, 9:] = -math.inf
+    x[4] = (x[4] / 4).round() * 4
+    x[5] = x[5].clamp(max=0.5)
+    for k in (20, 50, 180):
+        check(x, u, k=k)
+        check(x, u, T=1.3, k=k, p=0.8)
+
+
+def test_top_k_of_negative_logits_and_zeros():
+    x, u = logits(4, 20000, F32, seed=12)
+    x[0] = -x[0].abs() - 100
+    x[1, x[1] > 0] = -0.0
+    x[2, x[2] > 0] = 0.0
+    x[3] = 1e-40 * x[3]
+    for k in (3, 64):
+        check(x, u, k=k)
