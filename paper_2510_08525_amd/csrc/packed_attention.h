@@ -370,10 +370,10 @@ __device__ __forceinline__ Ends ends_of(bool valid) {
   const uint32_t lanes = (uint32_t)__ballot(valid);
   return {lanes ? __builtin_ctz(lanes) : -1, lanes ? 31 - __builtin_clz(lanes) : -1};
 }
-// False: no column of the block is of a sequence.
+// False: no column of the block, 32 for each of WAVES wavefronts (the workgroup may have them several times over), is of a sequence.
 template <int WAVES>
 __device__ __forceinline__ bool set_columns(const PackedCall& c, const Offsets& offsets, const ColumnBlock& b, Columns& x) {
-  const uint32_t from = (uint32_t)b.block * (WAVES * 32), column = from + (threadIdx.x >> 6) * 32 + (threadIdx.x & 31);
+  const uint32_t from = (uint32_t)b.block * (WAVES * 32), column = from + (threadIdx.x >> 6) % WAVES * 32 + (threadIdx.x & 31);
   x.pos = (int)c.by_group.of(column);
   x.head = b.head * c.group + (int)(column - (uint32_t)x.pos * c.group);
   x.full = b.full;
