@@ -242,3 +242,14 @@ def test_top_k_of_negative_logits_and_zeros():
     x[3] = 1e-40 * x[3]
     for k in (3, 64):
         check(x, u, k=k)
+
+
+@pytest.mark.parametrize("equal", [150, 300, 700, 2000, 2100])
+def test_top_k_among_equal_logits(equal):
+    """Lists of the most likely tokens that are far longer than top_k."""
+    x, u = logits(8, 40000, F32, seed=13)
+    x[:, torch.randperm(40000, generator=torch.Generator().manual_seed(equal))[:equal]] = 20.0
+    x[::2, 777] = 21.0
+    for k in (40, 170, 600):
+        check(x, u, k=k)
+        check(x, u, k=k, p=0.73, T=0.5, m=0.01)
