@@ -553,7 +553,7 @@ typedef struct {
 /* out = softmax(softmax_scale * q . K^T) V over the admitted keys, and lse = log sum exp of their scaled scores.
  *   q, out : RLKV_BF16, [tokens][n_q_heads];  k, v : [tokens][n_kv_heads]; token strides at most 2^24
  *   lse    : device, fp32, [n_q_heads][tokens], or NULL
- * Scores, softmax and sums are fp32; the weights enter their product with V in bf16.  What is not admitted does not count, whatever it holds
+ * out is none of the inputs.  Scores, softmax and sums are fp32; the weights enter their product with V in bf16.  What is not admitted does not count, whatever it holds
  * (infinities and NaN among it).  Equal calls give equal bits. */
 rlkv_status_t rlkv_packed_attention(const rlkv_packed_t* shape /* host */, const rlkv_heads_t* q /* host */,
                                     const rlkv_heads_t* k /* host */, const rlkv_heads_t* v /* host */,
@@ -564,7 +564,8 @@ rlkv_status_t rlkv_packed_attention(const rlkv_packed_t* shape /* host */, const
  *     grad_q[i] = softmax_scale * sum_j z[i][j] k[j]    grad_k[j] = softmax_scale * sum_i z[i][j] q[i]    grad_v[j] = sum_i w[i][j] grad_out[i]
  * grad_k and grad_v are summed over the group's query heads.  All tensors RLKV_BF16; w and z enter their products in bf16, sums are fp32, in a fixed
  * order: equal calls give equal bits.  The outputs are none of the inputs.
- *   workspace : device, 16-byte aligned, rlkv_packed_attention_grad_workspace bytes; its contents do not matter.  Calls that may overlap in time
+ *   workspace : device, 16-byte aligned, rlkv_packed_attention_grad_workspace bytes (some 128 MiB, for few tokens less, and 4 a token and query head);
+ *               its contents do not matter.  Calls that may overlap in time
  *               need one each (graphs that are replayed at the same time among them). */
 size_t rlkv_packed_attention_grad_workspace(int32_t tokens, int32_t n_q_heads, int32_t n_kv_heads);
 rlkv_status_t rlkv_packed_attention_grad(const rlkv_packed_t* shape /* host */, const rlkv_heads_t* q /* host */,

@@ -429,8 +429,8 @@ static GradSpace grad_space(int64_t tokens, int64_t n_q_heads, int64_t n_kv_head
   s.delta = 0;
   s.plan = align((size_t)(tokens * n_q_heads) * sizeof(float));
   s.slots = s.plan + align(sizeof(PackedPlan) + (size_t)(pairs + kMostParts) * sizeof(PlanItem) + (size_t)pairs * sizeof(PlanMerge));
-  // (parts have kLeastSteps steps at least, of which a pair has one for each head and 64 positions at most)
-  const int64_t steps = pairs * ((tokens + kStep - 1) / kStep) * group, parts = steps / kLeastSteps;
+  // (parts have kLeastSteps steps at least, of which a pair has one for each head and 64 positions at most; one of fewer than two parts' has no slot)
+  const int64_t of_pair = (tokens + kStep - 1) / kStep * group, steps = pairs * of_pair, parts = of_pair < 2 * kLeastSteps ? 0 : steps / kLeastSteps;
   s.bytes = s.slots + (size_t)(parts < kMostParts ? parts : kMostParts) * kSlotFloats * sizeof(float);
   return s;
 }

@@ -186,7 +186,7 @@ struct FirstBin {
     return z < (float)(kBins - 1) ? (int)z : kBins - 1;       // (NaN, of a masked logit at an infinite temperature: the last)
   }
 };
-__device__ __forceinline__ FirstBin first_bin(float top, const Settings& s) { return {top, (float)inverse(s.t) * kBinsPerUnit}; }
+__device__ __forceinline__ FirstBin first_bin(float top, const Settings& s) { return {top, fminf((float)inverse(s.t) * kBinsPerUnit, 3e38f)}; }      // (no infinity: 0 times it)
 
 // ---- the workspace ----
 struct Part {

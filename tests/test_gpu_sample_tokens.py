@@ -253,3 +253,11 @@ def test_top_k_among_equal_logits(equal):
     for k in (40, 170, 600):
         check(x, u, k=k)
         check(x, u, k=k, p=0.73, T=0.5, m=0.01)
+
+
+def test_temperatures_next_to_nothing():
+    """As good as greedy, without infinities of what is divided by them."""
+    x, u = logits(6, 30000, F32, seed=14)
+    for T in (1e-30, 1e-45, 5e-324):
+        for how in (dict(), dict(k=300), dict(k=20), dict(p=0.9), dict(m=0.5)):
+            check(x, u, T=T, **how)
