@@ -302,6 +302,16 @@ constexpr int kKeys = kStageRows;
 constexpr int kPackedWaves = 8;      // (with four, two workgroups a compute unit, every tile is fetched twice as often: 16384 tokens 3265 us against 2006)
 inline uint32_t column_blocks(const PackedCall& c, int waves) { return (uint32_t)(((int64_t)c.tokens * c.group + 32 * waves - 1) / (32 * waves)); }
 
+// Whether a workgroup has half as many columns and each half of its wavefronts every second tile of their keys, whose sums are added up at the end: where
+// that fits the card at once, and up to twice that where sequences are long, so that the longest workgroup is what the launch lasts.  Forward, us, 28 / 4
+// heads, without and with: one sequence of 70 tokens 10.2 and 8.8, 333 16.6 and 13.2, 1150 35.1 and 26.6, 2100 57.3 and 48.5, eight of 130 13.3 and 11.8, two of
+// 1000 33.2 and 31.5; but three of 700 27.0 and 33.7, sixteen of 100 14.2 and 18.0, one of 3000 84 and 92.  The gradient's queries:
+// 333 23.1 and 17.7, 1200 52.2 and 37.2, 2300 94 and 74, six of 300 23.9 and 31.4.
+inline bool keys_divided(const PackedCall& c) {
+  const int64_t workgroups = (int64_t)column_blocks(c, kPackedWaves) * c.n_kv_heads;
+  return workgroups <= 128 || (workgroups <= 256 && c.tokens >= (int64_t)c.n_seqs * 1000);
+}
+
 // Block and head of the launch's workgroup `index`: of all full heads the last blocks first, then of the local ones, so that the long workgroups are
 // handed out first; and neighbours in the launch, which the hardware deals to the 8 XCDs in turn, are of different heads: a head's keys are then read by
 // few of the L2s.

@@ -21,10 +21,7 @@ namespace {
 // fp32 sums and bf16 weights nothing, and the accumulators stay as they are.
 constexpr float kSlack = 8.f;
 
-// SPLIT 2: for launches of no more workgroups than there are compute units, which end with the longest one.  A workgroup has half as many columns, and of the
-// tiles every second one for each half of its wavefronts, whose sums are added up at the end.  One sequence of 28 / 4 heads, us without and with: 70
-// tokens 10.2 and 8.8, 333 16.6 and 13.2, 1150 35.1 and 26.6, 2300 62.8 and 55.5 (252 workgroups); beyond, tiles are fetched
-// twice as often for nothing: 3000 tokens 84 and 92.
+// SPLIT 2: the keys are divided between the halves of the workgroup (keys_divided).
 template <int WAVES, int SPLIT>
 __global__ __launch_bounds__(64 * WAVES) void packed_attention_kernel(PackedCall c, uint32_t blocks) {
   constexpr int kColumnWaves = WAVES / SPLIT;
@@ -167,7 +164,7 @@ __global__ __launch_bounds__(64 * WAVES) void packed_attention_kernel(PackedCall
 
 hipError_t launch_packed_attention(const PackedCall& call, hipStream_t stream) {
   const uint32_t blocks = column_blocks(call, kPackedWaves), few = column_blocks(call, kPackedWaves / 2);
-  if (blocks * (uint32_t)call.n_kv_heads <= 256)
+  if (keys_divided(call))
     packed_attention_kernel<kPackedWaves, 2><<<few * (uint32_t)call.n_kv_heads, 64 * kPackedWaves, 0, stream>>>(call, few);
   else
     packed_attention_kernel<kPackedWaves, 1><<<blocks * (uint32_t)call.n_kv_heads, 64 * kPackedWaves, 0, stream>>>(call, blocks);

@@ -117,11 +117,13 @@ __device__ void make_plan(const PackedCall& c, PlanSmem& sm) {
 }
 
 // ---- queries ------------------------------------------------------------------------------------------------------------------
-template <int WAVES>
+// SPLIT 2: the keys are divided between the halves of the workgroup (keys_divided).
+template <int WAVES, int SPLIT>
 __global__ __launch_bounds__(64 * WAVES) void packed_grad_q_kernel(PackedCall c, uint32_t blocks) {
-  __shared__ uint4 t0[2][kKeys * 16], t1[2][kKeys * 16];      // keys, values
+  constexpr int kColumnWaves = WAVES / SPLIT;
+  __shared__ uint4 t0[SPLIT][2][kKeys * 16], t1[SPLIT][2][kKeys * 16];      // keys, values
   __shared__ PlanSmem plan;
-  const int half = (threadIdx.x >> 5) & 1;
+  const int half = (threadIdx.x >> 5) & 1, part = SPLIT > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / kColumnWaves : 0;
   if (blockIdx.x == 0) {                                     // (the launch's first workgroup plans the next launch)
     make_plan(c, plan);
     return;
@@ -130,7 +132,7 @@ __global__ __launch_bounds__(64 * WAVES) void packed_grad_q_kernel(PackedCall c,
   const Offsets offsets(c);
   const ColumnBlock block = column_block(c, blockIdx.x - 1, blocks);
   Columns x;
-  if (!set_columns<WAVES>(c, offsets, block, x)) return;
+  if (!set_columns<kColumnWaves>(c, offsets, block, x)) return;
   if (threadIdx.x == 0) lost = 0;
 
   bf16x8 q[8], g[8];
@@ -152,8 +154,12 @@ __global__ __launch_bounds__(64 * WAVES) void packed_grad_q_kernel(PackedCall c,
   const float scale = c.scale * kLog2e;
   auto ask = [&](auto odd, int t) {
     constexpr int kOdd = decltype(odd)::value;
-    stage_rows<kQuads, WAVES>(c.k, x.tile_key(t), block.head, c.tokens, kOdd ? t1[0] : t0[0]);
-    stage_rows<kQuads, WAVES>(c.v, x.tile_key(t), block.head, c.tokens, kOdd ? t1[1] : t0[1]);
+#pragma unroll
+    for (int i = 0; i < SPLIT; ++i) {
+      if (i > 0 && t + i >= x.tiles) break;
+      stage_rows<kQuads, WAVES>(c.k, x.tile_key(t + i), block.head, c.tokens, kOdd ? t1[i][0] : t0[i][0]);
+      stage_rows<kQuads, WAVES>(c.v, x.tile_key(t + i), block.head, c.tokens, kOdd ? t1[i][1] : t0[i][1]);
+    }
   };
 
   // (while the first tile is under way)
@@ -162,7 +168,7 @@ __global__ __launch_bounds__(64 * WAVES) void packed_grad_q_kernel(PackedCall c,
 #pragma unroll
   for (int s = 0; s < 8; ++s) delta += dot_of_units(__builtin_bit_cast(uint4, g[s]), out[s]);
   delta = sum_of_halves(delta);
-  if (x.valid && half == 0) c.delta[stat] = delta;
+  if (x.valid && half == 0 && part == 0) c.delta[stat] = delta;
 
   floatx16 dq[4];
   auto walk = [&](auto careful) {
@@ -172,12 +178,13 @@ __global__ __launch_bounds__(64 * WAVES) void packed_grad_q_kernel(PackedCall c,
     if (kCareful) ask(std::integral_constant<int, 0>{}, 0);
     auto step = [&](auto odd, int t) {
       constexpr int kOdd = decltype(odd)::value;
-      const uint4 *kt = kOdd ? t1[0] : t0[0], *vt = kOdd ? t1[1] : t0[1];
+      const uint4 *kt = kOdd ? t1[part][0] : t0[part][0], *vt = kOdd ? t1[part][1] : t0[part][1];
       tile_arrived();
-      if (t + 1 < x.tiles) ask(std::integral_constant<int, 1 - kOdd>{}, t + 1);
+      if (t + SPLIT < x.tiles) ask(std::integral_constant<int, 1 - kOdd>{}, t + SPLIT);
+      if (part > 0 && t + part >= x.tiles) return;
 #pragma unroll
       for (int b = 0; b < kKeys; b += 32) {
-        const int key = x.tile_key(t) + b;
+        const int key = x.tile_key(t + part) + b;
         if (!x.any_of(key, 32)) continue;
         const bool all = x.all_of(key, 32);
         floatx16 w, z;
@@ -206,14 +213,35 @@ __global__ __launch_bounds__(64 * WAVES) void packed_grad_q_kernel(PackedCall c,
       }
     };
     int t = 0;
-    for (; t + 1 < x.tiles; t += 2) {
+    for (; t + SPLIT < x.tiles; t += 2 * SPLIT) {
       step(std::integral_constant<int, 0>{}, t);
-      step(std::integral_constant<int, 1>{}, t + 1);
+      step(std::integral_constant<int, 1>{}, t + SPLIT);
     }
     if (t < x.tiles) step(std::integral_constant<int, 0>{}, t);
   };
   walk(std::false_type{});
   if (any_of_workgroup(x.valid && zero_or_nan(dq) != 0.f, lost)) walk(std::true_type{});
+  if (SPLIT > 1) {
+    // the second half's sums to the first, in the tiles' place
+    float4* sums = reinterpret_cast<float4*>(t0);
+    const int at = threadIdx.x % (64 * kColumnWaves);
+    __syncthreads();
+    if (part == 1) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        sums[i * 64 * kColumnWaves + at] = make_float4(dq[i >> 2][4 * (i & 3)], dq[i >> 2][4 * (i & 3) + 1], dq[i >> 2][4 * (i & 3) + 2], dq[i >> 2][4 * (i & 3) + 3]);
+    }
+    __syncthreads();
+    if (part == 1) return;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float4 y = sums[i * 64 * kColumnWaves + at];
+      dq[i >> 2][4 * (i & 3)] += y.x;
+      dq[i >> 2][4 * (i & 3) + 1] += y.y;
+      dq[i >> 2][4 * (i & 3) + 2] += y.z;
+      dq[i >> 2][4 * (i & 3) + 3] += y.w;
+    }
+  }
   store_rows(c.grad_q.p + x.row * c.grad_q.token + x.head * c.grad_q.head, dq, c.scale, x.valid);
 }
 
@@ -443,8 +471,9 @@ hipError_t launch_packed_attention_grad(PackedCall call, hipStream_t stream) {
   call.plan = reinterpret_cast<PackedPlan*>(work + space.plan);
   call.slots = reinterpret_cast<float*>(work + space.slots);
   const int64_t pairs = tiles_of(call.tokens) * call.n_kv_heads;
-  const uint32_t blocks = column_blocks(call, kWaves);
-  packed_grad_q_kernel<kWaves><<<blocks * (uint32_t)call.n_kv_heads + 1, kThreads, 0, stream>>>(call, blocks);
+  const uint32_t blocks = column_blocks(call, kWaves), few = column_blocks(call, kWaves / 2);
+  if (keys_divided(call)) packed_grad_q_kernel<kWaves, 2><<<few * (uint32_t)call.n_kv_heads + 1, kThreads, 0, stream>>>(call, few);
+  else packed_grad_q_kernel<kWaves, 1><<<blocks * (uint32_t)call.n_kv_heads + 1, kThreads, 0, stream>>>(call, blocks);
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
   const int64_t parts = (int64_t)(space.bytes - space.slots) / (int64_t)(kSlotFloats * sizeof(float));

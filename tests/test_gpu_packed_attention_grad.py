@@ -189,3 +189,40 @@ def test_recorded_calls_and_a_workspace_of_any_contents():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(grads, want))
+
+
+@pytest.mark.parametrize("lengths", [[1500], [750, 0, 750], [100] * 15])
+def test_sequences_in_the_middle(lengths):
+    """Between 128 and 256 workgroups, where it depends on the lengths whether the queries' keys are divided."""
+    check(lengths, 28, 4, [1, 0, 0, 1], 30, 200, seed=len(lengths))
+
+
+@pytest.mark.parametrize("lengths, mask", [([1], None), ([0, 5, 0, 33, 0], None), ([63, 65, 1], None), ([300, 40, 129], [1, 0, 0, 1])])
+def test_in_a_buffer_of_many_rows(lengths, mask):
+    """More than 256 workgroups: keys are not divided."""
+    check(lengths, 8, 4, mask, 33, 70, first=2, tail=8600, seed=len(lengths))
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("tail", [20, 16800])
+def test_not_finite_rows_that_are_not_admitted(bad, tail):
+    """In either half's tiles, with keys divided and not: gradients of rows that have nothing to do with them are what they are without."""
+    lengths, mask, sink, recent = [200, 150], [0, 0], 4, 30
+    q, k, v, go, offsets = inputs(lengths, 4, 2, tail=tail)
+    out, lse, _, _ = ref.attention(q[:350], k[:350], v[:350], lengths, mask, sink, recent, SCALE)
+    full = lambda t, fill: torch.cat([t, torch.full((tail, *t.shape[1:]), fill, dtype=t.dtype)])      # noqa: E731
+    out, lse = full(out.to(BF), 0.0), torch.cat([lse.float(), torch.zeros(4, tail)], 1)
+    clean = [t[:350].clone() for t in (q, k, v, go)]
+    want, tol = ref.gradient(*clean[:3], out[:350], lse[:, :350], clean[3], lengths, mask, sink, recent, SCALE)
+    v[70], k[70] = bad, bad                                             # (admitted by 70 .. 99 of the first sequence alone)
+    q[350:], k[350:], v[350:], go[350:] = bad, bad, bad, bad
+    got = run(q, k, v, out, lse, go, offsets, mask, sink, recent)
+    rows = torch.ones(350, dtype=torch.bool)
+    rows[70:100] = False                                                # queries that see it
+    ref.near(got[0][:350][rows], want[0][rows], tol[0][rows])
+    keys = torch.ones(350, dtype=torch.bool)
+    keys[:4] = keys[41:100] = False                                     # keys that those queries see
+    for x, y, t in zip(got[1:], want[1:], tol[1:]):
+        ref.near(x[:350][keys], y[keys], t[keys])
+    for x in got:
+        assert (x[350:] == 7).all()

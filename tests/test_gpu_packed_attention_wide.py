@@ -66,3 +66,9 @@ def test_offsets_that_make_no_sense_stay_inside_the_tensors():
     for offsets in ([0, -5, 40], [50, 20, 10], [2 ** 31 - 1, 0, 2 ** 31 - 1], [-(2 ** 31), 2 ** 31 - 1]):
         run(q, k, v, torch.tensor(offsets, dtype=torch.int32), [0, 1], 3, 9, out=whole[70:n + 70])
         assert (whole[:70] == 7).all() and (whole[n + 70:] == 7).all()
+
+
+@pytest.mark.parametrize("lengths", [[1500], [1000, 500], [750, 0, 750], [100] * 15, [1499, 1]])
+def test_sequences_in_the_middle(lengths):
+    """Between 128 and 256 workgroups, where it depends on the lengths whether keys are divided."""
+    check(lengths, 28, 4, [1, 0, 0, 1], 30, 200, seed=len(lengths))
