@@ -15,7 +15,7 @@
 // Of rows with top_k the two in the middle do nothing where a logit that top_k tokens reach is found among the largest ones of each 128 tokens: the
 // last launch makes the list, from the chunks that reach it, and finds the token in the list (48 rows of 128011 in float32, most with a
 // top_k: 45 us, with bins for all of them 57).
-// Many rows are bound by the exponential's instructions (512 rows of 131072 in bf16: 60 us, 54 of them the parts' sums, 2.5 TB/s), few by the launches, each
+// Many rows are bound by the exponential's instructions (512 rows of 131072 in bf16: 56 us, 48 of them the parts' sums, 2.8 TB/s), few by the launches, each
 // a chain of some 2 us accesses to memory with a workgroup's work between them (one row of 131072 in float32 with top_p: 32 us; without filters, two
 // launches, 13).
 // A row whose list would be too long (thousands of like logits at the cut, a top_k of thousands) is cut by its last workgroup alone, in passes over the row.
@@ -115,24 +115,25 @@ __constant__ double kRoots[kRootCount] = {
 
 // The weight of a logit: 2^bits exp((x - ref) / t), rounded to a whole number.
 // With z = 128 log2(e) (x - ref) / t = 128 n + j + r, |r| <= 1/2:  2^n 2^(j / 128) (1 + a r + .. + (a r)^3 / 6), a = ln(2) / 128: the series ends 2.3e-12 of
-// it.  Eighteen instructions, which is what the launch over many rows is bound by.
+// it.  Fourteen instructions, which is what the launch over many rows is bound by.
 struct Weight {
-  const uint64_t* roots;     // in LDS, times 2^bits
-  double ref, c;             // 128 log2(e) / t
-  double lowest;             // -128 (bits + 600): what is below it, or masked (a place of -infinity, or NaN at an infinite temperature), has 2^-600
+  const uint64_t* roots;     // in LDS, times 2^bits; j / 128 less in the exponent, to which k / 128 is added with its fraction
+  double ref, c;             // 128 log2(e) / t, not 0: at an infinite temperature what is masked keeps its distance
+  double lowest;             // of x - ref, where z is -128 (bits + 600): what is below it, or masked (a place of -infinity), has 2^-600
   double least;              // least weight that counts, of 2^bits (min_p)
   __device__ __forceinline__ double real(float x) const {
-    const double z = fmax(((double)x - ref) * c, lowest);
-    const double shifted = z + 6755399441055744.;        // 1.5 * 2^52: the nearest whole number in the low bits
-    const int k = (int)(uint32_t)__double_as_longlong(shifted);
-    const double r = z - (shifted - 6755399441055744.);
+    const double way = fmax((double)x - ref, lowest);
+    const double shifted = __builtin_fma(way, c, 6755399441055744.);        // 1.5 * 2^52: the nearest whole number in the low bits
+    const uint32_t k = (uint32_t)__double_as_longlong(shifted);
+    const double r = __builtin_fma(way, c, -(shifted - 6755399441055744.));
     constexpr double a = 0.69314718055994530942 / kRootCount;
     double p = __builtin_fma(r, a * a * a / 6, a * a / 2);
     p = __builtin_fma(r, p, a);
     p = __builtin_fma(r, p, 1.);
-    const uint64_t root = roots[k & (kRootCount - 1)];
-    const uint32_t high = (uint32_t)(root >> 32) + ((uint32_t)(k & ~(kRootCount - 1)) << 13);      // (k / 128 into the exponent)
-    return __longlong_as_double((long long)((uint64_t)high << 32 | (uint32_t)root)) * p;
+    typedef uint32_t words __attribute__((ext_vector_type(2)));
+    words root = __builtin_bit_cast(words, roots[k & (kRootCount - 1)]);
+    root.y += k << 13;
+    return __builtin_bit_cast(double, root) * p;
   }
   __device__ __forceinline__ unsigned long long rounded(double w) const {       // (by adding 2^52)
     return (unsigned long long)__double_as_longlong(w + 4503599627370496.) - 0x4330000000000000ull;
@@ -175,7 +176,8 @@ __device__ __forceinline__ Settings settings_of(const SampleCall& c, int64_t n) 
 // (1 / t is at most 1e300: a way of 0 stays 0)
 __device__ __forceinline__ double inverse(double t) { return t > 1e-300 ? 1. / t : 1e300; }
 __device__ __forceinline__ Weight weight_of(const Settings& s, const uint64_t* roots, double ref, int bits, double least) {
-  return {roots, ref, inverse(s.t) * (kRootCount * 1.4426950408889634074), -1. * kRootCount * (bits + 600), least};
+  const double c = fmax(inverse(s.t), 1e-250) * (kRootCount * 1.4426950408889634074);
+  return {roots, ref, c, -1. * kRootCount * (bits + 600) / c, least};
 }
 
 // Steps down from the largest logit; not decreasing as x falls.
@@ -437,7 +439,7 @@ __device__ __forceinline__ void cut(Smem& sm, const T* row, int vocab, Row& r, c
 
 // ---- the launches ------------------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void load_roots(uint64_t* roots, int bits) {
-  if (threadIdx.x < kRootCount) roots[threadIdx.x] = (uint64_t)__double_as_longlong(kRoots[threadIdx.x]) + ((uint64_t)bits << 52);
+  if (threadIdx.x < kRootCount) roots[threadIdx.x] = (uint64_t)__double_as_longlong(kRoots[threadIdx.x]) + ((uint64_t)bits << 52) - ((uint64_t)threadIdx.x << 45);
 }
 // What a row's parts (a few dozen) come to, in every wavefront that asks: lane l reads the parts l, l + 64, ..
 struct RowParts {
