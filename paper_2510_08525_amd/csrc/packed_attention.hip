@@ -131,20 +131,22 @@ __global__ __launch_bounds__(64 * WAVES) void packed_attention_kernel(PackedCall
   if (SPLIT > 1) {
     // the second half's sums to the first: by lanes, piece behind piece, in the tiles' place
     float4* sums = reinterpret_cast<float4*>(t0);
-    float2* stats = reinterpret_cast<float2*>(t1);
+    float4* stats = reinterpret_cast<float4*>(t1);
     const int at = threadIdx.x % (64 * kColumnWaves);
     __syncthreads();
     if (part == 1) {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         sums[i * 64 * kColumnWaves + at] = make_float4(o[i >> 2][4 * (i & 3)], o[i >> 2][4 * (i & 3) + 1], o[i >> 2][4 * (i & 3) + 2], o[i >> 2][4 * (i & 3) + 3]);
-      stats[at] = make_float2(m, l);
+      stats[at] = make_float4(m, l, ref, 0.f);
     }
     __syncthreads();
     if (part == 1) return;
-    const float2 other = stats[at];
-    const float most = fmaxf(m, other.x), next = most == -INFINITY ? 0.f : most * scale;
-    const float mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m * scale - next), its = other.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other.x * scale - next);
+    // (from reference to reference as the weights have them: the products of m would be taken unrounded into the differences, and from scores of some
+    // ten thousand on the halves' weights would not fit each other)
+    const float4 other = stats[at];
+    const float most = fmaxf(m, other.x), next = m < other.x ? other.z : ref;
+    const float mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - next), its = other.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other.z - next);
     m = most;
     l = l * mine + other.y * its;
 #pragma unroll
