@@ -20,6 +20,10 @@ namespace {
 // The reference of the weights moves only when a score is more than this above it (in powers of two): until then weights are above 1, which costs
 // fp32 sums and bf16 weights nothing, and the accumulators stay as they are.
 constexpr float kSlack = 8.f;
+// A reference is a product rounded to fp32, while the products that it is taken from are not (one rounding for the difference): the largest weight is off 1
+// by up to half a step of the reference, 2^2 from here on, 2^64 at 2^31, and fits no float beyond.  From here on the walk is taken again with the
+// products' differences taken before the scale (careful), which the rounding of neither product enters; one instruction more a weight.
+constexpr float kLargeReference = 67108864.f;          // 2^26
 
 // SPLIT 2: the keys are divided between the halves of the workgroup (keys_divided).
 template <int WAVES, int SPLIT>
@@ -55,7 +59,7 @@ __global__ __launch_bounds__(64 * WAVES) void packed_attention_kernel(PackedCall
   floatx16 o[4];
   float m, l, ref;
   // A weight of 0 does not keep an infinity or a NaN of a masked value out of the products.  Where an output is not finite, the walk is taken again
-  // with the products of masked tiles one by one (careful).
+  // with the products of masked tiles one by one (careful), and where references are large.
   auto walk = [&](auto careful) {
     constexpr bool kCareful = decltype(careful)::value;
     m = -INFINITY;
@@ -90,18 +94,19 @@ __global__ __launch_bounds__(64 * WAVES) void packed_attention_kernel(PackedCall
       if (__any(mx > m + slack)) {
         mx = fmaxf(max_of_halves(mx), m);
         const float next = mx == -INFINITY ? 0.f : mx * scale;
-        const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - next);
+        const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(kCareful ? (m - mx) * scale : ref - next);
         m = mx;
         ref = next;
         l *= alpha;
 #pragma unroll
         for (int b = 0; b < 4; ++b) o[b] *= alpha;
       }
+      const float from = m == -INFINITY ? 0.f : m;
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          w[b][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(w[b][r], scale, -ref));
+          w[b][r] = __builtin_amdgcn_exp2f(kCareful ? (w[b][r] - from) * scale : __builtin_fmaf(w[b][r], scale, -ref));
           l += w[b][r];
         }
       if (kCareful && !all) {
@@ -125,7 +130,8 @@ __global__ __launch_bounds__(64 * WAVES) void packed_attention_kernel(PackedCall
     if (t < x.tiles) step(std::integral_constant<int, 0>{}, t);
   };
   walk(std::false_type{});
-  if (any_of_workgroup(x.valid && zero_or_nan(o) != 0.f, lost)) walk(std::true_type{});
+  const bool again = any_of_workgroup(x.valid && (zero_or_nan(o) + l * 0.f != 0.f || fabsf(ref) >= kLargeReference), lost);
+  if (again) walk(std::true_type{});
 
   l = sum_of_halves(l);
   if (SPLIT > 1) {
@@ -146,7 +152,8 @@ __global__ __launch_bounds__(64 * WAVES) void packed_attention_kernel(PackedCall
     // ten thousand on the halves' weights would not fit each other)
     const float4 other = stats[at];
     const float most = fmaxf(m, other.x), next = m < other.x ? other.z : ref;
-    const float mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - next), its = other.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other.z - next);
+    const float mine = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(again ? (m - most) * scale : ref - next);
+    const float its = other.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(again ? (other.x - most) * scale : other.z - next);
     m = most;
     l = l * mine + other.y * its;
 #pragma unroll
