@@ -77,6 +77,16 @@ def token_logprobs_grad(logits, tokens, lse, grad_logprobs, grad_logits, *, scal
     return grad_logits
 
 
+def _mask_bytes(mask):
+    """(By its entries: of a number, and of a tensor with one entry, `bytes` would take the value for a length.)"""
+    if mask is None:
+        return None
+    try:
+        return bytes(iter(mask))
+    except TypeError:
+        raise ValueError("mask: need a 0 or 1 for each KV head") from None
+
+
 def packed_attention(q, k, v, offsets, out, scale: float, *, lse=None, mask=None, sink: int = 0, recent: int = 0):
     """Attention over sequences packed one behind the other, q and out [tokens, q heads, 128], k and v [tokens, kv heads, 128] in bfloat16
     (heads and tokens at any stride, rows at multiples of 16 bytes): out = softmax(scale * q . k) v over the keys up to the query's own, and
@@ -84,7 +94,7 @@ def packed_attention(q, k, v, offsets, out, scale: float, *, lse=None, mask=None
 
     offsets: int32 [sequences + 1] on the device, where the sequences begin and the last one ends; rows of none are not written.
     mask: one 0 / 1 for each KV head, 1 = full, 0 = local (the first `sink` positions of the sequence and the last `recent`); None: all full."""
-    status = _calls.packed_attention(q, k, v, offsets, out, lse, scale, None if mask is None else bytes(mask), sink, recent)
+    status = _calls.packed_attention(q, k, v, offsets, out, lse, scale, _mask_bytes(mask), sink, recent)
     if status:
         _check(status, "rlkv_packed_attention")
     return out
@@ -100,8 +110,7 @@ def packed_attention_grad(q, k, v, offsets, out, lse, grad_out, grad_q, grad_k, 
         tokens, q_heads, kv_heads = (*q.shape[:2], k.shape[1]) if q.dim() == 3 and k.dim() == 3 else (0, 1, 1)
         need = load_library().rlkv_packed_attention_grad_workspace(tokens, q_heads, kv_heads)
         workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=q.device)
-    status = _calls.packed_attention_grad(q, k, v, offsets, out, lse, grad_out, grad_q, grad_k, grad_v, scale,
-                                          None if mask is None else bytes(mask), sink, recent, workspace)
+    status = _calls.packed_attention_grad(q, k, v, offsets, out, lse, grad_out, grad_q, grad_k, grad_v, scale, _mask_bytes(mask), sink, recent, workspace)
     if status:
         _check(status, "rlkv_packed_attention_grad")
     return grad_q, grad_k, grad_v
