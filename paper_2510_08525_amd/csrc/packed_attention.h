@@ -98,14 +98,15 @@ struct Offsets {
       if (at <= 0 || at > n_seqs) return {-1, -1};
       return clamped(__builtin_amdgcn_readlane(lanes, at - 1), __builtin_amdgcn_readlane(lanes, at), position, tokens);
     }
-    int from = 0, to = n_seqs + 1;               // the first offset behind the position is in [from, to]; 64 are looked at at a time
-    while (to - from > 0) {
-      const int each = (to - from + 63) / 64, at = from + (lane + 1) * each - 1;
-      const int below = __popcll(__ballot(at < to && p[at < to ? at : from] <= position));      // (not decreasing: the first ones)
+    // the first offset behind the position is in [from, to]; 64 are looked at at a time (unsigned: places past the last one may be beyond 2^31)
+    uint32_t from = 0, to = (uint32_t)n_seqs + 1;
+    while (from < to) {
+      const uint32_t each = (to - from + 63) / 64, at = from + (lane + 1) * each - 1;
+      const uint32_t below = __popcll(__ballot(at < to && p[at < to ? at : from] <= position));      // (not decreasing: the first ones)
       from += below * each;
       to = min(to, from + each - 1);
     }
-    if (from <= 0 || from > n_seqs) return {-1, -1};
+    if (from == 0 || from > (uint32_t)n_seqs) return {-1, -1};
     return clamped(p[from - 1], p[from], position, tokens);
   }
   // Positions that ascend over the lanes (over the first 32 of them, the others have the same again): each lane's own span, by as many turns as there are

@@ -64,7 +64,7 @@ __device__ __forceinline__ TileRange range_of(const PackedCall& c, int tile, boo
   if (first > last) return {0, 0};
   int lo = 0, hi = c.n_seqs + 1;              // (every thread has a tile of its own)
   while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
+    const int mid = lo + (hi - lo) / 2;
     if (offsets[mid] > last) hi = mid;
     else lo = mid + 1;
   }
