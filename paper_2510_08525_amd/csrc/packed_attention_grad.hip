@@ -51,6 +51,17 @@ __host__ __device__ inline int64_t tiles_of(int64_t tokens) { return (tokens + k
 __device__ __forceinline__ PlanItem* items_of(PackedPlan* p) { return reinterpret_cast<PlanItem*>(p + 1); }
 __device__ __forceinline__ PlanMerge* merges_of(PackedPlan* p, int64_t pairs) { return reinterpret_cast<PlanMerge*>(items_of(p) + pairs + kMostParts); }
 
+// Steps of a part: parts have at least as many and less than twice as many, so there are at most kMostParts of them; half as many where they are short.
+// (A call may have 2^45 steps, of which a tile's keys have 2^28 at most: a share of more than 2^31 divides none of them, and counts as 2^31 - 1.)
+__host__ __device__ constexpr int least_steps(unsigned long long total) {
+  const int64_t share = (int64_t)((total + kMostParts - 1) / kMostParts), twice = 2 * share < kEnoughSteps ? 2 * share : kEnoughSteps;
+  const int64_t least = share > twice ? share : twice;
+  return least > INT32_MAX ? INT32_MAX : least > kLeastSteps ? (int)least : kLeastSteps;
+}
+constexpr bool parts_fit(unsigned long long total) { return least_steps(total) > 1 << 28 || total / (unsigned long long)least_steps(total) <= kMostParts; }
+static_assert(least_steps(0) == 4 && least_steps(512) == 4 && least_steps(2049) == 10 && least_steps(4097) == 16 && least_steps(512 * 100) == 100, "");
+static_assert(parts_fit(3000) && parts_fit(1ull << 31) && parts_fit(1ull << 40) && parts_fit((1ull << 41) + (1 << 23)) && parts_fit(1ull << 45), "");
+
 struct PlanSmem {
   unsigned long long total;
   int32_t items, slots;
@@ -94,9 +105,7 @@ __device__ void make_plan(const PackedCall& c, PlanSmem& sm) {
   for (int64_t i = threadIdx.x; i < pairs; i += blockDim.x) mine += steps_of(pair(i, tile, h), c.group);
   atomicAdd(&sm.total, mine);
   __syncthreads();
-  // parts of at least `least` and less than twice as many steps, so at most kMostParts of them; half as many where they are short
-  const int64_t share = (int64_t)((sm.total + kMostParts - 1) / kMostParts);
-  const int least = (int)max(max(share, min(2 * share, (int64_t)kEnoughSteps)), (int64_t)kLeastSteps);
+  const int least = least_steps(sm.total);
   PlanItem* items = items_of(c.plan);
   PlanMerge* merges = merges_of(c.plan, pairs);
   // (the long ones in front of the others)
