@@ -601,7 +601,7 @@ rlkv_status_t rlkv_head_norm_rotary(const void* qkv /* device */, int64_t token_
  *   grad_q_weight, grad_k_weight : device, fp32 [128], each may be NULL (both are, without a norm); written, not added to; 0 without tokens
  *   workspace: device, 16-byte aligned, rlkv_head_norm_rotary_grad_workspace bytes, where a weight's gradient is wanted; its contents do not
  *              matter.  Calls that may overlap in time need one each.
- * Sums are fp32 over up to some hundred rows, then 64 bits, in a fixed order: equal calls give equal bits. */
+ * Sums are fp32 over up to 512 rows one behind the other and 32 such sums, then 64 bits, in a fixed order: equal calls give equal bits. */
 size_t rlkv_head_norm_rotary_grad_workspace(int32_t tokens, int32_t n_q_heads, int32_t n_kv_heads);
 rlkv_status_t rlkv_head_norm_rotary_grad(const void* qkv /* device */, int64_t token_stride, const int32_t* positions /* device */,
                                          const rlkv_rotary_t* rotary /* host */, const rlkv_head_norm_t* norm /* host */, int32_t tokens,

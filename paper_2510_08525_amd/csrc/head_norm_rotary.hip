@@ -37,13 +37,13 @@ struct Deal {
   int32_t heads[3];              // of a token (0 of values: they stay where they are)
   int32_t each[3], parts[3];     // heads of a part, at most; parts of a token
 };
-Deal deal_of(const HeadNormCall& c) {
+Deal deal_of(int tokens, int n_q_heads, int n_kv_heads, bool values) {
   Deal d;
-  d.heads[kQuery] = c.n_q_heads;
-  d.heads[kKey] = c.n_kv_heads;
-  d.heads[kValue] = c.v.p ? c.n_kv_heads : 0;
+  d.heads[kQuery] = n_q_heads;
+  d.heads[kKey] = n_kv_heads;
+  d.heads[kValue] = values ? n_kv_heads : 0;
   // (one head each where there are few rows)
-  const bool many = (int64_t)c.tokens * (c.n_q_heads + c.n_kv_heads) >= 65536;
+  const bool many = (int64_t)tokens * (n_q_heads + n_kv_heads) >= 65536;
   for (int k = 0; k < 3; ++k) {
     d.parts[k] = many ? (d.heads[k] + 7) / 8 : d.heads[k];
     d.each[k] = d.parts[k] ? (d.heads[k] + d.parts[k] - 1) / d.parts[k] : 0;
@@ -221,10 +221,22 @@ __global__ __launch_bounds__(kSumThreads) void weight_grad_kernel(const float* _
 }
 
 constexpr int kGradBlocks = 1024;          // four a compute unit
+constexpr int kRowsInTurn = 512;           // rows that a thread adds up one behind the other in fp32, at most: beyond them there are more workgroups
+
+// Workgroups of a kind of head: as many as all its items, as its share of kGradBlocks, and as its weight's sums need at least.
+int64_t all_blocks(int64_t tokens, const Deal& d, int k) { return (tokens * d.parts[k] + kItems - 1) / kItems; }
+int64_t share_blocks(const Deal& d, int k) {
+  const int64_t heads = d.heads[0] + d.heads[1] + d.heads[2];
+  return (kGradBlocks * (int64_t)d.heads[k] + heads - 1) / heads;
+}
+int64_t least_blocks(int64_t tokens, const Deal& d, int k) {
+  const int64_t turns = kRowsInTurn / (d.each[k] ? d.each[k] : 1);
+  return k == kValue ? 0 : (all_blocks(tokens, d, k) + turns - 1) / turns;
+}
 
 template <typename T>
 hipError_t launch_forward(const HeadNormCall& c, const RotaryTurns& turns, hipStream_t stream) {
-  const Deal deal = deal_of(c);
+  const Deal deal = deal_of(c.tokens, c.n_q_heads, c.n_kv_heads, c.v.p != nullptr);
   const int64_t items = (int64_t)c.tokens * (deal.parts[0] + deal.parts[1] + deal.parts[2]);
   const int64_t heads = deal.heads[0] + deal.heads[1] + deal.heads[2];
   const bool streams = c.tokens * heads * kHeadDim * 2 * (int64_t)sizeof(T) > kStreamBytes;
@@ -236,14 +248,15 @@ hipError_t launch_forward(const HeadNormCall& c, const RotaryTurns& turns, hipSt
 }
 template <typename T>
 hipError_t launch_backward(HeadNormCall c, const RotaryTurns& turns, hipStream_t stream) {
-  const Deal deal = deal_of(c);
+  const Deal deal = deal_of(c.tokens, c.n_q_heads, c.n_kv_heads, c.v.p != nullptr);
   const bool sums = c.grad_q_weight || c.grad_k_weight;
   if (!sums) c.partials = nullptr;
   const int64_t heads = deal.heads[0] + deal.heads[1] + deal.heads[2];
   GradGrid grid = {};
   for (int k = 0; k < 3; ++k) {
-    const int64_t all = ((int64_t)c.tokens * deal.parts[k] + kItems - 1) / kItems, share = (kGradBlocks * (int64_t)deal.heads[k] + heads - 1) / heads;
-    grid.first[k + 1] = grid.first[k] + (int)(all < share ? all : share);
+    const int64_t all = all_blocks(c.tokens, deal, k), share = share_blocks(deal, k), least = least_blocks(c.tokens, deal, k);
+    const int64_t blocks = share > least ? share : least;
+    grid.first[k + 1] = grid.first[k] + (int)(all < blocks ? all : blocks);
   }
   const bool streams = c.tokens * heads * kHeadDim * 3 * (int64_t)sizeof(T) > kStreamBytes;
   auto launch = [&](auto kernel) {
@@ -262,9 +275,16 @@ hipError_t launch_backward(HeadNormCall c, const RotaryTurns& turns, hipStream_t
 
 }  // namespace
 
+// (No less for more tokens.  A share is rounded up for each kind, and is no smaller where the values have none.)
 size_t head_norm_grad_workspace(int tokens, int n_q_heads, int n_kv_heads) {
-  const int64_t all = ((int64_t)tokens * (n_q_heads + 2 * (int64_t)n_kv_heads) + kItems - 1) / kItems + 2;      // (a share is rounded up for each kind)
-  return (size_t)(all < kGradBlocks + 3 ? all : kGradBlocks + 3) * kHeadDim * sizeof(float);
+  const int64_t all = ((int64_t)tokens * (n_q_heads + 2 * (int64_t)n_kv_heads) + kItems - 1) / kItems + 2;
+  const Deal deal = deal_of(tokens, n_q_heads, n_kv_heads, true);
+  int64_t blocks = kGradBlocks + 3;
+  for (int k = kQuery; k <= kKey; ++k) {
+    const int64_t share = share_blocks(deal, k), least = least_blocks(tokens, deal, k);
+    if (least > share) blocks += least - share;
+  }
+  return (size_t)(all < blocks ? all : blocks) * kHeadDim * sizeof(float);
 }
 
 hipError_t launch_head_norm_rotary(const HeadNormCall& call, const RotaryTurns& turns, int dtype, hipStream_t stream) {
