@@ -541,7 +541,7 @@ typedef struct {
 typedef struct {
   const int32_t* offsets;   /* device [n_seqs + 1], not decreasing, in 0 .. tokens; read when the call runs.  (Others name no sequences that make sense, but
                                nothing outside the tensors is read or written.) */
-  int32_t n_seqs;           /* >= 0                                                                               */
+  int32_t n_seqs;           /* 0 .. 2^31 - 2                                                                      */
   int32_t tokens;           /* rows of the tensors; those of no sequence are not written                                     */
   int32_t n_q_heads;        /* multiple of n_kv_heads; query head i reads KV head i / (n_q_heads / n_kv_heads); group at most 16 */
   int32_t n_kv_heads;       /* at most 256; tokens * n_q_heads is below 2^30                                        */
@@ -554,7 +554,9 @@ typedef struct {
  *   q, out : RLKV_BF16, [tokens][n_q_heads];  k, v : [tokens][n_kv_heads]; token strides at most 2^24
  *   lse    : device, fp32, [n_q_heads][tokens], or NULL
  * out is none of the inputs.  Scores, softmax and sums are fp32; the weights enter their product with V in bf16.  What is not admitted does not count, whatever it holds
- * (infinities and NaN among it).  Equal calls give equal bits. */
+ * (infinities and NaN among it).  q . k and scores may be any finite fp32 numbers; values are summed with weights of up to 2^10 before the division, so those beyond
+ * 2^118 / tokens may overflow.  Equal calls give equal bits.  (A row with scores from 2^25 on, or whose output is not finite, may change the last bit of other
+ * rows near it: the 256 of a workgroup, positions of the heads of one KV head, are then summed another way.) */
 rlkv_status_t rlkv_packed_attention(const rlkv_packed_t* shape /* host */, const rlkv_heads_t* q /* host */,
                                     const rlkv_heads_t* k /* host */, const rlkv_heads_t* v /* host */,
                                     const rlkv_heads_t* out /* host */, float* lse /* device */, void* stream);
@@ -563,7 +565,8 @@ rlkv_status_t rlkv_packed_attention(const rlkv_packed_t* shape /* host */, const
  *     z[i][j] = w[i][j] (grad_out[i] . v[j] - grad_out[i] . out[i])
  *     grad_q[i] = softmax_scale * sum_j z[i][j] k[j]    grad_k[j] = softmax_scale * sum_i z[i][j] q[i]    grad_v[j] = sum_i w[i][j] grad_out[i]
  * grad_k and grad_v are summed over the group's query heads.  All tensors RLKV_BF16; w and z enter their products in bf16, sums are fp32, in a fixed
- * order: equal calls give equal bits.  The outputs are none of the inputs.
+ * order: equal calls give equal bits.  The outputs are none of the inputs.  As score and lse are fp32, w is off by up to 2^-18 (1 + |lse|) of itself: scores of
+ * some thousand cost the gradient bits, and from 2^18 on it means nothing and need not be finite.
  *   workspace : device, 16-byte aligned, rlkv_packed_attention_grad_workspace bytes (some 128 MiB, for few tokens less, and 4 a token and query head);
  *               its contents do not matter.  Calls that may overlap in time
  *               need one each (graphs that are replayed at the same time among them). */

@@ -157,7 +157,7 @@ __device__ __forceinline__ uint32_t two_bf16(float a, float b) {      // rounded
 //   kQuads  in a block quads of units, in a quad the rows, every fourth row's quad permuted: the 16 rows of which 16 lanes read the same unit at a time,
 //           and the 4 rows x 4 units of which 32 lanes read 8 bytes each transposed, lie in banks of their own
 //   kPairs  in a block pairs of units, in a pair the rows: half of the reads' time is conflicts.  Yet the forward kernel is the faster with it, for
-//           reasons that its counters do not tell (16384 tokens of 32 / 8 heads 1925 us and 1995 with quads), and the gradient's slower
+//           reasons that its counters do not tell (16384 tokens of 32 / 8 heads 1893 us and 1990 with quads on one machine), and the gradient's slower
 //           (2 x 8192 2415 us and 2227)
 enum Layout { kQuads, kPairs };
 template <Layout L>
@@ -308,6 +308,8 @@ inline uint32_t column_blocks(const PackedCall& c, int waves) { return (uint32_t
 // heads, without and with: one sequence of 70 tokens 10.2 and 8.8, 333 16.6 and 13.2, 1150 35.1 and 26.6, 2100 57.3 and 48.5, eight of 130 13.3 and 11.8, two of
 // 1000 33.2 and 31.5; but three of 700 27.0 and 33.7, sixteen of 100 14.2 and 18.0, one of 3000 84 and 92.  The gradient's queries:
 // 333 23.1 and 17.7, 1200 52.2 and 37.2, 2300 94 and 74, six of 300 23.9 and 31.4.
+// The rule sees what the host does: the buffer's rows, those behind the last sequence among them, and all sequences, empty ones too.  2100 tokens of 28 / 4 heads
+// take 51 us, with two empty sequences behind them or in a buffer of 5100 rows 58 (undivided; 16 / 1 heads 42 and 56, 1100 tokens of 32 / 8 26 and 34).
 inline bool keys_divided(const PackedCall& c) {
   const int64_t workgroups = (int64_t)column_blocks(c, kPackedWaves) * c.n_kv_heads;
   return workgroups <= 128 || (workgroups <= 256 && c.tokens >= (int64_t)c.n_seqs * 1000);

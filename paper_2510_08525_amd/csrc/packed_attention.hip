@@ -7,10 +7,10 @@
 // few keys of other sequences are masked.  So blocks of columns need no plan, sequences of any lengths (none among them) fill them, and the launch is
 // the same whatever the offsets hold.  Keys x queries first: scores, weights, maximum and sum of a column are in its two lanes.
 //
-// 4 * 128 operations a pair of an admitted key and a query head.  One sequence of 16384 tokens, 32 / 8 heads: 1925 us, 1.14 PFLOP/s where the
-// library's product of 8192^3 reaches 1.24: the matrix cores are busy for 57 % of the time, and in the rest of it the vector instructions are, some 180 a
+// 4 * 128 operations a pair of an admitted key and a query head.  One sequence of 16384 tokens, 32 / 8 heads: 1990 us (1890 to 2085 over machines), 1.11 PFLOP/s
+// where the library's product of 8192^3 reaches 1.23: the matrix cores are busy for 57 % of the time, and in the rest of it the vector instructions are, some 180 a
 // wavefront and tile (exponentials, maxima, rounding), with which they hardly overlap; reads of LDS (128 bytes a clock) take less.  24 sequences of 100
-// to 2000 tokens, 28 / 4 heads, half of them local: 260 us, of which each of the eleven workgroups that a compute unit has one after the other spends 9 on
+// to 2000 tokens, 28 / 4 heads, half of them local: 251 to 272 us, of which each of the eleven workgroups that a compute unit has one after the other spends 9 on
 // its start and end (offsets, queries, the first tile, the stores): with 256 registers a lane there is no second one beside it.
 #include "packed_attention.h"
 
@@ -22,7 +22,8 @@ namespace {
 constexpr float kSlack = 8.f;
 // A reference is a product rounded to fp32, while the products that it is taken from are not (one rounding for the difference): the largest weight is off 1
 // by up to half a step of the reference, 2^2 from here on, 2^64 at 2^31, and fits no float beyond.  From here on the walk is taken again with the
-// products' differences taken before the scale (careful), which the rounding of neither product enters; one instruction more a weight.
+// products' differences taken before the scale (careful), which the rounding of neither product enters.  (333 tokens, 28 / 4 heads: 55 us for 13, most of it the
+// masked tiles' products one by one.)
 constexpr float kLargeReference = 67108864.f;          // 2^26
 
 // SPLIT 2: the keys are divided between the halves of the workgroup (keys_divided).

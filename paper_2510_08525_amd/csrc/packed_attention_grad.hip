@@ -7,9 +7,9 @@
 // and delta, the other over the columns of its keys and leaves grad_k and grad_v, summed over the group's heads in fp32 in a fixed order.
 // That is seven products where one kernel would do five, but none of them adds to memory that others add to: equal calls give equal bits.
 //
-// 2 x 8192 tokens, 32 / 8 heads, half of them local: 930 us for the queries (three products), 1370 for the keys (four), 29 for sums of shared keys;
-// seven products at the library's rate of 1.24 PFLOP/s would be 1770.  Both are bound by the matrix cores and the vector instructions between their
-// products, at two wavefronts a SIMD.  12 sequences of 50 to 700, 28 / 4 heads: 62, 90 and 13 us, where a step of 64 positions takes 3 us (its products 2) and a
+// 2 x 8192 tokens, 32 / 8 heads, half of them local: 884 us for the queries (three products), 1296 for the keys (four), 28 for sums of shared keys (2208 in all, to
+// 2370 over machines); seven products at the library's rate of 1.23 PFLOP/s would be 1770.  Both are bound by the matrix cores and the vector instructions between their
+// products, at two wavefronts a SIMD.  12 sequences of 50 to 700, 28 / 4 heads: 58, 85 and 13 us, where a step of 64 positions takes 3 us (its products 2) and a
 // workgroup's start and end 20: keys and values, the last barrier, and 256 KiB of sums each to memory (equal stretches of all steps a workgroup, several tiles
 // of keys one after the other, took 134 us for 90, and 1538 for 1370).
 #include <type_traits>
